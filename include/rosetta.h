@@ -346,6 +346,147 @@ void rosetta_destroy(rosetta_ctx *ctx);
 /* Static string naming a status code. */
 const char *rosetta_status_string(int status);
 
+/* ---------------------------------------------------------------------------
+ * The decoder layer around a bootstrapped table, in the clear, with 8-bit
+ * activations, weights and cache.  A table's range [lo, hi] is calibrated and
+ * the precision of its p-bit codes judged by running the quantised layer with
+ * the same tables in place (Evaluation, "Experimental Setup", and the input-range
+ * calibration of the paper's appendix); the codes that are encrypted for
+ * rosetta_pbs_batch are those that the layer's linear product before the table
+ * gives.  The paper defines none of these operators; their formulas stand here.
+ *
+ * Buffers are DEVICE memory of the handle's device unless said otherwise; the
+ * caller owns them.  Pitches and strides count elements of their buffer and may
+ * exceed the row (slices of wider buffers); element [row][column] lies at
+ * row * pitch + column, in 64-bit arithmetic.  Float buffers are aligned to their
+ * element and hold `type` values; sums, norms and softmax statistics are 32-bit floats or
+ * exact integers, and results are rounded to `type` once.  Calls are
+ * asynchronous on `stream`; argument errors are detected before anything is
+ * enqueued.  Sizes of zero (tokens, batch) are no-ops returning OK.
+ *
+ * A handle may be used from one host thread at a time, and its calls share one
+ * workspace: they are ordered on one stream, or by the caller (or one handle per
+ * stream).  The workspace grows on demand; what a smaller call used stays
+ * allocated until rosetta_clear_destroy, so a captured graph stays valid.  It does not grow
+ * while `stream` is captured (OOM): run the call once, or reserve it, before.
+ * ------------------------------------------------------------------------- */
+
+typedef struct rosetta_clear rosetta_clear; /* opaque, library-owned */
+
+typedef enum {
+  ROSETTA_FLOAT32 = 0,
+  ROSETTA_FLOAT16 = 1,
+  ROSETTA_BFLOAT16 = 2
+} rosetta_float_type;
+
+/* Create a handle on CUDA device `cuda_device` with a workspace of
+ * workspace_bytes (0: grow on demand).  Errors: INVALID_ARG, CUDA, OOM. */
+int rosetta_clear_init(rosetta_clear **out, int cuda_device, size_t workspace_bytes);
+
+/* Residual addition, root-mean-square norm, 8-bit output.  For each token
+ *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * gamma,
+ *   scale = max |y| / 127,  q = rint(y / scale) in [-127, 127] (0 where scale = 0)
+ * in 32-bit floats; sum_out receives h rounded to `type`.
+ *   x, residual, sum_out [tokens][width]; residual may be NULL (h = x), and so may
+ *     sum_out, which may also be x or residual itself (same pointer and pitch)
+ *   gamma [width], q [tokens][width], scale [tokens]
+ * A row with a NaN or an infinity gets the scale NaN.  width: 1 .. 2^20; tokens < 2^31.
+ * Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_norm(rosetta_clear *h, int type, const void *x, int64_t x_pitch, const void *residual,
+                       int64_t residual_pitch, const float *gamma, float eps, uint32_t tokens, uint32_t width,
+                       void *sum_out, int64_t sum_pitch, int8_t *q, int64_t q_pitch, float *scale, void *stream);
+
+/* Bytes of the packed form of int8 weights [channels][inner] (0: sizes out of range). */
+size_t rosetta_clear_packed_bytes(uint32_t channels, uint32_t inner);
+
+/* Lay weights [channels][inner] out for the linear products, once: tiles of 128
+ * channels x 64 inputs, zeros beyond the sizes.  packed: rosetta_clear_packed_bytes
+ * bytes, 16-byte aligned.  channels: 1 .. 2^24, inner: 1 .. 131071 (any sum of
+ * `inner` products of 8-bit integers fits 32 bits).  Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_pack_weights(rosetta_clear *h, const int8_t *weight, int64_t pitch, uint32_t channels,
+                               uint32_t inner, void *packed, void *stream);
+
+/* Product of 8-bit integers with scales for each token and channel:
+ *   acc[t][n] = sum_k q[t][k] weight[n][k]                (exact, 32-bit)
+ *   out[t][n] = (float(acc) * scale[t]) * w_scale[n] + bias[n]
+ * every step rounded to a 32-bit float, the result to `type`; bias may be NULL.
+ *   q [tokens][inner], scale [tokens], packed (rosetta_clear_pack_weights),
+ *   w_scale, bias [channels], out [tokens][channels].
+ * Errors: INVALID_ARG, CUDA, OOM. */
+int rosetta_clear_linear(rosetta_clear *h, const int8_t *q, int64_t q_pitch, const float *scale, uint32_t tokens,
+                         const void *packed, const float *w_scale, const float *bias, uint32_t channels,
+                         uint32_t inner, int type, void *out, int64_t out_pitch, void *stream);
+
+/* The same product up to the message codes of a 2^bits-entry table on [lo, hi]:
+ *   y = (float(acc) * scale[t]) * w_scale[n] + bias[n]
+ *   code[t][n] = clamp(floor((y - lo) * r), 0, 2^bits - 1),  r = float(2^bits / (hi - lo))
+ * (the codes that are encrypted for rosetta_pbs_batch; a NaN gives 0), and with a table
+ *   values[t][n] = table[code[t][n]]
+ * (the table's function in the clear, as 8-bit activations of the next product).
+ * bits: 1 .. 8, lo < hi finite.  table [2^bits] and values may both be NULL.
+ * Errors: INVALID_ARG, CUDA, OOM. */
+int rosetta_clear_linear_codes(rosetta_clear *h, const int8_t *q, int64_t q_pitch, const float *scale,
+                               uint32_t tokens, const void *packed, const float *w_scale, const float *bias,
+                               uint32_t channels, uint32_t inner, uint32_t bits, float lo, float hi, uint8_t *code,
+                               int64_t code_pitch, const int8_t *table, int8_t *values, int64_t values_pitch,
+                               void *stream);
+
+/* Paged 8-bit cache of keys and values.  Token p of sequence b lies in page
+ * page_table[b][p / page_tokens], row p % page_tokens; a page holds page_tokens rows
+ * of dim bytes for each of heads heads, and one scale per head:
+ *   value = q * scale[page][head].
+ *   k_cache, v_cache int8, element [page][head][row][d] at page * strides[0] +
+ *     head * strides[1] + row * strides[2] + d (bytes; both caches, multiples of 4,
+ *     the caches 4-byte aligned; multiples of 16 and 16-byte aligned for speed)
+ *   k_scale, v_scale [pages][heads]
+ *   page_table int32 [batch][table_pitch]
+ * dim: a multiple of 4, 4 .. 256; page_tokens: 1 .. 1024.  cache_strides,
+ * k_strides and v_strides are HOST arrays. */
+
+/* Append `tokens` new tokens to each sequence: token i of sequence b becomes position
+ * first[b] + i (first[b] < 0: the sequence appends nothing).
+ *   k, v [batch][tokens][heads][dim] of `type`, element at b * s[0] + i * s[1] +
+ *     head * s[2] + d with s = k_strides, v_strides
+ * For every page written and every head:
+ *   scale' = max(scale of the rows before the new ones, if the page has any; max |new| / 127)
+ *   old rows of the page: q' = rint(q * (scale / scale')), if the scale changed
+ *   new rows: q = rint(new / scale')                          (0 where scale' = 0)
+ * Rows after the new ones are left as they are.  A NaN or an infinity among the new
+ * values makes the scale NaN (and the page's values with it).  Page lists of different
+ * sequences must not share a page that is written.  A position past the page list
+ * (table_pitch pages) or a page outside [0, pages) is skipped and reported by
+ * rosetta_clear_sync_status as INVALID_ARG.  Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const int64_t *k_strides, const void *v,
+                               const int64_t *v_strides, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim,
+                               int8_t *k_cache, int8_t *v_cache, const int64_t *cache_strides, float *k_scale,
+                               float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                               uint32_t table_pitch, const int32_t *first, void *stream);
+
+/* Causal attention of `tokens` query tokens of each sequence over the cache.  Query t
+ * of sequence b stands at position lengths[b] - tokens + t and sees the positions
+ * up to its own (lengths counts the tokens in the cache, the queries' own among them):
+ *   out = softmax(softmax_scale * q K^T) V; a query at a negative position gets zeros.
+ *   q, out [batch][tokens][heads * group][dim] of `type`, element at b * s[0] + t * s[1] +
+ *     head * s[2] + d with s = q_strides, out_strides (HOST arrays); query head i reads
+ *     cached head i / group
+ *   lengths int32 [batch]; a length past the page list counts as the list's end, a page
+ *     outside [0, pages) as masked, and both are reported by rosetta_clear_sync_status as
+ *     INVALID_ARG
+ * group: 1 .. 128.  Errors: INVALID_ARG, CUDA, OOM. */
+int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch,
+                            uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, const int8_t *k_cache,
+                            const int8_t *v_cache, const int64_t *cache_strides, const float *k_scale,
+                            const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                            uint32_t table_pitch, const int32_t *lengths, float softmax_scale, void *out,
+                            const int64_t *out_strides, void *stream);
+
+/* Wait for all work on `stream` and report deferred errors of the handle's calls
+ * (CUDA; TIMEOUT; INVALID_ARG for a page or a length out of range), once. */
+int rosetta_clear_sync_status(rosetta_clear *h, void *stream);
+
+/* Free the handle and its workspace; waits for the device.  NULL is ignored. */
+void rosetta_clear_destroy(rosetta_clear *h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,10 @@ EXPORTS = ("rosetta_params_init", "rosetta_upload_bsk", "rosetta_upload_ksk", "r
            "rosetta_plaintext_mul_batch", "rosetta_upload_lookup_table", "rosetta_segmented_lookup_batch",
            "rosetta_selftest_wait_timeout", "rosetta_selftest_bounds", "rosetta_selftest_lost_words",
            "rosetta_pbs_batch_noalloc", "rosetta_ntt_primes",
-           "rosetta_sync_status", "rosetta_destroy", "rosetta_status_string")
+           "rosetta_sync_status", "rosetta_destroy", "rosetta_status_string",
+           "rosetta_clear_init", "rosetta_clear_norm", "rosetta_clear_packed_bytes", "rosetta_clear_pack_weights",
+           "rosetta_clear_linear", "rosetta_clear_linear_codes", "rosetta_clear_cache_append",
+           "rosetta_clear_attention", "rosetta_clear_sync_status", "rosetta_clear_destroy")
 
 
 class RosettaError(RuntimeError):
@@ -79,8 +82,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L.rosetta_destroy.restype = None
     L.rosetta_status_string.argtypes = [ctypes.c_int]
     L.rosetta_status_string.restype = ctypes.c_char_p
+    i32, i64, f32 = ctypes.c_int, ctypes.c_int64, ctypes.c_float
+    L.rosetta_clear_init.argtypes = [ctypes.POINTER(vp), i32, ctypes.c_size_t]
+    L.rosetta_clear_norm.argtypes = [vp, i32, vp, i64, vp, i64, vp, f32, u32, u32, vp, i64, vp, i64, vp, vp]
+    L.rosetta_clear_packed_bytes.argtypes = [u32, u32]
+    L.rosetta_clear_packed_bytes.restype = ctypes.c_size_t
+    L.rosetta_clear_pack_weights.argtypes = [vp, vp, i64, u32, u32, vp, vp]
+    L.rosetta_clear_linear.argtypes = [vp, vp, i64, vp, u32, vp, vp, vp, u32, u32, i32, vp, i64, vp]
+    L.rosetta_clear_linear_codes.argtypes = [vp, vp, i64, vp, u32, vp, vp, vp, u32, u32, u32, f32, f32, vp, i64, vp,
+                                             vp, i64, vp]
+    strides = ctypes.POINTER(i64)
+    cache = [vp, vp, strides, vp, vp, u32, u32, vp, u32]
+    L.rosetta_clear_cache_append.argtypes = [vp, i32, vp, strides, vp, strides, u32, u32, u32, u32, *cache, vp, vp]
+    L.rosetta_clear_attention.argtypes = [vp, i32, vp, strides, u32, u32, u32, u32, u32, *cache, vp, f32, vp, strides, vp]
+    L.rosetta_clear_sync_status.argtypes = [vp, vp]
+    L.rosetta_clear_destroy.argtypes = [vp]
+    L.rosetta_clear_destroy.restype = None
     for name in EXPORTS:
-        if name not in ("rosetta_destroy", "rosetta_status_string"):
+        if name not in ("rosetta_destroy", "rosetta_status_string", "rosetta_clear_packed_bytes", "rosetta_clear_destroy"):
             getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L

@@ -1,0 +1,131 @@
+// Internal declarations of the decoder layer in the clear (rosetta_clear_*):
+// argument structs and launchers of its kernels.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rosetta {
+
+struct ClearNormArgs {
+  const void *x, *residual;  // residual null: none
+  const float *gamma;
+  void *sum_out;             // null: not wanted
+  int8_t *q;
+  float *scale;
+  int64_t x_pitch, residual_pitch, sum_pitch, q_pitch;
+  uint32_t tokens, width;
+  float eps;
+};
+
+// Packed weights: [row tile][k step] tiles of 128 channels x 64 inputs, a tile as
+// four chunks of 16 inputs, a chunk as 128 rows of 16 bytes.
+constexpr uint32_t kPackRows = 128, kPackK = 64, kPackTile = kPackRows * kPackK;
+
+enum ClearOut : int { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutCodes = 3 };  // 0 .. 2: rosetta_float_type
+
+struct ClearLinearArgs {
+  const int8_t *q;
+  const float *scale;
+  const int8_t *packed;
+  const float *w_scale, *bias;  // bias null: none
+  void *out;                    // floats, or the codes
+  int64_t q_pitch, out_pitch;
+  const int8_t *table;          // null: none
+  int8_t *values;
+  int64_t values_pitch;
+  uint32_t tokens, channels, inner, k_steps;
+  float lo, inv, top;           // code = clamp(floor((y - lo) * inv), 0, top)
+  uint32_t *err_flag;
+};
+
+struct ClearAppendArgs {
+  const void *src[2];           // k, v
+  int64_t src_strides[2][3];    // batch, token, head
+  int8_t *cache[2];
+  int64_t cache_strides[3];     // page, head, row
+  float *scale[2];
+  const int32_t *page_table, *first;
+  uint32_t batch, tokens, heads, dim, pages, page_tokens, table_pitch;
+  uint32_t *err_flag;
+};
+
+struct ClearAttentionArgs {
+  const void *q;
+  void *out;
+  int64_t q_strides[3], out_strides[3];
+  const int8_t *k_cache, *v_cache;
+  int64_t cache_strides[3];
+  const float *k_scale, *v_scale;
+  const int32_t *page_table, *lengths;
+  uint32_t batch, tokens, heads, group, dim, pages, page_tokens, table_pitch;
+  float softmax_scale;
+  uint32_t *err_flag;
+};
+
+// float types by rosetta_float_type
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float<float>(float v) {
+  return v;
+}
+template <>
+__device__ __forceinline__ float to_float<__half>(__half v) {
+  return __half2float(v);
+}
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) {
+  return __bfloat162float(v);
+}
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) {
+  return v;
+}
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) {
+  return __float2half_rn(v);
+}
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) {
+  return __float2bfloat16_rn(v);
+}
+
+// A scaled sum of the linear product, each step rounded (no contraction): the
+// codes are decided by exactly these single-precision values.
+__device__ __forceinline__ float clear_scaled(int32_t acc, float scale, float w_scale, const float *bias, uint32_t n) {
+  const float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), scale), w_scale);
+  return bias ? __fadd_rn(y, bias[n]) : y;
+}
+
+// Store one output of the linear product.
+template <int OUT>
+__device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t, uint32_t n, float y) {
+  const int64_t at = static_cast<int64_t>(t) * a.out_pitch + n;
+  if constexpr (OUT == kOutF32) {
+    static_cast<float *>(a.out)[at] = y;
+  } else if constexpr (OUT == kOutF16) {
+    static_cast<__half *>(a.out)[at] = __float2half_rn(y);
+  } else if constexpr (OUT == kOutBf16) {
+    static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
+  } else {
+    // fmaxf drops a NaN: code 0
+    const float f = fminf(fmaxf(floorf(__fmul_rn(__fsub_rn(y, a.lo), a.inv)), 0.0f), a.top);
+    const uint32_t code = static_cast<uint32_t>(f);
+    static_cast<uint8_t *>(a.out)[at] = static_cast<uint8_t>(code);
+    if (a.values) a.values[static_cast<int64_t>(t) * a.values_pitch + n] = a.table[code];
+  }
+}
+
+cudaError_t launch_clear_norm(const ClearNormArgs &a, int type, cudaStream_t s);
+cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t channels, uint32_t inner, int8_t *packed,
+                              cudaStream_t s);
+cudaError_t launch_clear_linear(const ClearLinearArgs &a, int out_kind, cudaStream_t s);
+cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t s);
+cudaError_t launch_clear_attention(const ClearAttentionArgs &a, int type, cudaStream_t s);
+
+}  // namespace rosetta
