@@ -20,8 +20,9 @@ struct ClearNormArgs {
   float eps;
 };
 
-// Packed weights: [row tile][k step] tiles of 128 channels x 64 inputs, a tile as
-// four chunks of 16 inputs, a chunk as 128 rows of 16 bytes.
+// Packed weights: [row tile][k step] tiles of 128 channels x 64 inputs, a tile as eight
+// blocks of 16 channels (1 KB in a row), a block as four chunks of 16 inputs, a chunk as 16 rows of 16
+// bytes.
 constexpr uint32_t kPackRows = 128, kPackK = 64, kPackTile = kPackRows * kPackK;
 
 enum ClearOut : int { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutCodes = 3 };  // 0 .. 2: rosetta_float_type
@@ -124,7 +125,13 @@ __device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t
 cudaError_t launch_clear_norm(const ClearNormArgs &a, int type, cudaStream_t s);
 cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t channels, uint32_t inner, int8_t *packed,
                               cudaStream_t s);
-cudaError_t launch_clear_linear(const ClearLinearArgs &a, int out_kind, cudaStream_t s);
+// the linear product of up to kLinearFew tokens
+constexpr uint32_t kLinearFew = 32;
+cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s);
+// the same product on the tensor cores; work: linear_tc_bytes
+uint32_t linear_tc_columns(uint32_t tokens);
+size_t linear_tc_bytes(uint32_t tokens, uint32_t k_steps);
+cudaError_t launch_clear_linear_tc(const ClearLinearArgs &a, int out_kind, void *work, uint32_t sms, cudaStream_t s);
 cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t s);
 cudaError_t launch_clear_attention(const ClearAttentionArgs &a, int type, cudaStream_t s);
 

@@ -90,9 +90,44 @@ bool linear_overlap(const ClearLinearArgs &a, const void *out, size_t bytes) {
          overlaps(out, bytes, a.w_scale, 4ull * a.channels) || overlaps(out, bytes, a.bias, 4ull * a.channels);
 }
 
+// Make the workspace hold `bytes`; what it outgrows stays until the handle is freed.
+int ensure_work(rosetta_clear *h, size_t bytes, cudaStream_t s) {
+  if (h->work_bytes >= bytes) return ROSETTA_OK;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) {
+    cudaGetLastError();
+    return ROSETTA_ERR_CUDA;
+  }
+  if (capture != cudaStreamCaptureStatusNone) return ROSETTA_ERR_OOM;
+  try {
+    h->outgrown.reserve(h->outgrown.size() + 1);
+  } catch (...) {
+    return ROSETTA_ERR_OOM;
+  }
+  // (at least doubled, so that what stays behind is no more than the present one)
+  const size_t want = bytes > 2 * h->work_bytes ? bytes : 2 * h->work_bytes;
+  void *p = nullptr;
+  const cudaError_t e = cudaMalloc(&p, want);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return cuda_fail(e);
+  }
+  if (h->work) h->outgrown.push_back(h->work);
+  h->work = p;
+  h->work_bytes = want;
+  return ROSETTA_OK;
+}
+
 int run_linear(rosetta_clear *h, const ClearLinearArgs &a, int kind, cudaStream_t s) {
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
-  const cudaError_t e = launch_clear_linear(a, kind, s);
+  cudaError_t e;
+  if (a.tokens <= kLinearFew) {
+    e = launch_clear_linear_few(a, kind, h->sms, s);
+  } else {
+    const int r = ensure_work(h, linear_tc_bytes(a.tokens, a.k_steps), s);
+    if (r != ROSETTA_OK) return r;
+    e = launch_clear_linear_tc(a, kind, h->work, h->sms, s);
+  }
   return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
 }
 

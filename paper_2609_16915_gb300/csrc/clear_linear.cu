@@ -2,11 +2,10 @@
 //   acc[t][n] = sum_k q[t][k] w[n][k],   y = (acc scale[t]) w_scale[n] + bias[n].
 // The packing of the weights, and the kernel for few tokens.
 //
-// Few tokens: bound by reading the weights once.  A block takes 32 channels and up
-// to 8 tokens; its eight warps share out the chunks of 16 inputs, a lane has one
-// channel (the packed tiles make that 512 contiguous bytes a warp) and multiplies
-// by dp4a, four products an instruction, with the tokens' bytes broadcast from
-// shared memory.  Integer sums, so the warps' partial sums join exactly.
+// Few tokens (up to kLinearFew): bound by reading the weights once.  A block takes 32 channels; its warps share
+// out the steps of 64 inputs and join their integer sums in shared memory.  The weights go from global
+// memory to registers, 16 bytes a lane, and from 8 bits to f16 there; a 16 x 8 x 16 product of f16 is exact
+// (products below 2^14), and so are the f32 sums of 16 steps, which are then taken into integers.
 #include <stdint.h>
 
 #include "clear.h"
@@ -21,7 +20,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const int8_t *__restrict__ w,
                                                    uint64_t rows16) {
   const uint64_t id = static_cast<uint64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (id >= rows16) return;
-  const uint32_t row = id % kPackRows, chunk = id / kPackRows % 4;
+  const uint32_t row = id / 64 % 8 * 16 + id % 16, chunk = id / 16 % 4;
   const uint64_t tile = id / (kPackRows * 4);
   const uint64_t n = tile / k_steps * kPackRows + row;
   const uint32_t k0 = tile % k_steps * kPackK + chunk * 16;
@@ -35,75 +34,163 @@ __global__ void __launch_bounds__(256) pack_kernel(const int8_t *__restrict__ w,
   reinterpret_cast<uint4 *>(packed)[id] = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-constexpr uint32_t kFewWarps = 8, kFewSlab = 2048;  // bytes of a token's row in shared memory at a time
+// four 8-bit integers to four f16: 1024 + (v + 128) by byte permute, minus 1152
+__device__ __forceinline__ void int8x4_f16(uint32_t v, uint32_t &lo, uint32_t &hi) {
+  const uint32_t u = v ^ 0x80808080u;
+  const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+  uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+  const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&a), off), y = __hsub2(*reinterpret_cast<__half2 *>(&b), off);
+  lo = *reinterpret_cast<const uint32_t *>(&x);
+  hi = *reinterpret_cast<const uint32_t *>(&y);
+}
 
-template <int TB, int OUT>
-__global__ void __launch_bounds__(32 * kFewWarps) linear_few_kernel(const ClearLinearArgs a) {
-  __shared__ __align__(16) int8_t xs[TB][kFewSlab];
-  __shared__ int32_t part[kFewWarps][TB][32];
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const uint32_t n = blockIdx.x * 32 + lane, t0 = blockIdx.y * TB;
-  const int8_t *tiles = a.packed + static_cast<size_t>(blockIdx.x / 4) * a.k_steps * kPackTile + (blockIdx.x % 4 * 32 + lane) * 16;
-  int32_t acc[TB] = {};
-  for (uint32_t k0 = 0; k0 < a.inner; k0 += kFewSlab) {
-    const uint32_t len = min(kFewSlab, a.inner - k0), padded = (len + 15) / 16 * 16;
-    __syncthreads();
-    for (uint32_t t = 0; t < TB; ++t) {
-      const int8_t *src = a.q + static_cast<int64_t>(t0 + t) * a.q_pitch + k0;
-      for (uint32_t i = threadIdx.x; i < padded; i += blockDim.x)
-        xs[t][i] = t0 + t < a.tokens && i < len ? src[i] : static_cast<int8_t>(0);
-    }
-    __syncthreads();
-    // chunk c of 16 inputs: bytes c * 128 * 16 of the tiles, which follow one another
-    const int8_t *w = tiles + static_cast<size_t>(k0 / 16) * (kPackRows * 16);
-#pragma unroll 4
-    for (uint32_t c = warp; c < padded / 16; c += kFewWarps) {
-      const int4 wv = __ldg(reinterpret_cast<const int4 *>(w + static_cast<size_t>(c) * (kPackRows * 16)));
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// 16 bytes of a token's row from input k on, zeros from `inner` on
+__device__ __forceinline__ uint4 token_bytes(const int8_t *row, uint32_t k, uint32_t inner) {
+  uint32_t v[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        const int4 xv = *reinterpret_cast<const int4 *>(&xs[t][c * 16]);
-        acc[t] = __dp4a(wv.w, xv.w, __dp4a(wv.z, xv.z, __dp4a(wv.y, xv.y, __dp4a(wv.x, xv.x, acc[t]))));
+  for (uint32_t e = 0; e < 16; ++e)
+    if (k + e < inner) v[e >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(row[k + e])) << (8 * (e & 3u));
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// Tiles of 32 channels over NB groups of eight tokens, the steps of 64 inputs shared out over WARPS warps, U of
+// them loaded ahead.  Lane (g, t) = (lane / 4, lane % 4) of a warp holds, of one step, 16 bytes of channels
+// g, g + 8, g + 16, g + 24 and of token g of each group: chunk t of the step.  Word i of those is its share of
+// the i-th 16 x 8 x 16 product: the products take the inputs in another order than they are stored in,
+// the same for both operands.
+template <int NB, int WARPS>
+struct FewShape {
+  static constexpr uint32_t PITCH = NB * 8 + 4;  // of a row of sums
+  static constexpr uint32_t SMEM = WARPS * 32 * PITCH * 4;
+  static constexpr uint32_t BLOCKS = WARPS == 16 ? 1 : WARPS == 4 ? 3 : NB == 1 ? 4 : 3;  // an SM, at least
+};
+
+template <int NB, int U, int WARPS, bool ALIGNED>
+__global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linear_few_kernel(const ClearLinearArgs a, int out_kind) {
+  using S = FewShape<NB, WARPS>;
+  extern __shared__ __align__(16) int32_t parts[];  // [warp][channel][token]
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+  const uint32_t n0 = blockIdx.x * 32;
+  const int8_t *w = a.packed + static_cast<size_t>(n0 / kPackRows) * a.k_steps * kPackTile + n0 % kPackRows * kPackK + (t * 16 + g) * 16;
+  const int8_t *rows[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) rows[b] = a.q + static_cast<int64_t>(min(b * 8 + g, a.tokens - 1)) * a.q_pitch;
+  float d[2][NB][4] = {};
+  int32_t acc[2][NB][4] = {};
+  const auto take = [&]() {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[m][b][i] += __float2int_rn(d[m][b][i]);
+          d[m][b][i] = 0.0f;
+        }
+  };
+  uint32_t done = 0;  // steps since the sums were taken: 16 of 64 inputs are exact
+  for (uint32_t k0 = warp; k0 < a.k_steps; k0 += WARPS * U) {
+    uint4 wv[U][4], xv[U][NB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t k = k0 + u * WARPS;
+      if (k >= a.k_steps) break;
+      const uint32_t at = k * kPackK + t * 16;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)  // (read once: first to leave the caches)
+        wv[u][r] = __ldcs(reinterpret_cast<const uint4 *>(w + static_cast<size_t>(k) * kPackTile + r / 2 * (16 * kPackK) + r % 2 * 128));
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        xv[u][b] = make_uint4(0u, 0u, 0u, 0u);
+        if (b * 8 + g < a.tokens)
+          xv[u][b] = ALIGNED && at + 16 <= a.inner ? __ldg(reinterpret_cast<const uint4 *>(rows[b] + at)) : token_bytes(rows[b], at, a.inner);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * WARPS >= a.k_steps) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const auto word = [&](const uint4 &v) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; };
+        uint32_t f[2][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          int8x4_f16(word(wv[u][2 * m]), f[m][0], f[m][2]);
+          int8x4_f16(word(wv[u][2 * m + 1]), f[m][1], f[m][3]);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          uint32_t b0, b1;
+          int8x4_f16(word(xv[u][b]), b0, b1);
+          mma_16x8x16(d[0][b], f[0], b0, b1);
+          mma_16x8x16(d[1][b], f[1], b0, b1);
+        }
+      }
+      if (++done == 1024 / kPackK) {
+        done = 0;
+        take();
       }
     }
   }
+  take();
+  // the warps' sums, joined: exact in any order
 #pragma unroll
-  for (int t = 0; t < TB; ++t) part[warp][t][lane] = acc[t];
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        *reinterpret_cast<int2 *>(parts + (warp * 32 + m * 16 + i * 4 + g) * S::PITCH + b * 8 + 2 * t) =
+            make_int2(acc[m][b][i], acc[m][b][i + 1]);
   __syncthreads();
-  for (uint32_t t = warp; t < TB; t += kFewWarps) {
-    if (t0 + t >= a.tokens || n >= a.channels) continue;
+  for (uint32_t i = threadIdx.x; i < 32 * NB * 8; i += blockDim.x) {
+    const uint32_t row = i % 32, tok = i / 32, n = n0 + row;
+    if (tok >= a.tokens || n >= a.channels) continue;
     int32_t sum = 0;
 #pragma unroll
-    for (uint32_t w = 0; w < kFewWarps; ++w) sum += part[w][t][lane];
-    clear_store<OUT>(a, t0 + t, n, clear_scaled(sum, a.scale[t0 + t], a.w_scale[n], a.bias, n));
+    for (uint32_t v = 0; v < WARPS; ++v) sum += parts[(v * 32 + row) * S::PITCH + tok];
+    const float y = clear_scaled(sum, a.scale[tok], a.w_scale[n], a.bias, n);
+    if (out_kind == kOutF32)
+      clear_store<kOutF32>(a, tok, n, y);
+    else if (out_kind == kOutF16)
+      clear_store<kOutF16>(a, tok, n, y);
+    else if (out_kind == kOutBf16)
+      clear_store<kOutBf16>(a, tok, n, y);
+    else
+      clear_store<kOutCodes>(a, tok, n, y);
   }
 }
 
-template <int OUT>
-cudaError_t launch_few(const ClearLinearArgs &a, cudaStream_t s) {
-  const uint32_t blocks = (a.channels + 31) / 32;
-  // the tokens of a block: as many as there are, in a power of two up to 8
-  // (the grid's second dimension ends at 65535 blocks)
-  for (uint64_t t0 = 0; t0 < a.tokens; t0 += 8ull * 65535) {
-    ClearLinearArgs b = a;
-    b.tokens = static_cast<uint32_t>(a.tokens - t0 < 8ull * 65535 ? a.tokens - t0 : 8ull * 65535);
-    b.q += static_cast<int64_t>(t0) * a.q_pitch;
-    b.scale += t0;
-    const int64_t size = OUT == kOutF32 ? 4 : OUT == kOutCodes ? 1 : 2;
-    b.out = static_cast<char *>(a.out) + static_cast<int64_t>(t0) * a.out_pitch * size;
-    if (a.values) b.values += static_cast<int64_t>(t0) * a.values_pitch;
-    const uint32_t tokens = b.tokens;
-    if (tokens == 1)
-      linear_few_kernel<1, OUT><<<dim3(blocks, 1), 32 * kFewWarps, 0, s>>>(b);
-    else if (tokens == 2)
-      linear_few_kernel<2, OUT><<<dim3(blocks, 1), 32 * kFewWarps, 0, s>>>(b);
-    else if (tokens <= 4)
-      linear_few_kernel<4, OUT><<<dim3(blocks, 1), 32 * kFewWarps, 0, s>>>(b);
-    else
-      linear_few_kernel<8, OUT><<<dim3(blocks, (tokens + 7) / 8), 32 * kFewWarps, 0, s>>>(b);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+template <int NB, int U, int WARPS>
+cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, cudaStream_t s) {
+  using S = FewShape<NB, WARPS>;
+  const bool aligned = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>(a.tokens > 1 ? a.q_pitch : 0)) % 16 == 0;
+  auto kern = aligned ? linear_few_kernel<NB, U, WARPS, true> : linear_few_kernel<NB, U, WARPS, false>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::SMEM));
+  if (e != cudaSuccess) return e;
+  kern<<<(a.channels + 31) / 32, 32 * WARPS, S::SMEM, s>>>(a, out_kind);
+  return cudaGetLastError();
+}
+
+// The kernel lives on loads in flight: eight warps a block and several blocks an SM where the channels make
+// that many blocks, else sixteen warps with two steps each.  8 tokens, 4096 inputs: 14336 channels 12.3 us
+// against 17.2, 4096 channels 8.2 against 6.9.
+// Over 16 tokens the sums leave registers for four warps of two steps, or sixteen of one (24 tokens, 4096 inputs:
+// 14336 channels 25.6 us against 31.3 with eight warps).
+template <int NB>
+cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
+  const bool many = (a.channels + 31) / 32 >= 2 * sms;
+  if constexpr (NB == 4)
+    return many ? launch_few<NB, 2, 4>(a, out_kind, s) : launch_few<NB, 1, 16>(a, out_kind, s);
+  else
+    return many ? launch_few<NB, 1, 8>(a, out_kind, s) : launch_few<NB, 2, 16>(a, out_kind, s);
 }
 
 }  // namespace
@@ -117,13 +204,10 @@ cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t chan
   return cudaGetLastError();
 }
 
-cudaError_t launch_clear_linear(const ClearLinearArgs &a, int out_kind, cudaStream_t s) {
-  switch (out_kind) {
-    case kOutF32: return launch_few<kOutF32>(a, s);
-    case kOutF16: return launch_few<kOutF16>(a, s);
-    case kOutBf16: return launch_few<kOutBf16>(a, s);
-    default: return launch_few<kOutCodes>(a, s);
-  }
+cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
+  if (a.tokens <= 8) return launch_few<1>(a, out_kind, sms, s);
+  if (a.tokens <= 16) return launch_few<2>(a, out_kind, sms, s);
+  return launch_few<4>(a, out_kind, sms, s);
 }
 
 }  // namespace rosetta
