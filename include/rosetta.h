@@ -439,7 +439,7 @@ int rosetta_clear_linear_codes(rosetta_clear *h, const int8_t *q, int64_t q_pitc
  *     head * strides[1] + row * strides[2] + d (bytes; both caches, multiples of 4,
  *     the caches 4-byte aligned; multiples of 16 and 16-byte aligned for speed)
  *   k_scale, v_scale [pages][heads]
- *   page_table int32 [batch][table_pitch]
+ *   page_table int32 [batch][table_pitch], table_pitch * page_tokens at most 2^30
  * dim: a multiple of 4, 4 .. 256; page_tokens: 1 .. 1024.  cache_strides,
  * k_strides and v_strides are HOST arrays. */
 

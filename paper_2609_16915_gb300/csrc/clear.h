@@ -133,6 +133,12 @@ uint32_t linear_tc_columns(uint32_t tokens);
 size_t linear_tc_bytes(uint32_t tokens, uint32_t k_steps);
 cudaError_t launch_clear_linear_tc(const ClearLinearArgs &a, int out_kind, void *work, uint32_t sms, cudaStream_t s);
 cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t s);
+// attention for few rows a cached head: whole 16-position tiles in a page, heads a multiple of 16; work:
+// attend_few_bytes
+bool attend_few_takes(const ClearAttentionArgs &a);
+size_t attend_few_bytes(const ClearAttentionArgs &a);
+cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, cudaStream_t s);
+// and for every shape
 cudaError_t launch_clear_attention(const ClearAttentionArgs &a, int type, cudaStream_t s);
 
 }  // namespace rosetta

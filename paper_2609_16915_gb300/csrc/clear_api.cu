@@ -137,7 +137,7 @@ bool good_cache(const int8_t *k_cache, const int8_t *v_cache, const int64_t *str
                 const int32_t *page_table, uint32_t table_pitch) {
   if (!strides || !good_strides(strides)) return false;
   if (dim < 4 || dim > 256 || dim % 4 || page_tokens < 1 || page_tokens > 1024 || heads < 1 || heads > 4096) return false;
-  if (pages > 0x7fffffffu || table_pitch > 0x7fffffffu) return false;
+  if (pages > 0x7fffffffu || static_cast<uint64_t>(table_pitch) * page_tokens > (1u << 30)) return false;
   if (strides[2] < static_cast<int64_t>(dim)) return false;
   for (int i = 0; i < 3; ++i)
     if (strides[i] % 4) return false;
@@ -367,7 +367,15 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
   a.table_pitch = table_pitch;
   a.softmax_scale = softmax_scale;
   a.err_flag = h->d_err;
-  const cudaError_t e = launch_clear_attention(a, type, as_stream(stream));
+  const cudaStream_t s = as_stream(stream);
+  cudaError_t e;
+  if (attend_few_takes(a)) {
+    const int r = ensure_work(h, attend_few_bytes(a), s);
+    if (r != ROSETTA_OK) return r;
+    e = launch_clear_attention_few(a, type, h->work, s);
+  } else {
+    e = launch_clear_attention(a, type, s);
+  }
   return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
 }
 

@@ -1,0 +1,537 @@
+// Causal attention over the paged 8-bit cache for few query rows a cached head: decoding.
+//
+// Bound by reading keys and values once (two 8-bit rows a position and cached head, 79.8 us of copies at the
+// measured rate for 64 sequences of up to 8192 positions, 8 heads of 128).  Query rows of one cached head (its
+// group's heads, and the tokens of a short run) share what is read: they are the columns of
+//   S^T = K Q^T (16 positions x 8 rows x 16 dimensions a product)  and  O^T = V^T P^T (16 dimensions x 8 rows x
+// 16 positions), with the 8-bit values made f16 in registers (exact) and the scales kept outside the
+// products.  With p the weights relative to the running maximum m (in units of log 2, raised only where a
+// score passes it by 8, so p <= 2^8), and sv the largest value scale of the block's pages,
+//   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
+// what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
+// Single-precision queries are split into two f16 each, and so are the weights: 22 bits.
+//
+// A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
+// takes every fourth tile of 16 positions, copied ahead into a ring by cp.async (a lane copies what it will
+// read itself: no barriers).  Blocks of one sequence join through partial results (m, l, O) in the
+// workspace and attend_join_kernel; a sequence that fits one range is written at once.
+#include <stdint.h>
+
+#include "clear.h"
+#include "dsmem.cuh"
+
+namespace rosetta {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr uint32_t kSegment = 256;      // tiles whose pages and scales are in shared memory at a time
+constexpr float kRaise = 8.0f, kLift = 128.0f;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
+// an 8 x 8 matrix of f16, two of a row in each lane, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// bytes (biased by 128) of a permuted word pair as f16: 1024 + u, minus 1152
+__device__ __forceinline__ uint32_t biased_f16(uint32_t u, uint32_t select) {
+  const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
+  uint32_t v = __byte_perm(u, 0x64646464u, select);
+  const __half2 h = __hsub2(*reinterpret_cast<__half2 *>(&v), off);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool valid) {
+  const uint32_t size = valid ? BYTES : 0;  // (nothing is read for 0: zeros)
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
+
+// DP: the head's dimension, rounded up to 64, 128 or 256
+template <int DP>
+struct Few {
+  static constexpr uint32_t TILE = 16 * DP * 2;                      // bytes of a tile's keys and values
+  static constexpr uint32_t DEPTH = DP == 64 ? 6 : DP == 128 ? 3 : 2;  // tiles of a warp's ring
+  static constexpr uint32_t RING = kWarps * DEPTH * TILE;
+  static constexpr uint32_t BLOCKS = DP == 256 ? 2 : 4;              // an SM
+};
+
+struct FewArgs {
+  ClearAttentionArgs a;
+  float *part;              // [batch][head][split][rows of all groups][dim + 2]: l, m, O
+  uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
+};
+
+// The range of positions of split `s` of `splits`: shares of at least 512 positions, whole tiles of all warps.
+__device__ __forceinline__ uint32_t split_share(uint32_t end, uint32_t splits) {
+  const uint32_t share = (end + splits - 1) / splits;
+  return ((share < 512 ? 512 : share) + 63) / 64 * 64;
+}
+
+// Positions that the rows of a group see at most: up to the last token of the group.
+__device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64_t len, uint32_t last_row) {
+  const int64_t end = len - a.tokens + 1 + last_row / a.group;
+  return end > 0 ? static_cast<uint32_t>(end) : 0u;
+}
+
+__device__ __forceinline__ int64_t length_of(const ClearAttentionArgs &a, uint32_t b) {
+  const int64_t len = a.lengths[b], most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
+  if (len > most && threadIdx.x == 0) atomicMax(a.err_flag, 1u);
+  return len > most ? most : len;
+}
+
+template <typename T, int DP, int NB>
+__global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) attend_few_kernel(const FewArgs f) {
+  using F = Few<DP>;
+  constexpr bool SPLIT = sizeof(T) == 4;     // queries and weights in two halves
+  constexpr int H = SPLIT ? 2 : 1;
+  constexpr int KC = DP / 16;                // products of 16 dimensions
+  constexpr int MT = DP / 16;                // tiles of 16 dimensions of O^T
+  constexpr int VB = DP / 8;                 // bytes of a value row in a lane
+  const ClearAttentionArgs &a = f.a;
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ int32_t s_page[kSegment];
+  __shared__ float s_ks[kSegment], s_vs[kSegment], s_top[kWarps];
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+  const uint32_t split = blockIdx.x % f.splits, group = blockIdx.x / f.splits % f.groups;
+  const uint32_t bh = blockIdx.x / f.splits / f.groups, kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t rows = a.tokens * a.group, row0 = group * (8 * NB);
+  const int64_t len = length_of(a, b);
+  const uint32_t end = group_end(a, len, min(row0 + 8 * NB, rows) - 1);
+  const uint32_t share = split_share(end, f.splits), lo = split * share, hi = min(end, lo + share);
+  if (split > 0 && lo >= end) return;
+  const bool alone = end <= share;  // (the first block of an empty sequence writes its zeros)
+
+  // the rows' last positions, and their queries as B operands: row g of a group of eight, dimensions 16 t + 4 c
+  // (+ 64 for every four c)
+  int32_t last[NB][2];  // of rows 2 t, 2 t + 1
+  float factor[NB][2];
+  uint32_t qf[H][NB][KC][2];
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    const uint32_t row = row0 + n * 8 + g;
+    const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
+                 static_cast<int64_t>(row / a.group) * a.q_strides[1] +
+                 static_cast<int64_t>(kh * a.group + row % a.group) * a.q_strides[2];
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
+        const float v = row < rows && d < a.dim ? to_float(q[d]) : 0.0f;
+        top = fmaxf(top, fabsf(v));
+      }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // a power of two that brings the row's largest value to [1, 2): exact (within the range of exponents)
+    const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
+    const float down = __int_as_float((127 - ex) << 23), up = __int_as_float((127 + ex) << 23);
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
+        v[e] = row < rows && d < a.dim ? to_float(q[d]) * down : 0.0f;
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const __half2 x = __floats2half2_rn(v[2 * p], v[2 * p + 1]);
+          qf[h][n][c][p] = *reinterpret_cast<const uint32_t *>(&x);
+          v[2 * p] -= __low2float(x);
+          v[2 * p + 1] -= __high2float(x);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      factor[n][i] = __shfl_sync(0xffffffffu, up, (2 * t + i) * 4) * (a.softmax_scale * kLog2e);
+      const uint32_t r = row0 + n * 8 + 2 * t + i;
+      last[n][i] = r < rows ? static_cast<int32_t>(len - a.tokens + r / a.group) : -1;
+    }
+  }
+
+  float o[NB][MT][4] = {}, m[NB][2], l[NB][2] = {}, sv = 0.0f;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) m[n][0] = m[n][1] = neg_inf();
+  const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
+  unsigned char *own = ring + warp * (F::DEPTH * F::TILE);
+  const uint32_t own_addr = smem_addr(own);
+  const uint32_t tiles_hi = (hi + 15) / 16;
+  for (uint32_t seg = lo / 16; seg < tiles_hi; seg += kSegment) {
+    const uint32_t count = min(kSegment, tiles_hi - seg);
+    __syncthreads();
+    float top = 0.0f;
+    for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
+      int32_t page = table[(seg + i) * 16 / a.page_tokens];
+      if (page < 0 || static_cast<uint32_t>(page) >= a.pages) {
+        atomicMax(a.err_flag, 1u);
+        page = -1;
+      }
+      s_page[i] = page;
+      const size_t at = static_cast<size_t>(page) * a.heads + kh;
+      s_ks[i] = page < 0 ? 0.0f : a.k_scale[at];
+      float v = page < 0 ? 0.0f : a.v_scale[at];
+      if (fabsf(v) == -neg_inf()) v = __int_as_float(0x7fc00000);  // no number either: kept out of the maximum
+      s_vs[i] = v;
+      top = fmaxf(top, fabsf(v));
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), 1e-30f);
+    if (top > sv) {  // (the same for the block)
+      const float keep = sv / top;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[n][i][e] *= keep;
+      sv = top;
+    }
+    const float vlift = kLift / sv;
+
+    const auto issue = [&](uint32_t i, uint32_t slot) {
+      if (i < count) {
+        const int32_t page = s_page[i];
+        const bool in = page >= 0;
+        const int64_t at = in ? page * a.cache_strides[0] + static_cast<int64_t>(kh) * a.cache_strides[1] +
+                                    static_cast<int64_t>((seg + i) * 16 % a.page_tokens) * a.cache_strides[2]
+                              : 0;
+        const uint32_t dst = own_addr + slot * F::TILE;
+        // keys of positions g, g + 8: 16 bytes at 16 t of each 64
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int j = 0; j < DP / 64; ++j) {
+            const uint32_t d = 16 * t + 64 * j;
+            const bool ok = in && d < a.dim;
+            copy_async<16>(dst + ((r * (DP / 64) + j) * 32 + lane) * 16, a.k_cache + (ok ? at + (g + 8 * r) * a.cache_strides[2] + d : 0), ok);
+          }
+        // values of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9: VB bytes at VB g
+        const uint32_t vdst = dst + 16 * DP;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int8_t *src = a.v_cache + at + static_cast<int64_t>(2 * t + p % 2 + p / 2 * 8) * a.cache_strides[2];
+          if constexpr (VB == 8) {
+            const bool ok = in && 8 * g < a.dim;
+            copy_async<8>(vdst + (p * 32 + lane) * 8, ok ? src + 8 * g : a.v_cache, ok);
+          } else {
+#pragma unroll
+            for (int j = 0; j < VB / 16; ++j) {
+              const uint32_t d = VB * g + 16 * j;
+              const bool ok = in && d < a.dim;
+              copy_async<16>(vdst + ((p * (VB / 16) + j) * 32 + lane) * 16, ok ? src + d : a.v_cache, ok);
+            }
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (uint32_t i = 0; i + 1 < F::DEPTH; ++i) issue(warp + i * kWarps, i);
+    uint32_t slot = 0;
+    for (uint32_t i = warp; i < count; i += kWarps) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(F::DEPTH - 2) : "memory");
+      const unsigned char *tile = own + slot * F::TILE;
+      // ---- scores: positions g, g + 8 (rows of S^T), query rows 2 t, 2 t + 1 ----
+      float s[NB][4] = {};
+#pragma unroll
+      for (int j = 0; j < DP / 64; ++j) {
+        const uint4 x = reinterpret_cast<const uint4 *>(tile)[j * 32 + lane];
+        const uint4 y = reinterpret_cast<const uint4 *>(tile)[(DP / 64 + j) * 32 + lane];
+        const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t u = xw[c] ^ 0x80808080u, v = yw[c] ^ 0x80808080u;
+          const uint32_t k[4] = {biased_f16(u, 0x4140), biased_f16(v, 0x4140), biased_f16(u, 0x4342), biased_f16(v, 0x4342)};
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int h = 0; h < H; ++h) mma_16x8x16(s[n], k, qf[h][n][j * 4 + c]);
+        }
+      }
+      const float ks = s_ks[i], vs = s_vs[i] * vlift;
+      const int32_t p0 = static_cast<int32_t>((seg + i) * 16 + g);
+      const bool in = s_page[i] >= 0;
+      bool raise = false;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
+          s[n][e] = seen ? s[n][e] * (ks * factor[n][e % 2]) : neg_inf();
+          raise |= s[n][e] > m[n][e % 2] + kRaise;
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = fmaxf(fmaxf(s[n][e], s[n][e + 2]), m[n][e]);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            const float keep = m[n][e] == neg_inf() ? 0.0f : ex2(m[n][e] - top);
+            m[n][e] = top;
+            l[n][e] *= keep;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+              o[n][j][e] *= keep;
+              o[n][j][e + 2] *= keep;
+            }
+          }
+      }
+      uint32_t pf[H][NB][2];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float base = m[n][e % 2] == neg_inf() ? 0.0f : m[n][e % 2];
+          p[e] = ex2(s[n][e] - base);
+          l[n][e % 2] += p[e];
+          p[e] = s[n][e] == neg_inf() ? 0.0f : p[e] * vs;  // (no product with the scale of a page that a row does not see)
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const __half2 x = __floats2half2_rn(p[2 * r], p[2 * r + 1]);
+            pf[h][n][r] = transposed(*reinterpret_cast<const uint32_t *>(&x));
+            p[2 * r] -= __low2float(x);
+            p[2 * r + 1] -= __high2float(x);
+          }
+      }
+      // ---- O^T: four dimensions of four positions to two 16 x 8 x 16 operands ----
+      const unsigned char *vt = tile + 16 * DP;
+#pragma unroll
+      for (int j = 0; j < VB / 8; ++j) {
+        uint32_t w[4][2];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          uint2 x;
+          if constexpr (VB == 8)
+            x = reinterpret_cast<const uint2 *>(vt)[p * 32 + lane];
+          else
+            x = reinterpret_cast<const uint2 *>(vt)[((p * (VB / 16) + j / 2) * 32 + lane) * 2 + j % 2];
+          w[p][0] = x.x ^ 0x80808080u;
+          w[p][1] = x.y ^ 0x80808080u;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t x0 = __byte_perm(w[0][c], w[1][c], 0x5140), x1 = __byte_perm(w[0][c], w[1][c], 0x7362);
+          const uint32_t y0 = __byte_perm(w[2][c], w[3][c], 0x5140), y1 = __byte_perm(w[2][c], w[3][c], 0x7362);
+          const uint32_t v0[4] = {biased_f16(x0, 0x4140), biased_f16(x0, 0x4342), biased_f16(y0, 0x4140), biased_f16(y0, 0x4342)};
+          const uint32_t v1[4] = {biased_f16(x1, 0x4140), biased_f16(x1, 0x4342), biased_f16(y1, 0x4140), biased_f16(y1, 0x4342)};
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              mma_16x8x16(o[n][j * 4 + c * 2], v0, pf[h][n]);
+              mma_16x8x16(o[n][j * 4 + c * 2 + 1], v1, pf[h][n]);
+            }
+        }
+      }
+      issue(i + (F::DEPTH - 1) * kWarps, slot == 0 ? F::DEPTH - 1 : slot - 1);  // the slot read a round before
+      if (++slot == F::DEPTH) slot = 0;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  }
+
+  // ---- join the warps: [warp][row][dimension] and (m, l) in the ring ----
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int off = 4; off <= 16; off <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], off);
+  constexpr int PITCH = DP + 4;
+  float *joined = reinterpret_cast<float *>(ring);
+  float *stats = joined + kWarps * 8 * PITCH;  // [warp][8 rows][2]
+  const float back = sv / kLift;
+  for (int n = 0; n < NB; ++n) {
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NB; ++q) {
+      if (q != n) continue;
+#pragma unroll
+      for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) joined[(warp * 8 + 2 * t + e % 2) * PITCH + VB * g + 2 * j + e / 2] = o[q][j][e];
+      if (g == 0)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          stats[(warp * 8 + 2 * t + e) * 2] = m[q][e];
+          stats[(warp * 8 + 2 * t + e) * 2 + 1] = l[q][e];
+        }
+    }
+    __syncthreads();
+    // warp w joins rows 2 w, 2 w + 1
+    for (uint32_t r = warp * 2; r < warp * 2 + 2; ++r) {
+      const uint32_t row = row0 + n * 8 + r;
+      if (row >= rows) break;
+      float top = neg_inf(), keep[kWarps], sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stats[(w * 8 + r) * 2]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float mw = stats[(w * 8 + r) * 2];
+        keep[w] = mw == neg_inf() ? 0.0f : ex2(mw - top);
+        // (a warp that saw nothing but NaN has a NaN sum under m = -inf)
+        sum += mw == neg_inf() ? stats[(w * 8 + r) * 2 + 1] : stats[(w * 8 + r) * 2 + 1] * keep[w];
+      }
+      const float scale = alone ? (sum == 0.0f ? 0.0f : back / sum) : back;
+      float *part = f.part + ((static_cast<size_t>(bh) * f.splits + split) * rows + row) * (a.dim + 2);
+      T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] +
+               static_cast<int64_t>(row / a.group) * a.out_strides[1] +
+               static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
+      for (uint32_t d = lane; d < a.dim; d += 32) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += keep[w] * joined[(w * 8 + r) * PITCH + d];
+        if (alone)
+          out[d] = from_float<T>(v * scale);
+        else
+          part[2 + d] = v * scale;
+      }
+      if (!alone && lane == 0) {
+        part[0] = sum;
+        part[1] = top;
+      }
+    }
+  }
+}
+
+// Joins the splits of a row: a warp a row.
+template <typename T>
+__global__ void __launch_bounds__(128) attend_join_kernel(const FewArgs f, uint32_t group_rows) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const ClearAttentionArgs &a = f.a;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.tokens * a.group;
+  const uint64_t id = static_cast<uint64_t>(blockIdx.x) * 4 + warp;
+  if (id >= static_cast<uint64_t>(a.batch) * a.heads * rows) return;
+  const uint32_t bh = static_cast<uint32_t>(id / rows), row = static_cast<uint32_t>(id % rows), kh = bh % a.heads, b = bh / a.heads;
+  const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens, given = a.lengths[b], len = given > most ? most : given;
+  const uint32_t end = group_end(a, len, min(row / group_rows * group_rows + group_rows, rows) - 1);
+  const uint32_t share = split_share(end, f.splits);
+  if (end <= share) return;  // written already
+  const uint32_t count = (end + share - 1) / share;
+  const float *part = f.part + (static_cast<size_t>(bh) * f.splits * rows + row) * (a.dim + 2);
+  const size_t step = static_cast<size_t>(rows) * (a.dim + 2);
+  float top = neg_inf(), sum = 0.0f, o[8] = {};
+  for (uint32_t s = lane; s < count; s += 32) top = fmaxf(top, part[s * step + 1]);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+#pragma unroll 4
+  for (uint32_t s = 0; s < count; ++s) {
+    const float ms = part[s * step + 1], ls = part[s * step];
+    const float keep = ms == neg_inf() ? 0.0f : ex2(ms - top);
+    sum += ms == neg_inf() ? ls : ls * keep;  // (NaN stays)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (lane + 32 * i < a.dim) o[i] += keep * part[s * step + 2 + lane + 32 * i];
+  }
+  T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
+           static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (lane + 32 * i < a.dim) out[lane + 32 * i] = from_float<T>(sum == 0.0f ? 0.0f : o[i] / sum);
+}
+
+// Splits of a sequence: shares of 512 positions where they are needed to fill the SMs several times over
+// (uneven lengths then even out), fewer where there are many sequences.
+uint32_t splits_of(const ClearAttentionArgs &a, uint32_t groups) {
+  const uint64_t most = (static_cast<uint64_t>(a.table_pitch) * a.page_tokens + 511) / 512;
+  const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * groups;
+  uint64_t want = (8192 + blocks - 1) / blocks;
+  if (want > most) want = most;
+  return static_cast<uint32_t>(want < 1 ? 1 : want > 1024 ? 1024 : want);
+}
+
+uint32_t group_rows_of(const ClearAttentionArgs &a) { return a.tokens * a.group <= 8 ? 8 : 16; }
+
+template <typename T, int DP, int NB>
+cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+  auto kern = attend_few_kernel<T, DP, NB>;
+  constexpr uint32_t join = (kWarps * 8 * (DP + 4) + kWarps * 8 * 2) * 4;
+  constexpr uint32_t smem = Few<DP>::RING > join ? Few<DP>::RING : join;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, 32 * kWarps, smem, s>>>(f);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || f.splits == 1) return e;
+  cudaLaunchConfig_t cfg = {};
+  const uint64_t rows = static_cast<uint64_t>(f.a.batch) * f.a.heads * f.a.tokens * f.a.group;
+  cfg.gridDim = dim3(static_cast<uint32_t>((rows + 3) / 4));
+  cfg.blockDim = dim3(128);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attend_join_kernel<T>, f, static_cast<uint32_t>(8 * NB));
+}
+
+template <typename T, int DP>
+cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+  return group_rows_of(f.a) == 8 ? launch<T, DP, 1>(f, s) : launch<T, DP, 2>(f, s);
+}
+
+template <typename T>
+cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+  if (f.a.dim <= 64) return launch<T, 64>(f, s);
+  if (f.a.dim <= 128) return launch<T, 128>(f, s);
+  return launch<T, 256>(f, s);
+}
+
+}  // namespace
+
+bool attend_few_takes(const ClearAttentionArgs &a) {
+  return a.dim % 16 == 0 && a.page_tokens % 16 == 0 &&
+         (reinterpret_cast<uintptr_t>(a.k_cache) | reinterpret_cast<uintptr_t>(a.v_cache) |
+          static_cast<uintptr_t>(a.cache_strides[0] | a.cache_strides[1] | a.cache_strides[2])) % 16 == 0;
+}
+
+size_t attend_few_bytes(const ClearAttentionArgs &a) {
+  const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a), splits = splits_of(a, (rows + gr - 1) / gr);
+  return splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * splits * rows * (a.dim + 2) * sizeof(float);
+}
+
+cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, cudaStream_t s) {
+  FewArgs f{a, static_cast<float *>(work), 1, 1};
+  const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a);
+  f.groups = (rows + gr - 1) / gr;
+  f.splits = splits_of(a, f.groups);
+  if (type == kOutF32) return launch<float>(f, s);
+  if (type == kOutF16) return launch<__half>(f, s);
+  return launch<__nv_bfloat16>(f, s);
+}
+
+}  // namespace rosetta
