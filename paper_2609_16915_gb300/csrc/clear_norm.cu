@@ -5,7 +5,7 @@
 // The factor 1/sqrt(..) is the same for a whole row, so with M = max |h g|
 //   s = M / sqrt(mean h^2 + eps) / 127  and  q = rint(h g 127 / M):
 // one reduction (a sum and a maximum together) serves the norm and the scale.
-// A block per token.
+// Bound by reading x and r and writing h and q once: a row stays in registers between the two.
 #include <stdint.h>
 
 #include "clear.h"
@@ -53,8 +53,80 @@ __device__ __forceinline__ int8_t quantised(float hg, const RowScale &r) {
   return static_cast<int8_t>(__float2int_rn((hg * r.up) * r.inv));  // (a NaN converts to 0)
 }
 
+// VEC consecutive elements of a row, as one access
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) Pack {
+  T v[VEC];
+};
+
+// The row in registers, NV packs a thread, read once.  WARP: a warp per token, eight tokens a block;
+// otherwise a block per token.
+template <typename T, int VEC, int NV, bool WARP>
+__global__ void __launch_bounds__(WARP ? 256 : 1024) norm_kernel(const ClearNormArgs a) {
+  __shared__ float2 parts[32];
+  const uint32_t tid = WARP ? threadIdx.x % 32 : threadIdx.x, threads = WARP ? 32 : blockDim.x;
+  const size_t t = WARP ? static_cast<size_t>(blockIdx.x) * 8 + threadIdx.x / 32 : blockIdx.x;
+  if (WARP && t >= a.tokens) return;
+  const T *x = static_cast<const T *>(a.x) + t * a.x_pitch;
+  const T *res = a.residual ? static_cast<const T *>(a.residual) + t * a.residual_pitch : nullptr;
+  T *sum = a.sum_out ? static_cast<T *>(a.sum_out) + t * a.sum_pitch : nullptr;
+  using P = Pack<T, VEC>;
+  float h[NV][VEC];  // h, then h g
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const uint32_t i = (tid + j * threads) * VEC;
+    P px{}, pr{};
+    if (i < a.width) {
+      px = *reinterpret_cast<const P *>(x + i);
+      if (res) pr = *reinterpret_cast<const P *>(res + i);
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) h[j][e] = res ? to_float(px.v[e]) + to_float(pr.v[e]) : to_float(px.v[e]);
+  }
+  float s = 0.0f, m = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const uint32_t i = (tid + j * threads) * VEC;
+    if (i < a.width) {
+      const Pack<float, VEC> g = *reinterpret_cast<const Pack<float, VEC> *>(a.gamma + i);
+      P out;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        out.v[e] = from_float<T>(h[j][e]);
+        s += h[j][e] * h[j][e];
+        h[j][e] *= g.v[e];
+        m = fmaxf(m, fabsf(h[j][e]));
+      }
+      if (sum) *reinterpret_cast<P *>(sum + i) = out;
+    }
+  }
+  if constexpr (WARP) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+  } else {
+    block_sum_max(s, m, parts);
+  }
+  const RowScale r = row_scale(s, m, a.width, a.eps);
+  int8_t *q = a.q + t * a.q_pitch;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const uint32_t i = (tid + j * threads) * VEC;
+    if (i < a.width) {
+      Pack<int8_t, VEC> out;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) out.v[e] = quantised(h[j][e], r);
+      *reinterpret_cast<Pack<int8_t, VEC> *>(q + i) = out;
+    }
+  }
+  if (tid == 0) a.scale[t] = r.scale;
+}
+
+// Rows too long for a block's registers are read twice (the second time from the L2 cache).
 template <typename T>
-__global__ void __launch_bounds__(256) norm_kernel(const ClearNormArgs a) {
+__global__ void __launch_bounds__(1024) norm_long_kernel(const ClearNormArgs a) {
   __shared__ float2 parts[32];
   const size_t t = blockIdx.x;
   const T *x = static_cast<const T *>(a.x) + t * a.x_pitch;
@@ -77,16 +149,45 @@ __global__ void __launch_bounds__(256) norm_kernel(const ClearNormArgs a) {
   if (threadIdx.x == 0) a.scale[t] = r.scale;
 }
 
+template <typename T, int VEC, int NV>
+cudaError_t launch_block(const ClearNormArgs &a, cudaStream_t s) {
+  const uint32_t threads = ((a.width + VEC * NV - 1) / (VEC * NV) + 31) / 32 * 32;
+  norm_kernel<T, VEC, NV, false><<<a.tokens, threads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+// A warp per token while four packs a lane hold the row (scalars: eight), then blocks of up to 512 threads with two, up to
+// 1024 with 32 elements each (scalars: 16).
+template <typename T, int VEC>
+cudaError_t launch_vec(const ClearNormArgs &a, cudaStream_t s) {
+  constexpr int SMALL = VEC == 1 ? 8 : 4, MID = VEC == 1 ? 8 : 2, LARGE = VEC == 1 ? 16 : 32 / VEC;
+  if (a.width <= 32u * VEC * SMALL) {
+    norm_kernel<T, VEC, SMALL, true><<<(a.tokens + 7) / 8, 256, 0, s>>>(a);
+    return cudaGetLastError();
+  }
+  if (a.width <= 512u * VEC * MID) return launch_block<T, VEC, MID>(a, s);
+  if (a.width <= 1024u * VEC * LARGE) return launch_block<T, VEC, LARGE>(a, s);
+  norm_long_kernel<T><<<a.tokens, 1024, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_type(const ClearNormArgs &a, cudaStream_t s) {
+  constexpr int VEC = 16 / sizeof(T);
+  const auto at = [](const void *p) { return reinterpret_cast<uintptr_t>(p); };
+  // (a pitch is used from the second row on only)
+  const int64_t pitches = a.tokens > 1 ? (a.x_pitch | a.q_pitch | (a.residual ? a.residual_pitch : 0) | (a.sum_out ? a.sum_pitch : 0)) : 0;
+  const bool wide = ((at(a.x) | at(a.residual) | at(a.sum_out)) & 15u) == 0 && (at(a.gamma) & (4 * VEC - 1)) == 0 &&
+                    (at(a.q) & (VEC - 1)) == 0 && pitches % VEC == 0 && a.width % VEC == 0;
+  return wide ? launch_vec<T, VEC>(a, s) : launch_vec<T, 1>(a, s);
+}
+
 }  // namespace
 
 cudaError_t launch_clear_norm(const ClearNormArgs &a, int type, cudaStream_t s) {
-  if (type == kOutF32)
-    norm_kernel<float><<<a.tokens, 256, 0, s>>>(a);
-  else if (type == kOutF16)
-    norm_kernel<__half><<<a.tokens, 256, 0, s>>>(a);
-  else
-    norm_kernel<__nv_bfloat16><<<a.tokens, 256, 0, s>>>(a);
-  return cudaGetLastError();
+  if (type == kOutF32) return launch_type<float>(a, s);
+  if (type == kOutF16) return launch_type<__half>(a, s);
+  return launch_type<__nv_bfloat16>(a, s);
 }
 
 }  // namespace rosetta
