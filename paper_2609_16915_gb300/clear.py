@@ -19,6 +19,10 @@ _FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _Strides = ctypes.c_int64 * 3
 
 
+# (the second creates a Stream object each time)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+
+
 class PackedWeights:
     """int8 weights [channels][inner] laid out for Clear.linear."""
 
@@ -29,6 +33,14 @@ class PackedWeights:
 def _need(ok, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _float_type(name, t, dims):
+    """Number of the tensor's float type."""
+    kind = _FLOATS.get(t.dtype)
+    if kind is None or t.dim() != dims:
+        raise ValueError(f"{name} must be a tensor of floats with {dims} dimensions")
+    return kind
 
 
 class Clear:
@@ -54,39 +66,40 @@ class Clear:
     # ---- checks shared by the calls ----
     def _at(self, name, t, dtype, shape, contiguous=False):
         """Address of tensor `t`: on this device, of the type and shape, last dimension contiguous."""
-        _need(isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == self.device,
-              f"{name} must be a tensor on CUDA device {self.device}")
+        if (t.get_device() == self.device and t.dtype == dtype and t.shape == shape
+                and (t.is_contiguous() or (not contiguous and t.stride(-1) == 1))):
+            return t.data_ptr()
+        _need(t.get_device() == self.device, f"{name} must be a tensor on CUDA device {self.device}")
         _need(t.dtype == dtype, f"{name} must be {dtype}, not {t.dtype}")
-        _need(tuple(t.shape) == shape, f"{name} must have shape {shape}, not {tuple(t.shape)}")
-        if contiguous:
-            _need(t.is_contiguous(), f"{name} must be contiguous")
-        else:
-            _need(shape[-1] <= 1 or t.stride(-1) == 1, f"the last dimension of {name} must be contiguous")
+        _need(t.shape == shape, f"{name} must have shape {shape}, not {tuple(t.shape)}")
+        _need(not contiguous, f"{name} must be contiguous")
+        _need(shape[-1] <= 1, f"the last dimension of {name} must be contiguous")
         return t.data_ptr()
 
     def _rows(self, name, t, dtype, rows, width):
         """(address, pitch) of a matrix."""
         at = self._at(name, t, dtype, (rows, width))
         pitch = t.stride(0) if rows > 1 else width
-        _need(pitch >= width, f"the rows of {name} must not overlap")
+        if pitch < width:
+            raise ValueError(f"the rows of {name} must not overlap")
         return at, pitch
 
     def _stream(self, stream):
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return _current_stream(self.device)
         return getattr(stream, "cuda_stream", stream)
 
     # ---- the C entry points ----
     def rosetta_clear_norm(self, x, gamma, q, scale, residual=None, sum_out=None, eps=1e-6, stream=None):
         """q, scale of the root-mean-square norm of x (+ residual) [tokens][width]; sum_out receives the sum."""
-        _need(x.dim() == 2 and x.dtype in _FLOATS, "x must be a float matrix")
-        (t, w), dt = x.shape, x.dtype
+        kind, dt = _float_type("x", x, 2), x.dtype
+        t, w = x.shape
         xp, xs = self._rows("x", x, dt, t, w)
         rp, rs = self._rows("residual", residual, dt, t, w) if residual is not None else (None, 0)
         sp, ss = self._rows("sum_out", sum_out, dt, t, w) if sum_out is not None else (None, 0)
         qp, qs = self._rows("q", q, torch.int8, t, w)
         _check("rosetta_clear_norm", self._L.rosetta_clear_norm(
-            self._h, _FLOATS[dt], xp, xs, rp, rs, self._at("gamma", gamma, torch.float32, (w,)), eps, t, w, sp, ss, qp, qs,
+            self._h, kind, xp, xs, rp, rs, self._at("gamma", gamma, torch.float32, (w,)), eps, t, w, sp, ss, qp, qs,
             self._at("scale", scale, torch.float32, (t,)), self._stream(stream)))
         return q, scale
 
@@ -118,9 +131,9 @@ class Clear:
     def rosetta_clear_linear(self, q, scale, weights, w_scale, out, bias=None, stream=None):
         """out [tokens][channels] = (q weights^T) scale w_scale + bias."""
         t, n, args = self._linear(q, scale, weights, w_scale, bias)
-        _need(out.dtype in _FLOATS, "out must hold floats")
+        kind = _float_type("out", out, 2)
         op, os = self._rows("out", out, out.dtype, t, n)
-        _check("rosetta_clear_linear", self._L.rosetta_clear_linear(*args, _FLOATS[out.dtype], op, os, self._stream(stream)))
+        _check("rosetta_clear_linear", self._L.rosetta_clear_linear(*args, kind, op, os, self._stream(stream)))
         return out
 
     def rosetta_clear_linear_codes(self, q, scale, weights, w_scale, code, bits, lo, hi, bias=None, table=None,
@@ -155,19 +168,19 @@ class Clear:
 
     def rosetta_clear_cache_append(self, k, v, k_cache, v_cache, k_scale, v_scale, page_table, first, stream=None):
         """Append k, v [batch][tokens][heads][dim] at positions first[b] .. to the caches [pages][heads][page][dim]."""
-        _need(k.dim() == 4 and k.dtype in _FLOATS, "k must be floats [batch][tokens][heads][dim]")
+        kind = _float_type("k", k, 4)
         shape = b, t, h, d = tuple(k.shape)
         kp, ks = self._strided("k", k, k.dtype, shape)
         vp, vs = self._strided("v", v, k.dtype, shape)
         cache = self._cache(k_cache, v_cache, k_scale, v_scale, page_table, b, h, d)
         _check("rosetta_clear_cache_append", self._L.rosetta_clear_cache_append(
-            self._h, _FLOATS[k.dtype], kp, ks, vp, vs, b, t, h, d, *cache, self._at("first", first, torch.int32, (b,)),
+            self._h, kind, kp, ks, vp, vs, b, t, h, d, *cache, self._at("first", first, torch.int32, (b,)),
             self._stream(stream)))
 
     def rosetta_clear_attention(self, q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out,
                                 softmax_scale=None, stream=None):
         """Causal attention of q [batch][tokens][query heads][dim] over the cache; softmax_scale: dim^-1/2 unless given."""
-        _need(q.dim() == 4 and q.dtype in _FLOATS, "q must be floats [batch][tokens][heads][dim]")
+        kind = _float_type("q", q, 4)
         shape = b, t, hq, d = tuple(q.shape)
         heads = k_cache.shape[1]
         _need(hq and heads and hq % heads == 0, "the query heads must be a multiple of the cached heads")
@@ -175,7 +188,7 @@ class Clear:
         op, os = self._strided("out", out, q.dtype, shape)
         cache = self._cache(k_cache, v_cache, k_scale, v_scale, page_table, b, heads, d)
         _check("rosetta_clear_attention", self._L.rosetta_clear_attention(
-            self._h, _FLOATS[q.dtype], qp, qs, b, t, heads, hq // heads, d, *cache,
+            self._h, kind, qp, qs, b, t, heads, hq // heads, d, *cache,
             self._at("lengths", lengths, torch.int32, (b,)), d ** -0.5 if softmax_scale is None else softmax_scale, op, os,
             self._stream(stream)))
         return out

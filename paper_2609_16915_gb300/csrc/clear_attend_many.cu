@@ -1,0 +1,565 @@
+// Causal attention over the paged 8-bit cache for many query rows: prompts.
+//
+// Bound by the products (4 D operations per row and visible position) and, as closely, by one exponential
+// per row and position (the special-function unit computes 16 a clock and SM: as long as the tensor cores'
+// 2048 clocks per 256 rows x 128 positions at D = 128).  tcgen05, scores, weights and outputs in tensor memory.
+//
+// A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
+// over the positions 128 at a time:
+//   8 convert warps  the 8-bit keys and values, straight from the pages to f16 in shared memory, both K-major:
+//                    keys [position][dimension] (exact, and with the sign of their scale), values transposed
+//                    by byte permutes to [dimension][position] and times their scale over the largest one
+//   MMA warp         S = Q K^T, 128 x 128 a tile; O += P V with P from tensor memory.  The tiles' products alternate, so
+//                    that one tile's softmax runs under the other's products
+//   2 x 4 softmax warps  a thread a row: scores from tensor memory, times the page's key scale and the row's
+//                    factor, 2^(s - m + 7) with the running maximum m raised only where a score passes it by 8
+//                    (then O is scaled down in place), P as f16 over the scores' columns
+// Rows and pages that are not seen have weight 0; a page whose scale is not a number has its values zero and its key scale
+// NaN, which reaches exactly the rows that see it.
+//
+// Every wait gives up after about two seconds and sets the error flag; the tensor memory is then left
+// allocated, because products may be in flight.
+#include <stdint.h>
+
+#include "clear.h"
+#include "dsmem.cuh"
+#include "tcgen.cuh"
+
+namespace rosetta {
+
+namespace {
+
+constexpr uint32_t ROWS = 128, POS = 128, SOFT_WARPS = 8, CONVERT_WARPS = 8, WARPS = 20;
+// registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out;
+// more than was launched would wait forever
+constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 160, CONVERT_REGS = 64, MMA_REGS = 32;
+static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
+                  WARPS * LAUNCH_REGS,
+              "register shares");
+constexpr float kRaise = 8.0f, kLift = 7.0f;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
+
+template <int DP>
+struct Many {
+  static constexpr uint32_t Q_TILE = ROWS * DP * 2, K_TILE = POS * DP * 2, V_TILE = DP / 8 * V_GROUP;
+  static constexpr uint32_t K_AT = 2 * Q_TILE, V_AT = K_AT + 2 * K_TILE, SMEM = V_AT + 2 * V_TILE;
+  static constexpr uint32_t O_COL = 256;  // S tiles: columns 0 and 128
+};
+
+__device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t half2_bits(__half2 h) { return *reinterpret_cast<const uint32_t *>(&h); }
+__device__ __forceinline__ __half2 bits_half2(uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); }
+
+// no swizzle, K-major: core matrices of 8 rows x 16 bytes, K-adjacent ones 128 bytes apart, groups of 8 rows
+// `group` bytes apart
+__device__ __forceinline__ uint64_t desc_of(uint32_t saddr, uint32_t group) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(128u >> 4) << 16) |
+         (static_cast<uint64_t>(group >> 4) << 32) | (1ull << 46);
+}
+
+// kind::f16: D f32, A and B f16, both K-major, M = 128
+__host__ __device__ constexpr uint32_t idesc(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(id), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(id), "r"(accumulate)
+      : "memory");
+}
+
+// 32 consecutive columns of this thread's lane (complete after tmem_wait_ld)
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+        "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+        "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_st32f(uint32_t taddr, const float *v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]),
+      "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]),
+      "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+          taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// this thread's shared-memory writes before the tensor cores' reads
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// mbar_wait that reads no clock where the phase is complete already
+__device__ __forceinline__ bool wait_quick(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done || mbar_wait(bar, parity);
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearAttentionArgs a, uint32_t row_blocks) {
+  using M = Many<DP>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  enum : uint32_t { QFULL = 0, KFULL = 1, KEMPTY = 3, VFULL = 5, VEMPTY = 7, SFULL = 9, PFULL = 11, ODONE = 13, BARS = 15 };
+  __shared__ __align__(8) uint64_t bars[BARS];
+  __shared__ uint32_t tmem_slot, s_fail;
+  __shared__ float s_ks[4][POS / 16];   // key scales of the tile's groups of 16 positions, four tiles back
+  __shared__ uint32_t s_skip[4][POS / 16];  // pages out of range
+  __shared__ float s_top[WARPS], s_up[2 * ROWS];
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
+  const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
+
+  // (the blocks with the most positions first)
+  const uint32_t bh = blockIdx.x % (a.batch * a.heads), kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t block = row_blocks - 1 - blockIdx.x / (a.batch * a.heads);
+  const uint32_t rows = a.tokens * a.group, row0 = block * (2 * ROWS);
+  int64_t len = a.lengths[b];
+  const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
+  if (len > most) {
+    if (threadIdx.x == 0) atomicMax(a.err_flag, 1u);
+    len = most;
+  }
+  const int64_t seen = len - a.tokens + 1 + (min(row0 + 2 * ROWS, rows) - 1) / a.group;
+  const uint32_t end = seen > 0 ? static_cast<uint32_t>(seen) : 0u, n = (end + POS - 1) / POS;
+  const uint32_t row_tiles = rows - row0 > ROWS ? 2 : 1;
+  const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
+
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (threadIdx.x == 0) {
+    s_fail = 0u;
+    mbar_init(bar(QFULL), SOFT_WARPS);
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(bar(KFULL + i), CONVERT_WARPS);
+      mbar_init(bar(KEMPTY + i), 1);
+      mbar_init(bar(VFULL + i), CONVERT_WARPS);
+      mbar_init(bar(VEMPTY + i), 1);
+      mbar_init(bar(SFULL + i), 2);
+      mbar_init(bar(PFULL + i), 4);
+      mbar_init(bar(ODONE + i), 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // the largest value scale of the pages seen
+  float sv = 1e-30f;
+  for (uint32_t p = threadIdx.x; p < (end + a.page_tokens - 1) / a.page_tokens; p += blockDim.x) {
+    const int32_t page = table[p];
+    if (page >= 0 && static_cast<uint32_t>(page) < a.pages) {
+      const float v = fabsf(a.v_scale[static_cast<size_t>(page) * a.heads + kh]);
+      if (v < -neg_inf()) sv = fmaxf(sv, v);
+    } else {
+      atomicMax(a.err_flag, 1u);
+    }
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, off));
+  if (lane == 0) s_top[warp] = sv;
+  fence_before();
+  __syncthreads();
+  fence_after();
+#pragma unroll
+  for (uint32_t w = 0; w < WARPS; ++w) sv = fmaxf(sv, s_top[w]);
+  const uint32_t tmem = tmem_slot;
+  const auto give_up = [&]() {
+    atomicExch(a.err_flag, 2u);
+    atomicExch(&s_fail, 1u);
+  };
+
+  if (warp < SOFT_WARPS) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
+    const uint32_t r = warp / 4, row_in = threadIdx.x % ROWS, row = row0 + r * ROWS + row_in;
+    const uint32_t lanes = ((warp % 4) * 32u) << 16;
+    const uint32_t s_col = tmem + lanes + r * POS, o_col = tmem + lanes + M::O_COL + r * DP;
+    // ---- the warp's 32 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
+    // eight dimensions at a time ----
+    const uint32_t qr = lane % 8, qc = lane / 8;
+    const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
+#pragma unroll 1
+    for (uint32_t g = 0; g < 4; ++g) {
+      const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr, rw = row0 + r * ROWS + in_tile;
+      const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
+                   static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
+      float x[DP / 32][8], top = 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < DP / 32; ++i) {
+        const uint32_t d = (qc + 4 * i) * 8;
+        const bool in = rw < rows && d < a.dim;  // (dim is a multiple of 16)
+        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+        if (in && wide_q) raw = *reinterpret_cast<const uint4 *>(q + d);
+        const T *el = reinterpret_cast<const T *>(&raw);
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+          x[i][e] = in ? to_float(wide_q ? el[e] : q[d + e]) : 0.0f;
+          top = fmaxf(top, fabsf(x[i][e]));
+        }
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
+      const float down = copysignf(__int_as_float((127 - ex) << 23), a.softmax_scale);
+      if (qc == 0) s_up[r * ROWS + in_tile] = __int_as_float((127 + ex) << 23);
+#pragma unroll
+      for (uint32_t i = 0; i < DP / 32; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) w[e] = half2_bits(__floats2half2_rn(x[i][2 * e] * down, x[i][2 * e + 1] * down));
+        *reinterpret_cast<uint4 *>(smem + r * M::Q_TILE + (in_tile >> 3) * (DP * 16) + (qc + 4 * i) * 128 + qr * 16) =
+            make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    fence_async();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(QFULL));
+    const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
+    const int32_t last = row < rows ? static_cast<int32_t>(len - a.tokens + row / a.group) : -1;
+    float m = neg_inf(), l = 0.0f;
+    if (r < row_tiles) {
+      for (uint32_t j = 0; j < n; ++j) {
+        const uint32_t buf = j % 4;
+        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + r), j & 1u))) {
+          give_up();
+          goto done;
+        }
+        fence_after();
+        float v[POS];
+#pragma unroll
+        for (uint32_t c = 0; c < POS; c += 32) tmem_ld32(s_col + c, v + c);
+        tmem_wait_ld();
+        float kf[POS / 16];
+        uint32_t skip = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < POS / 16; ++i) {
+          kf[i] = s_ks[buf][i] * factor;
+          skip |= s_skip[buf][i];
+        }
+        float top2 = neg_inf();
+        // (the same for the warp)
+        const bool part = __any_sync(0xffffffffu, skip != 0 || static_cast<int32_t>(j * POS + POS - 1) > last);
+        if (part) {
+#pragma unroll
+          for (uint32_t i = 0; i < POS; ++i) {
+            const bool in = static_cast<int32_t>(j * POS + i) <= last && !s_skip[buf][i / 16];
+            v[i] = in ? v[i] * kf[i / 16] : neg_inf();
+            top2 = fmaxf(top2, v[i]);
+          }
+#pragma unroll
+          for (uint32_t i = 0; i < POS / 16; ++i) kf[i] = 1.0f;
+        } else {
+#pragma unroll
+          for (uint32_t i = 0; i < POS / 16; ++i) {
+            float t = v[i * 16];
+#pragma unroll
+            for (uint32_t e = 1; e < 16; ++e) t = fmaxf(t, v[i * 16 + e]);
+            top2 = fmaxf(top2, t * kf[i]);
+          }
+        }
+        if (__any_sync(0xffffffffu, top2 > m + kRaise)) {
+          const float raised = fmaxf(m, top2), keep = m == neg_inf() ? 0.0f : ex2(m - raised);
+          m = raised;
+          l *= keep;
+          if (j > 0) {
+            if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (j - 1) & 1u))) {
+              give_up();
+              goto done;
+            }
+            fence_after();
+#pragma unroll 1
+            for (uint32_t c = 0; c < DP; c += 32) {
+              float o[32];
+              tmem_ld32(o_col + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (uint32_t e = 0; e < 32; ++e) o[e] *= keep;
+              tmem_st32f(o_col + c, o);
+            }
+            tmem_wait_st();
+          }
+        }
+        const float off = kLift - (m == neg_inf() ? 0.0f : m);
+#pragma unroll
+        for (uint32_t c = 0; c < POS; c += 32) {
+          uint32_t w[16];
+#pragma unroll
+          for (uint32_t e = 0; e < 32; e += 2) {
+            const float p0 = ex2(fmaf(v[c + e], kf[(c + e) / 16], off)), p1 = ex2(fmaf(v[c + e + 1], kf[(c + e) / 16], off));
+            l += p0 + p1;
+            w[e / 2] = half2_bits(__floats2half2_rn(p0, p1));
+          }
+          tmem_st16(s_col + c / 2, w);
+        }
+        tmem_wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(PFULL + r));
+      }
+      if (n > 0) {
+        if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (n - 1) & 1u))) {
+          give_up();
+          goto done;
+        }
+        fence_after();
+      }
+      T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
+               static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
+      const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
+      const float scale = sv / l;
+#pragma unroll 1
+      for (uint32_t c = 0; c < DP; c += 32) {
+        float o[32];
+        if (n > 0) {
+          tmem_ld32(o_col + c, o);
+          tmem_wait_ld();
+        }
+        if (row >= rows) continue;
+#pragma unroll
+        for (uint32_t e = 0; e < 32; ++e) o[e] = n == 0 || l == 0.0f ? 0.0f : o[e] * scale;
+        if (wide) {
+#pragma unroll
+          for (uint32_t e = 0; e < 32; e += 8) {
+            T x[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) x[i] = from_float<T>(o[e + i]);
+            if (c + e < a.dim) *reinterpret_cast<uint4 *>(out + c + e) = *reinterpret_cast<const uint4 *>(x);
+          }
+        } else {
+#pragma unroll
+          for (uint32_t e = 0; e < 32; ++e)
+            if (c + e < a.dim) out[c + e] = from_float<T>(o[e]);
+        }
+      }
+    }
+  } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
+    // ---- keys and values to f16: a warp 16 positions of each tile ----
+    const uint32_t w = warp - SOFT_WARPS;
+    constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
+    const uint32_t kr = lane % 8, kc = lane / 8;             // row of 8, chunk of four
+    const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
+    // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store phase
+    // write the eight rows of a core matrix: dimension (e + turn) % 4 of its four in round e.
+    const uint32_t turn = lane / 2 % 4;
+    const uint32_t sel[4] = {0x5140u, 0x6251u, 0x7362u, 0x4073u};
+    const uint32_t sel_a = turn == 0 ? sel[0] : turn == 1 ? sel[1] : turn == 2 ? sel[2] : sel[3];
+    const uint32_t sel_b = turn == 0 ? sel[2] : turn == 1 ? sel[3] : turn == 2 ? sel[0] : sel[1];
+    const auto page_of = [&](uint32_t j) {
+      const uint32_t p = j * POS + w * 16;
+      return p < end ? table[p / a.page_tokens] : -1;
+    };
+    uint4 kx[2][DP / 64];
+    uint32_t vx[VG][8];
+    float ks = 0.0f, vs = 0.0f;
+    bool skip = false;
+    int32_t page = n > 0 ? page_of(0) : -1;
+    const auto fetch = [&](uint32_t j) {
+      const uint32_t p = j * POS + w * 16;
+      const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
+      skip = p < end && !in;
+      const int64_t at = in ? page * a.cache_strides[0] + static_cast<int64_t>(kh) * a.cache_strides[1] +
+                                  static_cast<int64_t>(p % a.page_tokens) * a.cache_strides[2]
+                            : 0;
+      const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
+      ks = in ? a.k_scale[sc] : 0.0f;
+      vs = in ? a.v_scale[sc] : 0.0f;
+#pragma unroll
+      for (uint32_t g = 0; g < 2; ++g)
+#pragma unroll
+        for (uint32_t i = 0; i < DP / 64; ++i) {
+          const uint32_t d = (kc + 4 * i) * 16;
+          kx[g][i] = in && d < a.dim ? __ldg(reinterpret_cast<const uint4 *>(a.k_cache + at + (g * 8 + kr) * a.cache_strides[2] + d))
+                                     : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+      for (uint32_t g = 0; g < VG; ++g)
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+          vx[g][e] = in && quad * 4 < a.dim
+                         ? __ldg(reinterpret_cast<const uint32_t *>(a.v_cache + at + ((g + vsub) * 8 + e) * a.cache_strides[2] + quad * 4))
+                         : 0u;
+    };
+    if (n > 0) fetch(0);
+    if (n > 1) page = page_of(1);
+    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
+    for (uint32_t j = 0; j < n; ++j) {
+      const uint32_t buf = j % 2, par = (j / 2 - 1) & 1u;
+      if (j >= 2 && !__all_sync(0xffffffffu, wait_quick(bar(KEMPTY + buf), par))) {
+        give_up();
+        goto done;
+      }
+      const bool number = fabsf(vs) < -neg_inf();  // (a NaN or an infinity: no)
+      if (lane == 0) {
+        s_ks[j % 4][w] = number ? fabsf(ks) : __int_as_float(0x7fc00000);
+        s_skip[j % 4][w] = skip;
+      }
+      // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
+      const uint32_t sign = ks < 0.0f ? 0xbc00bc00u : 0x3c003c00u;
+      const __half2 sg = bits_half2(sign), so = __hneg2(__hmul2(sg, off));
+      unsigned char *kt = smem + M::K_AT + buf * M::K_TILE;
+#pragma unroll
+      for (uint32_t g = 0; g < 2; ++g)
+#pragma unroll
+        for (uint32_t i = 0; i < DP / 64; ++i) {
+          const uint32_t x[4] = {kx[g][i].x, kx[g][i].y, kx[g][i].z, kx[g][i].w};
+          uint32_t o[8];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            const uint32_t u = x[e] ^ 0x80808080u;
+            o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
+            o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
+          }
+          unsigned char *dst = kt + (w * 2 + g) * (DP * 16) + (kc + 4 * i) * 256 + kr * 16;
+          *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(KFULL + buf));
+      if (j >= 2 && !__all_sync(0xffffffffu, wait_quick(bar(VEMPTY + buf), par))) {
+        give_up();
+        goto done;
+      }
+      const __half2 vr = __float2half2_rn(number ? vs / sv : 0.0f);
+      unsigned char *vt = smem + M::V_AT + buf * M::V_TILE;
+#pragma unroll
+      for (uint32_t g = 0; g < VG; ++g) {
+        uint32_t o[4][4];  // [round][pair of positions]
+#pragma unroll
+        for (uint32_t p = 0; p < 4; ++p) {
+          const uint32_t x = vx[g][2 * p] ^ 0x80808080u, y = vx[g][2 * p + 1] ^ 0x80808080u;
+          const uint32_t t0 = __byte_perm(x, y, sel_a), t1 = __byte_perm(x, y, sel_b);
+          o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), vr));
+          o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), vr));
+          o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), vr));
+          o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), vr));
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t d = quad * 4 + (e + turn) % 4;
+          *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 2 + g + vsub) * 128 + (d & 7u) * 16) =
+              make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
+        }
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(VFULL + buf));
+      if (j + 1 < n) fetch(j + 1);
+      if (j + 2 < n) page = page_of(j + 2);
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
+    if (warp == SOFT_WARPS + CONVERT_WARPS && lane == 0 && n > 0) {
+      // ---- products ----
+      const auto scores = [&](uint32_t r, uint32_t buf) {
+        const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + buf * M::K_TILE, DP * 16);
+#pragma unroll
+        for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
+          mma_ss(tmem + r * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0);
+        mbar_arrive(bar(SFULL + r));  // (also passes on the page scales that came with the keys)
+        mma_commit(bar(SFULL + r));
+      };
+      bool ok = wait_quick(bar(QFULL), 0) && wait_quick(bar(KFULL), 0);
+      if (ok) {
+        fence_after();
+        for (uint32_t r = 0; r < row_tiles; ++r) scores(r, 0);
+        mma_commit(bar(KEMPTY));
+      }
+      for (uint32_t j = 0; j < n && ok; ++j) {
+        const uint32_t buf = j % 2, next = (j + 1) % 2;
+        for (uint32_t r = 0; r < row_tiles; ++r) {
+          ok = wait_quick(bar(PFULL + r), j & 1u) && wait_quick(bar(VFULL + buf), (j / 2) & 1u);
+          if (!ok) break;
+          fence_after();
+          const uint64_t vd = desc_of(base + M::V_AT + buf * M::V_TILE, V_GROUP);
+#pragma unroll
+          for (uint32_t k = 0; k < POS / 16; ++k)
+            mma_ts(tmem + M::O_COL + r * DP, tmem + r * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0);
+          mma_commit(bar(ODONE + r));
+          if (j + 1 < n) {
+            ok = wait_quick(bar(KFULL + next), ((j + 1) / 2) & 1u);
+            if (!ok) break;
+            fence_after();
+            scores(r, next);
+          }
+        }
+        if (!ok) break;
+        if (j + 1 < n) mma_commit(bar(KEMPTY + next));
+        mma_commit(bar(VEMPTY + buf));
+      }
+      // the last of what was committed
+      if (ok) ok = wait_quick(bar(VEMPTY + (n - 1) % 2), ((n - 1) / 2) & 1u);
+      if (!ok) give_up();
+    }
+  }
+done:
+  __syncwarp();
+  fence_before();
+  __syncthreads();
+  if (warp == 0 && s_fail == 0u)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+template <typename T, int DP>
+cudaError_t launch(const ClearAttentionArgs &a, cudaStream_t s) {
+  auto kern = attend_many_kernel<T, DP>;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
+  if (e != cudaSuccess) return e;
+  const uint32_t row_blocks = (a.tokens * a.group + 2 * ROWS - 1) / (2 * ROWS);
+  kern<<<a.batch * a.heads * row_blocks, WARPS * 32, Many<DP>::SMEM, s>>>(a, row_blocks);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool attend_many_takes(const ClearAttentionArgs &a, int type) {
+  return type != kOutF32 && a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 64 && attend_few_takes(a);
+}
+
+cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, cudaStream_t s) {
+  if (type == kOutF16) return a.dim <= 64 ? launch<__half, 64>(a, s) : launch<__half, 128>(a, s);
+  return a.dim <= 64 ? launch<__nv_bfloat16, 64>(a, s) : launch<__nv_bfloat16, 128>(a, s);
+}
+
+}  // namespace rosetta

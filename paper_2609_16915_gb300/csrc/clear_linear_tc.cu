@@ -51,7 +51,9 @@ struct Shape {
   // Registers a thread: 96 at launch for 20 warps (80 for 24), then 64 for the conversion, 32 for the
   // copy and MMA warps, the rest for the sums: 256 x 64 + 256 x 160 + 128 x 32 = 61440 of 61440
   // (512 x 64 + 128 x 168 + 128 x 32 = 58368 of 61440)
-  static constexpr uint32_t DRAIN_REGS = NT == 256 ? 160 : 168;
+  static constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, DRAIN_REGS = NT == 256 ? 160 : 168;
+  // (more than was launched would wait forever)
+  static_assert(CONVERT_WARPS * 64 + DRAIN_WARPS * DRAIN_REGS + 4 * 32 <= WARPS * LAUNCH_REGS, "register shares");
 };
 
 // Instruction descriptor, kind::f16: D f32, A and B f16, both K-major, M = 128.
