@@ -6,7 +6,7 @@
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
 // over the positions 128 at a time:
-//   8 convert warps  the 8-bit keys and values, straight from the pages to f16 in shared memory, both K-major:
+//   4 convert warps  the 8-bit keys and values, straight from the pages to f16 in shared memory, both K-major:
 //                    keys [position][dimension] (exact, and with the sign of their scale), values transposed
 //                    by byte permutes to [dimension][position] and times their scale over the largest one
 //   MMA warp         S = Q K^T, 128 x 128 a tile; O += P V with P from tensor memory.  The tiles' products alternate, so
@@ -29,10 +29,10 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 128, SOFT_WARPS = 8, CONVERT_WARPS = 8, WARPS = 20;
+constexpr uint32_t ROWS = 128, POS = 128, SOFT_WARPS = 8, CONVERT_WARPS = 4, WARPS = 16;
 // registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out;
 // more than was launched would wait forever
-constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 160, CONVERT_REGS = 64, MMA_REGS = 32;
+constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 184, CONVERT_REGS = 104, MMA_REGS = 40;
 static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
                   WARPS * LAUNCH_REGS,
               "register shares");
@@ -140,12 +140,13 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearAttentionArgs a, uint32_t row_blocks) {
   using M = Many<DP>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  enum : uint32_t { QFULL = 0, KFULL = 1, KEMPTY = 3, VFULL = 5, VEMPTY = 7, SFULL = 9, PFULL = 11, ODONE = 13, BARS = 15 };
+  // PFULL: of each row tile, the weights of the first 64 positions and of the rest
+  enum : uint32_t { QFULL = 0, KFULL = 1, KEMPTY = 3, VFULL = 5, VEMPTY = 7, SFULL = 9, PFULL = 11, ODONE = 15, BARS = 17 };
   __shared__ __align__(8) uint64_t bars[BARS];
   __shared__ uint32_t tmem_slot, s_fail;
   __shared__ float s_ks[4][POS / 16];   // key scales of the tile's groups of 16 positions, four tiles back
   __shared__ uint32_t s_skip[4][POS / 16];  // pages out of range
-  __shared__ float s_top[WARPS], s_up[2 * ROWS];
+  __shared__ float s_top[CONVERT_WARPS], s_sv, s_up[2 * ROWS];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
@@ -165,6 +166,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   const uint32_t row_tiles = rows - row0 > ROWS ? 2 : 1;
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
 
+  if (n == 0) {  // no row of the block has a position: zeros
+    for (uint32_t i = warp; i < min(2 * ROWS, rows - row0); i += WARPS) {
+      const uint32_t row = row0 + i;
+      T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
+               static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
+      for (uint32_t d = lane; d < a.dim; d += 32) out[d] = from_float<T>(0.0f);
+    }
+    return;
+  }
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512)
                  : "memory");
@@ -179,30 +189,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       mbar_init(bar(VFULL + i), CONVERT_WARPS);
       mbar_init(bar(VEMPTY + i), 1);
       mbar_init(bar(SFULL + i), 2);
-      mbar_init(bar(PFULL + i), 4);
+      mbar_init(bar(PFULL + 2 * i), 4);
+      mbar_init(bar(PFULL + 2 * i + 1), 4);
       mbar_init(bar(ODONE + i), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // the largest value scale of the pages seen
-  float sv = 1e-30f;
-  for (uint32_t p = threadIdx.x; p < (end + a.page_tokens - 1) / a.page_tokens; p += blockDim.x) {
-    const int32_t page = table[p];
-    if (page >= 0 && static_cast<uint32_t>(page) < a.pages) {
-      const float v = fabsf(a.v_scale[static_cast<size_t>(page) * a.heads + kh]);
-      if (v < -neg_inf()) sv = fmaxf(sv, v);
-    } else {
-      atomicMax(a.err_flag, 1u);
-    }
-  }
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, off));
-  if (lane == 0) s_top[warp] = sv;
   fence_before();
   __syncthreads();
   fence_after();
-#pragma unroll
-  for (uint32_t w = 0; w < WARPS; ++w) sv = fmaxf(sv, s_top[w]);
   const uint32_t tmem = tmem_slot;
   const auto give_up = [&]() {
     atomicExch(a.err_flag, 2u);
@@ -269,32 +264,32 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
 #pragma unroll
         for (uint32_t c = 0; c < POS; c += 32) tmem_ld32(s_col + c, v + c);
         tmem_wait_ld();
-        float kf[POS / 16];
         uint32_t skip = 0;
 #pragma unroll
-        for (uint32_t i = 0; i < POS / 16; ++i) {
-          kf[i] = s_ks[buf][i] * factor;
-          skip |= s_skip[buf][i];
-        }
+        for (uint32_t i = 0; i < POS / 16; ++i) skip |= s_skip[buf][i];
         float top2 = neg_inf();
         // (the same for the warp)
         const bool part = __any_sync(0xffffffffu, skip != 0 || static_cast<int32_t>(j * POS + POS - 1) > last);
         if (part) {
 #pragma unroll
-          for (uint32_t i = 0; i < POS; ++i) {
-            const bool in = static_cast<int32_t>(j * POS + i) <= last && !s_skip[buf][i / 16];
-            v[i] = in ? v[i] * kf[i / 16] : neg_inf();
-            top2 = fmaxf(top2, v[i]);
-          }
+          for (uint32_t i = 0; i < POS / 16; ++i) {
+            const float kf = s_ks[buf][i] * factor;
+            const bool out = s_skip[buf][i] != 0;
 #pragma unroll
-          for (uint32_t i = 0; i < POS / 16; ++i) kf[i] = 1.0f;
+            for (uint32_t e = 0; e < 16; ++e) {
+              const bool in = static_cast<int32_t>(j * POS + i * 16 + e) <= last && !out;
+              v[i * 16 + e] = in ? v[i * 16 + e] * kf : neg_inf();
+              top2 = fmaxf(top2, v[i * 16 + e]);
+            }
+          }
         } else {
 #pragma unroll
           for (uint32_t i = 0; i < POS / 16; ++i) {
-            float t = v[i * 16];
+            float t[4];
 #pragma unroll
-            for (uint32_t e = 1; e < 16; ++e) t = fmaxf(t, v[i * 16 + e]);
-            top2 = fmaxf(top2, t * kf[i]);
+            for (uint32_t e = 0; e < 4; ++e)
+              t[e] = fmaxf(fmaxf(v[i * 16 + e], v[i * 16 + 4 + e]), fmaxf(v[i * 16 + 8 + e], v[i * 16 + 12 + e]));
+            top2 = fmaxf(top2, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * (s_ks[buf][i] * factor));
           }
         }
         if (__any_sync(0xffffffffu, top2 > m + kRaise)) {
@@ -320,43 +315,44 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
           }
         }
         const float off = kLift - (m == neg_inf() ? 0.0f : m);
+        float sum[4] = {};
 #pragma unroll
         for (uint32_t c = 0; c < POS; c += 32) {
           uint32_t w[16];
 #pragma unroll
           for (uint32_t e = 0; e < 32; e += 2) {
-            const float p0 = ex2(fmaf(v[c + e], kf[(c + e) / 16], off)), p1 = ex2(fmaf(v[c + e + 1], kf[(c + e) / 16], off));
-            l += p0 + p1;
+            const float kf = part ? 1.0f : s_ks[buf][(c + e) / 16] * factor;
+            const float p0 = ex2(fmaf(v[c + e], kf, off)), p1 = ex2(fmaf(v[c + e + 1], kf, off));
+            sum[e / 2 % 4] += p0 + p1;
             w[e / 2] = half2_bits(__floats2half2_rn(p0, p1));
           }
           tmem_st16(s_col + c / 2, w);
+          if (c % 64 == 32) {
+            tmem_wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(PFULL + 2 * r + c / 64));
+          }
         }
-        tmem_wait_st();
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(PFULL + r));
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
-      if (n > 0) {
-        if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (n - 1) & 1u))) {
-          give_up();
-          goto done;
-        }
-        fence_after();
+      if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (n - 1) & 1u))) {
+        give_up();
+        goto done;
       }
+      fence_after();
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
-      const float scale = sv / l;
+      const float scale = s_sv / l;
 #pragma unroll 1
       for (uint32_t c = 0; c < DP; c += 32) {
         float o[32];
-        if (n > 0) {
-          tmem_ld32(o_col + c, o);
-          tmem_wait_ld();
-        }
+        tmem_ld32(o_col + c, o);
+        tmem_wait_ld();
         if (row >= rows) continue;
 #pragma unroll
-        for (uint32_t e = 0; e < 32; ++e) o[e] = n == 0 || l == 0.0f ? 0.0f : o[e] * scale;
+        for (uint32_t e = 0; e < 32; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
         if (wide) {
 #pragma unroll
           for (uint32_t e = 0; e < 32; e += 8) {
@@ -374,10 +370,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
-    // ---- keys and values to f16: a warp 16 positions of each tile ----
+    // ---- keys and values to f16: a warp 32 positions of each tile, two groups of 16 with a page each ----
     const uint32_t w = warp - SOFT_WARPS;
-    constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
-    const uint32_t kr = lane % 8, kc = lane / 8;             // row of 8, chunk of four
+    constexpr uint32_t VG = DP == 128 ? 4 : 2;  // groups of 8 positions that a lane takes in turn
+    const uint32_t kr = lane % 8, kc = lane / 8;  // row of 8, chunk of four
     const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
     // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store phase
     // write the eight rows of a core matrix: dimension (e + turn) % 4 of its four in round e.
@@ -385,43 +381,92 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     const uint32_t sel[4] = {0x5140u, 0x6251u, 0x7362u, 0x4073u};
     const uint32_t sel_a = turn == 0 ? sel[0] : turn == 1 ? sel[1] : turn == 2 ? sel[2] : sel[3];
     const uint32_t sel_b = turn == 0 ? sel[2] : turn == 1 ? sel[3] : turn == 2 ? sel[0] : sel[1];
-    const auto page_of = [&](uint32_t j) {
-      const uint32_t p = j * POS + w * 16;
-      return p < end ? table[p / a.page_tokens] : -1;
-    };
-    uint4 kx[2][DP / 64];
+    uint4 kx[4][DP / 64];
     uint32_t vx[VG][8];
-    float ks = 0.0f, vs = 0.0f;
-    bool skip = false;
-    int32_t page = n > 0 ? page_of(0) : -1;
-    const auto fetch = [&](uint32_t j) {
-      const uint32_t p = j * POS + w * 16;
-      const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
-      skip = p < end && !in;
-      const int64_t at = in ? page * a.cache_strides[0] + static_cast<int64_t>(kh) * a.cache_strides[1] +
-                                  static_cast<int64_t>(p % a.page_tokens) * a.cache_strides[2]
-                            : 0;
-      const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
-      ks = in ? a.k_scale[sc] : 0.0f;
-      vs = in ? a.v_scale[sc] : 0.0f;
+    float ks[2] = {}, vs[2] = {};
+    bool skip[2] = {};
+    // the next tile to fetch: its groups' pages, the page's slot in the list and the first row in it
+    int32_t page[2] = {-1, -1};
+    uint32_t slot[2], row[2];
+    int64_t at[2];  // of the group's first row, less the cache
+    const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens;
+    const uint32_t slots_end = (end + a.page_tokens - 1) / a.page_tokens;
 #pragma unroll
-      for (uint32_t g = 0; g < 2; ++g)
+    for (uint32_t i = 0; i < 2; ++i) {
+      slot[i] = (w * 32 + i * 16) / a.page_tokens;
+      row[i] = (w * 32 + i * 16) % a.page_tokens;
+      page[i] = slot[i] < slots_end ? table[slot[i]] : -1;
+    }
+    const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
+    const auto locate = [&]() {
 #pragma unroll
-        for (uint32_t i = 0; i < DP / 64; ++i) {
-          const uint32_t d = (kc + 4 * i) * 16;
-          kx[g][i] = in && d < a.dim ? __ldg(reinterpret_cast<const uint4 *>(a.k_cache + at + (g * 8 + kr) * a.cache_strides[2] + d))
-                                     : make_uint4(0u, 0u, 0u, 0u);
+      for (uint32_t i = 0; i < 2; ++i)
+        at[i] = page[i] * a.cache_strides[0] + head_at + static_cast<int64_t>(row[i]) * a.cache_strides[2];
+    };
+    const auto advance = [&]() {
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        slot[i] += slots;
+        row[i] += more;
+        if (row[i] >= a.page_tokens) {
+          row[i] -= a.page_tokens;
+          ++slot[i];
         }
+        page[i] = slot[i] < slots_end ? table[slot[i]] : -1;
+      }
+    };
+    const auto valid = [&](uint32_t i) { return page[i] >= 0 && static_cast<uint32_t>(page[i]) < a.pages; };
+    const auto fetch_keys = [&]() {
 #pragma unroll
-      for (uint32_t g = 0; g < VG; ++g)
+      for (uint32_t i = 0; i < 2; ++i) {
+        const bool in = valid(i);
+        const int8_t *src = a.k_cache + (in ? at[i] + kr * a.cache_strides[2] + kc * 16 : 0);
+        skip[i] = slot[i] < slots_end && !in;
+        ks[i] = in ? a.k_scale[static_cast<size_t>(page[i]) * a.heads + kh] : 0.0f;
+        vs[i] = in ? a.v_scale[static_cast<size_t>(page[i]) * a.heads + kh] : 0.0f;
+#pragma unroll
+        for (uint32_t g = 0; g < 2; ++g)
+#pragma unroll
+          for (uint32_t c = 0; c < DP / 64; ++c) {
+            const uint32_t d = (kc + 4 * c) * 16;
+            kx[i * 2 + g][c] = in && d < a.dim ? __ldg(reinterpret_cast<const uint4 *>(src + g * 8 * a.cache_strides[2] + c * 64))
+                                               : make_uint4(0u, 0u, 0u, 0u);
+          }
+      }
+    };
+    const auto fetch_values = [&]() {
+#pragma unroll
+      for (uint32_t g = 0; g < VG; ++g) {
+        const uint32_t i = g * 2 / VG;  // (a lane's groups: two of each 16 positions, or one by its half of the warp)
+        const bool in = valid(i) && quad * 4 < a.dim;
+        const int8_t *src = a.v_cache + (in ? at[i] + (DP == 128 ? g % 2 * 8 : vsub * 8) * a.cache_strides[2] + quad * 4 : 0);
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e)
-          vx[g][e] = in && quad * 4 < a.dim
-                         ? __ldg(reinterpret_cast<const uint32_t *>(a.v_cache + at + ((g + vsub) * 8 + e) * a.cache_strides[2] + quad * 4))
-                         : 0u;
+          vx[g][e] = in ? __ldg(reinterpret_cast<const uint32_t *>(src + e * a.cache_strides[2])) : 0u;
+      }
     };
-    if (n > 0) fetch(0);
-    if (n > 1) page = page_of(1);
+    locate();
+    fetch_keys();
+    fetch_values();
+    // the largest value scale of the pages seen
+    float sv = 1e-30f;
+    for (uint32_t p = threadIdx.x - SOFT_WARPS * 32; p < (end + a.page_tokens - 1) / a.page_tokens; p += CONVERT_WARPS * 32) {
+      const int32_t id = table[p];
+      if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
+        const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
+        if (v < -neg_inf()) sv = fmaxf(sv, v);
+      } else {
+        atomicMax(a.err_flag, 1u);
+      }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, off));
+    if (lane == 0) s_top[w] = sv;
+    asm volatile("bar.sync 1, %0;" ::"n"(CONVERT_WARPS * 32) : "memory");
+#pragma unroll
+    for (uint32_t i = 0; i < CONVERT_WARPS; ++i) sv = fmaxf(sv, s_top[i]);
+    if (threadIdx.x == SOFT_WARPS * 32) s_sv = sv;
+    advance();
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
     for (uint32_t j = 0; j < n; ++j) {
       const uint32_t buf = j % 2, par = (j / 2 - 1) & 1u;
@@ -429,20 +474,24 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         give_up();
         goto done;
       }
-      const bool number = fabsf(vs) < -neg_inf();  // (a NaN or an infinity: no)
-      if (lane == 0) {
-        s_ks[j % 4][w] = number ? fabsf(ks) : __int_as_float(0x7fc00000);
-        s_skip[j % 4][w] = skip;
+      __half2 vr[2];
+#pragma unroll
+      for (uint32_t i = 0; i < 2; ++i) {
+        const bool number = fabsf(vs[i]) < -neg_inf();  // (a NaN or an infinity: no)
+        if (lane == 0) {
+          s_ks[j % 4][w * 2 + i] = number ? fabsf(ks[i]) : __int_as_float(0x7fc00000);
+          s_skip[j % 4][w * 2 + i] = skip[i];
+        }
+        vr[i] = __float2half2_rn(number ? vs[i] / sv : 0.0f);
       }
       // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
-      const uint32_t sign = ks < 0.0f ? 0xbc00bc00u : 0x3c003c00u;
-      const __half2 sg = bits_half2(sign), so = __hneg2(__hmul2(sg, off));
       unsigned char *kt = smem + M::K_AT + buf * M::K_TILE;
 #pragma unroll
-      for (uint32_t g = 0; g < 2; ++g)
+      for (uint32_t g = 0; g < 4; ++g) {
+        const __half2 sg = bits_half2(ks[g / 2] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
 #pragma unroll
-        for (uint32_t i = 0; i < DP / 64; ++i) {
-          const uint32_t x[4] = {kx[g][i].x, kx[g][i].y, kx[g][i].z, kx[g][i].w};
+        for (uint32_t c = 0; c < DP / 64; ++c) {
+          const uint32_t x[4] = {kx[g][c].x, kx[g][c].y, kx[g][c].z, kx[g][c].w};
           uint32_t o[8];
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) {
@@ -450,47 +499,54 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
             o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
             o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
           }
-          unsigned char *dst = kt + (w * 2 + g) * (DP * 16) + (kc + 4 * i) * 256 + kr * 16;
+          unsigned char *dst = kt + (w * 4 + g) * (DP * 16) + (kc + 4 * c) * 256 + kr * 16;
           *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
           *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
         }
+      }
       fence_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KFULL + buf));
+      // the next tile's keys on their way while the values are done, and the next values meanwhile
+      if (j + 1 < n) {
+        locate();
+        fetch_keys();
+      }
       if (j >= 2 && !__all_sync(0xffffffffu, wait_quick(bar(VEMPTY + buf), par))) {
         give_up();
         goto done;
       }
-      const __half2 vr = __float2half2_rn(number ? vs / sv : 0.0f);
       unsigned char *vt = smem + M::V_AT + buf * M::V_TILE;
 #pragma unroll
       for (uint32_t g = 0; g < VG; ++g) {
+        const uint32_t pos8 = DP == 128 ? g : g * 2 + vsub;  // group of 8 positions of the warp's four
+        const __half2 ratio = vr[g * 2 / VG];
         uint32_t o[4][4];  // [round][pair of positions]
 #pragma unroll
         for (uint32_t p = 0; p < 4; ++p) {
           const uint32_t x = vx[g][2 * p] ^ 0x80808080u, y = vx[g][2 * p + 1] ^ 0x80808080u;
           const uint32_t t0 = __byte_perm(x, y, sel_a), t1 = __byte_perm(x, y, sel_b);
-          o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), vr));
-          o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), vr));
-          o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), vr));
-          o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), vr));
+          o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
+          o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
+          o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
+          o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
         }
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) {
           const uint32_t d = quad * 4 + (e + turn) % 4;
-          *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 2 + g + vsub) * 128 + (d & 7u) * 16) =
+          *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 4 + pos8) * 128 + (d & 7u) * 16) =
               make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
         }
       }
       fence_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(VFULL + buf));
-      if (j + 1 < n) fetch(j + 1);
-      if (j + 2 < n) page = page_of(j + 2);
+      if (j + 1 < n) fetch_values();
+      advance();
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
-    if (warp == SOFT_WARPS + CONVERT_WARPS && lane == 0 && n > 0) {
+    if (warp == SOFT_WARPS + CONVERT_WARPS && lane == 0) {
       // ---- products ----
       const auto scores = [&](uint32_t r, uint32_t buf) {
         const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + buf * M::K_TILE, DP * 16);
@@ -509,13 +565,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       for (uint32_t j = 0; j < n && ok; ++j) {
         const uint32_t buf = j % 2, next = (j + 1) % 2;
         for (uint32_t r = 0; r < row_tiles; ++r) {
-          ok = wait_quick(bar(PFULL + r), j & 1u) && wait_quick(bar(VFULL + buf), (j / 2) & 1u);
-          if (!ok) break;
-          fence_after();
+          ok = wait_quick(bar(VFULL + buf), (j / 2) & 1u);
           const uint64_t vd = desc_of(base + M::V_AT + buf * M::V_TILE, V_GROUP);
 #pragma unroll
-          for (uint32_t k = 0; k < POS / 16; ++k)
-            mma_ts(tmem + M::O_COL + r * DP, tmem + r * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0);
+          for (uint32_t half = 0; half < 2; ++half) {
+            ok = ok && wait_quick(bar(PFULL + 2 * r + half), j & 1u);
+            if (!ok) break;
+            fence_after();
+#pragma unroll
+            for (uint32_t k = half * (POS / 32); k < (half + 1) * (POS / 32); ++k)
+              mma_ts(tmem + M::O_COL + r * DP, tmem + r * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0);
+          }
+          if (!ok) break;
           mma_commit(bar(ODONE + r));
           if (j + 1 < n) {
             ok = wait_quick(bar(KFULL + next), ((j + 1) / 2) & 1u);
