@@ -5,20 +5,22 @@
 // 2048 clocks per 256 rows x 128 positions at D = 128).  tcgen05, scores, weights and outputs in tensor memory.
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
-// over the positions 128 at a time:
-//   4 convert warps  the 8-bit keys and values, straight from the pages to f16 in shared memory, both K-major:
-//                    keys [position][dimension] (exact, and with the sign of their scale), values transposed
-//                    by byte permutes to [dimension][position] and times their scale over the largest one
-//   MMA warp         S = Q K^T, 128 x 128 a tile; O += P V with P from tensor memory.  The tiles' products alternate, so
-//                    that one tile's softmax runs under the other's products
+// over the positions 64 at a time:
+//   4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
+//                    in shared memory, both K-major: keys [position][dimension] (exact, and with the sign of their
+//                    scale), values transposed by byte permutes to [dimension][position] and times their scale over the
+//                    largest one
+//   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory
 //   2 x 4 softmax warps  a thread a row: scores from tensor memory, times the page's key scale and the row's
 //                    factor, 2^(s - m + 7) with the running maximum m raised only where a score passes it by 8
 //                    (then O is scaled down in place), P as f16 over the scores' columns
+// With two score tiles a row tile, one row tile's next scores are there when its softmax is done: the handing over
+// between warps and tensor cores (about 900 clocks a round) runs under the exponentials.
 // Rows and pages that are not seen have weight 0; a page whose scale is not a number has its values zero and its key scale
 // NaN, which reaches exactly the rows that see it.
 //
-// Every wait gives up after about two seconds and sets the error flag; the tensor memory is then left
-// allocated, because products may be in flight.
+// Every wait gives up after about two seconds and sets the error flag; the block then waits (again bounded) for the
+// products it issued before it frees the tensor memory.
 #include <stdint.h>
 
 #include "clear.h"
@@ -29,22 +31,18 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 128, SOFT_WARPS = 8, CONVERT_WARPS = 4, WARPS = 16;
-// registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out;
-// more than was launched would wait forever
-constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 184, CONVERT_REGS = 104, MMA_REGS = 40;
-static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
-                  WARPS * LAUNCH_REGS,
-              "register shares");
+constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 8, CONVERT_WARPS = 4, WARPS = 16;
+constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
 
 template <int DP>
 struct Many {
-  static constexpr uint32_t Q_TILE = ROWS * DP * 2, K_TILE = POS * DP * 2, V_TILE = DP / 8 * V_GROUP;
-  static constexpr uint32_t K_AT = 2 * Q_TILE, V_AT = K_AT + 2 * K_TILE, SMEM = V_AT + 2 * V_TILE;
-  static constexpr uint32_t O_COL = 256;  // S tiles: columns 0 and 128
+  static constexpr uint32_t Q_TILE = ROWS * DP * 2, K_TILE = POS * DP * 2, V_TILE = DP / 8 * V_GROUP, RAW = POS * DP;
+  static constexpr uint32_t K_AT = 2 * Q_TILE, V_AT = K_AT + RING * K_TILE, RAW_AT = V_AT + RING * V_TILE;
+  static constexpr uint32_t SMEM = RAW_AT + STAGED * 2 * RAW;
+  static constexpr uint32_t O_COL = 4 * POS;  // score tiles of the two row tiles: two of 64 columns each
 };
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -68,19 +66,35 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, uint32_t group) {
 // kind::f16: D f32, A and B f16, both K-major, M = 128
 __host__ __device__ constexpr uint32_t idesc(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+// One lane of the warp, the same each time.  The MMA warp runs converged and its instructions are predicated on this
+// lane, so that descriptors stay in uniform registers: with one lane branching off, issuing a product cost about 60 clocks.
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t accumulate, uint32_t elect) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elect)
       : "memory");
 }
 
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate, uint32_t elect) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(id), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(id), "r"(accumulate), "r"(elect)
+      : "memory");
+}
+
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t elect) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(elect)
       : "memory");
 }
 
@@ -136,16 +150,37 @@ __device__ __forceinline__ bool wait_quick(uint32_t bar, uint32_t parity) {
   return done || mbar_wait(bar, parity);
 }
 
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool valid) {
+  const uint32_t size = valid ? 16 : 0;  // (nothing is read for 0: zeros)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearAttentionArgs a, uint32_t row_blocks) {
   using M = Many<DP>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  // PFULL: of each row tile, the weights of the first 64 positions and of the rest
-  enum : uint32_t { QFULL = 0, KFULL = 1, KEMPTY = 3, VFULL = 5, VEMPTY = 7, SFULL = 9, PFULL = 11, ODONE = 15, BARS = 17 };
+  // USED: the values of tile j and the keys of tile j + 2; SFULL, PFULL: of each row tile, its two score tiles;
+  // LAST, BEFORE: the products of the last tile's weights and of the one before it; FIRST: the scores of the first two
+  // tiles; FREE: everything issued, after a wait that gave up
+  enum : uint32_t {
+    QFULL = 0,
+    KFULL = 1,
+    VFULL = KFULL + RING,
+    USED = VFULL + RING,
+    SFULL = USED + RING,
+    PFULL = SFULL + 4,
+    BEFORE = PFULL + 4,
+    LAST = BEFORE + 2,
+    FIRST = LAST + 2,
+    FREE,
+    BARS
+  };
   __shared__ __align__(8) uint64_t bars[BARS];
   __shared__ uint32_t tmem_slot, s_fail;
-  __shared__ float s_ks[4][POS / 16];   // key scales of the tile's groups of 16 positions, four tiles back
-  __shared__ uint32_t s_skip[4][POS / 16];  // pages out of range
+  // of the last eight tiles (the conversion is at most four ahead of a softmax), by groups of 16 positions: key
+  // scales, pages out of range
+  __shared__ float s_ks[8][POS / 16];
+  __shared__ uint32_t s_skip[8][POS / 16];
   __shared__ float s_top[CONVERT_WARPS], s_sv, s_up[2 * ROWS];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
@@ -183,15 +218,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   if (threadIdx.x == 0) {
     s_fail = 0u;
     mbar_init(bar(QFULL), SOFT_WARPS);
-    for (uint32_t i = 0; i < 2; ++i) {
+    for (uint32_t i = 0; i < RING; ++i) {
       mbar_init(bar(KFULL + i), CONVERT_WARPS);
-      mbar_init(bar(KEMPTY + i), 1);
       mbar_init(bar(VFULL + i), CONVERT_WARPS);
-      mbar_init(bar(VEMPTY + i), 1);
+      mbar_init(bar(USED + i), 1);
+    }
+    for (uint32_t i = 0; i < 4; ++i) {
       mbar_init(bar(SFULL + i), 2);
-      mbar_init(bar(PFULL + 2 * i), 4);
-      mbar_init(bar(PFULL + 2 * i + 1), 4);
-      mbar_init(bar(ODONE + i), 1);
+      mbar_init(bar(PFULL + i), 4);
+    }
+    mbar_init(bar(FIRST), 1);
+    mbar_init(bar(FREE), 1);
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init(bar(BEFORE + i), 1);
+      mbar_init(bar(LAST + i), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -205,10 +245,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   };
 
   if (warp < SOFT_WARPS) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
     const uint32_t r = warp / 4, row_in = threadIdx.x % ROWS, row = row0 + r * ROWS + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
-    const uint32_t s_col = tmem + lanes + r * POS, o_col = tmem + lanes + M::O_COL + r * DP;
+    const uint32_t o_col = tmem + lanes + M::O_COL + r * DP;
     // ---- the warp's 32 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
     // eight dimensions at a time ----
     const uint32_t qr = lane % 8, qc = lane / 8;
@@ -254,8 +293,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     float m = neg_inf(), l = 0.0f;
     if (r < row_tiles) {
       for (uint32_t j = 0; j < n; ++j) {
-        const uint32_t buf = j % 4;
-        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + r), j & 1u))) {
+        const uint32_t buf = j % 8, two = r * 2 + j % 2, s_col = tmem + lanes + two * POS;
+        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (j / 2) & 1u))) {
           give_up();
           goto done;
         }
@@ -297,7 +336,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
           m = raised;
           l *= keep;
           if (j > 0) {
-            if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (j - 1) & 1u))) {
+            // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
+            const uint32_t next = r * 2 + (j + 1) % 2;
+            if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
               give_up();
               goto done;
             }
@@ -327,16 +368,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
             w[e / 2] = half2_bits(__floats2half2_rn(p0, p1));
           }
           tmem_st16(s_col + c / 2, w);
-          if (c % 64 == 32) {
-            tmem_wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(PFULL + 2 * r + c / 64));
-          }
         }
+        tmem_wait_st();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(PFULL + two));
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
-      if (!__all_sync(0xffffffffu, wait_quick(bar(ODONE + r), (n - 1) & 1u))) {
+      if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
         give_up();
         goto done;
       }
@@ -356,7 +395,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         if (wide) {
 #pragma unroll
           for (uint32_t e = 0; e < 32; e += 8) {
-            T x[8];
+            alignas(16) T x[8];
 #pragma unroll
             for (uint32_t i = 0; i < 8; ++i) x[i] = from_float<T>(o[e + i]);
             if (c + e < a.dim) *reinterpret_cast<uint4 *>(out + c + e) = *reinterpret_cast<const uint4 *>(x);
@@ -369,10 +408,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       }
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
-    // ---- keys and values to f16: a warp 32 positions of each tile, two groups of 16 with a page each ----
+    // ---- keys and values to f16: a warp 16 positions of each tile, in one page ----
     const uint32_t w = warp - SOFT_WARPS;
-    constexpr uint32_t VG = DP == 128 ? 4 : 2;  // groups of 8 positions that a lane takes in turn
+    constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
     const uint32_t kr = lane % 8, kc = lane / 8;  // row of 8, chunk of four
     const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
     // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store phase
@@ -381,73 +419,51 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     const uint32_t sel[4] = {0x5140u, 0x6251u, 0x7362u, 0x4073u};
     const uint32_t sel_a = turn == 0 ? sel[0] : turn == 1 ? sel[1] : turn == 2 ? sel[2] : sel[3];
     const uint32_t sel_b = turn == 0 ? sel[2] : turn == 1 ? sel[3] : turn == 2 ? sel[0] : sel[1];
-    uint4 kx[4][DP / 64];
-    uint32_t vx[VG][8];
-    float ks[2] = {}, vs[2] = {};
-    bool skip[2] = {};
-    // the next tile to fetch: its groups' pages, the page's slot in the list and the first row in it
-    int32_t page[2] = {-1, -1};
-    uint32_t slot[2], row[2];
-    int64_t at[2];  // of the group's first row, less the cache
-    const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens;
-    const uint32_t slots_end = (end + a.page_tokens - 1) / a.page_tokens;
-#pragma unroll
-    for (uint32_t i = 0; i < 2; ++i) {
-      slot[i] = (w * 32 + i * 16) / a.page_tokens;
-      row[i] = (w * 32 + i * 16) % a.page_tokens;
-      page[i] = slot[i] < slots_end ? table[slot[i]] : -1;
-    }
+    // the next tile to copy: its page, the page's slot in the list and the first row in it
+    const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
+    uint32_t slot = w * 16 / a.page_tokens, row = w * 16 % a.page_tokens;
+    int32_t page = slot < slots_end ? table[slot] : -1;
     const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
-    const auto locate = [&]() {
+    // of the tiles copied: scales, and whether the page is out of range
+    float ks[STAGED] = {}, vs[STAGED] = {};
+    bool skip[STAGED] = {};
+    // a warp's share of a staged tile: keys [row of 8][chunk] by the lane that reads them, values row by row
+    const uint32_t raw = base + M::RAW_AT + w * (2 * 16 * DP);
+    const auto copy = [&](uint32_t st) {  // (st: a constant)
+      const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
+      skip[st] = slot < slots_end && !in;
+      const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
+      ks[st] = in ? a.k_scale[sc] : 0.0f;
+      vs[st] = in ? a.v_scale[sc] : 0.0f;
+      const int64_t at = in ? page * a.cache_strides[0] + head_at + static_cast<int64_t>(row) * a.cache_strides[2] : 0;
+      const uint32_t dst = raw + st * (2 * M::RAW);
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i)
-        at[i] = page[i] * a.cache_strides[0] + head_at + static_cast<int64_t>(row[i]) * a.cache_strides[2];
-    };
-    const auto advance = [&]() {
+      for (uint32_t g = 0; g < 2; ++g)
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        slot[i] += slots;
-        row[i] += more;
-        if (row[i] >= a.page_tokens) {
-          row[i] -= a.page_tokens;
-          ++slot[i];
+        for (uint32_t c = 0; c < DP / 64; ++c) {
+          const uint32_t d = (kc + 4 * c) * 16;
+          const bool ok = in && d < a.dim;
+          copy_async(dst + ((g * (DP / 64) + c) * 32 + lane) * 16, a.k_cache + (ok ? at + (g * 8 + kr) * a.cache_strides[2] + d : 0), ok);
         }
-        page[i] = slot[i] < slots_end ? table[slot[i]] : -1;
+#pragma unroll
+      for (uint32_t i = 0; i < DP / 32; ++i) {
+        const uint32_t piece = i * 32 + lane, r = piece / (DP / 16), d = piece % (DP / 16) * 16;
+        const bool ok = in && d < a.dim;
+        copy_async(dst + 16 * DP + piece * 16, a.v_cache + (ok ? at + r * a.cache_strides[2] + d : 0), ok);
       }
-    };
-    const auto valid = [&](uint32_t i) { return page[i] >= 0 && static_cast<uint32_t>(page[i]) < a.pages; };
-    const auto fetch_keys = [&]() {
-#pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        const bool in = valid(i);
-        const int8_t *src = a.k_cache + (in ? at[i] + kr * a.cache_strides[2] + kc * 16 : 0);
-        skip[i] = slot[i] < slots_end && !in;
-        ks[i] = in ? a.k_scale[static_cast<size_t>(page[i]) * a.heads + kh] : 0.0f;
-        vs[i] = in ? a.v_scale[static_cast<size_t>(page[i]) * a.heads + kh] : 0.0f;
-#pragma unroll
-        for (uint32_t g = 0; g < 2; ++g)
-#pragma unroll
-          for (uint32_t c = 0; c < DP / 64; ++c) {
-            const uint32_t d = (kc + 4 * c) * 16;
-            kx[i * 2 + g][c] = in && d < a.dim ? __ldg(reinterpret_cast<const uint4 *>(src + g * 8 * a.cache_strides[2] + c * 64))
-                                               : make_uint4(0u, 0u, 0u, 0u);
-          }
+      slot += slots;
+      row += more;
+      if (row >= a.page_tokens) {
+        row -= a.page_tokens;
+        ++slot;
       }
+      page = slot < slots_end ? table[slot] : -1;
     };
-    const auto fetch_values = [&]() {
 #pragma unroll
-      for (uint32_t g = 0; g < VG; ++g) {
-        const uint32_t i = g * 2 / VG;  // (a lane's groups: two of each 16 positions, or one by its half of the warp)
-        const bool in = valid(i) && quad * 4 < a.dim;
-        const int8_t *src = a.v_cache + (in ? at[i] + (DP == 128 ? g % 2 * 8 : vsub * 8) * a.cache_strides[2] + quad * 4 : 0);
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-          vx[g][e] = in ? __ldg(reinterpret_cast<const uint32_t *>(src + e * a.cache_strides[2])) : 0u;
-      }
-    };
-    locate();
-    fetch_keys();
-    fetch_values();
+    for (uint32_t i = 0; i + 1 < STAGED; ++i) {
+      if (i < n) copy(i);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
     // the largest value scale of the pages seen
     float sv = 1e-30f;
     for (uint32_t p = threadIdx.x - SOFT_WARPS * 32; p < (end + a.page_tokens - 1) / a.page_tokens; p += CONVERT_WARPS * 32) {
@@ -466,139 +482,167 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
 #pragma unroll
     for (uint32_t i = 0; i < CONVERT_WARPS; ++i) sv = fmaxf(sv, s_top[i]);
     if (threadIdx.x == SOFT_WARPS * 32) s_sv = sv;
-    advance();
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
-    for (uint32_t j = 0; j < n; ++j) {
-      const uint32_t buf = j % 2, par = (j / 2 - 1) & 1u;
-      if (j >= 2 && !__all_sync(0xffffffffu, wait_quick(bar(KEMPTY + buf), par))) {
-        give_up();
-        goto done;
-      }
-      __half2 vr[2];
+    uint32_t buf = 0;
+    for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
 #pragma unroll
-      for (uint32_t i = 0; i < 2; ++i) {
-        const bool number = fabsf(vs[i]) < -neg_inf();  // (a NaN or an infinity: no)
-        if (lane == 0) {
-          s_ks[j % 4][w * 2 + i] = number ? fabsf(ks[i]) : __int_as_float(0x7fc00000);
-          s_skip[j % 4][w * 2 + i] = skip[i];
+      for (uint32_t st = 0; st < STAGED; ++st) {
+        const uint32_t j = j0 + st;
+        if (j >= n) break;
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
+        __syncwarp();
+        const unsigned char *src = smem + M::RAW_AT + w * (2 * 16 * DP) + st * (2 * M::RAW);
+        // the keys that lay here were tile j - 3's, used with tile j - 5's values, or among the first two
+        if (j >= RING && !__all_sync(0xffffffffu, j >= 5 ? wait_quick(bar(USED + (j - 5) % RING), ((j - 5) / RING) & 1u)
+                                                         : wait_quick(bar(FIRST), 0))) {
+          give_up();
+          goto done;
         }
-        vr[i] = __float2half2_rn(number ? vs[i] / sv : 0.0f);
-      }
-      // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
-      unsigned char *kt = smem + M::K_AT + buf * M::K_TILE;
+        const bool number = fabsf(vs[st]) < -neg_inf();  // (a NaN or an infinity: no)
+        if (lane == 0) {
+          s_ks[j % 8][w] = number ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
+          s_skip[j % 8][w] = skip[st];
+        }
+        // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
+        const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
+        unsigned char *kt = smem + M::K_AT + buf * M::K_TILE;
 #pragma unroll
-      for (uint32_t g = 0; g < 4; ++g) {
-        const __half2 sg = bits_half2(ks[g / 2] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
+        for (uint32_t g = 0; g < 2; ++g)
 #pragma unroll
-        for (uint32_t c = 0; c < DP / 64; ++c) {
-          const uint32_t x[4] = {kx[g][c].x, kx[g][c].y, kx[g][c].z, kx[g][c].w};
-          uint32_t o[8];
+          for (uint32_t c = 0; c < DP / 64; ++c) {
+            const uint4 k = *reinterpret_cast<const uint4 *>(src + ((g * (DP / 64) + c) * 32 + lane) * 16);
+            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+            uint32_t o[8];
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+              const uint32_t u = x[e] ^ 0x80808080u;
+              o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
+              o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
+            }
+            unsigned char *dst = kt + (w * 2 + g) * (DP * 16) + (kc + 4 * c) * 256 + kr * 16;
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(KFULL + buf));
+        if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
+          give_up();
+          goto done;
+        }
+        const __half2 ratio = __float2half2_rn(number ? vs[st] / sv : 0.0f);
+        unsigned char *vt = smem + M::V_AT + buf * M::V_TILE;
+#pragma unroll
+        for (uint32_t g = 0; g < VG; ++g) {
+          const uint32_t pos8 = DP == 128 ? g : vsub;  // group of 8 positions of the warp's two
+          const unsigned char *rows8 = src + 16 * DP + pos8 * 8 * DP + quad * 4;
+          uint32_t o[4][4];  // [round][pair of positions]
+#pragma unroll
+          for (uint32_t p = 0; p < 4; ++p) {
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(rows8 + 2 * p * DP) ^ 0x80808080u;
+            const uint32_t y = *reinterpret_cast<const uint32_t *>(rows8 + (2 * p + 1) * DP) ^ 0x80808080u;
+            const uint32_t t0 = __byte_perm(x, y, sel_a), t1 = __byte_perm(x, y, sel_b);
+            o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
+            o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
+            o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
+            o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
+          }
 #pragma unroll
           for (uint32_t e = 0; e < 4; ++e) {
-            const uint32_t u = x[e] ^ 0x80808080u;
-            o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
-            o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
+            const uint32_t d = quad * 4 + (e + turn) % 4;
+            *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 2 + pos8) * 128 + (d & 7u) * 16) =
+                make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
           }
-          unsigned char *dst = kt + (w * 4 + g) * (DP * 16) + (kc + 4 * c) * 256 + kr * 16;
-          *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-          *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
         }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(VFULL + buf));
+        if (++buf == RING) buf = 0;
+        // into the place read in the round before this one (all lanes have passed a barrier since)
+        if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
-      fence_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(KFULL + buf));
-      // the next tile's keys on their way while the values are done, and the next values meanwhile
-      if (j + 1 < n) {
-        locate();
-        fetch_keys();
-      }
-      if (j >= 2 && !__all_sync(0xffffffffu, wait_quick(bar(VEMPTY + buf), par))) {
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    if (warp == SOFT_WARPS + CONVERT_WARPS) {
+      // ---- products ----
+      const uint32_t elect = elected();
+      const auto ready = [&](uint32_t i, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar(i), parity)); };
+      const auto scores = [&](uint32_t r, uint32_t j, uint32_t kbuf) {
+        const uint32_t two = r * 2 + j % 2;
+        const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
+#pragma unroll
+        for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
+          mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
+        if (elect) mbar_arrive(bar(SFULL + two));  // (also passes on the page scales that came with the keys)
+        commit(bar(SFULL + two), elect);
+      };
+      if (!ready(QFULL, 0)) {
         give_up();
         goto done;
       }
-      unsigned char *vt = smem + M::V_AT + buf * M::V_TILE;
-#pragma unroll
-      for (uint32_t g = 0; g < VG; ++g) {
-        const uint32_t pos8 = DP == 128 ? g : g * 2 + vsub;  // group of 8 positions of the warp's four
-        const __half2 ratio = vr[g * 2 / VG];
-        uint32_t o[4][4];  // [round][pair of positions]
-#pragma unroll
-        for (uint32_t p = 0; p < 4; ++p) {
-          const uint32_t x = vx[g][2 * p] ^ 0x80808080u, y = vx[g][2 * p + 1] ^ 0x80808080u;
-          const uint32_t t0 = __byte_perm(x, y, sel_a), t1 = __byte_perm(x, y, sel_b);
-          o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
-          o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
-          o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
-          o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
+      for (uint32_t j = 0; j < 2 && j < n; ++j) {
+        if (!ready(KFULL + j, 0)) {
+          give_up();
+          goto done;
         }
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) {
-          const uint32_t d = quad * 4 + (e + turn) % 4;
-          *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 4 + pos8) * 128 + (d & 7u) * 16) =
-              make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
-        }
-      }
-      fence_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(VFULL + buf));
-      if (j + 1 < n) fetch_values();
-      advance();
-    }
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
-    if (warp == SOFT_WARPS + CONVERT_WARPS && lane == 0) {
-      // ---- products ----
-      const auto scores = [&](uint32_t r, uint32_t buf) {
-        const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + buf * M::K_TILE, DP * 16);
-#pragma unroll
-        for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
-          mma_ss(tmem + r * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0);
-        mbar_arrive(bar(SFULL + r));  // (also passes on the page scales that came with the keys)
-        mma_commit(bar(SFULL + r));
-      };
-      bool ok = wait_quick(bar(QFULL), 0) && wait_quick(bar(KFULL), 0);
-      if (ok) {
         fence_after();
-        for (uint32_t r = 0; r < row_tiles; ++r) scores(r, 0);
-        mma_commit(bar(KEMPTY));
+        for (uint32_t r = 0; r < row_tiles; ++r) scores(r, j, j);
       }
-      for (uint32_t j = 0; j < n && ok; ++j) {
-        const uint32_t buf = j % 2, next = (j + 1) % 2;
-        for (uint32_t r = 0; r < row_tiles; ++r) {
-          ok = wait_quick(bar(VFULL + buf), (j / 2) & 1u);
-          const uint64_t vd = desc_of(base + M::V_AT + buf * M::V_TILE, V_GROUP);
-#pragma unroll
-          for (uint32_t half = 0; half < 2; ++half) {
-            ok = ok && wait_quick(bar(PFULL + 2 * r + half), j & 1u);
-            if (!ok) break;
-            fence_after();
-#pragma unroll
-            for (uint32_t k = half * (POS / 32); k < (half + 1) * (POS / 32); ++k)
-              mma_ts(tmem + M::O_COL + r * DP, tmem + r * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0);
-          }
-          if (!ok) break;
-          mma_commit(bar(ODONE + r));
-          if (j + 1 < n) {
-            ok = wait_quick(bar(KFULL + next), ((j + 1) / 2) & 1u);
-            if (!ok) break;
-            fence_after();
-            scores(r, next);
-          }
+      commit(bar(FIRST), elect);
+      uint32_t vbuf = 0, kbuf = 2, vpar = 0, kpar = 0;
+      for (uint32_t j = 0; j < n; ++j) {
+        if (!ready(VFULL + vbuf, vpar) || (j + 2 < n && !ready(KFULL + kbuf, kpar))) {
+          give_up();
+          goto done;
         }
-        if (!ok) break;
-        if (j + 1 < n) mma_commit(bar(KEMPTY + next));
-        mma_commit(bar(VEMPTY + buf));
+        const uint64_t vd = desc_of(base + M::V_AT + vbuf * M::V_TILE, V_GROUP);
+#pragma unroll
+        for (uint32_t r = 0; r < 2; ++r) {
+          if (r >= row_tiles) break;
+          const uint32_t two = r * 2 + j % 2;
+          if (!ready(PFULL + two, (j / 2) & 1u)) {
+            give_up();
+            goto done;
+          }
+          fence_after();
+#pragma unroll
+          for (uint32_t k = 0; k < POS / 16; ++k)
+            mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0, elect);
+          if (j + 2 < n)
+            scores(r, j + 2, kbuf);
+          else
+            commit(bar((j + 1 == n ? LAST : BEFORE) + r), elect);
+        }
+        commit(bar(USED + vbuf), elect);
+        if (++vbuf == RING) {
+          vbuf = 0;
+          vpar ^= 1u;
+        }
+        if (++kbuf == RING) {
+          kbuf = 0;
+          kpar ^= 1u;
+        }
       }
       // the last of what was committed
-      if (ok) ok = wait_quick(bar(VEMPTY + (n - 1) % 2), ((n - 1) / 2) & 1u);
-      if (!ok) give_up();
+      if (!ready(USED + (n - 1) % RING, ((n - 1) / RING) & 1u)) give_up();
     }
   }
 done:
   __syncwarp();
   fence_before();
   __syncthreads();
-  if (warp == 0 && s_fail == 0u)
+  if (s_fail != 0u) {
+    // what was issued ends by itself: the tensor memory is freed after it (a block that kept it would end in an error of
+    // the whole context), and only where this wait too gives up it stays allocated
+    if (warp == SOFT_WARPS + CONVERT_WARPS) {
+      commit(bar(FREE), elected());
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(FREE), 0)) && lane == 0) atomicExch(&s_fail, 2u);
+    }
+    __syncthreads();
+  }
+  if (warp == 0 && s_fail != 2u)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 

@@ -159,8 +159,8 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
     linear_tc_kernel(const ClearLinearArgs a, const uint8_t *__restrict__ tok, uint32_t row_tiles, uint32_t tok_tiles) {
   using S = Shape<NT>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  // wfull, wempty [W_STAGES]; bfull, afull, empty [STAGES]; dfull, dempty
-  __shared__ __align__(8) uint64_t bars[2 * W_STAGES + 3 * S::STAGES + 2];
+  // wfull, wempty [W_STAGES]; bfull, afull, empty [STAGES]; dfull, dempty, free
+  __shared__ __align__(8) uint64_t bars[2 * W_STAGES + 3 * S::STAGES + 3];
   __shared__ uint32_t tmem_slot;
   __shared__ uint32_t s_fail, s_unsafe;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
   const auto bfull = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + s); };
   const auto afull = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + S::STAGES + s); };
   const auto empty = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + 2 * S::STAGES + s); };
-  const uint32_t dfull = bar0 + 8u * (2 * W_STAGES + 3 * S::STAGES), dempty = dfull + 8u;
+  const uint32_t dfull = bar0 + 8u * (2 * W_STAGES + 3 * S::STAGES), dempty = dfull + 8u, free_bar = dempty + 8u;
   const uint32_t b_ring = base + W_STAGES * kPackTile;
 
   if (warp == 0) {
@@ -192,6 +192,7 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
     }
     mbar_init(dfull, 1);
     mbar_init(dempty, S::DRAIN_WARPS);
+    mbar_init(free_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -397,9 +398,16 @@ done:
     // no CTA leaves while another reads its shared memory
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
-  // After a wait that gave up, MMAs may be in flight: the tensor memory is left allocated rather
-  // than handed to another CTA, and the error flag reports TIMEOUT.
-  if (warp == 0 && !fail && !s_unsafe)
+  if (fail) {
+    // what was issued ends by itself: the tensor memory is freed after it (a CTA that kept it would end in an error of
+    // the whole context), and only where this wait too gives up, or copies may be in flight, it stays allocated
+    if (warp == S::CONVERT_WARPS + S::DRAIN_WARPS + 2 && lane == 0) {
+      mma_commit(free_bar);
+      if (!mbar_wait(free_bar, 0)) atomicExch(&s_unsafe, 1u);
+    }
+    __syncthreads();
+  }
+  if (warp == 0 && !s_unsafe)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM) : "memory");
 }
 
