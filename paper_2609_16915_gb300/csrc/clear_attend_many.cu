@@ -252,22 +252,39 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     // eight dimensions at a time ----
     const uint32_t qr = lane % 8, qc = lane / 8;
     const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
-#pragma unroll 1
+    uint4 raw[4][DP / 32];
+#pragma unroll
     for (uint32_t g = 0; g < 4; ++g) {
-      const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr, rw = row0 + r * ROWS + in_tile;
+      const uint32_t rw = row0 + r * ROWS + (warp % 4) * 32 + g * 8 + qr;
       const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                    static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
-      float x[DP / 32][8], top = 0.0f;
 #pragma unroll
       for (uint32_t i = 0; i < DP / 32; ++i) {
         const uint32_t d = (qc + 4 * i) * 8;
-        const bool in = rw < rows && d < a.dim;  // (dim is a multiple of 16)
-        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-        if (in && wide_q) raw = *reinterpret_cast<const uint4 *>(q + d);
-        const T *el = reinterpret_cast<const T *>(&raw);
+        raw[g][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (rw >= rows || d >= a.dim) continue;  // (dim is a multiple of 16)
+        if (wide_q) {
+          raw[g][i] = *reinterpret_cast<const uint4 *>(q + d);
+        } else {
+          const auto two = [&](uint32_t e) {
+            const T lo = q[d + e], hi = q[d + e + 1];
+            return static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&lo)) |
+                   static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&hi)) << 16;
+          };
+          raw[g][i] = make_uint4(two(0), two(2), two(4), two(6));
+        }
+      }
+    }
+#pragma unroll
+    for (uint32_t g = 0; g < 4; ++g) {
+      const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr;
+      float x[DP / 32][8], top = 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < DP / 32; ++i) {
+        const T *el = reinterpret_cast<const T *>(&raw[g][i]);
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) {
-          x[i][e] = in ? to_float(wide_q ? el[e] : q[d + e]) : 0.0f;
+          x[i][e] = to_float(el[e]);
           top = fmaxf(top, fabsf(x[i][e]));
         }
       }
@@ -419,10 +436,24 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     const uint32_t sel[4] = {0x5140u, 0x6251u, 0x7362u, 0x4073u};
     const uint32_t sel_a = turn == 0 ? sel[0] : turn == 1 ? sel[1] : turn == 2 ? sel[2] : sel[3];
     const uint32_t sel_b = turn == 0 ? sel[2] : turn == 1 ? sel[3] : turn == 2 ? sel[0] : sel[1];
-    // the next tile to copy: its page, the page's slot in the list and the first row in it
+    // the tiles to copy next: their pages, loaded a ring ahead; of the first, the page's slot in the list and the first row in it
     const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
     uint32_t slot = w * 16 / a.page_tokens, row = w * 16 % a.page_tokens;
-    int32_t page = slot < slots_end ? table[slot] : -1;
+    uint32_t ahead_slot = slot, ahead_row = row;
+    const auto next = [&](uint32_t &at_slot, uint32_t &at_row) {
+      at_slot += slots;
+      at_row += more;
+      if (at_row >= a.page_tokens) {
+        at_row -= a.page_tokens;
+        ++at_slot;
+      }
+    };
+    int32_t pages[STAGED];
+#pragma unroll
+    for (uint32_t i = 0; i < STAGED; ++i) {
+      pages[i] = ahead_slot < slots_end ? table[ahead_slot] : -1;
+      next(ahead_slot, ahead_row);
+    }
     const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
     // of the tiles copied: scales, and whether the page is out of range
     float ks[STAGED] = {}, vs[STAGED] = {};
@@ -430,6 +461,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     // a warp's share of a staged tile: keys [row of 8][chunk] by the lane that reads them, values row by row
     const uint32_t raw = base + M::RAW_AT + w * (2 * 16 * DP);
     const auto copy = [&](uint32_t st) {  // (st: a constant)
+      const int32_t page = pages[st];
       const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
       skip[st] = slot < slots_end && !in;
       const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
@@ -451,13 +483,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         const bool ok = in && d < a.dim;
         copy_async(dst + 16 * DP + piece * 16, a.v_cache + (ok ? at + r * a.cache_strides[2] + d : 0), ok);
       }
-      slot += slots;
-      row += more;
-      if (row >= a.page_tokens) {
-        row -= a.page_tokens;
-        ++slot;
-      }
-      page = slot < slots_end ? table[slot] : -1;
+      next(slot, row);
+      pages[st] = ahead_slot < slots_end ? table[ahead_slot] : -1;
+      next(ahead_slot, ahead_row);
     };
 #pragma unroll
     for (uint32_t i = 0; i + 1 < STAGED; ++i) {
