@@ -6,7 +6,7 @@
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
 // over the positions 64 at a time:
-//   4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
+//   4 + 4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
 //                    in shared memory, both K-major: keys [position][dimension] (exact, and with the sign of their
 //                    scale), values transposed by byte permutes to [dimension][position] and times their scale over the
 //                    largest one
@@ -31,8 +31,14 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 8, CONVERT_WARPS = 4, WARPS = 16;
+constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 8, CONVERT_WARPS = 8, WARPS = 20;
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
+// registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out; more
+// than was launched would wait forever
+constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 128, CONVERT_REGS = 80, MMA_REGS = 64;
+static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
+                  WARPS * LAUNCH_REGS,
+              "register shares");
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
@@ -181,7 +187,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
   __shared__ uint32_t s_skip[8][POS / 16];
-  __shared__ float s_top[CONVERT_WARPS], s_sv, s_up[2 * ROWS];
+  __shared__ float s_top[4], s_sv, s_up[2 * ROWS];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
@@ -219,8 +225,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     s_fail = 0u;
     mbar_init(bar(QFULL), SOFT_WARPS);
     for (uint32_t i = 0; i < RING; ++i) {
-      mbar_init(bar(KFULL + i), CONVERT_WARPS);
-      mbar_init(bar(VFULL + i), CONVERT_WARPS);
+      mbar_init(bar(KFULL + i), 4);
+      mbar_init(bar(VFULL + i), 4);
       mbar_init(bar(USED + i), 1);
     }
     for (uint32_t i = 0; i < 4; ++i) {
@@ -245,6 +251,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   };
 
   if (warp < SOFT_WARPS) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
     const uint32_t r = warp / 4, row_in = threadIdx.x % ROWS, row = row0 + r * ROWS + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
     const uint32_t o_col = tmem + lanes + M::O_COL + r * DP;
@@ -425,17 +432,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       }
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
-    // ---- keys and values to f16: a warp 16 positions of each tile, in one page ----
-    const uint32_t w = warp - SOFT_WARPS;
-    constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
-    const uint32_t kr = lane % 8, kc = lane / 8;  // row of 8, chunk of four
-    const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
-    // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store phase
-    // write the eight rows of a core matrix: dimension (e + turn) % 4 of its four in round e.
-    const uint32_t turn = lane / 2 % 4;
-    const uint32_t sel[4] = {0x5140u, 0x6251u, 0x7362u, 0x4073u};
-    const uint32_t sel_a = turn == 0 ? sel[0] : turn == 1 ? sel[1] : turn == 2 ? sel[2] : sel[3];
-    const uint32_t sel_b = turn == 0 ? sel[2] : turn == 1 ? sel[3] : turn == 2 ? sel[0] : sel[1];
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
+    // ---- keys (four warps) and values (four) to f16: a warp 16 positions of each tile, in one page ----
+    const uint32_t w = warp % 4;
+    const bool keys = warp < SOFT_WARPS + 4;
     // the tiles to copy next: their pages, loaded a ring ahead; of the first, the page's slot in the list and the first row in it
     const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
     uint32_t slot = w * 16 / a.page_tokens, row = w * 16 % a.page_tokens;
@@ -454,34 +454,30 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       pages[i] = ahead_slot < slots_end ? table[ahead_slot] : -1;
       next(ahead_slot, ahead_row);
     }
-    const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
+    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1];
+    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
     // of the tiles copied: scales, and whether the page is out of range
     float ks[STAGED] = {}, vs[STAGED] = {};
     bool skip[STAGED] = {};
-    // a warp's share of a staged tile: keys [row of 8][chunk] by the lane that reads them, values row by row
-    const uint32_t raw = base + M::RAW_AT + w * (2 * 16 * DP);
-    const auto copy = [&](uint32_t st) {  // (st: a constant)
+    // a warp's share of a staged tile: keys [row of 8][chunk of 16 bytes] by the lane that reads them, values row by row
+    const uint32_t raw_at = M::RAW_AT + (keys ? 0 : M::RAW) + w * (16 * DP);
+    const uint32_t kr = lane % 8, kc = lane / 8;  // a key row of 8, a chunk of four
+    const auto copy = [&](uint32_t st) {          // (st: a constant)
       const int32_t page = pages[st];
       const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
       skip[st] = slot < slots_end && !in;
       const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
-      ks[st] = in ? a.k_scale[sc] : 0.0f;
+      ks[st] = in && keys ? a.k_scale[sc] : 0.0f;
       vs[st] = in ? a.v_scale[sc] : 0.0f;
-      const int64_t at = in ? page * a.cache_strides[0] + head_at + static_cast<int64_t>(row) * a.cache_strides[2] : 0;
-      const uint32_t dst = raw + st * (2 * M::RAW);
-#pragma unroll
-      for (uint32_t g = 0; g < 2; ++g)
-#pragma unroll
-        for (uint32_t c = 0; c < DP / 64; ++c) {
-          const uint32_t d = (kc + 4 * c) * 16;
-          const bool ok = in && d < a.dim;
-          copy_async(dst + ((g * (DP / 64) + c) * 32 + lane) * 16, a.k_cache + (ok ? at + (g * 8 + kr) * a.cache_strides[2] + d : 0), ok);
-        }
+      const int8_t *src = cache + (in ? page * a.cache_strides[0] + static_cast<int64_t>(row) * a.cache_strides[2] : 0);
+      const uint32_t dst = base + raw_at + st * (2 * M::RAW) + lane * 16;
 #pragma unroll
       for (uint32_t i = 0; i < DP / 32; ++i) {
-        const uint32_t piece = i * 32 + lane, r = piece / (DP / 16), d = piece % (DP / 16) * 16;
+        const uint32_t piece = i * 32 + lane;
+        const uint32_t r = keys ? i / (DP / 64) * 8 + kr : piece / (DP / 16);
+        const uint32_t d = keys ? (kc + 4 * (i % (DP / 64))) * 16 : piece % (DP / 16) * 16;
         const bool ok = in && d < a.dim;
-        copy_async(dst + 16 * DP + piece * 16, a.v_cache + (ok ? at + r * a.cache_strides[2] + d : 0), ok);
+        copy_async(dst + i * 512, ok ? src + r * a.cache_strides[2] + d : cache, ok);
       }
       next(slot, row);
       pages[st] = ahead_slot < slots_end ? table[ahead_slot] : -1;
@@ -492,54 +488,35 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       if (i < n) copy(i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // the largest value scale of the pages seen
-    float sv = 1e-30f;
-    for (uint32_t p = threadIdx.x - SOFT_WARPS * 32; p < (end + a.page_tokens - 1) / a.page_tokens; p += CONVERT_WARPS * 32) {
-      const int32_t id = table[p];
-      if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
-        const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
-        if (v < -neg_inf()) sv = fmaxf(sv, v);
-      } else {
-        atomicMax(a.err_flag, 1u);
-      }
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, off));
-    if (lane == 0) s_top[w] = sv;
-    asm volatile("bar.sync 1, %0;" ::"n"(CONVERT_WARPS * 32) : "memory");
-#pragma unroll
-    for (uint32_t i = 0; i < CONVERT_WARPS; ++i) sv = fmaxf(sv, s_top[i]);
-    if (threadIdx.x == SOFT_WARPS * 32) s_sv = sv;
-    const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
     uint32_t buf = 0;
-    for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
+    if (keys) {
+      for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
 #pragma unroll
-      for (uint32_t st = 0; st < STAGED; ++st) {
-        const uint32_t j = j0 + st;
-        if (j >= n) break;
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
-        __syncwarp();
-        const unsigned char *src = smem + M::RAW_AT + w * (2 * 16 * DP) + st * (2 * M::RAW);
-        // the keys that lay here were tile j - 3's, used with tile j - 5's values, or among the first two
-        if (j >= RING && !__all_sync(0xffffffffu, j >= 5 ? wait_quick(bar(USED + (j - 5) % RING), ((j - 5) / RING) & 1u)
-                                                         : wait_quick(bar(FIRST), 0))) {
-          give_up();
-          goto done;
-        }
-        const bool number = fabsf(vs[st]) < -neg_inf();  // (a NaN or an infinity: no)
-        if (lane == 0) {
-          s_ks[j % 8][w] = number ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
-          s_skip[j % 8][w] = skip[st];
-        }
-        // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
-        const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
-        unsigned char *kt = smem + M::K_AT + buf * M::K_TILE;
+        for (uint32_t st = 0; st < STAGED; ++st) {
+          const uint32_t j = j0 + st;
+          if (j >= n) break;
+          asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
+          const unsigned char *src = smem + raw_at + st * (2 * M::RAW) + lane * 16;
+          uint4 k[DP / 32];
 #pragma unroll
-        for (uint32_t g = 0; g < 2; ++g)
+          for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
+          // the keys that lay here were tile j - 3's, used with tile j - 5's values, or among the first two
+          if (j >= RING && !__all_sync(0xffffffffu, j >= 5 ? wait_quick(bar(USED + (j - 5) % RING), ((j - 5) / RING) & 1u)
+                                                           : wait_quick(bar(FIRST), 0))) {
+            give_up();
+            goto done;
+          }
+          if (lane == 0) {
+            // (a value scale that is a NaN or an infinity: no number)
+            s_ks[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
+            s_skip[j % 8][w] = skip[st];
+          }
+          // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
+          const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
+          unsigned char *kt = smem + M::K_AT + buf * M::K_TILE + w * 2 * (DP * 16) + kc * 256 + kr * 16;
 #pragma unroll
-          for (uint32_t c = 0; c < DP / 64; ++c) {
-            const uint4 k = *reinterpret_cast<const uint4 *>(src + ((g * (DP / 64) + c) * 32 + lane) * 16);
-            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+          for (uint32_t i = 0; i < DP / 32; ++i) {
+            const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
             uint32_t o[8];
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
@@ -547,52 +524,93 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
               o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
               o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
             }
-            unsigned char *dst = kt + (w * 2 + g) * (DP * 16) + (kc + 4 * c) * 256 + kr * 16;
+            unsigned char *dst = kt + i / (DP / 64) * (DP * 16) + i % (DP / 64) * 1024;
             *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
           }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(KFULL + buf));
-        if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
-          give_up();
-          goto done;
+          fence_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(KFULL + buf));
+          if (++buf == RING) buf = 0;
+          // into the place read in the round before this one
+          if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
+          asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        const __half2 ratio = __float2half2_rn(number ? vs[st] / sv : 0.0f);
-        unsigned char *vt = smem + M::V_AT + buf * M::V_TILE;
-#pragma unroll
-        for (uint32_t g = 0; g < VG; ++g) {
-          const uint32_t pos8 = DP == 128 ? g : vsub;  // group of 8 positions of the warp's two
-          const unsigned char *rows8 = src + 16 * DP + pos8 * 8 * DP + quad * 4;
-          uint32_t o[4][4];  // [round][pair of positions]
-#pragma unroll
-          for (uint32_t p = 0; p < 4; ++p) {
-            const uint32_t x = *reinterpret_cast<const uint32_t *>(rows8 + 2 * p * DP) ^ 0x80808080u;
-            const uint32_t y = *reinterpret_cast<const uint32_t *>(rows8 + (2 * p + 1) * DP) ^ 0x80808080u;
-            const uint32_t t0 = __byte_perm(x, y, sel_a), t1 = __byte_perm(x, y, sel_b);
-            o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
-            o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
-            o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
-            o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
-          }
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e) {
-            const uint32_t d = quad * 4 + (e + turn) % 4;
-            *reinterpret_cast<uint4 *>(vt + (d >> 3) * V_GROUP + (w * 2 + pos8) * 128 + (d & 7u) * 16) =
-                make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
-          }
+      }
+    } else {
+      // the largest value scale of the pages seen
+      float sv = 1e-30f;
+      for (uint32_t p = threadIdx.x % 128; p < slots_end; p += 128) {
+        const int32_t id = table[p];
+        if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
+          const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
+          if (v < -neg_inf()) sv = fmaxf(sv, v);
+        } else {
+          atomicMax(a.err_flag, 1u);
         }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(VFULL + buf));
-        if (++buf == RING) buf = 0;
-        // into the place read in the round before this one (all lanes have passed a barrier since)
-        if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, o));
+      if (lane == 0) s_top[w] = sv;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) sv = fmaxf(sv, s_top[i]);
+      if (w == 0 && lane == 0) s_sv = sv;
+      const float per_sv = 1.0f / sv;
+      constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
+      const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
+      // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store
+      // phase write the eight rows of a core matrix: dimension (e + turn) % 4 of its four in round e.
+      const uint32_t turn = lane / 2 % 4;
+      const uint32_t sel_a = turn == 0 ? 0x5140u : turn == 1 ? 0x6251u : turn == 2 ? 0x7362u : 0x4073u;
+      const uint32_t sel_b = turn == 0 ? 0x7362u : turn == 1 ? 0x4073u : turn == 2 ? 0x5140u : 0x6251u;
+      for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
+#pragma unroll
+        for (uint32_t st = 0; st < STAGED; ++st) {
+          const uint32_t j = j0 + st;
+          if (j >= n) break;
+          asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
+          __syncwarp();
+          const unsigned char *src = smem + raw_at + st * (2 * M::RAW) + quad * 4;
+          uint32_t x[VG][8];
+#pragma unroll
+          for (uint32_t g = 0; g < VG; ++g)
+#pragma unroll
+            for (uint32_t p = 0; p < 8; ++p) x[g][p] = *reinterpret_cast<const uint32_t *>(src + ((g + vsub) * 8 + p) * DP) ^ 0x80808080u;
+          if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
+            give_up();
+            goto done;
+          }
+          const __half2 ratio = __float2half2_rn(fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f);
+          unsigned char *vt = smem + M::V_AT + buf * M::V_TILE + (quad >> 1) * V_GROUP + (w * 2 + vsub) * 128 + (quad & 1u) * 64;
+#pragma unroll
+          for (uint32_t g = 0; g < VG; ++g) {
+            uint32_t o[4][4];  // [round][pair of positions]
+#pragma unroll
+            for (uint32_t p = 0; p < 4; ++p) {
+              const uint32_t t0 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_a), t1 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_b);
+              o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
+              o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
+              o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
+              o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+              *reinterpret_cast<uint4 *>(vt + g * 128 + (e + turn) % 4 * 16) = make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(VFULL + buf));
+          if (++buf == RING) buf = 0;
+          // into the place read in the round before this one (all lanes have passed a barrier since)
+          if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        }
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
     if (warp == SOFT_WARPS + CONVERT_WARPS) {
       // ---- products ----
       const uint32_t elect = elected();
