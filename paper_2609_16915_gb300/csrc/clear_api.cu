@@ -121,7 +121,7 @@ int ensure_work(rosetta_clear *h, size_t bytes, cudaStream_t s) {
 int run_linear(rosetta_clear *h, const ClearLinearArgs &a, int kind, cudaStream_t s) {
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
   cudaError_t e;
-  if (a.tokens <= kLinearFew) {
+  if (linear_few_takes(a)) {
     e = launch_clear_linear_few(a, kind, h->sms, s);
   } else {
     const int r = ensure_work(h, linear_tc_bytes(a.tokens, a.k_steps), s);

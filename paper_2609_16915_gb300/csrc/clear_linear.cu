@@ -2,7 +2,7 @@
 //   acc[t][n] = sum_k q[t][k] w[n][k],   y = (acc scale[t]) w_scale[n] + bias[n].
 // The packing of the weights, and the kernel for few tokens.
 //
-// Few tokens (up to kLinearFew): bound by reading the weights once.  A block takes 32 channels; its warps share
+// Few tokens: bound by reading the weights once.  A block takes 32 channels; its warps share
 // out the steps of 64 inputs and join their integer sums in shared memory.  The weights go from global
 // memory to registers, 16 bytes a lane, and from 8 bits to f16 there; a 16 x 8 x 16 product of f16 is exact
 // (products below 2^14), and so are the f32 sums of 16 steps, which are then taken into integers.

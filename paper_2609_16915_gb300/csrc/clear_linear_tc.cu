@@ -31,11 +31,13 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t W_STAGES = 8, CHUNK_STEPS = 1024 / kPackK;
+constexpr uint32_t CHUNK_STEPS = 1024 / kPackK;
 
 template <uint32_t NT>
 struct Shape {
-  static constexpr uint32_t STAGES = NT == 256 ? 4 : 8;                    // token tiles and A operands
+  // as many as fit: the way of a step through copy, conversion and product takes 2 - 3 us
+  static constexpr uint32_t W_STAGES = NT <= 32 ? 16 : NT == 64 ? 14 : 8;  // weight tiles
+  static constexpr uint32_t STAGES = NT <= 32 ? 14 : NT == 64 ? 12 : NT == 128 ? 9 : 5;  // token tiles and A operands
   static constexpr uint32_t B_TILE = NT * kPackK * 2;
   static constexpr uint32_t DRAIN_WARPS = NT == 256 ? 8 : 4;
   static constexpr uint32_t COLS = NT / (DRAIN_WARPS / 4);                 // of one drain thread
@@ -45,6 +47,7 @@ struct Shape {
   static constexpr uint32_t A_COL = NT;                                    // first column of the A operands
   static constexpr uint32_t TMEM = NT + STAGES * 32 <= 256 ? 256 : 512;
   static constexpr uint32_t RING = W_STAGES * kPackTile + STAGES * B_TILE;
+  static_assert(RING <= 225 * 1024 && NT + STAGES * 32 <= 512, "shared and tensor memory");
   // over half an SM's shared memory: two CTAs of a cluster on one SM would wait for each other's
   // tensor memory
   static constexpr uint32_t SMEM = RING > 120 * 1024 ? RING : 120 * 1024;
@@ -60,12 +63,28 @@ struct Shape {
 template <uint32_t NT>
 constexpr uint32_t kIdescF16 = (1u << 4) | ((NT >> 3) << 17) | ((128u >> 4) << 24);
 
+// One lane of the warp, the same each time.  The MMA warp runs converged and its instructions are predicated on this
+// lane, so that descriptors stay in uniform registers.
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
+
 template <uint32_t NT>
-__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t accumulate, uint32_t elect) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(bdesc), "r"(kIdescF16<NT>), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(bdesc), "r"(kIdescF16<NT>), "r"(accumulate), "r"(elect)
+      : "memory");
+}
+
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t elect) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(elect)
       : "memory");
 }
 
@@ -159,19 +178,19 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
     linear_tc_kernel(const ClearLinearArgs a, const uint8_t *__restrict__ tok, uint32_t row_tiles, uint32_t tok_tiles) {
   using S = Shape<NT>;
   extern __shared__ __align__(1024) unsigned char smem[];
-  // wfull, wempty [W_STAGES]; bfull, afull, empty [STAGES]; dfull, dempty, free
-  __shared__ __align__(8) uint64_t bars[2 * W_STAGES + 3 * S::STAGES + 3];
+  // wfull, wempty [S::W_STAGES]; bfull, afull, empty [STAGES]; dfull, dempty, free
+  __shared__ __align__(8) uint64_t bars[2 * S::W_STAGES + 3 * S::STAGES + 3];
   __shared__ uint32_t tmem_slot;
   __shared__ uint32_t s_fail, s_unsafe;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
   const auto wfull = [&](uint32_t s) { return bar0 + 8u * s; };
-  const auto wempty = [&](uint32_t s) { return bar0 + 8u * (W_STAGES + s); };
-  const auto bfull = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + s); };
-  const auto afull = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + S::STAGES + s); };
-  const auto empty = [&](uint32_t s) { return bar0 + 8u * (2 * W_STAGES + 2 * S::STAGES + s); };
-  const uint32_t dfull = bar0 + 8u * (2 * W_STAGES + 3 * S::STAGES), dempty = dfull + 8u, free_bar = dempty + 8u;
-  const uint32_t b_ring = base + W_STAGES * kPackTile;
+  const auto wempty = [&](uint32_t s) { return bar0 + 8u * (S::W_STAGES + s); };
+  const auto bfull = [&](uint32_t s) { return bar0 + 8u * (2 * S::W_STAGES + s); };
+  const auto afull = [&](uint32_t s) { return bar0 + 8u * (2 * S::W_STAGES + S::STAGES + s); };
+  const auto empty = [&](uint32_t s) { return bar0 + 8u * (2 * S::W_STAGES + 2 * S::STAGES + s); };
+  const uint32_t dfull = bar0 + 8u * (2 * S::W_STAGES + 3 * S::STAGES), dempty = dfull + 8u, free_bar = dempty + 8u;
+  const uint32_t b_ring = base + S::W_STAGES * kPackTile;
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)),
@@ -181,7 +200,7 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
   }
   if (threadIdx.x == 0) {
     s_fail = s_unsafe = 0u;
-    for (uint32_t s = 0; s < W_STAGES; ++s) {
+    for (uint32_t s = 0; s < S::W_STAGES; ++s) {
       mbar_init(wfull(s), 1);
       mbar_init(wempty(s), 4);
     }
@@ -219,8 +238,8 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
     const uint32_t mine = first < tiles ? (tiles - 1 - first) / stride + 1 : 0;  // tiles of this CTA
     // warpgroup g takes the steps g, g + CONVERT_GROUPS, ...
     for (uint32_t it = warp / 4; it < mine * steps; it += S::CONVERT_GROUPS) {
-      const uint32_t ws = it % W_STAGES, s = it % S::STAGES;
-      if (!__all_sync(0xffffffffu, wait_quick(wfull(ws), (it / W_STAGES) & 1u))) {
+      const uint32_t ws = it % S::W_STAGES, s = it % S::STAGES;
+      if (!__all_sync(0xffffffffu, wait_quick(wfull(ws), (it / S::W_STAGES) & 1u))) {
         give_up();
         goto done;
       }
@@ -309,7 +328,7 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
           }
           expect_tx(wfull(slot), kPackTile);
           bulk_load(base + slot * kPackTile, src, kPackTile, wfull(slot));
-          if (++slot == W_STAGES) {
+          if (++slot == S::W_STAGES) {
             slot = 0;
             par ^= 1u;
           }
@@ -318,8 +337,8 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
       if (!ok) {
         give_up();
         // let the copies already issued land before the shared memory is released
-        for (uint32_t i = issued > W_STAGES ? issued - W_STAGES : 0; i < issued; ++i)
-          if (!mbar_wait(wfull(i % W_STAGES), (i / W_STAGES) & 1u)) atomicExch(&s_unsafe, 1u);
+        for (uint32_t i = issued > S::W_STAGES ? issued - S::W_STAGES : 0; i < issued; ++i)
+          if (!mbar_wait(wfull(i % S::W_STAGES), (i / S::W_STAGES) & 1u)) atomicExch(&s_unsafe, 1u);
       }
     } else if (role == 1 && lane == 0) {
       // ---- token copies, after the kernel that makes the tiles ----
@@ -346,14 +365,16 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
         for (uint32_t i = issued > S::STAGES ? issued - S::STAGES : 0; i < issued; ++i)
           if (!mbar_wait(bfull(i % S::STAGES), (i / S::STAGES) & 1u)) atomicExch(&s_unsafe, 1u);
       }
-    } else if (role == 2 && lane == 0) {
+    } else if (role == 2) {
       // ---- MMAs ----
+      const uint32_t elect = elected();
+      const auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar, parity)); };
       uint32_t slot = 0, par = 0, dpar = 1;
       for (uint32_t tile = first; tile < tiles; tile += stride)
         for (uint32_t k = 0; k < steps; ++k) {
-          bool ok = wait_quick(bfull(slot), par) && wait_quick(afull(slot), par);
+          bool ok = ready(bfull(slot), par) && ready(afull(slot), par);
           if (k % CHUNK_STEPS == 0) {  // the accumulators have been read
-            ok = ok && wait_quick(dempty, dpar);
+            ok = ok && ready(dempty, dpar);
             dpar ^= 1u;
           }
           if (!ok) {
@@ -365,9 +386,9 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
           const uint32_t sa = tmem + S::A_COL + slot * 32u;
 #pragma unroll
           for (uint32_t kk = 0; kk < kPackK / 16; ++kk)  // 256 bytes on: 16 in the descriptor's units
-            mma_f16<NT>(tmem, sa + kk * 8u, sb + kk * 16u, (k % CHUNK_STEPS | kk) != 0);
-          mma_commit(empty(slot));
-          if (k % CHUNK_STEPS == CHUNK_STEPS - 1 || k + 1 == steps) mma_commit(dfull);
+            mma_f16<NT>(tmem, sa + kk * 8u, sb + kk * 16u, (k % CHUNK_STEPS | kk) != 0, elect);
+          commit(empty(slot), elect);
+          if (k % CHUNK_STEPS == CHUNK_STEPS - 1 || k + 1 == steps) commit(dfull, elect);
           if (++slot == S::STAGES) {
             slot = 0;
             par ^= 1u;
@@ -401,8 +422,8 @@ done:
   if (fail) {
     // what was issued ends by itself: the tensor memory is freed after it (a CTA that kept it would end in an error of
     // the whole context), and only where this wait too gives up, or copies may be in flight, it stays allocated
-    if (warp == S::CONVERT_WARPS + S::DRAIN_WARPS + 2 && lane == 0) {
-      mma_commit(free_bar);
+    if (warp == S::CONVERT_WARPS + S::DRAIN_WARPS + 2) {
+      commit(free_bar, elected());
       if (!mbar_wait(free_bar, 0)) atomicExch(&s_unsafe, 1u);
     }
     __syncthreads();
