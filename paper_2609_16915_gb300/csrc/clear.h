@@ -138,8 +138,8 @@ cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t
 // attention for few rows a cached head: whole 16-position tiles in a page, heads a multiple of 16; work:
 // attend_few_bytes
 bool attend_few_takes(const ClearAttentionArgs &a);
-size_t attend_few_bytes(const ClearAttentionArgs &a);
-cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, cudaStream_t s);
+size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms);
+cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s);
 // for many (prompts), on the tensor cores: the same, heads up to 128, 16-bit floats
 bool attend_many_takes(const ClearAttentionArgs &a, int type);
 cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, cudaStream_t s);

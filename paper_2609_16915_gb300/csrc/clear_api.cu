@@ -372,9 +372,9 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
   if (attend_many_takes(a, type)) {
     e = launch_clear_attention_many(a, type, s);
   } else if (attend_few_takes(a)) {
-    const int r = ensure_work(h, attend_few_bytes(a), s);
+    const int r = ensure_work(h, attend_few_bytes(a, h->sms), s);
     if (r != ROSETTA_OK) return r;
-    e = launch_clear_attention_few(a, type, h->work, s);
+    e = launch_clear_attention_few(a, type, h->work, h->sms, s);
   } else {
     e = launch_clear_attention(a, type, s);
   }

@@ -79,14 +79,16 @@ struct Few {
 
 struct FewArgs {
   ClearAttentionArgs a;
-  float *part;              // [batch][head][split][rows of all groups][dim + 2]: l, m, O
+  float *part;              // [batch][head][split][rows of all groups]: O [dim]
+  float2 *stats;            // the same: l, m
   uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
+  uint32_t least;           // positions of a range at least
 };
 
-// The range of positions of split `s` of `splits`: shares of at least 512 positions, whole tiles of all warps.
-__device__ __forceinline__ uint32_t split_share(uint32_t end, uint32_t splits) {
-  const uint32_t share = (end + splits - 1) / splits;
-  return ((share < 512 ? 512 : share) + 63) / 64 * 64;
+// Positions of each range of a sequence of `end`: whole tiles of all warps.
+__device__ __forceinline__ uint32_t split_share(const FewArgs &f, uint32_t end) {
+  const uint32_t share = (end + f.splits - 1) / f.splits;
+  return ((share < f.least ? f.least : share) + 63) / 64 * 64;
 }
 
 // Positions that the rows of a group see at most: up to the last token of the group.
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   const uint32_t rows = a.tokens * a.group, row0 = group * (8 * NB);
   const int64_t len = length_of(a, b);
   const uint32_t end = group_end(a, len, min(row0 + 8 * NB, rows) - 1);
-  const uint32_t share = split_share(end, f.splits), lo = split * share, hi = min(end, lo + share);
+  const uint32_t share = split_share(f, end), lo = split * share, hi = min(end, lo + share);
   if (split > 0 && lo >= end) return;
   const bool alone = end <= share;  // (the first block of an empty sequence writes its zeros)
 
@@ -128,52 +130,6 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   int32_t last[NB][2];  // of rows 2 t, 2 t + 1
   float factor[NB][2];
   uint32_t qf[H][NB][KC][2];
-#pragma unroll
-  for (int n = 0; n < NB; ++n) {
-    const uint32_t row = row0 + n * 8 + g;
-    const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
-                 static_cast<int64_t>(row / a.group) * a.q_strides[1] +
-                 static_cast<int64_t>(kh * a.group + row % a.group) * a.q_strides[2];
-    float top = 0.0f;
-#pragma unroll
-    for (int c = 0; c < KC; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
-        const float v = row < rows && d < a.dim ? to_float(q[d]) : 0.0f;
-        top = fmaxf(top, fabsf(v));
-      }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // a power of two that brings the row's largest value to [1, 2): exact (within the range of exponents)
-    const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
-    const float down = __int_as_float((127 - ex) << 23), up = __int_as_float((127 + ex) << 23);
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
-        v[e] = row < rows && d < a.dim ? to_float(q[d]) * down : 0.0f;
-      }
-#pragma unroll
-      for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const __half2 x = __floats2half2_rn(v[2 * p], v[2 * p + 1]);
-          qf[h][n][c][p] = *reinterpret_cast<const uint32_t *>(&x);
-          v[2 * p] -= __low2float(x);
-          v[2 * p + 1] -= __high2float(x);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      factor[n][i] = __shfl_sync(0xffffffffu, up, (2 * t + i) * 4) * (a.softmax_scale * kLog2e);
-      const uint32_t r = row0 + n * 8 + 2 * t + i;
-      last[n][i] = r < rows ? static_cast<int32_t>(len - a.tokens + r / a.group) : -1;
-    }
-  }
-
   float o[NB][MT][4] = {}, m[NB][2], l[NB][2] = {}, sv = 0.0f;
 #pragma unroll
   for (int n = 0; n < NB; ++n) m[n][0] = m[n][1] = neg_inf();
@@ -181,6 +137,20 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   unsigned char *own = ring + warp * (F::DEPTH * F::TILE);
   const uint32_t own_addr = smem_addr(own);
   const uint32_t tiles_hi = (hi + 15) / 16;
+  // What a lane copies of a tile: of the keys whole rows in turn, 16 bytes a lane (half lines cost a third of the
+  // bandwidth), the chunks of odd rows moved by 64 bytes so that reading chunk t of each 64 of row g meets every bank
+  // once; of the values, rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, VB bytes at VB g, which it reads itself.
+  // (16 rows of a page lie within 2^31 bytes: attend_few_takes)
+  constexpr int CH = DP / 16;  // 16-byte chunks of a row
+  const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
+  const uint32_t row_step = static_cast<uint32_t>(a.cache_strides[2]);
+  const uint32_t k_off = lane / CH * row_step + lane % CH * 16, v_off = 2 * t * row_step + VB * g;
+  const uint32_t k_dst = lane / CH * DP + ((lane % CH) ^ (CH >= 8 ? (lane / CH & 1u) * 4 : 0u)) * 16;
+  const bool k_in = lane % CH * 16 < a.dim;
+  bool v_in[VB < 16 ? 1 : VB / 16];
+#pragma unroll
+  for (int j = 0; j < (VB < 16 ? 1 : VB / 16); ++j) v_in[j] = VB * g + 16 * j < a.dim;
+  int32_t whole = 0x7fffffff;  // the last position that every row sees
   for (uint32_t seg = lo / 16; seg < tiles_hi; seg += kSegment) {
     const uint32_t count = min(kSegment, tiles_hi - seg);
     __syncthreads();
@@ -220,34 +190,21 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
       if (i < count) {
         const int32_t page = s_page[i];
         const bool in = page >= 0;
-        const int64_t at = in ? page * a.cache_strides[0] + static_cast<int64_t>(kh) * a.cache_strides[1] +
-                                    static_cast<int64_t>((seg + i) * 16 % a.page_tokens) * a.cache_strides[2]
-                              : 0;
-        const uint32_t dst = own_addr + slot * F::TILE;
-        // keys of positions g, g + 8: 16 bytes at 16 t of each 64
+        const int64_t at = in ? page * a.cache_strides[0] + head_at + static_cast<int64_t>((seg + i) * 16 % a.page_tokens) * a.cache_strides[2] : 0;
+        const int8_t *kt = a.k_cache + at, *vt = a.v_cache + at;
+        const uint32_t dst = own_addr + slot * F::TILE, vdst = dst + 16 * DP;
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int j = 0; j < DP / 64; ++j) {
-            const uint32_t d = 16 * t + 64 * j;
-            const bool ok = in && d < a.dim;
-            copy_async<16>(dst + ((r * (DP / 64) + j) * 32 + lane) * 16, a.k_cache + (ok ? at + (g + 8 * r) * a.cache_strides[2] + d : 0), ok);
-          }
-        // values of positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9: VB bytes at VB g
-        const uint32_t vdst = dst + 16 * DP;
+        for (int i = 0; i < DP / 32; ++i)
+          copy_async<16>(dst + i * 512 + k_dst, kt + (k_in ? k_off + i * (512 / DP) * row_step : 0), in && k_in);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const int8_t *src = a.v_cache + at + static_cast<int64_t>(2 * t + p % 2 + p / 2 * 8) * a.cache_strides[2];
+          const uint32_t off = v_off + (p % 2 + p / 2 * 8) * row_step;
           if constexpr (VB == 8) {
-            const bool ok = in && 8 * g < a.dim;
-            copy_async<8>(vdst + (p * 32 + lane) * 8, ok ? src + 8 * g : a.v_cache, ok);
+            copy_async<8>(vdst + (p * 32 + lane) * 8, vt + (v_in[0] ? off : 0), in && v_in[0]);
           } else {
 #pragma unroll
-            for (int j = 0; j < VB / 16; ++j) {
-              const uint32_t d = VB * g + 16 * j;
-              const bool ok = in && d < a.dim;
-              copy_async<16>(vdst + ((p * (VB / 16) + j) * 32 + lane) * 16, ok ? src + d : a.v_cache, ok);
-            }
+            for (int j = 0; j < VB / 16; ++j)
+              copy_async<16>(vdst + ((p * (VB / 16) + j) * 32 + lane) * 16, vt + (v_in[j] ? off + 16 * j : 0), in && v_in[j]);
           }
         }
       }
@@ -255,16 +212,72 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
     };
 #pragma unroll
     for (uint32_t i = 0; i + 1 < F::DEPTH; ++i) issue(warp + i * kWarps, i);
+    if (seg == lo / 16) {  // (once, with the first tiles on their way)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const uint32_t row = row0 + n * 8 + g;
+        const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
+                     static_cast<int64_t>(row / a.group) * a.q_strides[1] +
+                     static_cast<int64_t>(kh * a.group + row % a.group) * a.q_strides[2];
+        float top = 0.0f;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
+            const float v = row < rows && d < a.dim ? to_float(q[d]) : 0.0f;
+            top = fmaxf(top, fabsf(v));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // a power of two that brings the row's largest value to [1, 2): exact (within the range of exponents)
+        const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const float down = __int_as_float((127 - ex) << 23), up = __int_as_float((127 + ex) << 23);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
+            v[e] = row < rows && d < a.dim ? to_float(q[d]) * down : 0.0f;
+          }
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const __half2 x = __floats2half2_rn(v[2 * p], v[2 * p + 1]);
+              qf[h][n][c][p] = *reinterpret_cast<const uint32_t *>(&x);
+              v[2 * p] -= __low2float(x);
+              v[2 * p + 1] -= __high2float(x);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          factor[n][i] = __shfl_sync(0xffffffffu, up, (2 * t + i) * 4) * (a.softmax_scale * kLog2e);
+          const uint32_t r = row0 + n * 8 + 2 * t + i;
+          last[n][i] = r < rows ? static_cast<int32_t>(len - a.tokens + r / a.group) : -1;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (row0 + n * 8 + 2 * t + e < rows) whole = min(whole, last[n][e]);
+      whole = min(whole, __shfl_xor_sync(0xffffffffu, whole, 1));
+      whole = min(whole, __shfl_xor_sync(0xffffffffu, whole, 2));
+    }
     uint32_t slot = 0;
     for (uint32_t i = warp; i < count; i += kWarps) {
       asm volatile("cp.async.wait_group %0;" ::"n"(F::DEPTH - 2) : "memory");
+      __syncwarp();
       const unsigned char *tile = own + slot * F::TILE;
       // ---- scores: positions g, g + 8 (rows of S^T), query rows 2 t, 2 t + 1 ----
       float s[NB][4] = {};
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) {
-        const uint4 x = reinterpret_cast<const uint4 *>(tile)[j * 32 + lane];
-        const uint4 y = reinterpret_cast<const uint4 *>(tile)[(DP / 64 + j) * 32 + lane];
+        const uint32_t chunk = (t + 4 * j) ^ (CH >= 8 ? (g & 1u) * 4 : 0u);
+        const uint4 x = reinterpret_cast<const uint4 *>(tile)[g * CH + chunk];
+        const uint4 y = reinterpret_cast<const uint4 *>(tile)[(g + 8) * CH + chunk];
         const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -277,17 +290,29 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         }
       }
       const float ks = s_ks[i], vs = s_vs[i] * vlift;
-      const int32_t p0 = static_cast<int32_t>((seg + i) * 16 + g);
-      const bool in = s_page[i] >= 0;
       bool raise = false;
+      // (rows past the last are scored too, of queries of zeros; nothing of them is written)
+      const bool part = s_page[i] < 0 || static_cast<int32_t>((seg + i) * 16 + 15) > whole;
+      if (part) {
+        const int32_t p0 = static_cast<int32_t>((seg + i) * 16 + g);
+        const bool in = s_page[i] >= 0;
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
-          s[n][e] = seen ? s[n][e] * (ks * factor[n][e % 2]) : neg_inf();
-          raise |= s[n][e] > m[n][e % 2] + kRaise;
-        }
+          for (int e = 0; e < 4; ++e) {
+            const bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
+            s[n][e] = seen ? s[n][e] * (ks * factor[n][e % 2]) : neg_inf();
+            raise |= s[n][e] > m[n][e % 2] + kRaise;
+          }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[n][e] *= ks * factor[n][e % 2];
+            raise |= s[n][e] > m[n][e % 2] + kRaise;
+          }
+      }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -316,7 +341,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
           const float base = m[n][e % 2] == neg_inf() ? 0.0f : m[n][e % 2];
           p[e] = ex2(s[n][e] - base);
           l[n][e % 2] += p[e];
-          p[e] = s[n][e] == neg_inf() ? 0.0f : p[e] * vs;  // (no product with the scale of a page that a row does not see)
+          p[e] = part && s[n][e] == neg_inf() ? 0.0f : p[e] * vs;  // (no product with the scale of a page that a row does not see)
         }
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -330,21 +355,26 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
       }
       // ---- O^T: four dimensions of four positions to two 16 x 8 x 16 operands ----
       const unsigned char *vt = tile + 16 * DP;
+      constexpr int VW = VB == 8 ? 2 : 4;  // words of a lane's access
 #pragma unroll
-      for (int j = 0; j < VB / 8; ++j) {
-        uint32_t w[4][2];
+      for (int j = 0; j < VB / (4 * VW); ++j) {
+        uint32_t w[4][VW];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          uint2 x;
-          if constexpr (VB == 8)
-            x = reinterpret_cast<const uint2 *>(vt)[p * 32 + lane];
-          else
-            x = reinterpret_cast<const uint2 *>(vt)[((p * (VB / 16) + j / 2) * 32 + lane) * 2 + j % 2];
-          w[p][0] = x.x ^ 0x80808080u;
-          w[p][1] = x.y ^ 0x80808080u;
+          if constexpr (VB == 8) {
+            const uint2 x = reinterpret_cast<const uint2 *>(vt)[p * 32 + lane];
+            w[p][0] = x.x ^ 0x80808080u;
+            w[p][1] = x.y ^ 0x80808080u;
+          } else {
+            const uint4 x = reinterpret_cast<const uint4 *>(vt)[(p * (VB / 16) + j) * 32 + lane];
+            w[p][0] = x.x ^ 0x80808080u;
+            w[p][1] = x.y ^ 0x80808080u;
+            w[p][2] = x.z ^ 0x80808080u;
+            w[p][3] = x.w ^ 0x80808080u;
+          }
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < VW; ++c) {
           const uint32_t x0 = __byte_perm(w[0][c], w[1][c], 0x5140), x1 = __byte_perm(w[0][c], w[1][c], 0x7362);
           const uint32_t y0 = __byte_perm(w[2][c], w[3][c], 0x5140), y1 = __byte_perm(w[2][c], w[3][c], 0x7362);
           const uint32_t v0[4] = {biased_f16(x0, 0x4140), biased_f16(x0, 0x4342), biased_f16(y0, 0x4140), biased_f16(y0, 0x4342)};
@@ -353,8 +383,8 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int h = 0; h < H; ++h) {
-              mma_16x8x16(o[n][j * 4 + c * 2], v0, pf[h][n]);
-              mma_16x8x16(o[n][j * 4 + c * 2 + 1], v1, pf[h][n]);
+              mma_16x8x16(o[n][(j * VW + c) * 2], v0, pf[h][n]);
+              mma_16x8x16(o[n][(j * VW + c) * 2 + 1], v1, pf[h][n]);
             }
         }
       }
@@ -407,7 +437,8 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         sum += mw == neg_inf() ? stats[(w * 8 + r) * 2 + 1] : stats[(w * 8 + r) * 2 + 1] * keep[w];
       }
       const float scale = alone ? (sum == 0.0f ? 0.0f : back / sum) : back;
-      float *part = f.part + ((static_cast<size_t>(bh) * f.splits + split) * rows + row) * (a.dim + 2);
+      const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
+      float *part = f.part + at * a.dim;
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] +
                static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
@@ -418,60 +449,94 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         if (alone)
           out[d] = from_float<T>(v * scale);
         else
-          part[2 + d] = v * scale;
+          part[d] = v * scale;
       }
-      if (!alone && lane == 0) {
-        part[0] = sum;
-        part[1] = top;
-      }
+      if (!alone && lane == 0) f.stats[at] = make_float2(sum, top);
     }
   }
 }
 
-// Joins the splits of a row: a warp a row.
+constexpr int kJoinWarps = 8;
+
+// Joins the splits of a row: a block a row, a warp every eighth split, a lane four dimensions (and 128 further on).
 template <typename T>
-__global__ void __launch_bounds__(128) attend_join_kernel(const FewArgs f, uint32_t group_rows) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const FewArgs f, uint32_t group_rows) {
+  __shared__ float s_o[kJoinWarps][256], s_m[kJoinWarps], s_l[kJoinWarps];
   const ClearAttentionArgs &a = f.a;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.tokens * a.group;
-  const uint64_t id = static_cast<uint64_t>(blockIdx.x) * 4 + warp;
-  if (id >= static_cast<uint64_t>(a.batch) * a.heads * rows) return;
-  const uint32_t bh = static_cast<uint32_t>(id / rows), row = static_cast<uint32_t>(id % rows), kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t bh = blockIdx.x / rows, row = blockIdx.x % rows, kh = bh % a.heads, b = bh / a.heads;
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens, given = a.lengths[b], len = given > most ? most : given;
   const uint32_t end = group_end(a, len, min(row / group_rows * group_rows + group_rows, rows) - 1);
-  const uint32_t share = split_share(end, f.splits);
+  const uint32_t share = split_share(f, end), count = (end + share - 1) / share;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (end <= share) return;  // written already
-  const uint32_t count = (end + share - 1) / share;
-  const float *part = f.part + (static_cast<size_t>(bh) * f.splits * rows + row) * (a.dim + 2);
-  const size_t step = static_cast<size_t>(rows) * (a.dim + 2);
-  float top = neg_inf(), sum = 0.0f, o[8] = {};
-  for (uint32_t s = lane; s < count; s += 32) top = fmaxf(top, part[s * step + 1]);
+  const size_t at = static_cast<size_t>(bh) * f.splits * rows + row;
+  float top = neg_inf(), sum = 0.0f;
+  float4 o[2] = {};
+  for (uint32_t s0 = warp; s0 < count; s0 += 32 * kJoinWarps) {  // lane i: split s0 + 8 i
+    const uint32_t mine = s0 + kJoinWarps * lane, n = min(32u, (count - s0 + kJoinWarps - 1) / kJoinWarps);
+    const float2 lm = mine < count ? f.stats[at + static_cast<size_t>(mine) * rows] : make_float2(0.0f, neg_inf());
+    float t = fmaxf(top, lm.y);
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int off = 16; off > 0; off >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, off));
+    const float fade = top == neg_inf() ? 0.0f : ex2(top - t);
+    const float keep = lm.y == neg_inf() ? 0.0f : ex2(lm.y - t);
+    float add = lm.y == neg_inf() ? lm.x : lm.x * keep;  // (a NaN sum under m = -inf stays)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) add += __shfl_xor_sync(0xffffffffu, add, off);
+    sum = sum * fade + add;
+    top = t;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) o[i] = make_float4(o[i].x * fade, o[i].y * fade, o[i].z * fade, o[i].w * fade);
+    const float *src = f.part + (at + static_cast<size_t>(s0) * rows) * a.dim + lane * 4;
+    const size_t step = static_cast<size_t>(kJoinWarps) * rows * a.dim;
 #pragma unroll 4
-  for (uint32_t s = 0; s < count; ++s) {
-    const float ms = part[s * step + 1], ls = part[s * step];
-    const float keep = ms == neg_inf() ? 0.0f : ex2(ms - top);
-    sum += ms == neg_inf() ? ls : ls * keep;  // (NaN stays)
+    for (uint32_t j = 0; j < n; ++j, src += step) {
+      const float k = __shfl_sync(0xffffffffu, keep, j);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (lane + 32 * i < a.dim) o[i] += keep * part[s * step + 2 + lane + 32 * i];
+      for (int i = 0; i < 2; ++i)
+        if (lane * 4 + 128 * i < a.dim) {
+          const float4 v = *reinterpret_cast<const float4 *>(src + 128 * i);
+          o[i] = make_float4(o[i].x + k * v.x, o[i].y + k * v.y, o[i].z + k * v.z, o[i].w + k * v.w);
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&s_o[warp][lane * 4 + 128 * i]) = o[i];
+  if (lane == 0) {
+    s_m[warp] = top;
+    s_l[warp] = sum;
+  }
+  __syncthreads();
+  top = neg_inf();
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w]);
+  sum = 0.0f;
+  float v = 0.0f;
+  const uint32_t d = threadIdx.x;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float keep = s_m[w] == neg_inf() ? 0.0f : ex2(s_m[w] - top);
+    sum += s_m[w] == neg_inf() ? s_l[w] : s_l[w] * keep;
+    v += keep * s_o[w][d];
   }
   T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
            static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (lane + 32 * i < a.dim) out[lane + 32 * i] = from_float<T>(sum == 0.0f ? 0.0f : o[i] / sum);
+  if (d < a.dim) out[d] = from_float<T>(sum == 0.0f ? 0.0f : v / sum);
 }
 
-// Splits of a sequence: shares of 512 positions where they are needed to fill the SMs several times over
-// (uneven lengths then even out), fewer where there are many sequences.
-uint32_t splits_of(const ClearAttentionArgs &a, uint32_t groups) {
-  const uint64_t most = (static_cast<uint64_t>(a.table_pitch) * a.page_tokens + 511) / 512;
-  const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * groups;
-  uint64_t want = (8192 + blocks - 1) / blocks;
-  if (want > most) want = most;
-  return static_cast<uint32_t>(want < 1 ? 1 : want > 1024 ? 1024 : want);
+// Splits of a sequence.  Ranges of 1024 positions, or 512 or 256 where those leave SMs without a block; no more of them
+// than fill the SMs four times over (uneven lengths then even out).  Longer ranges cost less to begin and to join
+// (8 sequences of 4096, 8 heads: 1024 positions 29.3 us, 512 32.7), shorter ones balance better.
+void split(FewArgs *f, uint32_t sms) {
+  const ClearAttentionArgs &a = f->a;
+  const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f->groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
+  f->least = 1024;
+  while (f->least > 256 && blocks * ((most + f->least - 1) / f->least) < 2 * sms) f->least /= 2;
+  const uint64_t longest = (most + f->least - 1) / f->least, want = (16ull * sms + blocks - 1) / blocks;
+  f->splits = static_cast<uint32_t>(want < longest ? want : longest);
+  if (f->splits < 1) f->splits = 1;
+  if (f->splits > 1024) f->splits = 1024;
 }
 
 uint32_t group_rows_of(const ClearAttentionArgs &a) { return a.tokens * a.group <= 8 ? 8 : 16; }
@@ -488,8 +553,8 @@ cudaError_t launch(const FewArgs &f, cudaStream_t s) {
   if (e != cudaSuccess || f.splits == 1) return e;
   cudaLaunchConfig_t cfg = {};
   const uint64_t rows = static_cast<uint64_t>(f.a.batch) * f.a.heads * f.a.tokens * f.a.group;
-  cfg.gridDim = dim3(static_cast<uint32_t>((rows + 3) / 4));
-  cfg.blockDim = dim3(128);
+  cfg.gridDim = dim3(static_cast<uint32_t>(rows));
+  cfg.blockDim = dim3(32 * kJoinWarps);
   cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -514,21 +579,32 @@ cudaError_t launch(const FewArgs &f, cudaStream_t s) {
 }  // namespace
 
 bool attend_few_takes(const ClearAttentionArgs &a) {
-  return a.dim % 16 == 0 && a.page_tokens % 16 == 0 &&
+  return a.dim % 16 == 0 && a.page_tokens % 16 == 0 && a.cache_strides[2] < (1 << 26) &&
          (reinterpret_cast<uintptr_t>(a.k_cache) | reinterpret_cast<uintptr_t>(a.v_cache) |
           static_cast<uintptr_t>(a.cache_strides[0] | a.cache_strides[1] | a.cache_strides[2])) % 16 == 0;
 }
 
-size_t attend_few_bytes(const ClearAttentionArgs &a) {
-  const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a), splits = splits_of(a, (rows + gr - 1) / gr);
-  return splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * splits * rows * (a.dim + 2) * sizeof(float);
-}
+namespace {
 
-cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, cudaStream_t s) {
-  FewArgs f{a, static_cast<float *>(work), 1, 1};
+FewArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
+  FewArgs f{a, static_cast<float *>(work), nullptr, 1, 1, 1};
   const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a);
   f.groups = (rows + gr - 1) / gr;
-  f.splits = splits_of(a, f.groups);
+  split(&f, sms);
+  // (rows of 16 floats at least: the statistics behind them are aligned)
+  f.stats = reinterpret_cast<float2 *>(f.part + static_cast<size_t>(a.batch) * a.heads * f.splits * rows * a.dim);
+  return f;
+}
+
+}  // namespace
+
+size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms) {
+  const FewArgs f = few_args(a, nullptr, sms);
+  return f.splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
+}
+
+cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s) {
+  const FewArgs f = few_args(a, work, sms);
   if (type == kOutF32) return launch<float>(f, s);
   if (type == kOutF16) return launch<__half>(f, s);
   return launch<__nv_bfloat16>(f, s);
