@@ -10,6 +10,7 @@ dimension contiguous.  Outputs are passed in and returned.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -21,6 +22,12 @@ _Strides = ctypes.c_int64 * 3
 
 # (the second creates a Stream object each time)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+
+
+@functools.lru_cache(maxsize=256)
+def _strides(stride):
+    """The first three strides as a C array (of which only the values matter)."""
+    return _Strides(*stride[:3])
 
 
 class PackedWeights:
@@ -150,7 +157,7 @@ class Clear:
 
     def _strided(self, name, t, dtype, shape):
         """(address, strides) of a tensor [.][.][.][dim]."""
-        return self._at(name, t, dtype, shape), _Strides(*t.stride()[:3])
+        return self._at(name, t, dtype, shape), _strides(t.stride())
 
     def _cache(self, k_cache, v_cache, k_scale, v_scale, page_table, batch, heads, dim):
         _need(k_cache.dim() == 4, "k_cache must be [pages][heads][page tokens][dim]")
