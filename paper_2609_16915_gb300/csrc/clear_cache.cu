@@ -3,7 +3,7 @@
 // A unit of work is one page of one sequence, one cached head, keys or values:
 //   s' = max(s of the rows before the new ones, max|new| / 127)
 //   old rows q' = rint(q (s / s')) where s' grew, new rows q = rint(x / s').
-// The new rows are read twice (the second time from the cache), the old rows only where the scale
+// The new rows are read once (what a thread cannot keep in registers, twice), the old rows only where the scale
 // grew.  Bound by reading the new values and writing their bytes; a decode step by its latency.
 #include <stdint.h>
 
@@ -13,24 +13,62 @@ namespace rosetta {
 
 namespace {
 
-__device__ __forceinline__ int8_t to_int8(float v) {
-  return static_cast<int8_t>(__float2int_rn(fminf(fmaxf(v, -127.0f), 127.0f)));  // (a NaN gives -127, under a NaN scale)
-}
+// The low byte of rint(v), |v| < 2^22: v + 1.5 * 2^23 has it in its last bits (ties to even).
+constexpr float kMagic = 12582912.0f;
+
+__device__ __forceinline__ uint32_t rint_bits(float v) { return __float_as_uint(v + kMagic); }
 
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack {
   T v[VEC];
 };
 
-// WARPS of a unit: a block's four, or one for units of few values.  VEC: 4 consecutive dimensions an access
-// where the strides keep them aligned, else 1.
-template <typename T, int VEC, int WARPS>
-__global__ void __launch_bounds__(128) append_kernel(const ClearAppendArgs a) {
-  __shared__ float parts[4];
+// rint(x / div) of a pack, bytes in order.  The quotient by multiplication is off by less than 1e-4 (|x / div| <= 127 and
+// 2^-22 of it): only where it lies that close to a half, or is no number, the division decides.
+template <int VEC>
+__device__ __forceinline__ Pack<int8_t, VEC> quotients(const float (&x)[VEC], float div, float inv) {
+  uint32_t bits[VEC];
+  bool close = false;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    const float r = x[e] * inv, t = r + kMagic;
+    bits[e] = __float_as_uint(t);
+    close |= !(fabsf(r - (t - kMagic)) < 0.4999f);
+  }
+  if (close) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) bits[e] = rint_bits(x[e] / div);
+  }
+  Pack<int8_t, VEC> out;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) out.v[e] = static_cast<int8_t>(bits[e]);
+  return out;
+}
+
+// A thread's walk over the packs of consecutive rows: every `threads`-th.
+struct Walk {
+  uint32_t row, col, packs, rows_on, cols_on;
+  __device__ Walk(uint32_t at, uint32_t packs_, uint32_t threads)
+      : row(at / packs_), col(at % packs_), packs(packs_), rows_on(threads / packs_), cols_on(threads % packs_) {}
+  __device__ void on() {
+    row += rows_on;
+    col += cols_on;
+    if (col >= packs) {
+      col -= packs;
+      ++row;
+    }
+  }
+};
+
+// WARPS of a unit: one (four units a block), four, or sixteen for large pages.  VEC consecutive dimensions an access.
+// KEPT packs of new values stay in a thread's registers between the two passes.
+template <typename T, int VEC, int WARPS, int KEPT>
+__global__ void __launch_bounds__(WARPS == 16 ? 512 : 128) append_kernel(const ClearAppendArgs a) {
+  __shared__ float parts[16];
   constexpr uint32_t THREADS = 32 * WARPS;
   const uint32_t tid = threadIdx.x % THREADS;
   // heads and keys / values, four of them a block where a warp takes a unit
-  const uint32_t unit = blockIdx.y * (4 / WARPS) + threadIdx.x / THREADS;
+  const uint32_t unit = blockIdx.y * (WARPS == 1 ? 4 : 1) + threadIdx.x / THREADS;
   const uint32_t kv = unit & 1u, head = unit >> 1;
   if (head >= a.heads) return;  // (whole warps; there is no barrier where a block has several units)
   const uint32_t b = blockIdx.z;
@@ -45,84 +83,105 @@ __global__ void __launch_bounds__(128) append_kernel(const ClearAppendArgs a) {
     return;
   }
   const int64_t lo = first > row0 ? first : row0, hi = end < row0 + a.page_tokens ? end : row0 + a.page_tokens;
-  const int64_t step = a.src_strides[kv][1], row = a.cache_strides[2];
+  const int64_t step = a.src_strides[kv][1], line = a.cache_strides[2];
   const T *src = static_cast<const T *>(a.src[kv]) + static_cast<int64_t>(b) * a.src_strides[kv][0] + (lo - first) * step +
                  static_cast<int64_t>(head) * a.src_strides[kv][2];
   int8_t *dst = a.cache[kv] + static_cast<int64_t>(page) * a.cache_strides[0] + static_cast<int64_t>(head) * a.cache_strides[1];
-  const uint32_t packs = a.dim / VEC, old_rows = static_cast<uint32_t>(lo - row0);
-  const uint32_t fresh = static_cast<uint32_t>(hi - lo) * packs;
+  const uint32_t packs = a.dim / VEC, old_rows = static_cast<uint32_t>(lo - row0), new_rows = static_cast<uint32_t>(hi - lo);
+  float *scale = a.scale[kv] + static_cast<size_t>(page) * a.heads + head;
+  const float was = old_rows ? *scale : 0.0f;
   using P = Pack<T, VEC>;
-  const auto load = [&](uint32_t i) { return *reinterpret_cast<const P *>(src + static_cast<int64_t>(i / packs) * step + i % packs * VEC); };
+  const auto load = [&](const Walk &w) { return *reinterpret_cast<const P *>(src + static_cast<int64_t>(w.row) * step + w.col * VEC); };
   float m = 0.0f;
   bool bad = false;  // a NaN or an infinity
-  P kept;            // a thread's first pack, not read again
-#pragma unroll 4
-  for (uint32_t i = tid; i < fresh; i += THREADS) {
-    const P x = load(i);
-    if (i == tid) kept = x;
+  const auto take = [&](const P &x) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const float v = fabsf(to_float(x.v[e]));
       bad |= !(v < __int_as_float(0x7f800000));
       m = fmaxf(m, v);
     }
-  }
+  };
+  const Walk begin(tid, packs, THREADS);
+  P kept[KEPT];
+  Walk w = begin;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i, w.on())
+    if (w.row < new_rows) kept[i] = load(w);
+  Walk rest = w;
+  w = begin;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i, w.on())
+    if (w.row < new_rows) take(kept[i]);
+  for (w = rest; w.row < new_rows; w.on()) take(load(w));
   if (bad) m = __int_as_float(0x7f800000);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float *scale = a.scale[kv] + static_cast<size_t>(page) * a.heads + head;
-  const float was = old_rows ? *scale : 0.0f;
-  if constexpr (WARPS == 4) {
+  if constexpr (WARPS > 1) {
     if (threadIdx.x % 32 == 0) parts[threadIdx.x / 32] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3]));
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) m = fmaxf(m, parts[i]);
   } else {
     __syncwarp();  // (the old scale is read before it is written)
   }
   // a non-finite maximum, or an old scale that is NaN, gives NaN
   const float now = m < __int_as_float(0x7f800000) && was == was ? fmaxf(was, m / 127.0f) : __int_as_float(0x7fc00000);
-  const float div = now > 0.0f ? now : 1.0f;
+  const float div = now > 0.0f ? now : 1.0f, inv = 1.0f / div;
   if (old_rows && now != was) {
     const float ratio = was / div;
-    for (uint32_t i = tid; i < old_rows * packs; i += THREADS) {
-      Pack<int8_t, VEC> *p = reinterpret_cast<Pack<int8_t, VEC> *>(dst + static_cast<int64_t>(i / packs) * row + i % packs * VEC);
+    for (w = begin; w.row < old_rows; w.on()) {
+      Pack<int8_t, VEC> *p = reinterpret_cast<Pack<int8_t, VEC> *>(dst + static_cast<int64_t>(w.row) * line + w.col * VEC);
       Pack<int8_t, VEC> v = *p;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v.v[e] = to_int8(static_cast<float>(v.v[e]) * ratio);
+      for (int e = 0; e < VEC; ++e) v.v[e] = static_cast<int8_t>(rint_bits(static_cast<float>(v.v[e]) * ratio));
       *p = v;
     }
   }
-#pragma unroll 4
-  for (uint32_t i = tid; i < fresh; i += THREADS) {
-    const P x = i == tid ? kept : load(i);
-    Pack<int8_t, VEC> v;
+  const auto put = [&](const Walk &w, const P &x) {
+    float v[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) v.v[e] = to_int8(to_float(x.v[e]) / div);
-    *reinterpret_cast<Pack<int8_t, VEC> *>(dst + static_cast<int64_t>(old_rows + i / packs) * row + i % packs * VEC) = v;
-  }
+    for (int e = 0; e < VEC; ++e) v[e] = to_float(x.v[e]);
+    *reinterpret_cast<Pack<int8_t, VEC> *>(dst + static_cast<int64_t>(old_rows + w.row) * line + w.col * VEC) = quotients<VEC>(v, div, inv);
+  };
+  w = begin;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i, w.on())
+    if (w.row < new_rows) put(w, kept[i]);
+  for (w = rest; w.row < new_rows; w.on()) put(w, load(w));
   if (tid == 0) *scale = now;
 }
 
 template <typename T, int VEC>
 cudaError_t launch_vec(const ClearAppendArgs &a, cudaStream_t s) {
   const uint32_t most = (a.page_tokens - 1 + a.tokens - 1) / a.page_tokens + 1;  // pages a sequence's tokens can touch
-  // a warp a unit while it has a pack or two a lane: a step of 256 sequences, 8 heads of 128
-  if (a.tokens * a.dim <= 64u * VEC)
-    append_kernel<T, VEC, 1><<<dim3(most, (2 * a.heads + 3) / 4, a.batch), 128, 0, s>>>(a);
+  // as few threads as keep a unit in registers (each pack kept costs its index work, used or not): single tokens a warp
+  // with two packs a lane; 16 rows of 128 two a thread, 32 rows four (8 x 2043 tokens 26 us, 35 with eight)
+  const uint64_t packs = static_cast<uint64_t>(a.tokens < a.page_tokens ? a.tokens : a.page_tokens) * a.dim / VEC;
+  const dim3 units(most, 2 * a.heads, a.batch);
+  if (packs <= 64)
+    append_kernel<T, VEC, 1, 2><<<dim3(most, (2 * a.heads + 3) / 4, a.batch), 128, 0, s>>>(a);
+  else if (packs <= 256)
+    append_kernel<T, VEC, 4, 2><<<units, 128, 0, s>>>(a);
+  else if (packs <= 512)
+    append_kernel<T, VEC, 4, 4><<<units, 128, 0, s>>>(a);
   else
-    append_kernel<T, VEC, 4><<<dim3(most, 2 * a.heads, a.batch), 128, 0, s>>>(a);
+    append_kernel<T, VEC, 16, 4><<<units, 512, 0, s>>>(a);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t launch_type(const ClearAppendArgs &a, cudaStream_t s) {
-  // (dimensions and cache strides are multiples of 4, the caches 4-byte aligned)
-  uintptr_t src = 0;
+  uintptr_t src = 0, dst = static_cast<uintptr_t>(a.cache_strides[0] | a.cache_strides[1] | a.cache_strides[2] | a.dim);
   int64_t strides = 0;
   for (int kv = 0; kv < 2; ++kv) {
     src |= reinterpret_cast<uintptr_t>(a.src[kv]);
+    dst |= reinterpret_cast<uintptr_t>(a.cache[kv]);
     for (int i = 0; i < 3; ++i) strides |= a.src_strides[kv][i];
   }
+  constexpr int WIDE = 16 / sizeof(T);
+  if (src % 16 == 0 && strides % WIDE == 0 && dst % WIDE == 0) return launch_vec<T, WIDE>(a, s);
+  // (dimensions and cache strides are multiples of 4, the caches 4-byte aligned)
   return src % (4 * sizeof(T)) == 0 && strides % 4 == 0 ? launch_vec<T, 4>(a, s) : launch_vec<T, 1>(a, s);
 }
 

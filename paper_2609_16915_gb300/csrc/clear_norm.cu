@@ -59,14 +59,16 @@ struct alignas(sizeof(T) * VEC) Pack {
   T v[VEC];
 };
 
-// The row in registers, NV packs a thread, read once.  WARP: a warp per token, eight tokens a block;
-// otherwise a block per token.
-template <typename T, int VEC, int NV, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 1024) norm_kernel(const ClearNormArgs a) {
+// The row in registers, NV packs a thread, read once.  LANES of a warp (8 or 32) per token, 256 / LANES tokens a block;
+// 0: a block per token.
+template <typename T, int VEC, int NV, int LANES>
+__global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(const ClearNormArgs a) {
   __shared__ float2 parts[32];
-  const uint32_t tid = WARP ? threadIdx.x % 32 : threadIdx.x, threads = WARP ? 32 : blockDim.x;
-  const size_t t = WARP ? static_cast<size_t>(blockIdx.x) * 8 + threadIdx.x / 32 : blockIdx.x;
-  if (WARP && t >= a.tokens) return;
+  constexpr uint32_t GROUP = LANES ? LANES : 32;
+  const uint32_t tid = LANES ? threadIdx.x % GROUP : threadIdx.x, threads = LANES ? GROUP : blockDim.x;
+  const size_t t = LANES ? static_cast<size_t>(blockIdx.x) * (256 / GROUP) + threadIdx.x / GROUP : blockIdx.x;
+  if (LANES && t >= a.tokens) return;
+  const uint32_t mask = LANES == 8 ? 0xffu << (threadIdx.x % 32 / 8 * 8) : 0xffffffffu;  // the token's lanes
   const T *x = static_cast<const T *>(a.x) + t * a.x_pitch;
   const T *res = a.residual ? static_cast<const T *>(a.residual) + t * a.residual_pitch : nullptr;
   T *sum = a.sum_out ? static_cast<T *>(a.sum_out) + t * a.sum_pitch : nullptr;
@@ -100,11 +102,11 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024) norm_kernel(const ClearNorm
       if (sum) *reinterpret_cast<P *>(sum + i) = out;
     }
   }
-  if constexpr (WARP) {
+  if constexpr (LANES > 0) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(mask, s, o);
+      m = fmaxf(m, __shfl_xor_sync(mask, m, o));
     }
   } else {
     block_sum_max(s, m, parts);
@@ -152,17 +154,21 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const ClearNormArgs a) 
 template <typename T, int VEC, int NV>
 cudaError_t launch_block(const ClearNormArgs &a, cudaStream_t s) {
   const uint32_t threads = ((a.width + VEC * NV - 1) / (VEC * NV) + 31) / 32 * 32;
-  norm_kernel<T, VEC, NV, false><<<a.tokens, threads, 0, s>>>(a);
+  norm_kernel<T, VEC, NV, 0><<<a.tokens, threads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
-// A warp per token while four packs a lane hold the row (scalars: eight), then blocks of up to 512 threads with two, up to
+// A quarter of a warp, then a warp per token while four packs a lane hold the row (scalars: eight), then blocks of up to 512 threads with two, up to
 // 1024 with 32 elements each (scalars: 16).
 template <typename T, int VEC>
 cudaError_t launch_vec(const ClearNormArgs &a, cudaStream_t s) {
   constexpr int SMALL = VEC == 1 ? 8 : 4, MID = VEC == 1 ? 8 : 2, LARGE = VEC == 1 ? 16 : 32 / VEC;
+  if (a.width <= 8u * VEC * SMALL) {
+    norm_kernel<T, VEC, SMALL, 8><<<(a.tokens + 31) / 32, 256, 0, s>>>(a);
+    return cudaGetLastError();
+  }
   if (a.width <= 32u * VEC * SMALL) {
-    norm_kernel<T, VEC, SMALL, true><<<(a.tokens + 7) / 8, 256, 0, s>>>(a);
+    norm_kernel<T, VEC, SMALL, 32><<<(a.tokens + 7) / 8, 256, 0, s>>>(a);
     return cudaGetLastError();
   }
   if (a.width <= 512u * VEC * MID) return launch_block<T, VEC, MID>(a, s);
