@@ -369,7 +369,7 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
   a.err_flag = h->d_err;
   const cudaStream_t s = as_stream(stream);
   cudaError_t e;
-  if (attend_many_takes(a, type)) {
+  if (attend_many_takes(a)) {
     e = launch_clear_attention_many(a, type, s);
   } else if (attend_few_takes(a)) {
     const int r = ensure_work(h, attend_few_bytes(a, h->sms), s);

@@ -164,6 +164,10 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
 template <typename T, int DP>
 __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearAttentionArgs a, uint32_t row_blocks) {
   using M = Many<DP>;
+  // Single precision: one row tile, its queries and its weights in two halves each; the values stay whole numbers and
+  // the weights take their scales.
+  constexpr bool SPLIT = sizeof(T) == 4;
+  constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
   extern __shared__ __align__(1024) unsigned char smem[];
   // USED: the values of tile j and the keys of tile j + 2; SFULL, PFULL: of each row tile, its two score tiles;
   // LAST, BEFORE: the products of the last tile's weights and of the one before it; FIRST: the scores of the first two
@@ -187,7 +191,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
   __shared__ uint32_t s_skip[8][POS / 16];
-  __shared__ float s_top[4], s_sv, s_up[2 * ROWS];
+  __shared__ float s_vr[8][POS / 16];  // (SPLIT: value scales over the largest)
+  __shared__ float s_top[8], s_sv, s_up[2 * ROWS];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
@@ -195,20 +200,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   // (the blocks with the most positions first)
   const uint32_t bh = blockIdx.x % (a.batch * a.heads), kh = bh % a.heads, b = bh / a.heads;
   const uint32_t block = row_blocks - 1 - blockIdx.x / (a.batch * a.heads);
-  const uint32_t rows = a.tokens * a.group, row0 = block * (2 * ROWS);
+  const uint32_t rows = a.tokens * a.group, row0 = block * BLOCK_ROWS;
   int64_t len = a.lengths[b];
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
   if (len > most) {
     if (threadIdx.x == 0) atomicMax(a.err_flag, 1u);
     len = most;
   }
-  const int64_t seen = len - a.tokens + 1 + (min(row0 + 2 * ROWS, rows) - 1) / a.group;
+  const int64_t seen = len - a.tokens + 1 + (min(row0 + BLOCK_ROWS, rows) - 1) / a.group;
   const uint32_t end = seen > 0 ? static_cast<uint32_t>(seen) : 0u, n = (end + POS - 1) / POS;
-  const uint32_t row_tiles = rows - row0 > ROWS ? 2 : 1;
+  const uint32_t row_tiles = !SPLIT && rows - row0 > ROWS ? 2 : 1;
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
 
   if (n == 0) {  // no row of the block has a position: zeros
-    for (uint32_t i = warp; i < min(2 * ROWS, rows - row0); i += WARPS) {
+    for (uint32_t i = warp; i < min(BLOCK_ROWS, rows - row0); i += WARPS) {
       const uint32_t row = row0 + i;
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
@@ -259,54 +264,100 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     // eight dimensions at a time ----
     const uint32_t qr = lane % 8, qc = lane / 8;
     const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
-    uint4 raw[4][DP / 32];
+    if constexpr (SPLIT) {
+#pragma unroll 1
+      for (uint32_t g = 0; g < 4 && r == 0; ++g) {
+        const uint32_t in_tile = warp * 32 + g * 8 + qr, rw = row0 + in_tile;
+        const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
+                     static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
+        float x[DP / 32][8], top = 0.0f;
 #pragma unroll
-    for (uint32_t g = 0; g < 4; ++g) {
-      const uint32_t rw = row0 + r * ROWS + (warp % 4) * 32 + g * 8 + qr;
-      const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
-                   static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          const uint32_t d = (qc + 4 * i) * 8;
+          const bool in = rw < rows && d < a.dim;  // (dim is a multiple of 16)
+          float4 y[2] = {};
+          if (in && wide_q) {
+            y[0] = *reinterpret_cast<const float4 *>(q + d);
+            y[1] = *reinterpret_cast<const float4 *>(q + d + 4);
+          } else if (in) {
+            y[0] = make_float4(to_float(q[d]), to_float(q[d + 1]), to_float(q[d + 2]), to_float(q[d + 3]));
+            y[1] = make_float4(to_float(q[d + 4]), to_float(q[d + 5]), to_float(q[d + 6]), to_float(q[d + 7]));
+          }
+          x[i][0] = y[0].x, x[i][1] = y[0].y, x[i][2] = y[0].z, x[i][3] = y[0].w;
+          x[i][4] = y[1].x, x[i][5] = y[1].y, x[i][6] = y[1].z, x[i][7] = y[1].w;
 #pragma unroll
-      for (uint32_t i = 0; i < DP / 32; ++i) {
-        const uint32_t d = (qc + 4 * i) * 8;
-        raw[g][i] = make_uint4(0u, 0u, 0u, 0u);
-        if (rw >= rows || d >= a.dim) continue;  // (dim is a multiple of 16)
-        if (wide_q) {
-          raw[g][i] = *reinterpret_cast<const uint4 *>(q + d);
-        } else {
-          const auto two = [&](uint32_t e) {
-            const T lo = q[d + e], hi = q[d + e + 1];
-            return static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&lo)) |
-                   static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&hi)) << 16;
-          };
-          raw[g][i] = make_uint4(two(0), two(2), two(4), two(6));
+          for (uint32_t e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[i][e]));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+        const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const float down = copysignf(__int_as_float((127 - ex) << 23), a.softmax_scale);
+        if (qc == 0) s_up[in_tile] = __int_as_float((127 + ex) << 23);
+#pragma unroll
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            const float u = x[i][2 * e] * down, v = x[i][2 * e + 1] * down;
+            const __half2 h = __floats2half2_rn(u, v);
+            hi[e] = half2_bits(h);
+            lo[e] = half2_bits(__floats2half2_rn(u - __low2float(h), v - __high2float(h)));
+          }
+          unsigned char *dst = smem + (in_tile >> 3) * (DP * 16) + (qc + 4 * i) * 128 + qr * 16;
+          *reinterpret_cast<uint4 *>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4 *>(dst + M::Q_TILE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
       }
-    }
+    } else {
+      uint4 raw[4][DP / 32];
 #pragma unroll
-    for (uint32_t g = 0; g < 4; ++g) {
-      const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr;
-      float x[DP / 32][8], top = 0.0f;
+      for (uint32_t g = 0; g < 4; ++g) {
+        const uint32_t rw = row0 + r * ROWS + (warp % 4) * 32 + g * 8 + qr;
+        const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
+                     static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
 #pragma unroll
-      for (uint32_t i = 0; i < DP / 32; ++i) {
-        const T *el = reinterpret_cast<const T *>(&raw[g][i]);
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-          x[i][e] = to_float(el[e]);
-          top = fmaxf(top, fabsf(x[i][e]));
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          const uint32_t d = (qc + 4 * i) * 8;
+          raw[g][i] = make_uint4(0u, 0u, 0u, 0u);
+          if (rw >= rows || d >= a.dim) continue;  // (dim is a multiple of 16)
+          if (wide_q) {
+            raw[g][i] = *reinterpret_cast<const uint4 *>(q + d);
+          } else {
+            const auto two = [&](uint32_t e) {
+              const T lo = q[d + e], hi = q[d + e + 1];
+              return static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&lo)) |
+                     static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&hi)) << 16;
+            };
+            raw[g][i] = make_uint4(two(0), two(2), two(4), two(6));
+          }
         }
       }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-      const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
-      const float down = copysignf(__int_as_float((127 - ex) << 23), a.softmax_scale);
-      if (qc == 0) s_up[r * ROWS + in_tile] = __int_as_float((127 + ex) << 23);
 #pragma unroll
-      for (uint32_t i = 0; i < DP / 32; ++i) {
-        uint32_t w[4];
+      for (uint32_t g = 0; g < 4; ++g) {
+        const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr;
+        float x[DP / 32][8], top = 0.0f;
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) w[e] = half2_bits(__floats2half2_rn(x[i][2 * e] * down, x[i][2 * e + 1] * down));
-        *reinterpret_cast<uint4 *>(smem + r * M::Q_TILE + (in_tile >> 3) * (DP * 16) + (qc + 4 * i) * 128 + qr * 16) =
-            make_uint4(w[0], w[1], w[2], w[3]);
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          const T *el = reinterpret_cast<const T *>(&raw[g][i]);
+#pragma unroll
+          for (uint32_t e = 0; e < 8; ++e) {
+            x[i][e] = to_float(el[e]);
+            top = fmaxf(top, fabsf(x[i][e]));
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+        const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
+        const float down = copysignf(__int_as_float((127 - ex) << 23), a.softmax_scale);
+        if (qc == 0) s_up[r * ROWS + in_tile] = __int_as_float((127 + ex) << 23);
+#pragma unroll
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) w[e] = half2_bits(__floats2half2_rn(x[i][2 * e] * down, x[i][2 * e + 1] * down));
+          *reinterpret_cast<uint4 *>(smem + r * M::Q_TILE + (in_tile >> 3) * (DP * 16) + (qc + 4 * i) * 128 + qr * 16) =
+              make_uint4(w[0], w[1], w[2], w[3]);
+        }
       }
     }
     fence_async();
@@ -383,15 +434,23 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         float sum[4] = {};
 #pragma unroll
         for (uint32_t c = 0; c < POS; c += 32) {
-          uint32_t w[16];
+          uint32_t w[16], rest[16];
 #pragma unroll
           for (uint32_t e = 0; e < 32; e += 2) {
             const float kf = part ? 1.0f : s_ks[buf][(c + e) / 16] * factor;
-            const float p0 = ex2(fmaf(v[c + e], kf, off)), p1 = ex2(fmaf(v[c + e + 1], kf, off));
+            float p0 = ex2(fmaf(v[c + e], kf, off)), p1 = ex2(fmaf(v[c + e + 1], kf, off));
             sum[e / 2 % 4] += p0 + p1;
-            w[e / 2] = half2_bits(__floats2half2_rn(p0, p1));
+            if constexpr (SPLIT) {
+              const float ratio = s_vr[buf][(c + e) / 16];
+              p0 *= ratio;
+              p1 *= ratio;
+            }
+            const __half2 h = __floats2half2_rn(p0, p1);
+            w[e / 2] = half2_bits(h);
+            if constexpr (SPLIT) rest[e / 2] = half2_bits(__floats2half2_rn(p0 - __low2float(h), p1 - __high2float(h)));
           }
           tmem_st16(s_col + c / 2, w);
+          if constexpr (SPLIT) tmem_st16(s_col + POS / 2 + c / 2, rest);
         }
         tmem_wait_st();
         fence_before();
@@ -418,10 +477,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         for (uint32_t e = 0; e < 32; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
         if (wide) {
 #pragma unroll
-          for (uint32_t e = 0; e < 32; e += 8) {
-            alignas(16) T x[8];
+          for (uint32_t e = 0; e < 32; e += 16 / sizeof(T)) {
+            alignas(16) T x[16 / sizeof(T)];
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) x[i] = from_float<T>(o[e + i]);
+            for (uint32_t i = 0; i < 16 / sizeof(T); ++i) x[i] = from_float<T>(o[e + i]);
             if (c + e < a.dim) *reinterpret_cast<uint4 *>(out + c + e) = *reinterpret_cast<const uint4 *>(x);
           }
         } else {
@@ -488,6 +547,27 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       if (i < n) copy(i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    float sv = 1e-30f;
+    if (!keys || SPLIT) {
+      // the largest value scale of the pages seen
+      for (uint32_t p = threadIdx.x % 128; p < slots_end; p += 128) {
+        const int32_t id = table[p];
+        if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
+          const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
+          if (v < -neg_inf()) sv = fmaxf(sv, v);
+        } else {
+          atomicMax(a.err_flag, 1u);
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, o));
+      if (lane == 0) s_top[warp - SOFT_WARPS] = sv;
+      asm volatile("bar.sync %0, 128;" ::"r"(keys ? 1 : 2) : "memory");
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) sv = fmaxf(sv, s_top[(keys ? 0 : 4) + i]);
+      if (!keys && w == 0 && lane == 0) s_sv = sv;
+    }
+    const float per_sv = 1.0f / sv;
     uint32_t buf = 0;
     if (keys) {
       for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
@@ -510,6 +590,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
             // (a value scale that is a NaN or an infinity: no number)
             s_ks[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
             s_skip[j % 8][w] = skip[st];
+            if constexpr (SPLIT) s_vr[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f;
           }
           // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
           const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
@@ -538,25 +619,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         }
       }
     } else {
-      // the largest value scale of the pages seen
-      float sv = 1e-30f;
-      for (uint32_t p = threadIdx.x % 128; p < slots_end; p += 128) {
-        const int32_t id = table[p];
-        if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
-          const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
-          if (v < -neg_inf()) sv = fmaxf(sv, v);
-        } else {
-          atomicMax(a.err_flag, 1u);
-        }
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, o));
-      if (lane == 0) s_top[w] = sv;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-#pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) sv = fmaxf(sv, s_top[i]);
-      if (w == 0 && lane == 0) s_sv = sv;
-      const float per_sv = 1.0f / sv;
       constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
       const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
       // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store
@@ -589,10 +651,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
 #pragma unroll
             for (uint32_t p = 0; p < 4; ++p) {
               const uint32_t t0 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_a), t1 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_b);
-              o[0][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4140)), off), ratio));
-              o[1][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t0, 0x64646464u, 0x4342)), off), ratio));
-              o[2][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4140)), off), ratio));
-              o[3][p] = half2_bits(__hmul2(__hsub2(bits_half2(__byte_perm(t1, 0x64646464u, 0x4342)), off), ratio));
+#pragma unroll
+              for (uint32_t e = 0; e < 4; ++e) {
+                const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
+                o[e][p] = half2_bits(SPLIT ? v : __hmul2(v, ratio));
+              }
             }
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e)
@@ -621,6 +684,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
 #pragma unroll
         for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
           mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
+        if constexpr (SPLIT) {
+          const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
+#pragma unroll
+          for (uint32_t k = 0; k < DP / 16; ++k) mma_ss(tmem + two * POS, rest + k * 16u, kd + k * 16u, idesc(POS), 1, elect);
+        }
         if (elect) mbar_arrive(bar(SFULL + two));  // (also passes on the page scales that came with the keys)
         commit(bar(SFULL + two), elect);
       };
@@ -656,6 +724,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
             mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0, elect);
+          if constexpr (SPLIT) {
+#pragma unroll
+            for (uint32_t k = 0; k < POS / 16; ++k)
+              mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), 1, elect);
+          }
           if (j + 2 < n)
             scores(r, j + 2, kbuf);
           else
@@ -697,18 +770,20 @@ cudaError_t launch(const ClearAttentionArgs &a, cudaStream_t s) {
   auto kern = attend_many_kernel<T, DP>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
-  const uint32_t row_blocks = (a.tokens * a.group + 2 * ROWS - 1) / (2 * ROWS);
+  constexpr uint32_t block_rows = sizeof(T) == 4 ? ROWS : 2 * ROWS;
+  const uint32_t row_blocks = (a.tokens * a.group + block_rows - 1) / block_rows;
   kern<<<a.batch * a.heads * row_blocks, WARPS * 32, Many<DP>::SMEM, s>>>(a, row_blocks);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-bool attend_many_takes(const ClearAttentionArgs &a, int type) {
-  return type != kOutF32 && a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 64 && attend_few_takes(a);
+bool attend_many_takes(const ClearAttentionArgs &a) {
+  return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 64 && attend_few_takes(a);
 }
 
 cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, cudaStream_t s) {
+  if (type == kOutF32) return a.dim <= 64 ? launch<float, 64>(a, s) : launch<float, 128>(a, s);
   if (type == kOutF16) return a.dim <= 64 ? launch<__half, 64>(a, s) : launch<__half, 128>(a, s);
   return a.dim <= 64 ? launch<__nv_bfloat16, 64>(a, s) : launch<__nv_bfloat16, 128>(a, s);
 }
