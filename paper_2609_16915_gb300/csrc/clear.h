@@ -142,7 +142,8 @@ size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms);
 cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s);
 // for many (prompts), on the tensor cores: the same, heads up to 128
 bool attend_many_takes(const ClearAttentionArgs &a);
-cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, cudaStream_t s);
+size_t attend_many_bytes(const ClearAttentionArgs &a, int type, uint32_t sms);
+cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s);
 // and for every shape
 cudaError_t launch_clear_attention(const ClearAttentionArgs &a, int type, cudaStream_t s);
 

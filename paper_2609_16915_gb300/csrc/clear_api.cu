@@ -370,7 +370,9 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
   const cudaStream_t s = as_stream(stream);
   cudaError_t e;
   if (attend_many_takes(a)) {
-    e = launch_clear_attention_many(a, type, s);
+    const int r = ensure_work(h, attend_many_bytes(a, type, h->sms), s);
+    if (r != ROSETTA_OK) return r;
+    e = launch_clear_attention_many(a, type, h->work, h->sms, s);
   } else if (attend_few_takes(a)) {
     const int r = ensure_work(h, attend_few_bytes(a, h->sms), s);
     if (r != ROSETTA_OK) return r;

@@ -1,0 +1,45 @@
+// What both attention kernels share: the ranges that a sequence's positions are split into, and the join of their
+// partial results.
+#pragma once
+#include <stdint.h>
+
+#include "clear.h"
+
+namespace rosetta {
+
+struct AttendArgs {
+  ClearAttentionArgs a;
+  float *part;              // [batch][head][split][rows of all groups]: O [dim]
+  float2 *stats;            // the same: l, m
+  uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
+  uint32_t least;           // positions of a range at least
+};
+
+// Positions of each range of a sequence of `end`: whole tiles of all warps.
+__device__ __forceinline__ uint32_t split_share(const AttendArgs &f, uint32_t end) {
+  const uint32_t share = (end + f.splits - 1) / f.splits;
+  return ((share < f.least ? f.least : share) + 63) / 64 * 64;
+}
+
+// Positions that the rows of a group see at most: up to the last token of the group.
+__device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64_t len, uint32_t last_row) {
+  const int64_t end = len - a.tokens + 1 + last_row / a.group;
+  return end > 0 ? static_cast<uint32_t>(end) : 0u;
+}
+
+// Join the splits of every row; group_rows: rows that one block's ranges were laid out for.
+cudaError_t launch_attend_join(const AttendArgs &f, int type, uint32_t group_rows, cudaStream_t s);
+
+// Floats of the partial results, and their place in the workspace (rows of 16 floats at least: the statistics behind
+// them are aligned).
+inline size_t attend_part_bytes(const AttendArgs &f) {
+  const ClearAttentionArgs &a = f.a;
+  return f.splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
+}
+inline void attend_place(AttendArgs *f, void *work) {
+  const ClearAttentionArgs &a = f->a;
+  f->part = static_cast<float *>(work);
+  f->stats = reinterpret_cast<float2 *>(f->part + static_cast<size_t>(a.batch) * a.heads * f->splits * (a.tokens * a.group) * a.dim);
+}
+
+}  // namespace rosetta

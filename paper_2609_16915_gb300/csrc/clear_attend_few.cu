@@ -17,7 +17,7 @@
 // workspace and attend_join_kernel; a sequence that fits one range is written at once.
 #include <stdint.h>
 
-#include "clear.h"
+#include "clear_attend.cuh"
 #include "dsmem.cuh"
 
 namespace rosetta {
@@ -77,26 +77,6 @@ struct Few {
   static constexpr uint32_t BLOCKS = DP == 256 ? 2 : 4;              // an SM
 };
 
-struct FewArgs {
-  ClearAttentionArgs a;
-  float *part;              // [batch][head][split][rows of all groups]: O [dim]
-  float2 *stats;            // the same: l, m
-  uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
-  uint32_t least;           // positions of a range at least
-};
-
-// Positions of each range of a sequence of `end`: whole tiles of all warps.
-__device__ __forceinline__ uint32_t split_share(const FewArgs &f, uint32_t end) {
-  const uint32_t share = (end + f.splits - 1) / f.splits;
-  return ((share < f.least ? f.least : share) + 63) / 64 * 64;
-}
-
-// Positions that the rows of a group see at most: up to the last token of the group.
-__device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64_t len, uint32_t last_row) {
-  const int64_t end = len - a.tokens + 1 + last_row / a.group;
-  return end > 0 ? static_cast<uint32_t>(end) : 0u;
-}
-
 __device__ __forceinline__ int64_t length_of(const ClearAttentionArgs &a, uint32_t b) {
   const int64_t len = a.lengths[b], most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
   if (len > most && threadIdx.x == 0) atomicMax(a.err_flag, 1u);
@@ -104,7 +84,7 @@ __device__ __forceinline__ int64_t length_of(const ClearAttentionArgs &a, uint32
 }
 
 template <typename T, int DP, int NB>
-__global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) attend_few_kernel(const FewArgs f) {
+__global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) attend_few_kernel(const AttendArgs f) {
   using F = Few<DP>;
   constexpr bool SPLIT = sizeof(T) == 4;     // queries and weights in two halves
   constexpr int H = SPLIT ? 2 : 1;
@@ -458,23 +438,26 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 
 constexpr int kJoinWarps = 8;
 
-// Joins the splits of a row: a block a row, a warp every eighth split, a lane four dimensions (and 128 further on).
-template <typename T>
-__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const FewArgs f, uint32_t group_rows) {
+// Joins the splits of a row: WARPS warps a row (8: a block a row; 1: eight rows a block), a warp every WARPS-th split, a lane
+// four dimensions (and 128 further on).
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const AttendArgs f, uint32_t group_rows) {
   __shared__ float s_o[kJoinWarps][256], s_m[kJoinWarps], s_l[kJoinWarps];
   const ClearAttentionArgs &a = f.a;
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = a.tokens * a.group;
-  const uint32_t bh = blockIdx.x / rows, row = blockIdx.x % rows, kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t warp = threadIdx.x / 32 % WARPS, lane = threadIdx.x % 32, rows = a.tokens * a.group;
+  const uint32_t id = blockIdx.x * (kJoinWarps / WARPS) + threadIdx.x / (32 * WARPS);
+  const bool real = id < a.batch * a.heads * rows;
+  const uint32_t bh = real ? id / rows : 0, row = id % rows, kh = bh % a.heads, b = bh / a.heads;
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens, given = a.lengths[b], len = given > most ? most : given;
   const uint32_t end = group_end(a, len, min(row / group_rows * group_rows + group_rows, rows) - 1);
   const uint32_t share = split_share(f, end), count = (end + share - 1) / share;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (end <= share) return;  // written already
+  if (!real || end <= share) return;  // (whole rows; written already)
   const size_t at = static_cast<size_t>(bh) * f.splits * rows + row;
   float top = neg_inf(), sum = 0.0f;
   float4 o[2] = {};
-  for (uint32_t s0 = warp; s0 < count; s0 += 32 * kJoinWarps) {  // lane i: split s0 + 8 i
-    const uint32_t mine = s0 + kJoinWarps * lane, n = min(32u, (count - s0 + kJoinWarps - 1) / kJoinWarps);
+  for (uint32_t s0 = warp; s0 < count; s0 += 32 * WARPS) {  // lane i: split s0 + WARPS i
+    const uint32_t mine = s0 + WARPS * lane, n = min(32u, (count - s0 + WARPS - 1) / WARPS);
     const float2 lm = mine < count ? f.stats[at + static_cast<size_t>(mine) * rows] : make_float2(0.0f, neg_inf());
     float t = fmaxf(top, lm.y);
 #pragma unroll
@@ -489,7 +472,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const FewA
 #pragma unroll
     for (int i = 0; i < 2; ++i) o[i] = make_float4(o[i].x * fade, o[i].y * fade, o[i].z * fade, o[i].w * fade);
     const float *src = f.part + (at + static_cast<size_t>(s0) * rows) * a.dim + lane * 4;
-    const size_t step = static_cast<size_t>(kJoinWarps) * rows * a.dim;
+    const size_t step = static_cast<size_t>(WARPS) * rows * a.dim;
 #pragma unroll 4
     for (uint32_t j = 0; j < n; ++j, src += step) {
       const float k = __shfl_sync(0xffffffffu, keep, j);
@@ -501,34 +484,47 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const FewA
         }
     }
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&s_o[warp][lane * 4 + 128 * i]) = o[i];
-  if (lane == 0) {
-    s_m[warp] = top;
-    s_l[warp] = sum;
-  }
-  __syncthreads();
-  top = neg_inf();
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w]);
-  sum = 0.0f;
-  float v = 0.0f;
-  const uint32_t d = threadIdx.x;
-#pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) {
-    const float keep = s_m[w] == neg_inf() ? 0.0f : ex2(s_m[w] - top);
-    sum += s_m[w] == neg_inf() ? s_l[w] : s_l[w] * keep;
-    v += keep * s_o[w][d];
-  }
   T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
            static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
-  if (d < a.dim) out[d] = from_float<T>(sum == 0.0f ? 0.0f : v / sum);
+  if constexpr (WARPS == 1) {
+    const float scale = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t d = lane * 4 + 128 * i;
+      if (d >= a.dim) continue;
+      out[d] = from_float<T>(o[i].x * scale);
+      out[d + 1] = from_float<T>(o[i].y * scale);
+      out[d + 2] = from_float<T>(o[i].z * scale);
+      out[d + 3] = from_float<T>(o[i].w * scale);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&s_o[warp][lane * 4 + 128 * i]) = o[i];
+    if (lane == 0) {
+      s_m[warp] = top;
+      s_l[warp] = sum;
+    }
+    __syncthreads();
+    top = neg_inf();
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_m[w]);
+    sum = 0.0f;
+    float v = 0.0f;
+    const uint32_t d = threadIdx.x;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+      const float keep = s_m[w] == neg_inf() ? 0.0f : ex2(s_m[w] - top);
+      sum += s_m[w] == neg_inf() ? s_l[w] : s_l[w] * keep;
+      v += keep * s_o[w][d];
+    }
+    if (d < a.dim) out[d] = from_float<T>(sum == 0.0f ? 0.0f : v / sum);
+  }
 }
 
 // Splits of a sequence.  Ranges of 1024 positions, or 512 or 256 where those leave SMs without a block; no more of them
 // than fill the SMs four times over (uneven lengths then even out).  Longer ranges cost less to begin and to join
 // (8 sequences of 4096, 8 heads: 1024 positions 29.3 us, 512 32.7), shorter ones balance better.
-void split(FewArgs *f, uint32_t sms) {
+void split(AttendArgs *f, uint32_t sms) {
   const ClearAttentionArgs &a = f->a;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f->groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
   f->least = 1024;
@@ -542,35 +538,23 @@ void split(FewArgs *f, uint32_t sms) {
 uint32_t group_rows_of(const ClearAttentionArgs &a) { return a.tokens * a.group <= 8 ? 8 : 16; }
 
 template <typename T, int DP, int NB>
-cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   auto kern = attend_few_kernel<T, DP, NB>;
   constexpr uint32_t join = (kWarps * 8 * (DP + 4) + kWarps * 8 * 2) * 4;
   constexpr uint32_t smem = Few<DP>::RING > join ? Few<DP>::RING : join;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   kern<<<f.a.batch * f.a.heads * f.groups * f.splits, 32 * kWarps, smem, s>>>(f);
-  e = cudaGetLastError();
-  if (e != cudaSuccess || f.splits == 1) return e;
-  cudaLaunchConfig_t cfg = {};
-  const uint64_t rows = static_cast<uint64_t>(f.a.batch) * f.a.heads * f.a.tokens * f.a.group;
-  cfg.gridDim = dim3(static_cast<uint32_t>(rows));
-  cfg.blockDim = dim3(32 * kJoinWarps);
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attend_join_kernel<T>, f, static_cast<uint32_t>(8 * NB));
+  return cudaGetLastError();
 }
 
 template <typename T, int DP>
-cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   return group_rows_of(f.a) == 8 ? launch<T, DP, 1>(f, s) : launch<T, DP, 2>(f, s);
 }
 
 template <typename T>
-cudaError_t launch(const FewArgs &f, cudaStream_t s) {
+cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   if (f.a.dim <= 64) return launch<T, 64>(f, s);
   if (f.a.dim <= 128) return launch<T, 128>(f, s);
   return launch<T, 256>(f, s);
@@ -586,28 +570,46 @@ bool attend_few_takes(const ClearAttentionArgs &a) {
 
 namespace {
 
-FewArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
-  FewArgs f{a, static_cast<float *>(work), nullptr, 1, 1, 1};
+AttendArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
+  AttendArgs f{a, nullptr, nullptr, 1, 1, 1};
   const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a);
   f.groups = (rows + gr - 1) / gr;
   split(&f, sms);
-  // (rows of 16 floats at least: the statistics behind them are aligned)
-  f.stats = reinterpret_cast<float2 *>(f.part + static_cast<size_t>(a.batch) * a.heads * f.splits * rows * a.dim);
+  attend_place(&f, work);
   return f;
+}
+
+template <typename T>
+cudaError_t launch_join(const AttendArgs &f, uint32_t group_rows, cudaStream_t s) {
+  const uint64_t rows = static_cast<uint64_t>(f.a.batch) * f.a.heads * f.a.tokens * f.a.group;
+  const bool many = f.splits > 8;  // a warp reads eight partial rows as fast as eight warps would start
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<uint32_t>(many ? rows : (rows + kJoinWarps - 1) / kJoinWarps));
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return many ? cudaLaunchKernelEx(&cfg, attend_join_kernel<T, kJoinWarps>, f, group_rows)
+              : cudaLaunchKernelEx(&cfg, attend_join_kernel<T, 1>, f, group_rows);
 }
 
 }  // namespace
 
-size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms) {
-  const FewArgs f = few_args(a, nullptr, sms);
-  return f.splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
+cudaError_t launch_attend_join(const AttendArgs &f, int type, uint32_t group_rows, cudaStream_t s) {
+  if (type == kOutF32) return launch_join<float>(f, group_rows, s);
+  if (type == kOutF16) return launch_join<__half>(f, group_rows, s);
+  return launch_join<__nv_bfloat16>(f, group_rows, s);
 }
 
+size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms) { return attend_part_bytes(few_args(a, nullptr, sms)); }
+
 cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s) {
-  const FewArgs f = few_args(a, work, sms);
-  if (type == kOutF32) return launch<float>(f, s);
-  if (type == kOutF16) return launch<__half>(f, s);
-  return launch<__nv_bfloat16>(f, s);
+  const AttendArgs f = few_args(a, work, sms);
+  const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
+  return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, group_rows_of(a), s);
 }
 
 }  // namespace rosetta

@@ -23,7 +23,7 @@
 // products it issued before it frees the tensor memory.
 #include <stdint.h>
 
-#include "clear.h"
+#include "clear_attend.cuh"
 #include "dsmem.cuh"
 #include "tcgen.cuh"
 
@@ -162,7 +162,8 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearAttentionArgs a, uint32_t row_blocks) {
+__global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const AttendArgs f) {
+  const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
   // Single precision: one row tile, its queries and its weights in two halves each; the values stay whole numbers and
   // the weights take their scales.
@@ -198,8 +199,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
 
   // (the blocks with the most positions first)
-  const uint32_t bh = blockIdx.x % (a.batch * a.heads), kh = bh % a.heads, b = bh / a.heads;
-  const uint32_t block = row_blocks - 1 - blockIdx.x / (a.batch * a.heads);
+  const uint32_t split = blockIdx.x % f.splits, bh = blockIdx.x / f.splits % (a.batch * a.heads), kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t block = f.groups - 1 - blockIdx.x / f.splits / (a.batch * a.heads);
   const uint32_t rows = a.tokens * a.group, row0 = block * BLOCK_ROWS;
   int64_t len = a.lengths[b];
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
@@ -207,8 +208,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     if (threadIdx.x == 0) atomicMax(a.err_flag, 1u);
     len = most;
   }
-  const int64_t seen = len - a.tokens + 1 + (min(row0 + BLOCK_ROWS, rows) - 1) / a.group;
-  const uint32_t end = seen > 0 ? static_cast<uint32_t>(seen) : 0u, n = (end + POS - 1) / POS;
+  // this block's range of the positions that its rows see
+  const uint32_t all = group_end(a, len, min(row0 + BLOCK_ROWS, rows) - 1), share = split_share(f, all);
+  const uint32_t start = split * share, end = min(all, start + share);
+  if (split > 0 && start >= all) return;
+  const bool alone = all <= share;
+  const uint32_t n = (end - start + POS - 1) / POS;
   const uint32_t row_tiles = !SPLIT && rows - row0 > ROWS ? 2 : 1;
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
 
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         for (uint32_t i = 0; i < POS / 16; ++i) skip |= s_skip[buf][i];
         float top2 = neg_inf();
         // (the same for the warp)
-        const bool part = __any_sync(0xffffffffu, skip != 0 || static_cast<int32_t>(j * POS + POS - 1) > last);
+        const bool part = __any_sync(0xffffffffu, skip != 0 || static_cast<int32_t>(start + j * POS + POS - 1) > last);
         if (part) {
 #pragma unroll
           for (uint32_t i = 0; i < POS / 16; ++i) {
@@ -391,7 +396,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
             const bool out = s_skip[buf][i] != 0;
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
-              const bool in = static_cast<int32_t>(j * POS + i * 16 + e) <= last && !out;
+              const bool in = static_cast<int32_t>(start + j * POS + i * 16 + e) <= last && !out;
               v[i * 16 + e] = in ? v[i * 16 + e] * kf : neg_inf();
               top2 = fmaxf(top2, v[i * 16 + e]);
             }
@@ -466,7 +471,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
-      const float scale = s_sv / l;
+      // (O and l are both lifted; partial results are not)
+      const float scale = alone ? s_sv / l : s_sv * 0.0078125f;
+      const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
+      if (!alone && row < rows) f.stats[at] = make_float2(l * 0.0078125f, m);
 #pragma unroll 1
       for (uint32_t c = 0; c < DP; c += 32) {
         float o[32];
@@ -475,7 +483,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
         if (row >= rows) continue;
 #pragma unroll
         for (uint32_t e = 0; e < 32; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
-        if (wide) {
+        if (!alone) {
+#pragma unroll
+          for (uint32_t e = 0; e < 32; e += 4)
+            if (c + e < a.dim) *reinterpret_cast<float4 *>(f.part + at * a.dim + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        } else if (wide) {
 #pragma unroll
           for (uint32_t e = 0; e < 32; e += 16 / sizeof(T)) {
             alignas(16) T x[16 / sizeof(T)];
@@ -497,7 +509,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     const bool keys = warp < SOFT_WARPS + 4;
     // the tiles to copy next: their pages, loaded a ring ahead; of the first, the page's slot in the list and the first row in it
     const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
-    uint32_t slot = w * 16 / a.page_tokens, row = w * 16 % a.page_tokens;
+    uint32_t slot = (start + w * 16) / a.page_tokens, row = (start + w * 16) % a.page_tokens;
     uint32_t ahead_slot = slot, ahead_row = row;
     const auto next = [&](uint32_t &at_slot, uint32_t &at_row) {
       at_slot += slots;
@@ -550,7 +562,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const ClearA
     float sv = 1e-30f;
     if (!keys || SPLIT) {
       // the largest value scale of the pages seen
-      for (uint32_t p = threadIdx.x % 128; p < slots_end; p += 128) {
+      for (uint32_t p = start / a.page_tokens + threadIdx.x % 128; p < slots_end; p += 128) {
         const int32_t id = table[p];
         if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
           const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
@@ -765,27 +777,49 @@ done:
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+uint32_t block_rows_of(int type) { return type == kOutF32 ? ROWS : 2 * ROWS; }
+
+// Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least.
+AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t sms) {
+  AttendArgs f{a, nullptr, nullptr, 1, 1, 512};
+  const uint32_t block = block_rows_of(type);
+  f.groups = (a.tokens * a.group + block - 1) / block;
+  const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
+  const uint64_t want = sms / blocks, longest = (most + 511) / 512;
+  f.splits = static_cast<uint32_t>(want < longest ? want : longest);
+  if (f.splits < 1) f.splits = 1;
+  attend_place(&f, work);
+  return f;
+}
+
 template <typename T, int DP>
-cudaError_t launch(const ClearAttentionArgs &a, cudaStream_t s) {
+cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   auto kern = attend_many_kernel<T, DP>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
-  constexpr uint32_t block_rows = sizeof(T) == 4 ? ROWS : 2 * ROWS;
-  const uint32_t row_blocks = (a.tokens * a.group + block_rows - 1) / block_rows;
-  kern<<<a.batch * a.heads * row_blocks, WARPS * 32, Many<DP>::SMEM, s>>>(a, row_blocks);
+  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, WARPS * 32, Many<DP>::SMEM, s>>>(f);
   return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
+  return f.a.dim <= 64 ? launch<T, 64>(f, s) : launch<T, 128>(f, s);
 }
 
 }  // namespace
 
+// From 48 rows a cached head on: the other kernel takes 16 at a time (0.65 us an SM for 64 positions), this one 256 in 1.4 us
+// (128 of single precision).
 bool attend_many_takes(const ClearAttentionArgs &a) {
-  return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 64 && attend_few_takes(a);
+  return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 48 && attend_few_takes(a);
 }
 
-cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, cudaStream_t s) {
-  if (type == kOutF32) return a.dim <= 64 ? launch<float, 64>(a, s) : launch<float, 128>(a, s);
-  if (type == kOutF16) return a.dim <= 64 ? launch<__half, 64>(a, s) : launch<__half, 128>(a, s);
-  return a.dim <= 64 ? launch<__nv_bfloat16, 64>(a, s) : launch<__nv_bfloat16, 128>(a, s);
+size_t attend_many_bytes(const ClearAttentionArgs &a, int type, uint32_t sms) { return attend_part_bytes(many_args(a, type, nullptr, sms)); }
+
+cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s) {
+  const AttendArgs f = many_args(a, type, work, sms);
+  const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
+  return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, block_rows_of(type), s);
 }
 
 }  // namespace rosetta
