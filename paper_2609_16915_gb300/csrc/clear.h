@@ -20,9 +20,8 @@ struct ClearNormArgs {
   float eps;
 };
 
-// Packed weights: [row tile][k step] tiles of 128 channels x 64 inputs, a tile as eight
-// blocks of 16 channels (1 KB in a row), a block as four chunks of 16 inputs, a chunk as 16 rows of 16
-// bytes.
+// Packed weights: [row tile][k step] tiles of 128 channels x 64 inputs, a row 64 bytes with its chunk c (of 16 inputs)
+// at c ^ (row / 2 % 4): eight lanes read 128 bytes in a row of memory, and one chunk of eight rows every bank once.
 constexpr uint32_t kPackRows = 128, kPackK = 64, kPackTile = kPackRows * kPackK;
 
 enum ClearOut : int { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutCodes = 3 };  // 0 .. 2: rosetta_float_type

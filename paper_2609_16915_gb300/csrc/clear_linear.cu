@@ -20,7 +20,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const int8_t *__restrict__ w,
                                                    uint64_t rows16) {
   const uint64_t id = static_cast<uint64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (id >= rows16) return;
-  const uint32_t row = id / 64 % 8 * 16 + id % 16, chunk = id / 16 % 4;
+  const uint32_t row = id / 4 % kPackRows, chunk = (id % 4) ^ (row >> 1 & 3u);
   const uint64_t tile = id / (kPackRows * 4);
   const uint64_t n = tile / k_steps * kPackRows + row;
   const uint32_t k0 = tile % k_steps * kPackK + chunk * 16;
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linea
   extern __shared__ __align__(16) int32_t parts[];  // [warp][channel][token]
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t n0 = blockIdx.x * 32;
-  const int8_t *w = a.packed + static_cast<size_t>(n0 / kPackRows) * a.k_steps * kPackTile + n0 % kPackRows * kPackK + (t * 16 + g) * 16;
+  const int8_t *w = a.packed + static_cast<size_t>(n0 / kPackRows) * a.k_steps * kPackTile + n0 % kPackRows * kPackK + (g * 4 + (t ^ (g >> 1 & 3u))) * 16;
   const int8_t *rows[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) rows[b] = a.q + static_cast<int64_t>(min(b * 8 + g, a.tokens - 1)) * a.q_pitch;
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linea
       const uint32_t at = k * kPackK + t * 16;
 #pragma unroll
       for (int r = 0; r < 4; ++r)  // (read once: first to leave the caches)
-        wv[u][r] = __ldcs(reinterpret_cast<const uint4 *>(w + static_cast<size_t>(k) * kPackTile + r / 2 * (16 * kPackK) + r % 2 * 128));
+        wv[u][r] = __ldcs(reinterpret_cast<const uint4 *>(w + static_cast<size_t>(k) * kPackTile + r * (8 * kPackK)));
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         xv[u][b] = make_uint4(0u, 0u, 0u, 0u);

@@ -244,10 +244,11 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
         goto done;
       }
       uint32_t v[32];
-      const uint4 *src = reinterpret_cast<const uint4 *>(smem + ws * kPackTile) + threadIdx.x % kPackRows / 16 * 64 + threadIdx.x % 16;
+      const uint32_t turn = threadIdx.x >> 1 & 3u;  // how this row's chunks are moved
+      const uint4 *src = reinterpret_cast<const uint4 *>(smem + ws * kPackTile) + threadIdx.x % kPackRows * 4;
 #pragma unroll
       for (uint32_t c = 0; c < 4; ++c) {
-        const uint4 w = src[c * 16];
+        const uint4 w = src[c ^ turn];
         int8x4_f16(w.x, v[c * 8 + 0], v[c * 8 + 1]);
         int8x4_f16(w.y, v[c * 8 + 2], v[c * 8 + 3]);
         int8x4_f16(w.z, v[c * 8 + 4], v[c * 8 + 5]);
