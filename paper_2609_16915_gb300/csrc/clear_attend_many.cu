@@ -11,7 +11,7 @@
 //                    scale), values transposed by byte permutes to [dimension][position] and times their scale over the
 //                    largest one
 //   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory
-//   2 x 4 softmax warps  a thread a row: scores from tensor memory, times the page's key scale and the row's
+//   2 x 8 softmax warps  two threads a row, 32 positions each: scores from tensor memory, times the page's key scale and the row's
 //                    factor, 2^(s - m + 7) with the running maximum m raised only where a score passes it by 8
 //                    (then O is scaled down in place), P as f16 over the scores' columns
 // With two score tiles a row tile, one row tile's next scores are there when its softmax is done: the handing over
@@ -31,11 +31,11 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 8, CONVERT_WARPS = 8, WARPS = 20;
+constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 16, CONVERT_WARPS = 8, WARPS = 28;
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
 // registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out; more
 // than was launched would wait forever
-constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 128, CONVERT_REGS = 80, MMA_REGS = 64;
+constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 72, CONVERT_REGS = 80, MMA_REGS = 56;
 static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
                   WARPS * LAUNCH_REGS,
               "register shares");
@@ -116,16 +116,22 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v) {
       : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld16f(uint32_t taddr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void tmem_st32f(uint32_t taddr, const float *v) {
+__device__ __forceinline__ void tmem_st16f(uint32_t taddr, const float (&v)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+          taddr),
       "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]),
-      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]),
-      "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]),
-      "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+      "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -188,12 +194,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   };
   __shared__ __align__(8) uint64_t bars[BARS];
   __shared__ uint32_t tmem_slot, s_fail;
+  __shared__ uint32_t s_quit[SOFT_WARPS / 2];  // the meeting at which one of two softmax warps gave up
   // of the last eight tiles (the conversion is at most four ahead of a softmax), by groups of 16 positions: key
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
   __shared__ uint32_t s_skip[8][POS / 16];
   __shared__ float s_vr[8][POS / 16];  // (SPLIT: value scales over the largest)
-  __shared__ float s_top[8], s_sv, s_up[2 * ROWS];
+  __shared__ float s_top[8], s_sv;
+  // what the two threads of a row exchange; before the first tile, the power of two of each row's queries
+  __shared__ float s_max[2][2 * ROWS];
+  float *s_up = s_max[0];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t base = smem_addr(smem), bar0 = smem_addr(bars);
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
@@ -233,6 +243,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   }
   if (threadIdx.x == 0) {
     s_fail = 0u;
+    for (uint32_t i = 0; i < SOFT_WARPS / 2; ++i) s_quit[i] = 0u;
     mbar_init(bar(QFULL), SOFT_WARPS);
     for (uint32_t i = 0; i < RING; ++i) {
       mbar_init(bar(KFULL + i), 4);
@@ -241,7 +252,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     }
     for (uint32_t i = 0; i < 4; ++i) {
       mbar_init(bar(SFULL + i), 2);
-      mbar_init(bar(PFULL + i), 4);
+      mbar_init(bar(PFULL + i), SOFT_WARPS / 2);
     }
     mbar_init(bar(FIRST), 1);
     mbar_init(bar(FREE), 1);
@@ -261,18 +272,39 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   };
 
   if (warp < SOFT_WARPS) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFT_REGS));
-    const uint32_t r = warp / 4, row_in = threadIdx.x % ROWS, row = row0 + r * ROWS + row_in;
+    static_assert(SOFT_REGS == LAUNCH_REGS, "no share to ask for");
+    // row tile, half of the columns, row: two threads a row, in warps that share a quarter of tensor memory
+    const uint32_t r = warp / 8, half = warp / 4 % 2, row_in = (warp % 4) * 32 + lane, row = row0 + r * ROWS + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
-    const uint32_t o_col = tmem + lanes + M::O_COL + r * DP;
-    // ---- the warp's 32 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
+    const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
+    // The two warps of a row meet at barrier 3 + pair.  A warp whose wait gave up meets the other once more and says
+    // at which meeting, so that neither waits for one that has left.
+    const uint32_t pair = r * 4 + warp % 4;
+    uint32_t meetings = 0;
+    const auto meet = [&](bool mine) {  // does either of the two say so?
+      uint32_t any;
+      asm volatile(
+          "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+          : "=r"(any)
+          : "r"(static_cast<uint32_t>(mine)), "r"(3 + pair)
+          : "memory");
+      ++meetings;
+      return any != 0u;
+    };
+    const auto other_left = [&]() { return *const_cast<volatile uint32_t *>(&s_quit[pair]) == meetings; };
+    const auto leave = [&]() {
+      give_up();
+      s_quit[pair] = meetings + 1;
+      meet(false);
+    };
+    // ---- the warp's 16 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
     // eight dimensions at a time ----
     const uint32_t qr = lane % 8, qc = lane / 8;
     const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
     if constexpr (SPLIT) {
 #pragma unroll 1
-      for (uint32_t g = 0; g < 4 && r == 0; ++g) {
-        const uint32_t in_tile = warp * 32 + g * 8 + qr, rw = row0 + in_tile;
+      for (uint32_t g = 0; g < 2 && r == 0; ++g) {
+        const uint32_t in_tile = warp * 16 + g * 8 + qr, rw = row0 + in_tile;
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
         float x[DP / 32][8], top = 0.0f;
@@ -314,10 +346,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
         }
       }
     } else {
-      uint4 raw[4][DP / 32];
+      uint4 raw[2][DP / 32];
 #pragma unroll
-      for (uint32_t g = 0; g < 4; ++g) {
-        const uint32_t rw = row0 + r * ROWS + (warp % 4) * 32 + g * 8 + qr;
+      for (uint32_t g = 0; g < 2; ++g) {
+        const uint32_t rw = row0 + r * ROWS + (warp % 8) * 16 + g * 8 + qr;
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
 #pragma unroll
@@ -338,8 +370,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
         }
       }
 #pragma unroll
-      for (uint32_t g = 0; g < 4; ++g) {
-        const uint32_t in_tile = (warp % 4) * 32 + g * 8 + qr;
+      for (uint32_t g = 0; g < 2; ++g) {
+        const uint32_t in_tile = (warp % 8) * 16 + g * 8 + qr;
         float x[DP / 32][8], top = 0.0f;
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
@@ -368,142 +400,149 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     fence_async();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(QFULL));
+    asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
     const int32_t last = row < rows ? static_cast<int32_t>(len - a.tokens + row / a.group) : -1;
+    constexpr uint32_t COLS = POS / 2;
     float m = neg_inf(), l = 0.0f;
     if (r < row_tiles) {
       for (uint32_t j = 0; j < n; ++j) {
-        const uint32_t buf = j % 8, two = r * 2 + j % 2, s_col = tmem + lanes + two * POS;
+        const uint32_t buf = j % 8, two = r * 2 + j % 2, s_tile = tmem + lanes + two * POS;
         if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (j / 2) & 1u))) {
-          give_up();
+          leave();
           goto done;
         }
         fence_after();
-        float v[POS];
-#pragma unroll
-        for (uint32_t c = 0; c < POS; c += 32) tmem_ld32(s_col + c, v + c);
-        tmem_wait_ld();
-        uint32_t skip = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < POS / 16; ++i) skip |= s_skip[buf][i];
-        float top2 = neg_inf();
+        float v[COLS];
+        tmem_ld32(s_tile + half * COLS, v);
         // (the same for the warp)
-        const bool part = __any_sync(0xffffffffu, skip != 0 || static_cast<int32_t>(start + j * POS + POS - 1) > last);
+        const uint32_t first = start + j * POS + half * COLS;  // this half's first position
+        const bool part = __any_sync(0xffffffffu, (s_skip[buf][half * 2] | s_skip[buf][half * 2 + 1]) != 0 ||
+                                                      static_cast<int32_t>(first + COLS - 1) > last);
+        float kf[2] = {s_ks[buf][half * 2] * factor, s_ks[buf][half * 2 + 1] * factor};
+        tmem_wait_ld();
+        float top = neg_inf();
         if (part) {
 #pragma unroll
-          for (uint32_t i = 0; i < POS / 16; ++i) {
-            const float kf = s_ks[buf][i] * factor;
-            const bool out = s_skip[buf][i] != 0;
+          for (uint32_t i = 0; i < 2; ++i) {
+            const bool out = s_skip[buf][half * 2 + i] != 0;
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
-              const bool in = static_cast<int32_t>(start + j * POS + i * 16 + e) <= last && !out;
-              v[i * 16 + e] = in ? v[i * 16 + e] * kf : neg_inf();
-              top2 = fmaxf(top2, v[i * 16 + e]);
+              const bool in = static_cast<int32_t>(first + i * 16 + e) <= last && !out;
+              v[i * 16 + e] = in ? v[i * 16 + e] * kf[i] : neg_inf();
+              top = fmaxf(top, v[i * 16 + e]);
             }
+            kf[i] = 1.0f;
           }
         } else {
 #pragma unroll
-          for (uint32_t i = 0; i < POS / 16; ++i) {
+          for (uint32_t i = 0; i < 2; ++i) {
             float t[4];
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e)
               t[e] = fmaxf(fmaxf(v[i * 16 + e], v[i * 16 + 4 + e]), fmaxf(v[i * 16 + 8 + e], v[i * 16 + 12 + e]));
-            top2 = fmaxf(top2, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * (s_ks[buf][i] * factor));
+            top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * kf[i]);
           }
         }
-        if (__any_sync(0xffffffffu, top2 > m + kRaise)) {
-          const float raised = fmaxf(m, top2), keep = m == neg_inf() ? 0.0f : ex2(m - raised);
+        // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
+        const bool raise = meet(top > m + kRaise);
+        if (other_left()) goto done;
+        if (raise) {
+          s_max[half][r * ROWS + row_in] = top;
+          meet(false);
+          if (other_left()) goto done;
+          const float raised = fmaxf(fmaxf(m, top), s_max[half ^ 1u][r * ROWS + row_in]);
+          const float keep = m == neg_inf() ? 0.0f : ex2(m - raised);
           m = raised;
           l *= keep;
           if (j > 0) {
             // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
             const uint32_t next = r * 2 + (j + 1) % 2;
             if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
-              give_up();
+              leave();
               goto done;
             }
             fence_after();
 #pragma unroll 1
-            for (uint32_t c = 0; c < DP; c += 32) {
-              float o[32];
-              tmem_ld32(o_col + c, o);
+            for (uint32_t c = 0; c < DP / 2; c += 16) {
+              float o[16];
+              tmem_ld16f(o_col + c, o);
               tmem_wait_ld();
 #pragma unroll
-              for (uint32_t e = 0; e < 32; ++e) o[e] *= keep;
-              tmem_st32f(o_col + c, o);
+              for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
+              tmem_st16f(o_col + c, o);
             }
             tmem_wait_st();
           }
         }
         const float off = kLift - (m == neg_inf() ? 0.0f : m);
-        float sum[4] = {};
+        float sum[2] = {};
+        uint32_t w[16], rest[16];
 #pragma unroll
-        for (uint32_t c = 0; c < POS; c += 32) {
-          uint32_t w[16], rest[16];
-#pragma unroll
-          for (uint32_t e = 0; e < 32; e += 2) {
-            const float kf = part ? 1.0f : s_ks[buf][(c + e) / 16] * factor;
-            float p0 = ex2(fmaf(v[c + e], kf, off)), p1 = ex2(fmaf(v[c + e + 1], kf, off));
-            sum[e / 2 % 4] += p0 + p1;
-            if constexpr (SPLIT) {
-              const float ratio = s_vr[buf][(c + e) / 16];
-              p0 *= ratio;
-              p1 *= ratio;
-            }
-            const __half2 h = __floats2half2_rn(p0, p1);
-            w[e / 2] = half2_bits(h);
-            if constexpr (SPLIT) rest[e / 2] = half2_bits(__floats2half2_rn(p0 - __low2float(h), p1 - __high2float(h)));
+        for (uint32_t e = 0; e < COLS; e += 2) {
+          float p0 = ex2(fmaf(v[e], kf[e / 16], off)), p1 = ex2(fmaf(v[e + 1], kf[e / 16], off));
+          sum[e / 2 % 2] += p0 + p1;
+          if constexpr (SPLIT) {
+            const float ratio = s_vr[buf][half * 2 + e / 16];
+            p0 *= ratio;
+            p1 *= ratio;
           }
-          tmem_st16(s_col + c / 2, w);
-          if constexpr (SPLIT) tmem_st16(s_col + POS / 2 + c / 2, rest);
+          const __half2 h = __floats2half2_rn(p0, p1);
+          w[e / 2] = half2_bits(h);
+          if constexpr (SPLIT) rest[e / 2] = half2_bits(__floats2half2_rn(p0 - __low2float(h), p1 - __high2float(h)));
         }
+        tmem_st16(s_tile + half * (COLS / 2), w);
+        if constexpr (SPLIT) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
         tmem_wait_st();
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PFULL + two));
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l += sum[0] + sum[1];
       }
       if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
-        give_up();
+        leave();
         goto done;
       }
       fence_after();
+      s_max[half][r * ROWS + row_in] = l;
+      meet(false);
+      if (other_left()) goto done;
+      l += s_max[half ^ 1u][r * ROWS + row_in];
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
       // (O and l are both lifted; partial results are not)
       const float scale = alone ? s_sv / l : s_sv * 0.0078125f;
       const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
-      if (!alone && row < rows) f.stats[at] = make_float2(l * 0.0078125f, m);
+      if (!alone && row < rows && half == 0) f.stats[at] = make_float2(l * 0.0078125f, m);
 #pragma unroll 1
-      for (uint32_t c = 0; c < DP; c += 32) {
-        float o[32];
-        tmem_ld32(o_col + c, o);
+      for (uint32_t c = 0; c < DP / 2; c += 16) {
+        float o[16];
+        tmem_ld16f(o_col + c, o);
         tmem_wait_ld();
-        if (row >= rows) continue;
+        const uint32_t d0 = half * (DP / 2) + c;
+        if (row >= rows || d0 >= a.dim) continue;  // (dim is a multiple of 16)
 #pragma unroll
-        for (uint32_t e = 0; e < 32; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
+        for (uint32_t e = 0; e < 16; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
         if (!alone) {
 #pragma unroll
-          for (uint32_t e = 0; e < 32; e += 4)
-            if (c + e < a.dim) *reinterpret_cast<float4 *>(f.part + at * a.dim + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (uint32_t e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(f.part + at * a.dim + d0 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         } else if (wide) {
 #pragma unroll
-          for (uint32_t e = 0; e < 32; e += 16 / sizeof(T)) {
+          for (uint32_t e = 0; e < 16; e += 16 / sizeof(T)) {
             alignas(16) T x[16 / sizeof(T)];
 #pragma unroll
             for (uint32_t i = 0; i < 16 / sizeof(T); ++i) x[i] = from_float<T>(o[e + i]);
-            if (c + e < a.dim) *reinterpret_cast<uint4 *>(out + c + e) = *reinterpret_cast<const uint4 *>(x);
+            *reinterpret_cast<uint4 *>(out + d0 + e) = *reinterpret_cast<const uint4 *>(x);
           }
         } else {
 #pragma unroll
-          for (uint32_t e = 0; e < 32; ++e)
-            if (c + e < a.dim) out[c + e] = from_float<T>(o[e]);
+          for (uint32_t e = 0; e < 16; ++e) out[d0 + e] = from_float<T>(o[e]);
         }
       }
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
     // ---- keys (four warps) and values (four) to f16: a warp 16 positions of each tile, in one page ----
     const uint32_t w = warp % 4;
     const bool keys = warp < SOFT_WARPS + 4;
