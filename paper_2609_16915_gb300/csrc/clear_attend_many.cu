@@ -795,8 +795,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
           kpar ^= 1u;
         }
       }
-      // the last of what was committed
-      if (!ready(USED + (n - 1) % RING, ((n - 1) / RING) & 1u)) give_up();
+      // no commit arrives after the block's end: each barrier's last one (the softmax waits for SFULL)
+      bool ok = ready(FIRST, 0);
+      for (uint32_t j = n > RING ? n - RING : 0; j < n; ++j) ok = ready(USED + j % RING, (j / RING) & 1u) && ok;
+      for (uint32_t r = 0; r < row_tiles; ++r) ok = ready(LAST + r, 0) && (n == 1 || ready(BEFORE + r, 0)) && ok;
+      if (!ok) give_up();
     }
   }
 done:

@@ -395,6 +395,13 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
             par ^= 1u;
           }
         }
+      // no commit arrives after the CTA's end: the last one of every slot in use
+      const uint32_t total = first < tiles ? ((tiles - 1 - first) / stride + 1) * steps : 0;
+      for (uint32_t i = total > S::STAGES ? total - S::STAGES : 0; i < total; ++i)
+        if (!ready(empty(i % S::STAGES), (i / S::STAGES) & 1u)) {
+          give_up();
+          goto done;
+        }
     }
   }
 done:
