@@ -59,6 +59,34 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(x), "f"(y), "f"(z));
+  return m;
+}
+
+// two numbers of a register pair in one instruction
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+  return p;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t p) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 __device__ __forceinline__ uint32_t half2_bits(__half2 h) { return *reinterpret_cast<const uint32_t *>(&h); }
 __device__ __forceinline__ __half2 bits_half2(uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); }
 
@@ -437,11 +465,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
         } else {
 #pragma unroll
           for (uint32_t i = 0; i < 2; ++i) {
-            float t[4];
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-              t[e] = fmaxf(fmaxf(v[i * 16 + e], v[i * 16 + 4 + e]), fmaxf(v[i * 16 + 8 + e], v[i * 16 + 12 + e]));
-            top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * kf[i]);
+            const float *x = v + i * 16;
+            const float t = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[8]));
+            top = fmaxf(top, max3(t, max3(x[9], x[10], x[11]), max3(fmaxf(x[12], x[13]), x[14], x[15])) * kf[i]);
           }
         }
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
@@ -476,12 +502,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
           }
         }
         const float off = kLift - (m == neg_inf() ? 0.0f : m);
-        float sum[2] = {};
+        const uint64_t off2 = pair_of(off, off), kf2[2] = {pair_of(kf[0], kf[0]), pair_of(kf[1], kf[1])};
+        uint64_t sum[2] = {};
         uint32_t w[16], rest[16];
 #pragma unroll
         for (uint32_t e = 0; e < COLS; e += 2) {
-          float p0 = ex2(fmaf(v[e], kf[e / 16], off)), p1 = ex2(fmaf(v[e + 1], kf[e / 16], off));
-          sum[e / 2 % 2] += p0 + p1;
+          const float2 x = floats_of(fma2(pair_of(v[e], v[e + 1]), kf2[e / 16], off2));
+          float p0 = ex2(x.x), p1 = ex2(x.y);
+          sum[e / 2 % 2] = add2(sum[e / 2 % 2], pair_of(p0, p1));
           if constexpr (SPLIT) {
             const float ratio = s_vr[buf][half * 2 + e / 16];
             p0 *= ratio;
@@ -497,7 +525,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PFULL + two));
-        l += sum[0] + sum[1];
+        const float2 both = floats_of(add2(sum[0], sum[1]));
+        l += both.x + both.y;
       }
       if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
         leave();
