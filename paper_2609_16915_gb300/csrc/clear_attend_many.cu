@@ -31,14 +31,8 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 16, CONVERT_WARPS = 8, WARPS = 28;
+constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 16, CONVERT_WARPS = 8, WARPS = SOFT_WARPS + CONVERT_WARPS + 1;  // (72 registers a thread)
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
-// registers of a thread: as launched (65536 over the block's threads, rounded down to eights), and as shared out; more
-// than was launched would wait forever
-constexpr uint32_t LAUNCH_REGS = 65536 / (WARPS * 32) / 8 * 8, SOFT_REGS = 72, CONVERT_REGS = 80, MMA_REGS = 56;
-static_assert(SOFT_WARPS * SOFT_REGS + CONVERT_WARPS * CONVERT_REGS + (WARPS - SOFT_WARPS - CONVERT_WARPS) * MMA_REGS <=
-                  WARPS * LAUNCH_REGS,
-              "register shares");
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
@@ -249,8 +243,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   // this block's range of the positions that its rows see
   const uint32_t all = group_end(a, len, min(row0 + BLOCK_ROWS, rows) - 1), share = split_share(f, all);
   const uint32_t start = split * share, end = min(all, start + share);
-  if (split > 0 && start >= all) return;
   const bool alone = all <= share;
+  if (split > 0 && start >= all) return;
   const uint32_t n = (end - start + POS - 1) / POS;
   const uint32_t row_tiles = !SPLIT && rows - row0 > ROWS ? 2 : 1;
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
@@ -264,12 +258,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     }
     return;
   }
-  if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == (WARPS - 1) * 32) {  // (of the MMA warp)
     s_fail = 0u;
     for (uint32_t i = 0; i < SOFT_WARPS / 2; ++i) s_quit[i] = 0u;
     mbar_init(bar(QFULL), SOFT_WARPS);
@@ -290,21 +279,24 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = tmem_slot;
+  // What needs neither the barriers nor the tensor memory is begun before the block meets: loads of queries, copies of
+  // the first tiles.
+  uint32_t tmem = 0;
+  const auto start_block = [&]() {
+    fence_before();
+    asm volatile("bar.sync 0, %0;" ::"n"(WARPS * 32) : "memory");
+    fence_after();
+    tmem = tmem_slot;
+  };
   const auto give_up = [&]() {
     atomicExch(a.err_flag, 2u);
     atomicExch(&s_fail, 1u);
   };
 
   if (warp < SOFT_WARPS) {
-    static_assert(SOFT_REGS == LAUNCH_REGS, "no share to ask for");
     // row tile, half of the columns, row: two threads a row, in warps that share a quarter of tensor memory
     const uint32_t r = warp / 8, half = warp / 4 % 2, row_in = (warp % 4) * 32 + lane, row = row0 + r * ROWS + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
-    const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
     // The two warps of a row meet at barrier 3 + pair.  A warp whose wait gave up meets the other once more and says
     // at which meeting, so that neither waits for one that has left.
     const uint32_t pair = r * 4 + warp % 4;
@@ -330,6 +322,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     const uint32_t qr = lane % 8, qc = lane / 8;
     const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
     if constexpr (SPLIT) {
+      start_block();
 #pragma unroll 1
       for (uint32_t g = 0; g < 2 && r == 0; ++g) {
         const uint32_t in_tile = warp * 16 + g * 8 + qr, rw = row0 + in_tile;
@@ -397,6 +390,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
           }
         }
       }
+      start_block();
 #pragma unroll
       for (uint32_t g = 0; g < 2; ++g) {
         const uint32_t in_tile = (warp % 8) * 16 + g * 8 + qr;
@@ -431,6 +425,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
     const int32_t last = row < rows ? static_cast<int32_t>(len - a.tokens + row / a.group) : -1;
+    const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
     constexpr uint32_t COLS = POS / 2;
     float m = neg_inf(), l = 0.0f;
     if (r < row_tiles) {
@@ -544,34 +539,58 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
       const float scale = alone ? s_sv / l : s_sv * 0.0078125f;
       const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
       if (!alone && row < rows && half == 0) f.stats[at] = make_float2(l * 0.0078125f, m);
+      // The warp's rows go out through shared memory (the queries' place: their products are done), so that a store writes
+      // whole lines (16 bytes of 32 rows at a time: 5 % longer at 4 x 1024 queries, single precision 6 %).
+      const auto write_rows = [&](auto type, decltype(type) *to) {  // (to: this thread's row)
+        using E = decltype(type);
+        constexpr uint32_t PASS = DP / sizeof(E), PIECE = 16 / sizeof(E), PIECES = DP / 16;  // (an eighth of a tile)
+        const uint32_t key = PIECES == 8 ? lane % 8 : lane / 2 % 4;
+        unsigned char *stage = smem + r * M::Q_TILE + warp % 8 * (M::Q_TILE / 8);
 #pragma unroll 1
-      for (uint32_t c = 0; c < DP / 2; c += 16) {
-        float o[16];
-        tmem_ld16f(o_col + c, o);
-        tmem_wait_ld();
-        const uint32_t d0 = half * (DP / 2) + c;
-        if (row >= rows || d0 >= a.dim) continue;  // (dim is a multiple of 16)
+        for (uint32_t c = 0; c < DP / 2; c += PASS) {
 #pragma unroll
-        for (uint32_t e = 0; e < 16; ++e) o[e] = l == 0.0f ? 0.0f : o[e] * scale;
-        if (!alone) {
+          for (uint32_t h = 0; h < PASS; h += 16) {
+            float o[16];
+            tmem_ld16f(o_col + c + h, o);
+            tmem_wait_ld();
 #pragma unroll
-          for (uint32_t e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(f.part + at * a.dim + d0 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        } else if (wide) {
+            for (uint32_t e = 0; e < 16; e += PIECE) {
+              alignas(16) E x[PIECE];
 #pragma unroll
-          for (uint32_t e = 0; e < 16; e += 16 / sizeof(T)) {
-            alignas(16) T x[16 / sizeof(T)];
-#pragma unroll
-            for (uint32_t i = 0; i < 16 / sizeof(T); ++i) x[i] = from_float<T>(o[e + i]);
-            *reinterpret_cast<uint4 *>(out + d0 + e) = *reinterpret_cast<const uint4 *>(x);
+              for (uint32_t i = 0; i < PIECE; ++i) x[i] = from_float<E>(l == 0.0f ? 0.0f : o[e + i] * scale);
+              *reinterpret_cast<uint4 *>(stage + lane * (PIECES * 16) + (((h + e) / PIECE) ^ key) * 16) = *reinterpret_cast<const uint4 *>(x);
+            }
           }
-        } else {
+          __syncwarp();
 #pragma unroll
-          for (uint32_t e = 0; e < 16; ++e) out[d0 + e] = from_float<T>(o[e]);
+          for (uint32_t i = 0; i < PIECES; ++i) {
+            const uint32_t of = (i * 32 + lane) / PIECES, piece = lane % PIECES, at_key = PIECES == 8 ? of % 8 : of / 2 % 4;
+            const uint4 x = *reinterpret_cast<const uint4 *>(stage + of * (PIECES * 16) + (piece ^ at_key) * 16);
+            E *dst = reinterpret_cast<E *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(to), of));
+            const uint32_t d = half * (DP / 2) + c + piece * PIECE;
+            if (row - lane + of < rows && d < a.dim) *reinterpret_cast<uint4 *>(dst + d) = x;  // (dim is a multiple of 16)
+          }
+          __syncwarp();
+        }
+      };
+      if (!alone) {
+        write_rows(0.0f, f.part + at * a.dim);
+      } else if (wide) {
+        write_rows(T(), out);
+      } else {
+#pragma unroll 1
+        for (uint32_t c = 0; c < DP / 2; c += 16) {
+          float o[16];
+          tmem_ld16f(o_col + c, o);
+          tmem_wait_ld();
+          const uint32_t d0 = half * (DP / 2) + c;
+          if (row >= rows || d0 >= a.dim) continue;
+#pragma unroll
+          for (uint32_t e = 0; e < 16; ++e) out[d0 + e] = from_float<T>(l == 0.0f ? 0.0f : o[e] * scale);
         }
       }
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CONVERT_REGS));
     // ---- keys (four warps) and values (four) to f16: a warp 16 positions of each tile, in one page ----
     const uint32_t w = warp % 4;
     const bool keys = warp < SOFT_WARPS + 4;
@@ -627,6 +646,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
       if (i < n) copy(i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    start_block();
     float sv = 1e-30f;
     if (!keys || SPLIT) {
       // the largest value scale of the pages seen
@@ -753,83 +773,84 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(MMA_REGS));
-    if (warp == SOFT_WARPS + CONVERT_WARPS) {
-      // ---- products ----
-      const uint32_t elect = elected();
-      const auto ready = [&](uint32_t i, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar(i), parity)); };
-      const auto scores = [&](uint32_t r, uint32_t j, uint32_t kbuf) {
-        const uint32_t two = r * 2 + j % 2;
-        const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    start_block();
+    // ---- products ----
+    const uint32_t elect = elected();
+    const auto ready = [&](uint32_t i, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar(i), parity)); };
+    const auto scores = [&](uint32_t r, uint32_t j, uint32_t kbuf) {
+      const uint32_t two = r * 2 + j % 2;
+      const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
 #pragma unroll
-        for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
-          mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
-        if constexpr (SPLIT) {
-          const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
+      for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
+        mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
+      if constexpr (SPLIT) {
+        const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
 #pragma unroll
-          for (uint32_t k = 0; k < DP / 16; ++k) mma_ss(tmem + two * POS, rest + k * 16u, kd + k * 16u, idesc(POS), 1, elect);
-        }
-        if (elect) mbar_arrive(bar(SFULL + two));  // (also passes on the page scales that came with the keys)
-        commit(bar(SFULL + two), elect);
-      };
-      if (!ready(QFULL, 0)) {
+        for (uint32_t k = 0; k < DP / 16; ++k) mma_ss(tmem + two * POS, rest + k * 16u, kd + k * 16u, idesc(POS), 1, elect);
+      }
+      if (elect) mbar_arrive(bar(SFULL + two));  // (also passes on the page scales that came with the keys)
+      commit(bar(SFULL + two), elect);
+    };
+    if (!ready(QFULL, 0)) {
+      give_up();
+      goto done;
+    }
+    for (uint32_t j = 0; j < 2 && j < n; ++j) {
+      if (!ready(KFULL + j, 0)) {
         give_up();
         goto done;
       }
-      for (uint32_t j = 0; j < 2 && j < n; ++j) {
-        if (!ready(KFULL + j, 0)) {
+      fence_after();
+      for (uint32_t r = 0; r < row_tiles; ++r) scores(r, j, j);
+    }
+    commit(bar(FIRST), elect);
+    uint32_t vbuf = 0, kbuf = 2, vpar = 0, kpar = 0;
+    for (uint32_t j = 0; j < n; ++j) {
+      if (!ready(VFULL + vbuf, vpar) || (j + 2 < n && !ready(KFULL + kbuf, kpar))) {
+        give_up();
+        goto done;
+      }
+      const uint64_t vd = desc_of(base + M::V_AT + vbuf * M::V_TILE, V_GROUP);
+#pragma unroll
+      for (uint32_t r = 0; r < 2; ++r) {
+        if (r >= row_tiles) break;
+        const uint32_t two = r * 2 + j % 2;
+        if (!ready(PFULL + two, (j / 2) & 1u)) {
           give_up();
           goto done;
         }
         fence_after();
-        for (uint32_t r = 0; r < row_tiles; ++r) scores(r, j, j);
-      }
-      commit(bar(FIRST), elect);
-      uint32_t vbuf = 0, kbuf = 2, vpar = 0, kpar = 0;
-      for (uint32_t j = 0; j < n; ++j) {
-        if (!ready(VFULL + vbuf, vpar) || (j + 2 < n && !ready(KFULL + kbuf, kpar))) {
-          give_up();
-          goto done;
-        }
-        const uint64_t vd = desc_of(base + M::V_AT + vbuf * M::V_TILE, V_GROUP);
 #pragma unroll
-        for (uint32_t r = 0; r < 2; ++r) {
-          if (r >= row_tiles) break;
-          const uint32_t two = r * 2 + j % 2;
-          if (!ready(PFULL + two, (j / 2) & 1u)) {
-            give_up();
-            goto done;
-          }
-          fence_after();
+        for (uint32_t k = 0; k < POS / 16; ++k)
+          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0, elect);
+        if constexpr (SPLIT) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
-            mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0, elect);
-          if constexpr (SPLIT) {
-#pragma unroll
-            for (uint32_t k = 0; k < POS / 16; ++k)
-              mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), 1, elect);
-          }
-          if (j + 2 < n)
-            scores(r, j + 2, kbuf);
-          else
-            commit(bar((j + 1 == n ? LAST : BEFORE) + r), elect);
+            mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), 1, elect);
         }
-        commit(bar(USED + vbuf), elect);
-        if (++vbuf == RING) {
-          vbuf = 0;
-          vpar ^= 1u;
-        }
-        if (++kbuf == RING) {
-          kbuf = 0;
-          kpar ^= 1u;
-        }
+        if (j + 2 < n)
+          scores(r, j + 2, kbuf);
+        else
+          commit(bar((j + 1 == n ? LAST : BEFORE) + r), elect);
       }
-      // no commit arrives after the block's end: each barrier's last one (the softmax waits for SFULL)
-      bool ok = ready(FIRST, 0);
-      for (uint32_t j = n > RING ? n - RING : 0; j < n; ++j) ok = ready(USED + j % RING, (j / RING) & 1u) && ok;
-      for (uint32_t r = 0; r < row_tiles; ++r) ok = ready(LAST + r, 0) && (n == 1 || ready(BEFORE + r, 0)) && ok;
-      if (!ok) give_up();
+      commit(bar(USED + vbuf), elect);
+      if (++vbuf == RING) {
+        vbuf = 0;
+        vpar ^= 1u;
+      }
+      if (++kbuf == RING) {
+        kbuf = 0;
+        kpar ^= 1u;
+      }
     }
+    // no commit arrives after the block's end: each barrier's last one (the softmax waits for SFULL)
+    bool ok = ready(FIRST, 0);
+    for (uint32_t j = n > RING ? n - RING : 0; j < n; ++j) ok = ready(USED + j % RING, (j / RING) & 1u) && ok;
+    for (uint32_t r = 0; r < row_tiles; ++r) ok = ready(LAST + r, 0) && (n == 1 || ready(BEFORE + r, 0)) && ok;
+    if (!ok) give_up();
   }
 done:
   __syncwarp();
@@ -844,7 +865,7 @@ done:
     }
     __syncthreads();
   }
-  if (warp == 0 && s_fail != 2u)
+  if (warp == SOFT_WARPS + CONVERT_WARPS && s_fail != 2u)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
