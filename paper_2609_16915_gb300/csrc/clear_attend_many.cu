@@ -31,7 +31,15 @@ namespace rosetta {
 
 namespace {
 
-constexpr uint32_t ROWS = 128, POS = 64, SOFT_WARPS = 16, CONVERT_WARPS = 8, WARPS = SOFT_WARPS + CONVERT_WARPS + 1;  // (72 registers a thread)
+constexpr uint32_t ROWS = 128, POS = 64, TILE_WARPS = 8, CONVERT_WARPS = 8;  // (TILE_WARPS: softmax warps of a row tile)
+// Single precision: one row tile, its queries and its weights in two halves each; the values stay whole numbers and
+// the weights take their scales.
+template <typename T>
+constexpr bool kSplit = sizeof(T) == 4;
+template <typename T>
+constexpr uint32_t kSoftWarps = kSplit<T> ? TILE_WARPS : 2 * TILE_WARPS;
+template <typename T>
+constexpr uint32_t kWarps = kSoftWarps<T> + CONVERT_WARPS + 1;  // (25 leave 72 registers a thread)
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -190,12 +198,11 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
 }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const AttendArgs f) {
+__global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
-  // Single precision: one row tile, its queries and its weights in two halves each; the values stay whole numbers and
-  // the weights take their scales.
-  constexpr bool SPLIT = sizeof(T) == 4;
+  constexpr bool SPLIT = kSplit<T>;
+  constexpr uint32_t SOFT_WARPS = kSoftWarps<T>, WARPS = kWarps<T>;
   constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
   extern __shared__ __align__(1024) unsigned char smem[];
   // USED: the values of tile j and the keys of tile j + 2; SFULL, PFULL: of each row tile, its two score tiles;
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   };
   __shared__ __align__(8) uint64_t bars[BARS];
   __shared__ uint32_t tmem_slot, s_fail;
-  __shared__ uint32_t s_quit[SOFT_WARPS / 2];  // the meeting at which one of two softmax warps gave up
+  __shared__ uint32_t s_quit[TILE_WARPS];  // the meeting at which one of two softmax warps gave up
   // of the last eight tiles (the conversion is at most four ahead of a softmax), by groups of 16 positions: key
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
@@ -260,7 +267,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
   }
   if (threadIdx.x == (WARPS - 1) * 32) {  // (of the MMA warp)
     s_fail = 0u;
-    for (uint32_t i = 0; i < SOFT_WARPS / 2; ++i) s_quit[i] = 0u;
+    for (uint32_t i = 0; i < TILE_WARPS; ++i) s_quit[i] = 0u;
     mbar_init(bar(QFULL), SOFT_WARPS);
     for (uint32_t i = 0; i < RING; ++i) {
       mbar_init(bar(KFULL + i), 4);
@@ -269,7 +276,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     }
     for (uint32_t i = 0; i < 4; ++i) {
       mbar_init(bar(SFULL + i), 2);
-      mbar_init(bar(PFULL + i), SOFT_WARPS / 2);
+      mbar_init(bar(PFULL + i), TILE_WARPS);
     }
     mbar_init(bar(FIRST), 1);
     mbar_init(bar(FREE), 1);
@@ -324,7 +331,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attend_many_kernel(const Attend
     if constexpr (SPLIT) {
       start_block();
 #pragma unroll 1
-      for (uint32_t g = 0; g < 2 && r == 0; ++g) {
+      for (uint32_t g = 0; g < 2; ++g) {
         const uint32_t in_tile = warp * 16 + g * 8 + qr, rw = row0 + in_tile;
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
@@ -889,7 +896,7 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   auto kern = attend_many_kernel<T, DP>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
-  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, WARPS * 32, Many<DP>::SMEM, s>>>(f);
+  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
   return cudaGetLastError();
 }
 
