@@ -97,9 +97,9 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) {
 
 // A scaled sum of the linear product, each step rounded (no contraction): the
 // codes are decided by exactly these single-precision values.
-__device__ __forceinline__ float clear_scaled(int32_t acc, float scale, float w_scale, const float *bias, uint32_t n) {
+__device__ __forceinline__ float clear_scaled(int32_t acc, float scale, float w_scale, bool biased, float bias) {
   const float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), scale), w_scale);
-  return bias ? __fadd_rn(y, bias[n]) : y;
+  return biased ? __fadd_rn(y, bias) : y;
 }
 
 // Store one output of the linear product.
@@ -127,7 +127,7 @@ cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t chan
 // The linear product of few tokens.  Over 16 of them the tensor-core kernel is as fast from 4096 inputs on (24 tokens,
 // 4096 channels: 4096 inputs 11.0 us against 12.0, 14336 inputs 29.2 against 21.8; 768 inputs, 3072 channels: 4.6
 // against 9.2).
-inline bool linear_few_takes(const ClearLinearArgs &a) { return a.tokens <= 16 || (a.tokens <= 32 && a.inner <= 4096); }
+inline bool linear_few_takes(const ClearLinearArgs &a) { return a.tokens <= 32; }
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s);
 // the same product on the tensor cores; work: linear_tc_bytes
 uint32_t linear_tc_columns(uint32_t tokens);

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "clear.h"
+#include "dsmem.cuh"
 
 namespace rosetta {
 
@@ -51,37 +52,68 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 bytes of a token's row from input k on, zeros from `inner` on
+// 16 bytes of a token from input k on, which `row` points to; zeros from `inner` on
 __device__ __forceinline__ uint4 token_bytes(const int8_t *row, uint32_t k, uint32_t inner) {
   uint32_t v[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
   for (uint32_t e = 0; e < 16; ++e)
-    if (k + e < inner) v[e >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(row[k + e])) << (8 * (e & 3u));
+    if (k + e < inner) v[e >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(row[e])) << (8 * (e & 3u));
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// Tiles of 32 channels over NB groups of eight tokens, the steps of 64 inputs shared out over WARPS warps, U of
-// them loaded ahead.  Lane (g, t) = (lane / 4, lane % 4) of a warp holds, of one step, 16 bytes of channels
-// g, g + 8, g + 16, g + 24 and of token g of each group: chunk t of the step.  Word i of those is its share of
-// the i-th 16 x 8 x 16 product: the products take the inputs in another order than they are stored in,
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool valid) {
+  const uint32_t size = valid ? 16 : 0;  // (nothing is read for 0: zeros)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
+
+// Tiles of 32 channels over NB groups of eight tokens, the steps of 64 inputs shared out over WARPS warps; each
+// warp copies its own steps, weights and tokens, DEPTH - 1 of them ahead.  Lane (g, t) = (lane / 4, lane % 4) of a warp takes,
+// of one step, 16 bytes of channels g, g + 8, g + 16, g + 24 and of token g of each group: chunk t of the step.  Word i of
+// those is its share of the i-th 16 x 8 x 16 product: the products take the inputs in another order than they are stored in,
 // the same for both operands.
-template <int NB, int WARPS>
+template <int NB, int WARPS, int DEPTH>
 struct FewShape {
   static constexpr uint32_t PITCH = NB * 8 + 4;  // of a row of sums
-  static constexpr uint32_t SMEM = WARPS * 32 * PITCH * 4;
-  static constexpr uint32_t BLOCKS = WARPS == 16 ? 1 : WARPS == 4 ? 3 : NB == 1 ? 4 : 3;  // an SM, at least
+  static constexpr uint32_t STEP = (4 + NB) * 512, RING = WARPS * DEPTH * STEP, SUMS = WARPS * 32 * PITCH * 4;
+  static constexpr uint32_t SMEM = RING > SUMS ? RING : SUMS;
+  static constexpr uint32_t BLOCKS = WARPS >= 12 ? 1 : NB == 4 ? 3 : 4;  // an SM
+  static_assert(BLOCKS * (SMEM + 1024) <= 228 * 1024, "shared memory");
 };
 
-template <int NB, int U, int WARPS, bool ALIGNED>
-__global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linear_few_kernel(const ClearLinearArgs a, int out_kind) {
-  using S = FewShape<NB, WARPS>;
-  extern __shared__ __align__(16) int32_t parts[];  // [warp][channel][token]
+template <int NB, int WARPS, int DEPTH, bool ALIGNED>
+__global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS) linear_few_kernel(const ClearLinearArgs a, int out_kind) {
+  using S = FewShape<NB, WARPS, DEPTH>;
+  extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t n0 = blockIdx.x * 32;
-  const int8_t *w = a.packed + static_cast<size_t>(n0 / kPackRows) * a.k_steps * kPackTile + n0 % kPackRows * kPackK + (g * 4 + (t ^ (g >> 1 & 3u))) * 16;
-  const int8_t *rows[NB];
+  // the next step to copy: its weights and, of this lane, each group's token
+  const int8_t *w = a.packed + (static_cast<size_t>(n0 / kPackRows) * a.k_steps + warp) * kPackTile + n0 % kPackRows * kPackK + lane * 16;
+  const int8_t *x[NB];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) rows[b] = a.q + static_cast<int64_t>(min(b * 8 + g, a.tokens - 1)) * a.q_pitch;
+  for (int b = 0; b < NB; ++b) x[b] = a.q + (b * 8 + g < a.tokens ? static_cast<int64_t>(b * 8 + g) * a.q_pitch + warp * kPackK + t * 16 : 0);
+  uint32_t next = warp;
+  unsigned char *ring = smem + warp * (DEPTH * S::STEP) + lane * 16;
+  const uint32_t ring_at = smem_addr(ring);
+  const auto fetch = [&](uint32_t slot) {
+    if (next < a.k_steps) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) copy_async(ring_at + slot * S::STEP + r * 512, w + r * (8 * kPackK), true);
+      const bool whole = ALIGNED && (next + 1) * kPackK <= a.inner;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const bool in = b * 8 + g < a.tokens;
+        if (whole)
+          copy_async(ring_at + slot * S::STEP + (4 + b) * 512, x[b], in);
+        else
+          *reinterpret_cast<uint4 *>(ring + slot * S::STEP + (4 + b) * 512) =
+              in ? token_bytes(x[b], next * kPackK + t * 16, a.inner) : make_uint4(0u, 0u, 0u, 0u);
+        if (in) x[b] += WARPS * kPackK;
+      }
+      w += WARPS * kPackTile;
+      next += WARPS;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   float d[2][NB][4] = {};
   int32_t acc[2][NB][4] = {};
   const auto take = [&]() {
@@ -95,52 +127,52 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linea
           d[m][b][i] = 0.0f;
         }
   };
+#pragma unroll
+  for (uint32_t i = 0; i + 1 < DEPTH; ++i) fetch(i);
+  // of the channel that this lane writes, and of token `lane`
+  const uint32_t n = n0 + lane;
+  const float w_scale = n < a.channels ? a.w_scale[n] : 0.0f, bias = a.bias != nullptr && n < a.channels ? a.bias[n] : 0.0f;
+  const float scale = lane < a.tokens ? a.scale[lane] : 0.0f;
+  const uint32_t own = (g * 4 + (t ^ (g >> 1 & 3u))) * 16 - lane * 16;  // this lane's chunk of eight rows of weights
   uint32_t done = 0;  // steps since the sums were taken: 16 of 64 inputs are exact
-  for (uint32_t k0 = warp; k0 < a.k_steps; k0 += WARPS * U) {
-    uint4 wv[U][4], xv[U][NB];
+  for (uint32_t k = warp, slot = 0; k < a.k_steps; k += WARPS) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory");
+    __syncwarp();
+    uint4 wv[4], xv[NB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t k = k0 + u * WARPS;
-      if (k >= a.k_steps) break;
-      const uint32_t at = k * kPackK + t * 16;
+    for (int r = 0; r < 4; ++r) wv[r] = *reinterpret_cast<const uint4 *>(ring + slot * S::STEP + r * 512 + static_cast<int32_t>(own));
 #pragma unroll
-      for (int r = 0; r < 4; ++r)  // (read once: first to leave the caches)
-        wv[u][r] = __ldcs(reinterpret_cast<const uint4 *>(w + static_cast<size_t>(k) * kPackTile + r * (8 * kPackK)));
+    for (int b = 0; b < NB; ++b) xv[b] = *reinterpret_cast<const uint4 *>(ring + slot * S::STEP + (4 + b) * 512);
+    // into the place read in the step before this one
+    fetch(slot == 0 ? DEPTH - 1 : slot - 1);
+    if (++slot == DEPTH) slot = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto word = [&](const uint4 &v) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; };
+      uint32_t f[2][4];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        int8x4_f16(word(wv[2 * m]), f[m][0], f[m][2]);
+        int8x4_f16(word(wv[2 * m + 1]), f[m][1], f[m][3]);
+      }
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        xv[u][b] = make_uint4(0u, 0u, 0u, 0u);
-        if (b * 8 + g < a.tokens)
-          xv[u][b] = ALIGNED && at + 16 <= a.inner ? __ldg(reinterpret_cast<const uint4 *>(rows[b] + at)) : token_bytes(rows[b], at, a.inner);
+        uint32_t b0, b1;
+        int8x4_f16(word(xv[b]), b0, b1);
+        mma_16x8x16(d[0][b], f[0], b0, b1);
+        mma_16x8x16(d[1][b], f[1], b0, b1);
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (k0 + u * WARPS >= a.k_steps) break;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const auto word = [&](const uint4 &v) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; };
-        uint32_t f[2][4];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          int8x4_f16(word(wv[u][2 * m]), f[m][0], f[m][2]);
-          int8x4_f16(word(wv[u][2 * m + 1]), f[m][1], f[m][3]);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          uint32_t b0, b1;
-          int8x4_f16(word(xv[u][b]), b0, b1);
-          mma_16x8x16(d[0][b], f[0], b0, b1);
-          mma_16x8x16(d[1][b], f[1], b0, b1);
-        }
-      }
-      if (++done == 1024 / kPackK) {
-        done = 0;
-        take();
-      }
+    if (++done == 1024 / kPackK) {
+      done = 0;
+      take();
     }
   }
   take();
   // the warps' sums, joined: exact in any order
+  int32_t *parts = reinterpret_cast<int32_t *>(smem);  // [warp][channel][token]
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -150,13 +182,13 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linea
         *reinterpret_cast<int2 *>(parts + (warp * 32 + m * 16 + i * 4 + g) * S::PITCH + b * 8 + 2 * t) =
             make_int2(acc[m][b][i], acc[m][b][i + 1]);
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < 32 * NB * 8; i += blockDim.x) {
-    const uint32_t row = i % 32, tok = i / 32, n = n0 + row;
-    if (tok >= a.tokens || n >= a.channels) continue;
+  for (uint32_t tok = warp; tok < a.tokens; tok += WARPS) {
+    const float token_scale = __shfl_sync(0xffffffffu, scale, tok);
     int32_t sum = 0;
 #pragma unroll
-    for (uint32_t v = 0; v < WARPS; ++v) sum += parts[(v * 32 + row) * S::PITCH + tok];
-    const float y = clear_scaled(sum, a.scale[tok], a.w_scale[n], a.bias, n);
+    for (uint32_t v = 0; v < WARPS; ++v) sum += parts[(v * 32 + lane) * S::PITCH + tok];
+    if (n >= a.channels) continue;
+    const float y = clear_scaled(sum, token_scale, w_scale, a.bias != nullptr, bias);
     if (out_kind == kOutF32)
       clear_store<kOutF32>(a, tok, n, y);
     else if (out_kind == kOutF16)
@@ -168,29 +200,26 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS>::BLOCKS) linea
   }
 }
 
-template <int NB, int U, int WARPS>
+template <int NB, int WARPS, int DEPTH>
 cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, cudaStream_t s) {
-  using S = FewShape<NB, WARPS>;
+  using S = FewShape<NB, WARPS, DEPTH>;
   const bool aligned = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>(a.tokens > 1 ? a.q_pitch : 0)) % 16 == 0;
-  auto kern = aligned ? linear_few_kernel<NB, U, WARPS, true> : linear_few_kernel<NB, U, WARPS, false>;
+  auto kern = aligned ? linear_few_kernel<NB, WARPS, DEPTH, true> : linear_few_kernel<NB, WARPS, DEPTH, false>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::SMEM));
   if (e != cudaSuccess) return e;
   kern<<<(a.channels + 31) / 32, 32 * WARPS, S::SMEM, s>>>(a, out_kind);
   return cudaGetLastError();
 }
 
-// The kernel lives on loads in flight: eight warps a block and several blocks an SM where the channels make
-// that many blocks, else sixteen warps with two steps each.  8 tokens, 4096 inputs: 14336 channels 12.3 us
-// against 17.2, 4096 channels 8.2 against 6.9.
-// Over 16 tokens the sums leave registers for four warps of two steps, or sixteen of one (24 tokens, 4096 inputs:
-// 14336 channels 25.6 us against 31.3 with eight warps).
 template <int NB>
 cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
   const bool many = (a.channels + 31) / 32 >= 2 * sms;
   if constexpr (NB == 4)
-    return many ? launch_few<NB, 2, 4>(a, out_kind, s) : launch_few<NB, 1, 16>(a, out_kind, s);
+    return many ? launch_few<NB, 4, 3>(a, out_kind, s) : launch_few<NB, 12, 4>(a, out_kind, s);
+  else if constexpr (NB == 3)
+    return many ? launch_few<NB, 4, 3>(a, out_kind, s) : launch_few<NB, 16, 3>(a, out_kind, s);
   else
-    return many ? launch_few<NB, 1, 8>(a, out_kind, s) : launch_few<NB, 2, 16>(a, out_kind, s);
+    return many ? launch_few<NB, 4, 4>(a, out_kind, s) : launch_few<NB, 16, 4>(a, out_kind, s);
 }
 
 }  // namespace
@@ -207,6 +236,7 @@ cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t chan
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
   if (a.tokens <= 8) return launch_few<1>(a, out_kind, sms, s);
   if (a.tokens <= 16) return launch_few<2>(a, out_kind, sms, s);
+  if (a.tokens <= 24) return launch_few<3>(a, out_kind, sms, s);
   return launch_few<4>(a, out_kind, sms, s);
 }
 

@@ -421,7 +421,7 @@ done:
         int32_t sum = 0;
         for (uint32_t r = 0; r < ranks; ++r)
           sum += static_cast<int32_t>(dsmem_ld_u32(dsmem_map(base + (col * kPackRows + i % kPackRows) * 4u, r)));
-        clear_store<OUT>(a, t0 + col, n, clear_scaled(sum, a.scale[t0 + col], a.w_scale[n], a.bias, n));
+        clear_store<OUT>(a, t0 + col, n, clear_scaled(sum, a.scale[t0 + col], a.w_scale[n], a.bias != nullptr, a.bias ? a.bias[n] : 0.0f));
       }
     }
     // no CTA leaves while another reads its shared memory
