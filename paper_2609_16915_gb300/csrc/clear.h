@@ -124,9 +124,9 @@ __device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t
 cudaError_t launch_clear_norm(const ClearNormArgs &a, int type, cudaStream_t s);
 cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t channels, uint32_t inner, int8_t *packed,
                               cudaStream_t s);
-// The linear product of few tokens.  Over 16 of them the tensor-core kernel is as fast from 4096 inputs on (24 tokens,
-// 4096 channels: 4096 inputs 11.0 us against 12.0, 14336 inputs 29.2 against 21.8; 768 inputs, 3072 channels: 4.6
-// against 9.2).
+// The linear product of few tokens: up to 32 it beats the tensor-core kernel (32 tokens against that one's 33, in us: 4096 inputs,
+// 14336 channels 17.8 and 22.7; 14336 inputs, 4096 channels 19.2 and 22.9; 768 inputs, 3072 channels 4.3 and 9.5), from 33 on it
+// does not (48 tokens: 26, 34 and 9.2 against 22.7, 22.9 and 9.5).
 inline bool linear_few_takes(const ClearLinearArgs &a) { return a.tokens <= 32; }
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s);
 // the same product on the tensor cores; work: linear_tc_bytes
