@@ -130,8 +130,7 @@ cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t chan
 inline bool linear_few_takes(const ClearLinearArgs &a) { return a.tokens <= 32; }
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s);
 // the same product on the tensor cores; work: linear_tc_bytes
-uint32_t linear_tc_columns(uint32_t tokens);
-size_t linear_tc_bytes(uint32_t tokens, uint32_t k_steps);
+size_t linear_tc_bytes(const ClearLinearArgs &a, uint32_t sms);
 cudaError_t launch_clear_linear_tc(const ClearLinearArgs &a, int out_kind, void *work, uint32_t sms, cudaStream_t s);
 cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t s);
 // attention for few rows a cached head: whole 16-position tiles in a page, heads a multiple of 16; work:

@@ -124,7 +124,7 @@ int run_linear(rosetta_clear *h, const ClearLinearArgs &a, int kind, cudaStream_
   if (linear_few_takes(a)) {
     e = launch_clear_linear_few(a, kind, h->sms, s);
   } else {
-    const int r = ensure_work(h, linear_tc_bytes(a.tokens, a.k_steps), s);
+    const int r = ensure_work(h, linear_tc_bytes(a, h->sms), s);
     if (r != ROSETTA_OK) return r;
     e = launch_clear_linear_tc(a, kind, h->work, h->sms, s);
   }

@@ -36,8 +36,8 @@ constexpr uint32_t CHUNK_STEPS = 1024 / kPackK;
 template <uint32_t NT>
 struct Shape {
   // as many as fit: the way of a step through copy, conversion and product takes 2 - 3 us
-  static constexpr uint32_t W_STAGES = NT <= 32 ? 16 : NT == 64 ? 14 : 8;  // weight tiles
-  static constexpr uint32_t STAGES = NT <= 32 ? 14 : NT == 64 ? 12 : NT == 128 ? 9 : 5;  // token tiles and A operands
+  static constexpr uint32_t W_STAGES = NT == 64 ? 14 : 8;                 // weight tiles
+  static constexpr uint32_t STAGES = NT == 64 ? 12 : NT == 128 ? 9 : 5;  // token tiles and A operands
   static constexpr uint32_t B_TILE = NT * kPackK * 2;
   static constexpr uint32_t DRAIN_WARPS = NT == 256 ? 8 : 4;
   static constexpr uint32_t COLS = NT / (DRAIN_WARPS / 4);                 // of one drain thread
@@ -442,8 +442,44 @@ done:
 
 namespace {
 
+// Columns of a tile, and CTAs that share out its inputs.
+struct Plan {
+  uint32_t columns, ranks;
+};
+
+// A cluster is doubled while the GPU holds all of them at once (of 152 SMs 76 clusters of two, 36 of four, 15 of eight: a
+// second round costs more than it saves, 2048 inputs and channels, 64 tokens 15.9 us with eight and 10.3 with four) and
+// four steps are left to each CTA.
+uint32_t ranks_of(uint64_t tiles, uint32_t k_steps, uint32_t sms) {
+  uint32_t ranks = 1;
+  while (ranks < 8 && tiles <= (ranks == 1 ? sms / 2 : ranks == 2 ? sms * 9 / 38 : sms / 10) && k_steps >= ranks * 2 * 4) ranks *= 2;
+  return ranks;
+}
+
+// The columns by an estimate of the time: a start and an end, longer for more columns and for the join of a cluster's sums, and
+// so much a step, as measured.  Wide tiles save conversions of weights, narrow ones make more CTAs: 256 tokens, 4096 inputs,
+// 14336 channels 33.2 us with 256 columns, 49 with 128, 54 with 64; 768 inputs, 3072 channels 17.2, 12.1, 9.8.
+Plan plan_of(const ClearLinearArgs &a, uint32_t sms) {
+  const uint32_t row_tiles = (a.channels + kPackRows - 1) / kPackRows;
+  Plan best = {64, 1};
+  uint64_t least = ~0ull;
+  for (uint32_t nt = 256; nt >= 64; nt /= 2) {
+    if (nt > 64 && a.tokens <= nt / 2) continue;
+    const uint64_t tiles = static_cast<uint64_t>(row_tiles) * ((a.tokens + nt - 1) / nt);
+    const uint32_t ranks = ranks_of(tiles, a.k_steps, sms);
+    const uint64_t steps = ranks > 1 ? (a.k_steps + ranks - 1) / ranks : (tiles + sms - 1) / sms * a.k_steps;
+    const uint64_t ns = (nt == 256 ? (ranks > 1 ? 14500 : 11000) : nt == 128 ? 10000 : ranks > 1 ? 9300 : 8500) +
+                        steps * (nt == 256 ? 275 : nt == 128 ? 285 : 210);
+    if (ns < least) {
+      least = ns;
+      best = {nt, ranks};
+    }
+  }
+  return best;
+}
+
 template <uint32_t NT, int OUT>
-cudaError_t launch_tc(const ClearLinearArgs &a, void *work, uint32_t sms, cudaStream_t s) {
+cudaError_t launch_tc(const ClearLinearArgs &a, uint32_t ranks, void *work, uint32_t sms, cudaStream_t s) {
   using S = Shape<NT>;
   const uint32_t row_tiles = (a.channels + kPackRows - 1) / kPackRows, tok_tiles = (a.tokens + NT - 1) / NT;
   const uint64_t items = static_cast<uint64_t>(tok_tiles) * a.k_steps * NT * 8;
@@ -455,8 +491,6 @@ cudaError_t launch_tc(const ClearLinearArgs &a, void *work, uint32_t sms, cudaSt
   e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::SMEM));
   if (e != cudaSuccess) return e;
   const uint64_t tiles = static_cast<uint64_t>(row_tiles) * tok_tiles;
-  uint32_t ranks = 1;
-  while (ranks < 8 && tiles * ranks * 2 <= sms && a.k_steps >= ranks * 2 * 4) ranks *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ranks > 1 ? static_cast<uint32_t>(tiles) * ranks : static_cast<uint32_t>(tiles < sms ? tiles : sms));
   cfg.blockDim = dim3(S::WARPS * 32);
@@ -475,27 +509,17 @@ cudaError_t launch_tc(const ClearLinearArgs &a, void *work, uint32_t sms, cudaSt
 
 template <int OUT>
 cudaError_t launch_out(const ClearLinearArgs &a, void *work, uint32_t sms, cudaStream_t s) {
-  switch (linear_tc_columns(a.tokens)) {
-    case 16: return launch_tc<16, OUT>(a, work, sms, s);
-    case 32: return launch_tc<32, OUT>(a, work, sms, s);
-    case 64: return launch_tc<64, OUT>(a, work, sms, s);
-    case 128: return launch_tc<128, OUT>(a, work, sms, s);
-    default: return launch_tc<256, OUT>(a, work, sms, s);
-  }
+  const Plan p = plan_of(a, sms);
+  return p.columns == 64    ? launch_tc<64, OUT>(a, p.ranks, work, sms, s)
+         : p.columns == 128 ? launch_tc<128, OUT>(a, p.ranks, work, sms, s)
+                            : launch_tc<256, OUT>(a, p.ranks, work, sms, s);
 }
 
 }  // namespace
 
-// Columns of a tile: the least power of two that holds the tokens.
-uint32_t linear_tc_columns(uint32_t tokens) {
-  uint32_t nt = 16;
-  while (nt < 256 && nt < tokens) nt *= 2;
-  return nt;
-}
-
-size_t linear_tc_bytes(uint32_t tokens, uint32_t k_steps) {
-  const uint32_t nt = linear_tc_columns(tokens);
-  return static_cast<size_t>((tokens + nt - 1) / nt) * k_steps * nt * (kPackK * 2);
+size_t linear_tc_bytes(const ClearLinearArgs &a, uint32_t sms) {
+  const uint32_t nt = plan_of(a, sms).columns;
+  return static_cast<size_t>((a.tokens + nt - 1) / nt) * a.k_steps * nt * (kPackK * 2);
 }
 
 cudaError_t launch_clear_linear_tc(const ClearLinearArgs &a, int out_kind, void *work, uint32_t sms, cudaStream_t s) {
