@@ -15,6 +15,11 @@ struct AttendArgs {
   uint32_t least;           // positions of a range at least
 };
 
+// The tensor cores cut the terms of their sums off instead of rounding them: an output comes out up to 7e-9 of itself short for
+// every position that one accumulator has taken (values of one sign; 1e-9 otherwise).  So no accumulator takes more
+// positions than this (2^-12, half a unit of f16's rounding), and single precision adds its accumulators up much sooner.
+constexpr uint32_t kMostPositions = 1u << 15;
+
 // Positions of each range of a sequence of `end`: whole tiles of all warps.
 __device__ __forceinline__ uint32_t split_share(const AttendArgs &f, uint32_t end) {
   const uint32_t share = (end + f.splits - 1) / f.splits;

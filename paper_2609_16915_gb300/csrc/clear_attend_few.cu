@@ -9,7 +9,8 @@
 // score passes it by 8, so p <= 2^8), and sv the largest value scale of the block's pages,
 //   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
 // what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
-// Single-precision queries are split into two f16 each, and so are the weights: 22 bits.
+// Single-precision queries are split into two f16 each, and so are the weights: 22 bits.  The tensor cores cut sums off
+// instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
 //
 // A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
 // takes every fourth tile of 16 positions, copied ahead into a ring by cp.async (a lane copies what it will
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
       __syncwarp();
       const unsigned char *tile = own + slot * F::TILE;
       // ---- scores: positions g, g + 8 (rows of S^T), query rows 2 t, 2 t + 1 ----
-      float s[NB][4] = {};
+      float s[NB][4] = {}, fine[NB][4] = {};  // (fine: of the queries' second halves)
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) {
         const uint32_t chunk = (t + 4 * j) ^ (CH >= 8 ? (g & 1u) * 4 : 0u);
@@ -256,8 +257,14 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
           for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int h = 0; h < H; ++h) mma_16x8x16(s[n], k, qf[h][n][j * 4 + c]);
+            for (int h = 0; h < H; ++h) mma_16x8x16(h == 0 ? s[n] : fine[n], k, qf[h][n][j * 4 + c]);
         }
+      }
+      if constexpr (H == 2) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] += fine[n][e];
       }
       const float ks = s_ks[i], vs = s_vs[i] * vlift;
       bool raise = false;
@@ -350,12 +357,24 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
           const uint32_t v0[4] = {biased_f16(x0, 0x4140), biased_f16(x0, 0x4342), biased_f16(y0, 0x4140), biased_f16(y0, 0x4342)};
           const uint32_t v1[4] = {biased_f16(x1, 0x4140), biased_f16(x1, 0x4342), biased_f16(y1, 0x4140), biased_f16(y1, 0x4342)};
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
+          for (int n = 0; n < NB; ++n) {
+            if constexpr (H == 1) {
+              mma_16x8x16(o[n][(j * VW + c) * 2], v0, pf[0][n]);
+              mma_16x8x16(o[n][(j * VW + c) * 2 + 1], v1, pf[0][n]);
+            } else {
+              float tile0[4] = {}, tile1[4] = {};
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-              mma_16x8x16(o[n][(j * VW + c) * 2], v0, pf[h][n]);
-              mma_16x8x16(o[n][(j * VW + c) * 2 + 1], v1, pf[h][n]);
+              for (int h = H - 1; h >= 0; --h) {
+                mma_16x8x16(tile0, v0, pf[h][n]);
+                mma_16x8x16(tile1, v1, pf[h][n]);
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                o[n][(j * VW + c) * 2][e] += tile0[e];
+                o[n][(j * VW + c) * 2 + 1][e] += tile1[e];
+              }
             }
+          }
         }
       }
       issue(i + (F::DEPTH - 1) * kWarps, slot == 0 ? F::DEPTH - 1 : slot - 1);  // the slot read a round before
@@ -523,6 +542,8 @@ void split(AttendArgs *f, uint32_t sms) {
   f->splits = static_cast<uint32_t>(want < longest ? want : longest);
   if (f->splits < 1) f->splits = 1;
   if (f->splits > 1024) f->splits = 1024;
+  const uint64_t least = (most + kWarps * kMostPositions - 1) / (kWarps * kMostPositions);  // (a warp takes a quarter)
+  if (f->splits < least) f->splits = static_cast<uint32_t>(least);
 }
 
 uint32_t group_rows_of(const ClearAttentionArgs &a) { return a.tokens * a.group <= 8 ? 8 : 16; }

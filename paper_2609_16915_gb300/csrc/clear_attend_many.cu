@@ -41,6 +41,9 @@ constexpr uint32_t kSoftWarps = kSplit<T> ? TILE_WARPS : 2 * TILE_WARPS;
 template <typename T>
 constexpr uint32_t kWarps = kSoftWarps<T> + CONVERT_WARPS + 1;  // (25 leave 72 registers a thread)
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
+// Single precision adds its accumulators to a sum of their own every FOLD tiles: 256 positions lose up to 2e-6 (8 x 256 queries
+// at 4096 positions 305 us; 285 with 8 tiles, 265 without, where 4096 positions lose up to 3e-5).
+constexpr uint32_t FOLD = 4;
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
@@ -433,6 +436,22 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
     const int32_t last = row < rows ? static_cast<int32_t>(len - a.tokens + row / a.group) : -1;
     const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
+    // (SPLIT: behind O the products of the weights' second halves, in the other row tile's place of the scores the sum of the
+    // tiles up to the last fold)
+    const uint32_t sum_col = tmem + lanes + 2 * POS + half * (DP / 2);
+    const auto read_all = [&](uint32_t c, bool folded, float (&o)[16]) {
+      float fine[16], before[16];
+      tmem_ld16f(o_col + c, o);
+      if constexpr (SPLIT) {
+        tmem_ld16f(o_col + DP + c, fine);
+        if (folded) tmem_ld16f(sum_col + c, before);
+      }
+      tmem_wait_ld();
+      if constexpr (SPLIT) {
+#pragma unroll
+        for (uint32_t e = 0; e < 16; ++e) o[e] += folded ? fine[e] + before[e] : fine[e];
+      }
+    };
     constexpr uint32_t COLS = POS / 2;
     float m = neg_inf(), l = 0.0f;
     if (r < row_tiles) {
@@ -475,33 +494,16 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
         const bool raise = meet(top > m + kRaise);
         if (other_left()) goto done;
+        const bool fold = SPLIT && j > 0 && j % FOLD == 0;
+        float keep = 1.0f;
         if (raise) {
           s_max[half][r * ROWS + row_in] = top;
           meet(false);
           if (other_left()) goto done;
           const float raised = fmaxf(fmaxf(m, top), s_max[half ^ 1u][r * ROWS + row_in]);
-          const float keep = m == neg_inf() ? 0.0f : ex2(m - raised);
+          keep = m == neg_inf() ? 0.0f : ex2(m - raised);
           m = raised;
           l *= keep;
-          if (j > 0) {
-            // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
-            const uint32_t next = r * 2 + (j + 1) % 2;
-            if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
-              leave();
-              goto done;
-            }
-            fence_after();
-#pragma unroll 1
-            for (uint32_t c = 0; c < DP / 2; c += 16) {
-              float o[16];
-              tmem_ld16f(o_col + c, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
-              tmem_st16f(o_col + c, o);
-            }
-            tmem_wait_st();
-          }
         }
         const float off = kLift - (m == neg_inf() ? 0.0f : m);
         const uint64_t off2 = pair_of(off, off), kf2[2] = {pair_of(kf[0], kf[0]), pair_of(kf[1], kf[1])};
@@ -523,12 +525,48 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
         tmem_st16(s_tile + half * (COLS / 2), w);
         if constexpr (SPLIT) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
+        const float2 both = floats_of(add2(sum[0], sum[1]));
+        l += both.x + both.y;
+        if (j > 0 && (raise || fold)) {
+          // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
+          const uint32_t next = r * 2 + (j + 1) % 2;
+          if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
+            leave();
+            goto done;
+          }
+          fence_after();
+#pragma unroll 1
+          for (uint32_t c = 0; c < DP / 2; c += 16) {
+            float o[16];
+            if (fold) {
+              read_all(c, j > FOLD, o);
+            } else {
+              tmem_ld16f(o_col + c, o);
+              tmem_wait_ld();
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
+            tmem_st16f((fold ? sum_col : o_col) + c, o);
+            if (SPLIT && !fold) {
+              tmem_ld16f(o_col + DP + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
+              tmem_st16f(o_col + DP + c, o);
+              if (j > FOLD) {
+                tmem_ld16f(sum_col + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
+                tmem_st16f(sum_col + c, o);
+              }
+            }
+          }
+        }
         tmem_wait_st();
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PFULL + two));
-        const float2 both = floats_of(add2(sum[0], sum[1]));
-        l += both.x + both.y;
       }
       if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
         leave();
@@ -558,8 +596,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
           for (uint32_t h = 0; h < PASS; h += 16) {
             float o[16];
-            tmem_ld16f(o_col + c + h, o);
-            tmem_wait_ld();
+            read_all(c + h, n > FOLD, o);
 #pragma unroll
             for (uint32_t e = 0; e < 16; e += PIECE) {
               alignas(16) E x[PIECE];
@@ -588,8 +625,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll 1
         for (uint32_t c = 0; c < DP / 2; c += 16) {
           float o[16];
-          tmem_ld16f(o_col + c, o);
-          tmem_wait_ld();
+          read_all(c, n > FOLD, o);
           const uint32_t d0 = half * (DP / 2) + c;
           if (row >= rows || d0 >= a.dim) continue;
 #pragma unroll
@@ -790,14 +826,14 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const auto scores = [&](uint32_t r, uint32_t j, uint32_t kbuf) {
       const uint32_t two = r * 2 + j % 2;
       const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
-#pragma unroll
-      for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
-        mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
-      if constexpr (SPLIT) {
+      if constexpr (SPLIT) {  // (the small products first: less is cut off)
         const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
 #pragma unroll
-        for (uint32_t k = 0; k < DP / 16; ++k) mma_ss(tmem + two * POS, rest + k * 16u, kd + k * 16u, idesc(POS), 1, elect);
+        for (uint32_t k = 0; k < DP / 16; ++k) mma_ss(tmem + two * POS, rest + k * 16u, kd + k * 16u, idesc(POS), k != 0, elect);
       }
+#pragma unroll
+      for (uint32_t k = 0; k < DP / 16; ++k)  // 256 bytes on: 16 in the descriptor's units
+        mma_ss(tmem + two * POS, qd + k * 16u, kd + k * 16u, idesc(POS), SPLIT || k != 0, elect);
       if (elect) mbar_arrive(bar(SFULL + two));  // (also passes on the page scales that came with the keys)
       commit(bar(SFULL + two), elect);
     };
@@ -832,11 +868,11 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_after();
 #pragma unroll
         for (uint32_t k = 0; k < POS / 16; ++k)
-          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), (j | k) != 0, elect);
+          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : j) | k) != 0, elect);
         if constexpr (SPLIT) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
-            mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), 1, elect);
+            mma_ts(tmem + M::O_COL + DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), (j % FOLD | k) != 0, elect);
         }
         if (j + 2 < n)
           scores(r, j + 2, kbuf);
@@ -878,14 +914,16 @@ done:
 
 uint32_t block_rows_of(int type) { return type == kOutF32 ? ROWS : 2 * ROWS; }
 
-// Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least.
+// Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least; and of contexts too long for one
+// accumulator.
 AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t sms) {
   AttendArgs f{a, nullptr, nullptr, 1, 1, 512};
   const uint32_t block = block_rows_of(type);
   f.groups = (a.tokens * a.group + block - 1) / block;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
-  const uint64_t want = sms / blocks, longest = (most + 511) / 512;
+  const uint64_t want = sms / blocks, longest = (most + 511) / 512, least = (most + kMostPositions - 1) / kMostPositions;
   f.splits = static_cast<uint32_t>(want < longest ? want : longest);
+  if (f.splits < least) f.splits = static_cast<uint32_t>(least);
   if (f.splits < 1) f.splits = 1;
   attend_place(&f, work);
   return f;

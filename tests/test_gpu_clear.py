@@ -465,6 +465,26 @@ def test_attention_and_append_beyond_32_bits(lib):
         assert torch.all((out.cpu().double() - ref).abs() <= U.UNIT[q.dtype] * ref.abs() + 2.0 ** -10 * size + 1e-9)
 
 
+@pytest.mark.parametrize("group", [4, 50])
+@pytest.mark.parametrize("dtype,context", [(torch.float32, 1 << 16), (torch.float32, 1 << 19), (torch.float16, 1 << 19)])
+def test_attention_of_long_contexts(lib, dtype, context, group):
+    """Page lists that repeat 2048 positions, values of one sign: what sums lose as they grow would show.  Single precision within
+    2^-18 of the sum (products in 22 bits, and 512 positions to an accumulator that is cut off at 24), f16 as over short contexts."""
+    batch, pages, page, dim = 160, 32, 64, 128
+    kc, vc = U.int8(5, pages, 1, page, dim), U.int8(6, pages, 1, page, dim, lo=1)
+    ks, vs = torch.rand(pages, 1, generator=torch.Generator().manual_seed(7)) / 60, torch.rand(pages, 1, generator=torch.Generator().manual_seed(8)) / 60
+    q = U.rand(9, 1, 1, group, dim).to(dtype)
+    each = context // page
+    table = (torch.arange(each) * 7 % pages).to(torch.int32)
+    out = torch.empty((batch, 1, group, dim), dtype=dtype, device="cuda")
+    lib.attention(q.cuda().expand(batch, -1, -1, -1).contiguous(), kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda(),
+                  table.cuda().expand(batch, -1).contiguous(), torch.full((batch,), context, dtype=torch.int32, device="cuda"), out)
+    lib.sync_status()
+    want, size = U.attention(q, kc, vc, ks, vs, torch.arange(pages, dtype=torch.int32)[None], [pages * page], dim ** -0.5)
+    bound = 2.0 ** -18 * size if dtype == torch.float32 else U.UNIT[dtype] * want.abs() + 2.0 ** -10 * size
+    assert torch.all((out.cpu().double() - want).abs() <= bound)
+
+
 def test_cache_of_other_orders(lib):
     """Caches stored [page][row][head][dim], and with gaps."""
     lens, page, heads, dim = [50, 33], 16, 3, 64
