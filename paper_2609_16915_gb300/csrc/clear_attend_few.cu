@@ -9,7 +9,8 @@
 // score passes it by 8, so p <= 2^8), and sv the largest value scale of the block's pages,
 //   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
 // what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
-// Single-precision queries are split into two f16 each, and so are the weights: 22 bits.  The tensor cores cut sums off
+// Single-precision queries are split into two f16 each, and the weights too but for bfloat16, whose own rounding hides that of
+// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 115 us against 111).  The tensor cores cut sums off
 // instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
 //
 // A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
@@ -17,6 +18,8 @@
 // read itself: no barriers).  Blocks of one sequence join through partial results (m, l, O) in the
 // workspace and attend_join_kernel; a sequence that fits one range is written at once.
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "clear_attend.cuh"
 #include "dsmem.cuh"
@@ -85,6 +88,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   using F = Few<DP>;
   constexpr bool SPLIT = sizeof(T) == 4;     // queries and weights in two halves
   constexpr int H = SPLIT ? 2 : 1;
+  constexpr int HP = std::is_same<T, __nv_bfloat16>::value ? 1 : 2;  // parts of a weight
   constexpr int KC = DP / 16;                // products of 16 dimensions
   constexpr int MT = DP / 16;                // tiles of 16 dimensions of O^T
   constexpr int VB = DP / 8;                 // bytes of a value row in a lane
@@ -309,7 +313,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
             }
           }
       }
-      uint32_t pf[H][NB][2];
+      uint32_t pf[HP][NB][2];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         float p[4];
@@ -321,7 +325,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
           p[e] = part && s[n][e] == neg_inf() ? 0.0f : p[e] * vs;  // (no product with the scale of a page that a row does not see)
         }
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+        for (int h = 0; h < HP; ++h)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
             const __half2 x = __floats2half2_rn(p[2 * r], p[2 * r + 1]);
@@ -359,12 +363,15 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
           for (int n = 0; n < NB; ++n) {
             if constexpr (H == 1) {
-              mma_16x8x16(o[n][(j * VW + c) * 2], v0, pf[0][n]);
-              mma_16x8x16(o[n][(j * VW + c) * 2 + 1], v1, pf[0][n]);
+#pragma unroll
+              for (int h = 0; h < HP; ++h) {
+                mma_16x8x16(o[n][(j * VW + c) * 2], v0, pf[h][n]);
+                mma_16x8x16(o[n][(j * VW + c) * 2 + 1], v1, pf[h][n]);
+              }
             } else {
               float tile0[4] = {}, tile1[4] = {};
 #pragma unroll
-              for (int h = H - 1; h >= 0; --h) {
+              for (int h = HP - 1; h >= 0; --h) {
                 mma_16x8x16(tile0, v0, pf[h][n]);
                 mma_16x8x16(tile1, v1, pf[h][n]);
               }

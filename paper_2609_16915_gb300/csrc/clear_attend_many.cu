@@ -1,15 +1,15 @@
 // Causal attention over the paged 8-bit cache for many query rows: prompts.
 //
-// Bound by the products (4 D operations per row and visible position) and, as closely, by one exponential
-// per row and position (the special-function unit computes 16 a clock and SM: as long as the tensor cores'
-// 2048 clocks per 256 rows x 128 positions at D = 128).  tcgen05, scores, weights and outputs in tensor memory.
+// Bound by the issue of the softmax's and the conversions' instructions (about 60 % of the issue slots; the tensor pipe is
+// active for 35 % of the time, DRAM for 5 %): 8 x 256 queries at 4096 positions, 32 heads over 8 of 128, 160 us, 830 TFLOP/s
+// of 4 D operations per row and visible position.  tcgen05, scores, weights and outputs in tensor memory.
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
 // over the positions 64 at a time:
 //   4 + 4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
 //                    in shared memory, both K-major: keys [position][dimension] (exact, and with the sign of their
-//                    scale), values transposed by byte permutes to [dimension][position] and times their scale over the
-//                    largest one
+//                    scale), values transposed by byte permutes to [dimension][position] and, but where the weights take
+//                    it, times their scale over the largest one
 //   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory
 //   2 x 8 softmax warps  two threads a row, 32 positions each: scores from tensor memory, times the page's key scale and the row's
 //                    factor, 2^(s - m + 7) with the running maximum m raised only where a score passes it by 8
@@ -23,6 +23,8 @@
 // products it issued before it frees the tensor memory.
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "clear_attend.cuh"
 #include "dsmem.cuh"
 #include "tcgen.cuh"
@@ -32,10 +34,14 @@ namespace rosetta {
 namespace {
 
 constexpr uint32_t ROWS = 128, POS = 64, TILE_WARPS = 8, CONVERT_WARPS = 8;  // (TILE_WARPS: softmax warps of a row tile)
-// Single precision: one row tile, its queries and its weights in two halves each; the values stay whole numbers and
-// the weights take their scales.
+// Single precision: one row tile, its queries in two halves.
 template <typename T>
 constexpr bool kSplit = sizeof(T) == 4;
+// Weights in two halves, and the values whole numbers, whose scales the weights take: all but bfloat16, whose own rounding hides
+// that of weights and values to 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 8 x 256 queries at
+// 4096 positions 185 us against 160).
+template <typename T>
+constexpr bool kFine = !std::is_same<T, __nv_bfloat16>::value;
 template <typename T>
 constexpr uint32_t kSoftWarps = kSplit<T> ? TILE_WARPS : 2 * TILE_WARPS;
 template <typename T>
@@ -204,7 +210,7 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
-  constexpr bool SPLIT = kSplit<T>;
+  constexpr bool SPLIT = kSplit<T>, FINE = kFine<T>;
   constexpr uint32_t SOFT_WARPS = kSoftWarps<T>, WARPS = kWarps<T>;
   constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -231,7 +237,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
   __shared__ uint32_t s_skip[8][POS / 16];
-  __shared__ float s_vr[8][POS / 16];  // (SPLIT: value scales over the largest)
+  __shared__ float s_vr[8][POS / 16];  // (FINE: value scales over the largest)
   __shared__ float s_top[8], s_sv;
   // what the two threads of a row exchange; before the first tile, the power of two of each row's queries
   __shared__ float s_max[2][2 * ROWS];
@@ -514,17 +520,17 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           const float2 x = floats_of(fma2(pair_of(v[e], v[e + 1]), kf2[e / 16], off2));
           float p0 = ex2(x.x), p1 = ex2(x.y);
           sum[e / 2 % 2] = add2(sum[e / 2 % 2], pair_of(p0, p1));
-          if constexpr (SPLIT) {
+          if constexpr (FINE) {
             const float ratio = s_vr[buf][half * 2 + e / 16];
             p0 *= ratio;
             p1 *= ratio;
           }
           const __half2 h = __floats2half2_rn(p0, p1);
           w[e / 2] = half2_bits(h);
-          if constexpr (SPLIT) rest[e / 2] = half2_bits(__floats2half2_rn(p0 - __low2float(h), p1 - __high2float(h)));
+          if constexpr (FINE) rest[e / 2] = half2_bits(__floats2half2_rn(p0 - __low2float(h), p1 - __high2float(h)));
         }
         tmem_st16(s_tile + half * (COLS / 2), w);
-        if constexpr (SPLIT) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
+        if constexpr (FINE) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
         const float2 both = floats_of(add2(sum[0], sum[1]));
         l += both.x + both.y;
         if (j > 0 && (raise || fold)) {
@@ -691,7 +697,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     }
     start_block();
     float sv = 1e-30f;
-    if (!keys || SPLIT) {
+    if (!keys || FINE) {
       // the largest value scale of the pages seen
       for (uint32_t p = start / a.page_tokens + threadIdx.x % 128; p < slots_end; p += 128) {
         const int32_t id = table[p];
@@ -733,7 +739,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             // (a value scale that is a NaN or an infinity: no number)
             s_ks[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
             s_skip[j % 8][w] = skip[st];
-            if constexpr (SPLIT) s_vr[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f;
+            if constexpr (FINE) s_vr[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f;
           }
           // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
           const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
@@ -797,7 +803,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
               for (uint32_t e = 0; e < 4; ++e) {
                 const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
-                o[e][p] = half2_bits(SPLIT ? v : __hmul2(v, ratio));
+                o[e][p] = half2_bits(FINE ? v : __hmul2(v, ratio));
               }
             }
 #pragma unroll
@@ -869,10 +875,11 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
         for (uint32_t k = 0; k < POS / 16; ++k)
           mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : j) | k) != 0, elect);
-        if constexpr (SPLIT) {
+        if constexpr (FINE) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
-            mma_ts(tmem + M::O_COL + DP, tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), (j % FOLD | k) != 0, elect);
+            mma_ts(tmem + M::O_COL + (SPLIT ? DP : r * DP), tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), !SPLIT || (j % FOLD | k) != 0,
+                     elect);
         }
         if (j + 2 < n)
           scores(r, j + 2, kbuf);
