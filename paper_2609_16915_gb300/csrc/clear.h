@@ -124,12 +124,13 @@ __device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t
 cudaError_t launch_clear_norm(const ClearNormArgs &a, int type, cudaStream_t s);
 cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t channels, uint32_t inner, int8_t *packed,
                               cudaStream_t s);
-// The linear product of few tokens: up to 32 it beats the tensor-core kernel (32 tokens against that one's 33, in us: 4096 inputs,
-// 14336 channels 17.8 and 22.7; 14336 inputs, 4096 channels 19.2 and 22.9; 768 inputs, 3072 channels 4.3 and 9.5), from 33 on it
-// does not (48 tokens: 26, 34 and 9.2 against 22.7, 22.9 and 9.5).
-inline bool linear_few_takes(const ClearLinearArgs &a) { return a.tokens <= 32; }
+// The linear product of few tokens, and the one on the tensor cores: estimates of their times, and the launches (work:
+// linear_tc_bytes).  The first takes what few blocks finish, at every width up to 32 tokens and small matrices up to some hundred:
+// 4096 inputs, 14336 channels, 32 tokens 17.8 us against 22.7, 40 tokens 26 against 22.7; 768 inputs, 3072 channels, 64 tokens
+// 4.3 against 9.7, 256 as fast.
+uint64_t linear_few_ns(const ClearLinearArgs &a, uint32_t sms);
+uint64_t linear_tc_ns(const ClearLinearArgs &a, uint32_t sms);
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s);
-// the same product on the tensor cores; work: linear_tc_bytes
 size_t linear_tc_bytes(const ClearLinearArgs &a, uint32_t sms);
 cudaError_t launch_clear_linear_tc(const ClearLinearArgs &a, int out_kind, void *work, uint32_t sms, cudaStream_t s);
 cudaError_t launch_clear_append(const ClearAppendArgs &a, int type, cudaStream_t s);

@@ -121,7 +121,7 @@ int ensure_work(rosetta_clear *h, size_t bytes, cudaStream_t s) {
 int run_linear(rosetta_clear *h, const ClearLinearArgs &a, int kind, cudaStream_t s) {
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
   cudaError_t e;
-  if (linear_few_takes(a)) {
+  if (linear_few_ns(a, h->sms) <= linear_tc_ns(a, h->sms)) {
     e = launch_clear_linear_few(a, kind, h->sms, s);
   } else {
     const int r = ensure_work(h, linear_tc_bytes(a, h->sms), s);

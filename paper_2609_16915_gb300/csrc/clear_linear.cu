@@ -6,8 +6,9 @@
 // warps that the sums leave registers for.  A block takes 32 channels; its warps share out the steps of 64 inputs and join their
 // integer sums in shared memory.  A warp copies its own weights and tokens ahead (cp.async, in the order of the lanes) and converts
 // them from 8 bits to f16; a 16 x 8 x 16 product of f16 is exact (products below 2^14), and so are the f32 sums of 16 steps,
-// which are then taken into integers.  4096 inputs, 14336 channels (8.7 us at the copy rate): 1 token 11.4 us,
-// 8 tokens 11.6, 16 12.6, 24 15.4, 32 17.8.
+// which are then taken into integers.  More tokens are further groups of blocks, which read the weights from the L2.  4096
+// inputs, 14336 channels (8.7 us at the copy rate): 1 token 11.3 us, 8 tokens 11.6, 16 12.7, 24 15.3, 32 17.5; 768 inputs, 3072
+// channels: 1 token 2.1, 24 to 40 tokens 3.2, 64 4.3, 128 6.7.
 #include <stdint.h>
 
 #include "clear.h"
@@ -87,12 +88,12 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS
   using S = FewShape<NB, WARPS, DEPTH>;
   extern __shared__ __align__(16) unsigned char smem[];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-  const uint32_t n0 = blockIdx.x * 32;
+  const uint32_t n0 = blockIdx.x * 32, t0 = blockIdx.y * (NB * 8), tokens = min(a.tokens - t0, NB * 8u);
   // the next step to copy: its weights and, of this lane, each group's token
   const int8_t *w = a.packed + (static_cast<size_t>(n0 / kPackRows) * a.k_steps + warp) * kPackTile + n0 % kPackRows * kPackK + lane * 16;
   const int8_t *x[NB];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) x[b] = a.q + (b * 8 + g < a.tokens ? static_cast<int64_t>(b * 8 + g) * a.q_pitch + warp * kPackK + t * 16 : 0);
+  for (int b = 0; b < NB; ++b) x[b] = a.q + (b * 8 + g < tokens ? static_cast<int64_t>(t0 + b * 8 + g) * a.q_pitch + warp * kPackK + t * 16 : 0);
   uint32_t next = warp;
   unsigned char *ring = smem + warp * (DEPTH * S::STEP) + lane * 16;
   const uint32_t ring_at = smem_addr(ring);
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS
       const bool whole = ALIGNED && (next + 1) * kPackK <= a.inner;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const bool in = b * 8 + g < a.tokens;
+        const bool in = b * 8 + g < tokens;
         if (whole)
           copy_async(ring_at + slot * S::STEP + (4 + b) * 512, x[b], in);
         else
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS
   // of the channel that this lane writes, and of token `lane`
   const uint32_t n = n0 + lane;
   const float w_scale = n < a.channels ? a.w_scale[n] : 0.0f, bias = a.bias != nullptr && n < a.channels ? a.bias[n] : 0.0f;
-  const float scale = lane < a.tokens ? a.scale[lane] : 0.0f;
+  const float scale = lane < tokens ? a.scale[t0 + lane] : 0.0f;
   const uint32_t own = (g * 4 + (t ^ (g >> 1 & 3u))) * 16 - lane * 16;  // this lane's chunk of eight rows of weights
   uint32_t done = 0;  // steps since the sums were taken: 16 of 64 inputs are exact
   for (uint32_t k = warp, slot = 0; k < a.k_steps; k += WARPS) {
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS
         *reinterpret_cast<int2 *>(parts + (warp * 32 + m * 16 + i * 4 + g) * S::PITCH + b * 8 + 2 * t) =
             make_int2(acc[m][b][i], acc[m][b][i + 1]);
   __syncthreads();
-  for (uint32_t tok = warp; tok < a.tokens; tok += WARPS) {
+  for (uint32_t tok = warp; tok < tokens; tok += WARPS) {
     const float token_scale = __shfl_sync(0xffffffffu, scale, tok);
     int32_t sum = 0;
 #pragma unroll
@@ -192,40 +193,61 @@ __global__ void __launch_bounds__(32 * WARPS, FewShape<NB, WARPS, DEPTH>::BLOCKS
     if (n >= a.channels) continue;
     const float y = clear_scaled(sum, token_scale, w_scale, a.bias != nullptr, bias);
     if (out_kind == kOutF32)
-      clear_store<kOutF32>(a, tok, n, y);
+      clear_store<kOutF32>(a, t0 + tok, n, y);
     else if (out_kind == kOutF16)
-      clear_store<kOutF16>(a, tok, n, y);
+      clear_store<kOutF16>(a, t0 + tok, n, y);
     else if (out_kind == kOutBf16)
-      clear_store<kOutBf16>(a, tok, n, y);
+      clear_store<kOutBf16>(a, t0 + tok, n, y);
     else
-      clear_store<kOutCodes>(a, tok, n, y);
+      clear_store<kOutCodes>(a, t0 + tok, n, y);
   }
+}
+
+bool aligned_of(const ClearLinearArgs &a) {
+  return (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>(a.tokens > 1 ? a.q_pitch : 0)) % 16 == 0;
 }
 
 template <int NB, int WARPS, int DEPTH>
 cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, cudaStream_t s) {
   using S = FewShape<NB, WARPS, DEPTH>;
-  const bool aligned = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>(a.tokens > 1 ? a.q_pitch : 0)) % 16 == 0;
-  auto kern = aligned ? linear_few_kernel<NB, WARPS, DEPTH, true> : linear_few_kernel<NB, WARPS, DEPTH, false>;
+  auto kern = aligned_of(a) ? linear_few_kernel<NB, WARPS, DEPTH, true> : linear_few_kernel<NB, WARPS, DEPTH, false>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::SMEM));
   if (e != cudaSuccess) return e;
-  kern<<<(a.channels + 31) / 32, 32 * WARPS, S::SMEM, s>>>(a, out_kind);
+  kern<<<dim3((a.channels + 31) / 32, (a.tokens + NB * 8 - 1) / (NB * 8)), 32 * WARPS, S::SMEM, s>>>(a, out_kind);
   return cudaGetLastError();
 }
 
-// Four warps a block and up to four blocks an SM where the channels make that many blocks, else sixteen warps: 4096 inputs,
-// 8 tokens, 14336 channels 11.7 us against 12.2 with six warps, 24 tokens 15.4 against 16.2 with eight.  Over 24 tokens the
-// sums leave registers for twelve warps an SM (32 tokens, 14336 channels 17.8 us against 19.4 with sixteen, which spill;
-// 4096 channels 8.6 against 9.9).
+uint64_t blocks_of(const ClearLinearArgs &a, uint32_t nb) {
+  return static_cast<uint64_t>((a.channels + 31) / 32) * ((a.tokens + nb * 8 - 1) / (nb * 8));
+}
+
+// An estimate of the time with groups of 8 nb tokens, from measurements.  Up to a block an SM: a start, and the steps of 16 warps
+// (12 over 24 tokens: the sums leave no registers for more).  Else four warps a block and up to four blocks an SM, each
+// with its steps.  Tokens that no 16-byte copy can take are read byte by byte.
+uint64_t ns_of(const ClearLinearArgs &a, uint32_t nb, bool aligned, uint32_t sms) {
+  static constexpr uint32_t kStart[4] = {1400, 2200, 3150, 3400}, kStep[4] = {710, 830, 1000, 850}, kBlock[4] = {300, 300, 600, 800},
+                            kBlockStep[4] = {110, 155, 220, 290};
+  const uint64_t blocks = blocks_of(a, nb), bytes = aligned ? 1 : 3;
+  if (blocks <= sms) {
+    const uint32_t warps = nb == 4 ? 12 : 16;
+    return kStart[nb - 1] + (a.k_steps + warps - 1) / warps * kStep[nb - 1] * bytes;
+  }
+  const uint64_t steps = (a.k_steps + 3) / 4;
+  return 1600 + 150 * steps + (kBlock[nb - 1] + kBlockStep[nb - 1] * steps) * bytes * blocks / sms;
+}
+
+uint32_t group_of(const ClearLinearArgs &a, uint32_t sms) {
+  const bool aligned = aligned_of(a);
+  uint32_t best = 1;
+  for (uint32_t nb = 2; nb <= 4 && nb * 8 < a.tokens + 8; ++nb)
+    if (ns_of(a, nb, aligned, sms) < ns_of(a, best, aligned, sms)) best = nb;
+  return best;
+}
+
 template <int NB>
 cudaError_t launch_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
-  const bool many = (a.channels + 31) / 32 >= 2 * sms;
-  if constexpr (NB == 4)
-    return many ? launch_few<NB, 4, 3>(a, out_kind, s) : launch_few<NB, 12, 3>(a, out_kind, s);
-  else if constexpr (NB == 3)
-    return many ? launch_few<NB, 4, 3>(a, out_kind, s) : launch_few<NB, 16, 3>(a, out_kind, s);
-  else
-    return many ? launch_few<NB, 4, 4>(a, out_kind, s) : launch_few<NB, 16, 4>(a, out_kind, s);
+  constexpr int DEPTH = NB > 2 ? 3 : 4;
+  return blocks_of(a, NB) > sms ? launch_few<NB, 4, DEPTH>(a, out_kind, s) : launch_few<NB, NB == 4 ? 12 : 16, DEPTH>(a, out_kind, s);
 }
 
 }  // namespace
@@ -239,11 +261,18 @@ cudaError_t launch_clear_pack(const int8_t *weight, int64_t pitch, uint32_t chan
   return cudaGetLastError();
 }
 
+uint64_t linear_few_ns(const ClearLinearArgs &a, uint32_t sms) {
+  if (a.tokens > 65535 * 8u) return ~0ull;  // (groups of a grid)
+  return ns_of(a, group_of(a, sms), aligned_of(a), sms);
+}
+
 cudaError_t launch_clear_linear_few(const ClearLinearArgs &a, int out_kind, uint32_t sms, cudaStream_t s) {
-  if (a.tokens <= 8) return launch_few<1>(a, out_kind, sms, s);
-  if (a.tokens <= 16) return launch_few<2>(a, out_kind, sms, s);
-  if (a.tokens <= 24) return launch_few<3>(a, out_kind, sms, s);
-  return launch_few<4>(a, out_kind, sms, s);
+  switch (group_of(a, sms)) {
+    case 1: return launch_few<1>(a, out_kind, sms, s);
+    case 2: return launch_few<2>(a, out_kind, sms, s);
+    case 3: return launch_few<3>(a, out_kind, sms, s);
+    default: return launch_few<4>(a, out_kind, sms, s);
+  }
 }
 
 }  // namespace rosetta

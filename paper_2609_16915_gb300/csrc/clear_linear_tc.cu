@@ -445,6 +445,7 @@ namespace {
 // Columns of a tile, and CTAs that share out its inputs.
 struct Plan {
   uint32_t columns, ranks;
+  uint64_t ns;
 };
 
 // A cluster is doubled while the GPU holds all of them at once (of 152 SMs 76 clusters of two, 36 of four, 15 of eight: a
@@ -461,8 +462,7 @@ uint32_t ranks_of(uint64_t tiles, uint32_t k_steps, uint32_t sms) {
 // 14336 channels 33.2 us with 256 columns, 49 with 128, 54 with 64; 768 inputs, 3072 channels 17.2, 12.1, 9.8.
 Plan plan_of(const ClearLinearArgs &a, uint32_t sms) {
   const uint32_t row_tiles = (a.channels + kPackRows - 1) / kPackRows;
-  Plan best = {64, 1};
-  uint64_t least = ~0ull;
+  Plan best = {64, 1, ~0ull};
   for (uint32_t nt = 256; nt >= 64; nt /= 2) {
     if (nt > 64 && a.tokens <= nt / 2) continue;
     const uint64_t tiles = static_cast<uint64_t>(row_tiles) * ((a.tokens + nt - 1) / nt);
@@ -470,10 +470,7 @@ Plan plan_of(const ClearLinearArgs &a, uint32_t sms) {
     const uint64_t steps = ranks > 1 ? (a.k_steps + ranks - 1) / ranks : (tiles + sms - 1) / sms * a.k_steps;
     const uint64_t ns = (nt == 256 ? (ranks > 1 ? 14500 : 11000) : nt == 128 ? 10000 : ranks > 1 ? 9300 : 8500) +
                         steps * (nt == 256 ? 275 : nt == 128 ? 285 : 210);
-    if (ns < least) {
-      least = ns;
-      best = {nt, ranks};
-    }
+    if (ns < best.ns) best = {nt, ranks, ns};
   }
   return best;
 }
@@ -516,6 +513,8 @@ cudaError_t launch_out(const ClearLinearArgs &a, void *work, uint32_t sms, cudaS
 }
 
 }  // namespace
+
+uint64_t linear_tc_ns(const ClearLinearArgs &a, uint32_t sms) { return plan_of(a, sms).ns; }
 
 size_t linear_tc_bytes(const ClearLinearArgs &a, uint32_t sms) {
   const uint32_t nt = plan_of(a, sms).columns;

@@ -178,6 +178,26 @@ def test_linear_codes(lib, tokens, inner, channels, bits):
     assert torch.equal(values.cpu(), table[torch.from_numpy(want).long()])
 
 
+TILED = [  # tiles of 64, 128 and 256 tokens, each alone, in several rounds, and in clusters of 2, 4 and 8
+    (65, 129, 6000), (200, 64, 6000), (33, 2100, 6000), (100, 2100, 1300), (33, 40000, 4), (257, 1024, 4100), (65, 2100, 6000),
+    (65, 2100, 2500), (100, 8192, 1300), (700, 512, 4100), (257, 2048, 4100), (200, 4096, 2500), (200, 8192, 1300), (333, 1021, 2999),
+    # groups of 8, 16, 24 and 32 tokens of the kernel for few, one of them and several
+    (40, 3072, 768), (64, 768, 3072), (96, 2048, 2000), (24, 1000, 6000), (30, 4096, 4100), (128, 768, 3072), (32, 14336, 300)]
+
+
+@pytest.mark.parametrize("tokens,inner,channels", TILED)
+def test_linear_tiles_and_groups(lib, tokens, inner, channels):
+    q, weight = U.int8(1, tokens, inner, lo=-128), U.int8(2, channels, inner, lo=-128)
+    scale, w_scale, bias = U.rand(3, tokens).abs() / 50, U.rand(4, channels) / 70, U.rand(5, channels)
+    acc = (q.double() @ weight.double().T).numpy()          # (whole numbers below 2^31: exact)
+    want = acc.astype(np.float32) * scale.numpy()[:, None] * w_scale.numpy() + bias.numpy()
+    assert torch.equal(run_linear(lib, q, scale, weight, w_scale, bias, torch.float32), torch.from_numpy(want))
+    code = torch.empty((tokens, channels), dtype=torch.uint8, device="cuda")
+    lib.linear_codes(q.cuda(), scale.cuda(), lib.pack_weights(weight.cuda()), w_scale.cuda(), code, 8, -300.0, 250.0, bias=bias.cuda())
+    lib.sync_status()
+    assert np.array_equal(code.cpu().numpy(), U.codes(want, 8, -300.0, 250.0))
+
+
 @pytest.mark.parametrize("tokens", [1, 13, 90])
 def test_linear_codes_of_values_without_a_number(lib, tokens):
     q, weight = U.int8(1, tokens, 64), U.int8(2, 40, 64)
