@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(WARPS == 16 ? 512 : 128) append_kernel(const C
   const uint32_t b = blockIdx.z;
   const int64_t first = a.first[b];
   if (first < 0) return;
-  const int64_t slot = first / a.page_tokens + blockIdx.x, row0 = slot * a.page_tokens, end = first + a.tokens;
+  const int64_t slot = static_cast<uint32_t>(first) / a.page_tokens + static_cast<int64_t>(blockIdx.x), row0 = slot * a.page_tokens, end = first + a.tokens;
   if (row0 >= end) return;
   int32_t page = -1;
   if (slot < a.table_pitch) page = a.page_table[static_cast<size_t>(b) * a.table_pitch + slot];
