@@ -1,7 +1,8 @@
 // Causal attention over the paged 8-bit cache for few query rows a cached head: decoding.
 //
 // Bound by reading keys and values once (two 8-bit rows a position and cached head, 79.8 us of copies at the
-// measured rate for 64 sequences of up to 8192 positions, 8 heads of 128).  Query rows of one cached head (its
+// measured rate for 64 sequences of up to 8192 positions, 8 heads of 128: 108 us, 5.0 TB/s; all of 8192: 188 us, 5.7 TB/s),
+// and as closely by converting each value for at most 8 rows.  Query rows of one cached head (its
 // group's heads, and the tokens of a short run) share what is read: they are the columns of
 //   S^T = K Q^T (16 positions x 8 rows x 16 dimensions a product)  and  O^T = V^T P^T (16 dimensions x 8 rows x
 // 16 positions), with the 8-bit values made f16 in registers (exact) and the scales kept outside the
@@ -10,7 +11,7 @@
 //   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
 // what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
 // Single-precision queries are split into two f16 each, and the weights too but for bfloat16, whose own rounding hides that of
-// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 115 us against 111).  The tensor cores cut sums off
+// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 113 us against 108).  The tensor cores cut sums off
 // instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
 //
 // A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
@@ -95,6 +96,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   const ClearAttentionArgs &a = f.a;
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ int32_t s_page[kSegment];
+  __shared__ int64_t s_at[kSegment];  // where the tiles lie in the caches
   __shared__ float s_ks[kSegment], s_vs[kSegment], s_top[kWarps];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t split = blockIdx.x % f.splits, group = blockIdx.x / f.splits % f.groups;
@@ -129,9 +131,10 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   };
   const int64_t head_at = static_cast<int64_t>(kh) * a.cache_strides[1];
   const uint32_t row_step = static_cast<uint32_t>(a.cache_strides[2]);
-  const uint32_t lane_at = lane / CH * row_step + lane % CH * 16;
   const uint32_t k_dst = lane / CH * DP + ((lane % CH) ^ (CH >= 8 ? (lane / CH & 1u) * 4 : 0u)) * 16;
   const bool inside = lane % CH * 16 < a.dim;
+  // of a lane's copies of a tile: place in the first, way on to the next (zero where it reads nothing)
+  const uint32_t lane_at = inside ? lane / CH * row_step + lane % CH * 16 : 0, lane_on = inside ? 512 / DP * row_step : 0;
   int32_t whole = 0x7fffffff;  // the last position that every row sees
   for (uint32_t seg = lo / 16; seg < tiles_hi; seg += kSegment) {
     const uint32_t count = min(kSegment, tiles_hi - seg);
@@ -144,6 +147,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         page = -1;
       }
       s_page[i] = page;
+      s_at[i] = page < 0 ? 0 : page * a.cache_strides[0] + head_at + static_cast<int64_t>((seg + i) * 16 % a.page_tokens) * a.cache_strides[2];
       const size_t at = static_cast<size_t>(page) * a.heads + kh;
       s_ks[i] = page < 0 ? 0.0f : a.k_scale[at];
       float v = page < 0 ? 0.0f : a.v_scale[at];
@@ -170,17 +174,15 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 
     const auto issue = [&](uint32_t i, uint32_t slot) {
       if (i < count) {
-        const int32_t page = s_page[i];
-        const bool in = page >= 0;
-        const int64_t at = in ? page * a.cache_strides[0] + head_at + static_cast<int64_t>((seg + i) * 16 % a.page_tokens) * a.cache_strides[2] : 0;
-        const int8_t *kt = a.k_cache + at, *vt = a.v_cache + at;
+        const bool in = s_page[i] >= 0 && inside;
+        const int8_t *kt = a.k_cache + s_at[i], *vt = a.v_cache + s_at[i];
         const uint32_t dst = own_addr + slot * F::TILE, vdst = dst + 16 * DP;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i) {
-          const uint32_t at_row = i * (512 / DP) * row_step;
-          copy_async(dst + i * 512 + k_dst, kt + (inside ? lane_at + at_row : 0), in && inside);
+          const uint32_t from = lane_at + i * lane_on;
+          copy_async(dst + i * 512 + k_dst, kt + from, in);
           const uint32_t row = i * (512 / DP) + lane / CH;
-          copy_async(vdst + row * DP + ((lane % CH) ^ move(row)) * 16, vt + (inside ? lane_at + at_row : 0), in && inside);
+          copy_async(vdst + row * DP + ((lane % CH) ^ move(row)) * 16, vt + from, in);
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
