@@ -102,6 +102,11 @@ __device__ __forceinline__ float clear_scaled(int32_t acc, float scale, float w_
   return biased ? __fadd_rn(y, bias) : y;
 }
 
+__device__ __forceinline__ uint32_t clear_code(const ClearLinearArgs &a, float y) {
+  // fmaxf drops a NaN: code 0
+  return static_cast<uint32_t>(fminf(fmaxf(floorf(__fmul_rn(__fsub_rn(y, a.lo), a.inv)), 0.0f), a.top));
+}
+
 // Store one output of the linear product.
 template <int OUT>
 __device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t, uint32_t n, float y) {
@@ -113,9 +118,7 @@ __device__ __forceinline__ void clear_store(const ClearLinearArgs &a, uint32_t t
   } else if constexpr (OUT == kOutBf16) {
     static_cast<__nv_bfloat16 *>(a.out)[at] = __float2bfloat16_rn(y);
   } else {
-    // fmaxf drops a NaN: code 0
-    const float f = fminf(fmaxf(floorf(__fmul_rn(__fsub_rn(y, a.lo), a.inv)), 0.0f), a.top);
-    const uint32_t code = static_cast<uint32_t>(f);
+    const uint32_t code = clear_code(a, y);
     static_cast<uint8_t *>(a.out)[at] = static_cast<uint8_t>(code);
     if (a.values) a.values[static_cast<int64_t>(t) * a.values_pitch + n] = a.table[code];
   }

@@ -298,13 +298,39 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
       if (ranks == 1) {
         if (n < a.channels) {
           const float w_scale = a.w_scale[n], bias = a.bias ? a.bias[n] : 0.0f;
+          // a few tokens at a time, all of whose loads (scales, table entries) go before their stores, which would hold them back
+          constexpr uint32_t STEP = 8;
 #pragma unroll
-          for (uint32_t i = 0; i < S::COLS; ++i)
-            if (t0 + i < a.tokens) {
-              float y = __fmul_rn(__fmul_rn(__int2float_rn(acc[i]), __ldg(a.scale + t0 + i)), w_scale);
-              if (a.bias) y = __fadd_rn(y, bias);
-              clear_store<OUT>(a, t0 + i, n, y);
+          for (uint32_t i = 0; i < S::COLS; i += STEP) {
+            if (t0 + i >= a.tokens) break;
+            float y[STEP];
+#pragma unroll
+            for (uint32_t e = 0; e < STEP; ++e) y[e] = __ldg(a.scale + min(t0 + i + e, a.tokens - 1));
+#pragma unroll
+            for (uint32_t e = 0; e < STEP; ++e) y[e] = clear_scaled(acc[i + e], y[e], w_scale, a.bias != nullptr, bias);
+            if constexpr (OUT != kOutCodes) {
+#pragma unroll
+              for (uint32_t e = 0; e < STEP; ++e)
+                if (t0 + i + e < a.tokens) clear_store<OUT>(a, t0 + i + e, n, y[e]);
+            } else {
+              uint32_t code[STEP];
+              int8_t value[STEP];
+#pragma unroll
+              for (uint32_t e = 0; e < STEP; ++e) code[e] = clear_code(a, y[e]);
+              if (a.values) {
+#pragma unroll
+                for (uint32_t e = 0; e < STEP; ++e) value[e] = __ldg(a.table + code[e]);
+              }
+              uint8_t *out = static_cast<uint8_t *>(a.out) + static_cast<int64_t>(t0 + i) * a.out_pitch + n;
+              int8_t *to = a.values + static_cast<int64_t>(t0 + i) * a.values_pitch + n;
+#pragma unroll
+              for (uint32_t e = 0; e < STEP; ++e, out += a.out_pitch, to += a.values_pitch) {
+                if (t0 + i + e >= a.tokens) break;
+                *out = static_cast<uint8_t>(code[e]);
+                if (a.values) *to = value[e];
+              }
             }
+          }
         }
       } else {
         // (one tile per cluster) the rings are idle now: this CTA's sums into them, [token][channel]
