@@ -11,7 +11,7 @@
 //   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
 // what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
 // Single-precision queries are split into two f16 each, and the weights too but for bfloat16, whose own rounding hides that of
-// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 113 us against 108).  The tensor cores cut sums off
+// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 112 us against 108).  The tensor cores cut sums off
 // instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
 //
 // A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
@@ -196,15 +196,50 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(row / a.group) * a.q_strides[1] +
                      static_cast<int64_t>(kh * a.group + row % a.group) * a.q_strides[2];
+        // four consecutive elements an access, kept as they are where their f16 will be
+        const bool four = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % (4 * sizeof(T)) == 0;
+        struct alignas(4 * sizeof(T)) Four {
+          T v[4];
+        };
+        const auto place = [](int c) { return 64 * (c / 4) + 4 * (c % 4); };
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const uint32_t d = 16 * t + place(c);
+          Four x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[e] = from_float<T>(0.0f);
+          if (row < rows && d < a.dim) {  // (dim is a multiple of 16)
+            if (four) {
+              x = *reinterpret_cast<const Four *>(q + d);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x.v[e] = q[d + e];
+            }
+          }
+          const uint32_t *bits = reinterpret_cast<const uint32_t *>(&x);
+#pragma unroll
+          for (int h = 0; h < H; ++h) qf[h][n][c][0] = bits[2 * h], qf[h][n][c][1] = bits[2 * h + 1];
+        }
+        const auto given = [&](int c, float (&v)[4]) {
+          if constexpr (H == 2) {
+            v[0] = __uint_as_float(qf[0][n][c][0]), v[1] = __uint_as_float(qf[0][n][c][1]);
+            v[2] = __uint_as_float(qf[H - 1][n][c][0]), v[3] = __uint_as_float(qf[H - 1][n][c][1]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint16_t half = static_cast<uint16_t>(qf[0][n][c][e / 2] >> (e % 2 * 16));
+              v[e] = to_float(*reinterpret_cast<const T *>(&half));
+            }
+          }
+        };
         float top = 0.0f;
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
+        for (int c = 0; c < KC; ++c) {
+          float v[4];
+          given(c, v);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
-            const float v = row < rows && d < a.dim ? to_float(q[d]) : 0.0f;
-            top = fmaxf(top, fabsf(v));
-          }
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(v[e]));
+        }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // a power of two that brings the row's largest value to [1, 2): exact (within the range of exponents)
@@ -213,11 +248,9 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           float v[4];
+          given(c, v);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t d = 16 * t + 64 * (c / 4) + 4 * (c % 4) + e;
-            v[e] = row < rows && d < a.dim ? to_float(q[d]) * down : 0.0f;
-          }
+          for (int e = 0; e < 4; ++e) v[e] *= down;
 #pragma unroll
           for (int h = 0; h < H; ++h)
 #pragma unroll
@@ -541,7 +574,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const Atte
 
 // Splits of a sequence.  Ranges of 1024 positions, or 512 or 256 where those leave SMs without a block; no more of them
 // than fill the SMs four times over (uneven lengths then even out).  Longer ranges cost less to begin and to join
-// (8 sequences of 4096, 8 heads: 1024 positions 29.3 us, 512 32.7), shorter ones balance better.
+// (8 sequences of 4096, 8 heads: 1024 positions a tenth less than 512), shorter ones balance better.
 void split(AttendArgs *f, uint32_t sms) {
   const ClearAttentionArgs &a = f->a;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f->groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
