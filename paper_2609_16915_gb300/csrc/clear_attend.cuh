@@ -17,7 +17,8 @@ struct AttendArgs {
 
 // The tensor cores cut the terms of their sums off instead of rounding them: an output comes out up to 7e-9 of itself short for
 // every position that one accumulator has taken (values of one sign; 1e-9 otherwise).  So no accumulator takes more
-// positions than this (2^-12, half a unit of f16's rounding), and single precision adds its accumulators up much sooner.
+// positions than this (2^-12, half a unit of float16's rounding; bfloat16's prompts four times as many), and single
+// precision adds its accumulators up much sooner (its running sums of longer ranges round off more than 2^-18).
 constexpr uint32_t kMostPositions = 1u << 15;
 
 // Positions of each range of a sequence of `end`: whole tiles of all warps.

@@ -901,7 +901,8 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
   const uint32_t block = block_rows_of(type);
   f.groups = (a.tokens * a.group + block - 1) / block;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
-  const uint64_t want = sms / blocks, longest = (most + 511) / 512, least = (most + kMostPositions - 1) / kMostPositions;
+  const uint64_t want = sms / blocks, longest = (most + 511) / 512;
+  const uint64_t each = type == kOutBf16 ? 4 * kMostPositions : kMostPositions, least = (most + each - 1) / each;
   f.splits = static_cast<uint32_t>(want < longest ? want : longest);
   if (f.splits < least) f.splits = static_cast<uint32_t>(least);
   if (f.splits < 1) f.splits = 1;

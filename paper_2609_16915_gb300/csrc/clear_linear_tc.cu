@@ -15,6 +15,9 @@
 //   MMA warp         four tcgen05.mma (K = 16), A from tensor memory, B from shared memory
 //   4 or 8 drain warps  every 1024 inputs the accumulators are read back, added up as integers,
 //                    and after the last scaled and stored while the next tile runs
+// Bound by the products and, between them, by the drains that exactness asks for (tensor pipe 69 % active): 4096 tokens, 4096
+// inputs, 14336 channels 315 us, 1.53 PFLOP/s (82 % of the measured bf16 rate), 1024 tokens 86 us; from 33 to 256 tokens by
+// the way of a step through copy, conversion and product, and by 7 us to begin and to end (33 tokens 22.7 us, 256 33).
 // A launch is persistent over the tiles; where there are few tiles, a cluster of up to eight CTAs
 // shares out one tile's inputs and joins the integer sums through distributed shared memory.
 //
