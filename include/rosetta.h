@@ -390,7 +390,7 @@ int rosetta_clear_init(rosetta_clear **out, int cuda_device, size_t workspace_by
  *   x, residual, sum_out [tokens][width]; residual may be NULL (h = x), and so may
  *     sum_out, which may also be x or residual itself (same pointer and pitch)
  *   gamma [width], q [tokens][width], scale [tokens]
- * A row with a NaN or an infinity gets the scale NaN.  width: 1 .. 2^20; tokens < 2^31.
+ * A row with a NaN or an infinity in h or in h * gamma gets the scale NaN.  width: 1 .. 2^20; tokens < 2^31.
  * Errors: INVALID_ARG, CUDA. */
 int rosetta_clear_norm(rosetta_clear *h, int type, const void *x, int64_t x_pitch, const void *residual,
                        int64_t residual_pitch, const float *gamma, float eps, uint32_t tokens, uint32_t width,

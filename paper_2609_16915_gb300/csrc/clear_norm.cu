@@ -14,13 +14,20 @@ namespace rosetta {
 
 namespace {
 
+// The larger, a NaN where there is one: a value that is no number reaches the row's scale.
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(x), "f"(y));
+  return m;
+}
+
 // Sum of `s` and maximum of `m` over the block, in every thread.
 __device__ __forceinline__ void block_sum_max(float &s, float &m, float2 *parts) {
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     s += __shfl_xor_sync(0xffffffffu, s, o);
-    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
   }
   if (lane == 0) parts[warp] = make_float2(s, m);
   __syncthreads();
@@ -28,7 +35,7 @@ __device__ __forceinline__ void block_sum_max(float &s, float &m, float2 *parts)
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y = fmaxf(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
+    v.y = max_nan(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
   }
   s = v.x;
   m = v.y;
@@ -43,7 +50,9 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(float sumsq, float top, uint32_t width, float eps) {
   RowScale r;
   const float rms = rsqrtf(sumsq / static_cast<float>(width) + eps);
-  r.scale = top * rms / 127.0f;  // NaN where sumsq is NaN, or infinite by an infinity (0 * inf)
+  // an infinity leaves no trace in the rest of the row: 1 / sqrt of it is 0, and a gamma of 0 hides it from `top`
+  const float infinite = __int_as_float(0x7f800000);
+  r.scale = sumsq < infinite && top < infinite ? top * rms / 127.0f : __int_as_float(0x7fc00000);
   r.up = top < 1e-30f ? 1.2676506e30f : 1.0f;  // 2^100
   r.inv = r.scale == 0.0f ? 0.0f : 127.0f / (top * r.up);
   return r;
@@ -97,7 +106,7 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(const ClearNor
         out.v[e] = from_float<T>(h[j][e]);
         s += h[j][e] * h[j][e];
         h[j][e] *= g.v[e];
-        m = fmaxf(m, fabsf(h[j][e]));
+        m = max_nan(m, fabsf(h[j][e]));
       }
       if (sum) *reinterpret_cast<P *>(sum + i) = out;
     }
@@ -106,7 +115,7 @@ __global__ void __launch_bounds__(LANES ? 256 : 1024) norm_kernel(const ClearNor
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) {
       s += __shfl_xor_sync(mask, s, o);
-      m = fmaxf(m, __shfl_xor_sync(mask, m, o));
+      m = max_nan(m, __shfl_xor_sync(mask, m, o));
     }
   } else {
     block_sum_max(s, m, parts);
@@ -138,7 +147,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const ClearNormArgs a) 
   for (uint32_t i = threadIdx.x; i < a.width; i += blockDim.x) {
     const float h = to_float(x[i]) + (res ? to_float(res[i]) : 0.0f);
     s += h * h;
-    m = fmaxf(m, fabsf(h * a.gamma[i]));
+    m = max_nan(m, fabsf(h * a.gamma[i]));
   }
   block_sum_max(s, m, parts);
   const RowScale r = row_scale(s, m, a.width, a.eps);
