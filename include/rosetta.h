@@ -386,7 +386,7 @@ int rosetta_clear_init(rosetta_clear **out, int cuda_device, size_t workspace_by
 /* Residual addition, root-mean-square norm, 8-bit output.  For each token
  *   h = x + residual,  y = h / sqrt(mean(h^2) + eps) * gamma,
  *   scale = max |y| / 127,  q = rint(y / scale) in [-127, 127] (0 where scale = 0)
- * in 32-bit floats; sum_out receives h rounded to `type`.
+ * in 32-bit floats (squares that leave their range are taken scaled); sum_out receives h rounded to `type`.
  *   x, residual, sum_out [tokens][width]; residual may be NULL (h = x), and so may
  *     sum_out, which may also be x or residual itself (same pointer and pitch)
  *   gamma [width], q [tokens][width], scale [tokens]

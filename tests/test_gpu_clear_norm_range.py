@@ -47,3 +47,22 @@ def test_sum_beyond_single_precision(lib):
     x[1] = 1
     scale = run_norm(lib, x, x.clone(), torch.ones(64), 1e-6)[1]
     assert torch.isnan(scale[0]) and torch.isfinite(scale[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_squares_beyond_single_precision(lib, dtype, width):
+    """Rows from 2^57 to 2^121: their sums of squares pass 2^114 to 2^255; one large value among small ones; and rows
+    far below, which have the same norm without eps."""
+    powers = [57, 60, 63, 64, 80, 100, 121]
+    x = torch.cat([U.rand(1, 1, width) * 2.0 ** p for p in powers] + [U.rand(2, 3, width)])
+    x[len(powers), 0] = 1e30
+    x[len(powers) + 1, -1] = -2e25
+    gamma = 1 + 0.2 * U.rand(3, width)
+    x = x.to(dtype)
+    check_norm(x, None, gamma, 1e-6, run_norm(lib, x, None, gamma, 1e-6))
+    r = (x.float() * 0.5).to(dtype)
+    check_norm(x, r, gamma, 1e-6, run_norm(lib, x, r, gamma, 1e-6, alias=True))
+    low = torch.cat([U.rand(4, 1, width) * 2.0 ** -p for p in (40, 52, 56, 63, 75, 100, 115)]).to(dtype)
+    check_norm(low, None, gamma, 0.0, run_norm(lib, low, None, gamma, 0.0))
+    check_norm(low, None, gamma, 1e-38, run_norm(lib, low, None, gamma, 1e-38))
