@@ -21,6 +21,29 @@ struct AttendArgs {
 // precision adds its accumulators up much sooner (its running sums of longer ranges round off more than 2^-18).
 constexpr uint32_t kMostPositions = 1u << 15;
 
+// Value scales as exponents of two.  Weights for the product with V are 2^(s - m) vs / sv with the running maximum m of
+// s + log2(vs / sv), so that each row's largest term is near the largest f16 whatever other pages' scales are.  sv = 2^unit keeps
+// the sums of weights in range: 1 for scales within 2^20 of 1 (a row's words then do not depend on pages that it does not
+// see), or near the largest one.
+constexpr int32_t kNoScale = -1000;
+constexpr float kLeastAbove = -80.0f;  // scales further below sv are taken as if this far: 2^-100 of sv still keeps ten bits
+
+// floor(log2 |v|); less than every number's for 0, NaN and infinity
+__device__ __forceinline__ int32_t scale_exponent(float v) {
+  const int32_t e = static_cast<int32_t>(__float_as_uint(v) >> 23 & 255u);
+  return v == 0.0f || e == 255 ? kNoScale : e - 127;
+}
+
+__device__ __forceinline__ int32_t scale_unit(int32_t most) {
+  return most == kNoScale || (most >= -20 && most <= 20) ? 0 : max(most, -100);
+}
+
+// What a page's scale adds to its scores in the running maximum: at least log2 |v / sv|, less than 1 more.
+__device__ __forceinline__ float scale_above(float v, int32_t unit) {
+  const float up = static_cast<float>(static_cast<int32_t>(__float_as_uint(v) >> 23 & 255u) - 126 - unit);
+  return fminf(fmaxf(up, kLeastAbove), 24.0f);  // (24: no number)
+}
+
 // Positions of each range of a sequence of `end`: whole tiles of all warps.
 __device__ __forceinline__ uint32_t split_share(const AttendArgs &f, uint32_t end) {
   const uint32_t share = (end + f.splits - 1) / f.splits;

@@ -6,10 +6,11 @@
 // group's heads, and the tokens of a short run) share what is read: they are the columns of
 //   S^T = K Q^T (16 positions x 8 rows x 16 dimensions a product)  and  O^T = V^T P^T (16 dimensions x 8 rows x
 // 16 positions), with the 8-bit values made f16 in registers (exact) and the scales kept outside the
-// products.  With p the weights relative to the running maximum m (in units of log 2, raised only where a
-// score passes it by 8, so p <= 2^8), and sv the largest value scale of the block's pages,
-//   O = sum p (vs / sv) 2^7 V,  l = sum p,  out = O sv 2^-7 / l:
-// what is rounded to f16 is at most 2^15, and 2^-14 (the least normal f16) is far below its largest.
+// products.  In units of log 2, with sv a power of two,
+//   P = 2^(s - m),  l = sum P,  O = sum P (vs / sv) 2^7 V,  out = O sv 2^-7 / l,
+// where m is no more than 8 below the largest s + log2(vs / sv) that the row has seen: what is rounded to f16 is at most 2^15,
+// and 2^-14 (the least normal f16) is far below the largest of the row's own terms, whatever the scales of pages without
+// weight in it or out of its sight.  (A reference of the scores alone, and terms over the largest scale, lost those bits.)
 // Single-precision queries are split into two f16 each, and the weights too but for bfloat16, whose own rounding hides that of
 // 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 112 us against 108).  The tensor cores cut sums off
 // instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
@@ -97,7 +98,8 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   extern __shared__ __align__(16) unsigned char ring[];
   __shared__ int32_t s_page[kSegment];
   __shared__ int64_t s_at[kSegment];  // where the tiles lie in the caches
-  __shared__ float s_ks[kSegment], s_vs[kSegment], s_top[kWarps];
+  __shared__ float s_ks[kSegment], s_vs[kSegment];
+  __shared__ int32_t s_top[kWarps];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t split = blockIdx.x % f.splits, group = blockIdx.x / f.splits % f.groups;
   const uint32_t bh = blockIdx.x / f.splits / f.groups, kh = bh % a.heads, b = bh / a.heads;
@@ -113,7 +115,8 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   int32_t last[NB][2];  // of rows 2 t, 2 t + 1
   float factor[NB][2];
   uint32_t qf[H][NB][KC][2];
-  float o[NB][MT][4] = {}, m[NB][2], l[NB][2] = {}, sv = 0.0f;
+  float o[NB][MT][4] = {}, m[NB][2], l[NB][2] = {};
+  int32_t most = kNoScale, unit = 0;  // of the value scales so far: the largest exponent, and that of sv
 #pragma unroll
   for (int n = 0; n < NB; ++n) m[n][0] = m[n][1] = neg_inf();
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
@@ -139,7 +142,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   for (uint32_t seg = lo / 16; seg < tiles_hi; seg += kSegment) {
     const uint32_t count = min(kSegment, tiles_hi - seg);
     __syncthreads();
-    float top = 0.0f;
+    int32_t top = kNoScale;
     for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
       int32_t page = table[(seg + i) * 16 / a.page_tokens];
       if (page < 0 || static_cast<uint32_t>(page) >= a.pages) {
@@ -153,24 +156,34 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
       float v = page < 0 ? 0.0f : a.v_scale[at];
       if (fabsf(v) == -neg_inf()) v = __int_as_float(0x7fc00000);  // no number either: kept out of the maximum
       s_vs[i] = v;
-      top = fmaxf(top, fabsf(v));
+      top = max(top, scale_exponent(v));
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    top = __reduce_max_sync(0xffffffffu, top);
     if (lane == 0) s_top[warp] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), 1e-30f);
-    if (top > sv) {  // (the same for the block)
-      const float keep = sv / top;
+    most = max(most, max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
+    const int32_t grown = scale_unit(most) - unit;  // (the same for the block)
+    if (grown != 0) {
+      // from here on s + log2(vs / sv) counts from a larger sv: m goes down by as much, or as far as l has room, and O the rest
+      unit += grown;
+      if (seg != lo / 16) {
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+          for (int e = 0; e < 2; ++e) {
+            const int32_t down = min(grown, max(0, 100 + 127 - static_cast<int32_t>(__float_as_uint(l[n][e]) >> 23)));
+            m[n][e] -= static_cast<float>(down);
+            l[n][e] = scalbnf(l[n][e], down);
+            const float keep = scalbnf(1.0f, down - grown);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[n][i][e] *= keep;
-      sv = top;
+            for (int i = 0; i < MT; ++i) {
+              o[n][i][e] *= keep;
+              o[n][i][e + 2] *= keep;
+            }
+          }
+      }
     }
-    const float vlift = kLift / sv;
+    const float vlift = scalbnf(kLift, -unit);
 
     const auto issue = [&](uint32_t i, uint32_t slot) {
       if (i < count) {
@@ -305,7 +318,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[n][e] += fine[n][e];
       }
-      const float ks = s_ks[i], vs = s_vs[i] * vlift;
+      const float ks = s_ks[i], vs = s_vs[i] * vlift, above = scale_above(s_vs[i], unit), limit = kRaise - above;
       bool raise = false;
       // (rows past the last are scored too, of queries of zeros; nothing of them is written)
       const bool part = s_page[i] < 0 || static_cast<int32_t>((seg + i) * 16 + 15) > whole;
@@ -318,7 +331,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
           for (int e = 0; e < 4; ++e) {
             const bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
             s[n][e] = seen ? s[n][e] * (ks * factor[n][e % 2]) : neg_inf();
-            raise |= s[n][e] > m[n][e % 2] + kRaise;
+            raise |= s[n][e] > m[n][e % 2] + limit;
           }
       } else {
 #pragma unroll
@@ -326,7 +339,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             s[n][e] *= ks * factor[n][e % 2];
-            raise |= s[n][e] > m[n][e % 2] + kRaise;
+            raise |= s[n][e] > m[n][e % 2] + limit;
           }
       }
       if (__any_sync(0xffffffffu, raise)) {
@@ -334,7 +347,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float top = fmaxf(fmaxf(s[n][e], s[n][e + 2]), m[n][e]);
+            float top = fmaxf(fmaxf(s[n][e], s[n][e + 2]) + above, m[n][e]);
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -435,7 +448,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   constexpr int PITCH = DP + 4;
   float *joined = reinterpret_cast<float *>(ring);
   float *stats = joined + kWarps * 8 * PITCH;  // [warp][8 rows][2]
-  const float back = sv / kLift;
+  const float back = scalbnf(1.0f / kLift, unit);
   for (int n = 0; n < NB; ++n) {
     __syncthreads();
 #pragma unroll
@@ -467,7 +480,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         // (a warp that saw nothing but NaN has a NaN sum under m = -inf)
         sum += mw == neg_inf() ? stats[(w * 8 + r) * 2 + 1] : stats[(w * 8 + r) * 2 + 1] * keep[w];
       }
-      const float scale = alone ? (sum == 0.0f ? 0.0f : back / sum) : back;
+      const float scale = alone ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
       const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
       float *part = f.part + at * a.dim;
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] +
@@ -478,9 +491,9 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) v += keep[w] * joined[(w * 8 + r) * PITCH + d];
         if (alone)
-          out[d] = from_float<T>(v * scale);
+          out[d] = from_float<T>(v * scale * back);  // (back is a power of two that may be tiny)
         else
-          part[d] = v * scale;
+          part[d] = v * back;
       }
       if (!alone && lane == 0) f.stats[at] = make_float2(sum, top);
     }

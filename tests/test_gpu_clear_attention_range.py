@@ -1,0 +1,123 @@
+"""Attention where the value scales of pages lie far apart.  A row's weights are rounded relative to what the row
+itself sees: pages it does not see, or gives no weight to, take nothing from it, whatever their scales.
+
+Bounds: the output's rounding; the weights' for the product with V (11 bits for bfloat16, 22 otherwise), and scores in
+single precision, both relative to sum p |v| of the row."""
+
+import pytest
+import torch
+
+from tests import clear_util as U
+from tests.test_gpu_clear import FLOATS, lib, make_cache  # noqa: F401  (lib: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def check(lib, dtype, q, c, s, table, lens, rows=None):
+    """rows[b]: the tokens of sequence b that are compared (all)."""
+    dim = q.shape[3]
+    lengths = torch.tensor(lens, dtype=torch.int32)
+    out = torch.full(q.shape, 9.0, dtype=dtype, device="cuda")
+    lib.attention(q.cuda(), *[t.cuda() for t in (*c, *s)], table.cuda(), lengths.cuda(), out)
+    lib.sync_status()
+    want, size = U.attention(q, *c, *s, table, lengths, dim ** -0.5)
+    weights = 2.0 ** -10 if dtype == torch.bfloat16 else 2.0 ** -16
+    err = (out.cpu().double() - want).abs()
+    bound = 1.01 * U.UNIT[dtype] * want.abs() + weights * size + (2.0 ** -25 if dtype == torch.float16 else 1e-42)
+    for b in range(len(lens)):
+        t = slice(None) if rows is None else rows[b]
+        assert torch.all(err[b, t] <= bound[b, t]), float((err[b, t] / (size[b, t] + 1e-300)).max())
+
+
+EXPONENTS = [10, 14, 20, 27, 60, 90]
+DECODE = [  # new, heads, group, dim, page
+    (1, 2, 4, 128, 16), (1, 12, 1, 64, 32), (2, 1, 8, 96, 16), (3, 2, 5, 256, 16), (1, 2, 2, 20, 16)]
+PROMPTS = [(40, 2, 4, 128, 16), (70, 1, 1, 64, 32), (90, 2, 3, 96, 16), (40, 1, 2, 256, 16), (20, 2, 2, 20, 16)]
+
+
+def without_weight(lib, dtype, exponent, new, heads, group, dim, page, lens):
+    c, s, table = make_cache(3, lens, page, heads, dim)
+    q = (1 + 0.3 * U.rand(4, len(lens), new, heads * group, dim)).to(dtype)
+    for b in range(len(lens)):
+        p = table[b, 1].long()      # scores of about -60: weights of 2^-86
+        c[0][p], s[0][p] = -127, 60 / (127 * dim ** 0.5)
+        s[1][p] *= 2.0 ** exponent
+    # (rows that see nothing else do not exist: the first page is before it)
+    check(lib, dtype, q, c, s, table, lens)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("new,heads,group,dim,page", DECODE)
+def test_decoding_beside_a_page_without_weight(lib, dtype, exponent, new, heads, group, dim, page):
+    if exponent < 90:               # (2^-86 of 2^90 is weight again)
+        without_weight(lib, dtype, exponent, new, heads, group, dim, page, [150, 64])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", [14, 27, 60])
+def test_decoding_over_ranges_of_a_long_context(lib, dtype, exponent):
+    without_weight(lib, dtype, exponent, 1, 2, 4, 128, 16, [3000, 1500])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", EXPONENTS)
+def test_decoding_before_a_page_of_another_token(lib, dtype, exponent):
+    """Three tokens, the last alone on its page: the first two do not see it."""
+    lens, page, heads, dim = [97, 33], 16, 2, 64
+    c, s, table = make_cache(5, lens, page, heads, dim)
+    for b, n in enumerate(lens):
+        s[1][table[b, (n - 1) // page].long()] *= 2.0 ** exponent
+    q = U.rand(6, 2, 3, heads * 2, dim).to(dtype)
+    check(lib, dtype, q, c, s, table, lens, [slice(0, 2)] * 2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent", [14, 20, 27, 60])
+def test_decoding_values_that_shrink_from_page_to_page(lib, dtype, exponent):
+    """The weight lies on pages of ever smaller and ever larger scales."""
+    lens, page, heads, dim = [200, 90], 16, 2, 64
+    for sign in (-1, 1):
+        c, s, table = make_cache(7, lens, page, heads, dim)
+        q = (1 + 0.3 * U.rand(8, 2, 1, heads * 4, dim)).to(dtype)
+        for b, n in enumerate(lens):
+            last = (n - 1) // page
+            for j in range(last + 1):
+                p = table[b, j].long()
+                s[1][p] *= 2.0 ** (sign * exponent * j / last)
+                c[0][p], s[0][p] = 127, 20 * (1 + sign * -j / last) / (127 * dim ** 0.5)      # weights that go the other way
+        check(lib, dtype, q, c, s, table, lens)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent,score", [(-30, 5.0), (-30, 27.0), (-90, 20.0), (30, 0.0), (30, -20.0), (None, 3.0)])
+def test_decoding_scales_that_change_far_into_a_long_context(lib, dtype, exponent, score):
+    """Ranges of over 4096 positions, whose first 4096 have other scales (None: zeros) and other scores than the rest."""
+    batch, context, page, dim, group, half = 160, 1 << 16, 64, 64, 4, 32
+    c = [U.int8(i, 2 * half, 1, page, dim) for i in (1, 2)]
+    s = [(1 + U.rand(i, 2 * half, 1).abs()) / 60 for i in (3, 4)]
+    c[0][:half], s[0][:half] = 127 if score >= 0 else -127, max(abs(score), 1e-3) / (127 * dim ** 0.5)
+    s[1][:half] *= 0.0 if exponent is None else 2.0 ** exponent
+    q = (1 + 0.3 * U.rand(5, 1, 1, group, dim)).to(dtype)
+    at = torch.arange(context // page)
+    table = torch.where(at < 64, at * 7 % half, half + at * 5 % half).to(torch.int32)[None]
+    out = torch.empty((batch, 1, group, dim), dtype=dtype, device="cuda")
+    lib.attention(q.cuda().expand(batch, -1, -1, -1).contiguous(), *[t.cuda() for t in (*c, *s)],
+                  table.cuda().expand(batch, -1).contiguous(), torch.full((batch,), context, dtype=torch.int32, device="cuda"), out)
+    lib.sync_status()
+    want, size = U.attention(q, *c, *s, table, [context], dim ** -0.5)
+    weights = 2.0 ** -10 if dtype == torch.bfloat16 else 2.0 ** -16
+    assert torch.all((out.cpu().double() - want).abs() <= 1.01 * U.UNIT[dtype] * want.abs() + weights * size + 1e-42)
+
+
+def at_the_ends(lib, dtype, exponent, new):
+    lens, page, heads, dim = [100, 64], 16, 2, 64
+    c, s, table = make_cache(13, lens, page, heads, dim)
+    s[1] *= 2.0 ** exponent
+    check(lib, dtype, U.rand(14, 2, new, heads * 2, dim).to(dtype), c, s, table, lens)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent", [-112, -60, 60, 118])
+def test_decoding_scales_at_the_ends_of_single_precision(lib, dtype, exponent):
+    at_the_ends(lib, dtype, exponent, 1)
