@@ -1,23 +1,22 @@
 // Causal attention over the paged 8-bit cache for many query rows: prompts.
 //
 // Bound by the issue of the softmax's and the conversions' instructions (about 60 % of the issue slots; the tensor pipe is
-// active for 35 % of the time, DRAM for 5 %): 8 x 256 queries at 4096 positions, 32 heads over 8 of 128, 160 us, 830 TFLOP/s
+// active for 35 % of the time, DRAM for 5 %): 8 x 256 queries at 4096 positions, 32 heads over 8 of 128, 167 us, 797 TFLOP/s
 // of 4 D operations per row and visible position.  tcgen05, scores, weights and outputs in tensor memory.
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
 // over the positions 64 at a time:
 //   4 + 4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
-//                    in shared memory, both K-major: keys [position][dimension] (exact, and with the sign of their
-//                    scale), values transposed by byte permutes to [dimension][position] and, but where the weights take
-//                    it, times their scale over the largest one
+//                    in shared memory, both K-major and exact: keys [position][dimension], with the sign of their
+//                    scale, values transposed by byte permutes to [dimension][position]
 //   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory
 //   2 x 8 softmax warps  two threads a row, 32 positions each: scores from tensor memory, times the page's key scale and the row's
-//                    factor, 2^(s - m + 7) with the running maximum m raised only where a score passes it by 8
-//                    (then O is scaled down in place), P as f16 over the scores' columns
+//                    factor, 2^(s - m + 7) with the running maximum m of s + log2(vs / sv) raised only where it is passed
+//                    by 8 (then O is scaled down in place), P vs / sv as f16 over the scores' columns
 // With two score tiles a row tile, one row tile's next scores are there when its softmax is done: the handing over
 // between warps and tensor cores (about 900 clocks a round) runs under the exponentials.
-// Rows and pages that are not seen have weight 0; a page whose scale is not a number has its values zero and its key scale
-// NaN, which reaches exactly the rows that see it.
+// Rows and pages that are not seen have weight 0; a page whose value scale is not a number has the scale zero and a key scale
+// of NaN, which reaches exactly the rows that see it.
 //
 // Every wait gives up after about two seconds and sets the error flag; the block then waits (again bounded) for the
 // products it issued before it frees the tensor memory.
@@ -38,9 +37,8 @@ constexpr uint32_t ROWS = 128, POS = 64, TILE_WARPS = 8, CONVERT_WARPS = 8;  // 
 // Single precision: one row tile, its queries in two halves.
 template <typename T>
 constexpr bool kSplit = sizeof(T) == 4;
-// Weights in two halves, and the values whole numbers, whose scales the weights take: all but bfloat16, whose own rounding hides
-// that of weights and values to 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 8 x 256 queries at
-// 4096 positions 185 us against 160).
+// Weights in two halves: all but bfloat16, whose own rounding hides that of weights to 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 8 x 256 queries at
+// 4096 positions 186 us against 167).
 template <typename T>
 constexpr bool kFine = !std::is_same<T, __nv_bfloat16>::value;
 template <typename T>
@@ -210,8 +208,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   // scales, pages out of range
   __shared__ float s_ks[8][POS / 16];
   __shared__ uint32_t s_skip[8][POS / 16];
-  __shared__ float s_vr[8][POS / 16];  // (FINE: value scales over the largest)
-  __shared__ float s_top[8], s_sv;
+  __shared__ float s_vr[8][POS / 16], s_above[8][POS / 16];  // value scales over sv, and what they add to scores in the running maximum
+  __shared__ int32_t s_top[4];
+  __shared__ float s_sv;
   // what the two threads of a row exchange; before the first tile, the power of two of each row's queries
   __shared__ float s_max[2][2 * ROWS];
   float *s_up = s_max[0];
@@ -448,18 +447,21 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         const bool part = __any_sync(0xffffffffu, (s_skip[buf][half * 2] | s_skip[buf][half * 2 + 1]) != 0 ||
                                                       static_cast<int32_t>(first + COLS - 1) > last);
         float kf[2] = {s_ks[buf][half * 2] * factor, s_ks[buf][half * 2 + 1] * factor};
+        const float above[2] = {s_above[buf][half * 2], s_above[buf][half * 2 + 1]};
         tmem_wait_ld();
         float top = neg_inf();
         if (part) {
 #pragma unroll
           for (uint32_t i = 0; i < 2; ++i) {
             const bool out = s_skip[buf][half * 2 + i] != 0;
+            float t = neg_inf();
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
               const bool in = static_cast<int32_t>(first + i * 16 + e) <= last && !out;
               v[i * 16 + e] = in ? v[i * 16 + e] * kf[i] : neg_inf();
-              top = fmaxf(top, v[i * 16 + e]);
+              t = fmaxf(t, v[i * 16 + e]);
             }
+            top = fmaxf(top, t + above[i]);
             kf[i] = 1.0f;
           }
         } else {
@@ -467,7 +469,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           for (uint32_t i = 0; i < 2; ++i) {
             const float *x = v + i * 16;
             const float t = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), max3(x[6], x[7], x[8]));
-            top = fmaxf(top, max3(t, max3(x[9], x[10], x[11]), max3(fmaxf(x[12], x[13]), x[14], x[15])) * kf[i]);
+            top = fmaxf(top, fmaf(max3(t, max3(x[9], x[10], x[11]), max3(fmaxf(x[12], x[13]), x[14], x[15])), kf[i], above[i]));
           }
         }
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
@@ -493,10 +495,14 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           const float2 x = floats_of(fma2(pair_of(v[e], v[e + 1]), kf2[e / 16], off2));
           float p0 = ex2(x.x), p1 = ex2(x.y);
           sum[e / 2 % 2] = add2(sum[e / 2 % 2], pair_of(p0, p1));
-          if constexpr (FINE) {
-            const float ratio = s_vr[buf][half * 2 + e / 16];
-            p0 *= ratio;
-            p1 *= ratio;
+          const float vr = s_vr[buf][half * 2 + e / 16];
+          if constexpr (FINE) {  // (2 - 3 % faster than both in one instruction; 2 % slower for bfloat16)
+            p0 *= vr;
+            p1 *= vr;
+          } else {
+            const float2 p = floats_of(mul2(pair_of(p0, p1), pair_of(vr, vr)));
+            p0 = p.x;
+            p1 = p.y;
           }
           const __half2 h = __floats2half2_rn(p0, p1);
           w[e / 2] = half2_bits(h);
@@ -504,8 +510,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
         tmem_st16(s_tile + half * (COLS / 2), w);
         if constexpr (FINE) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
-        const float2 both = floats_of(add2(sum[0], sum[1]));
-        l += both.x + both.y;
+        const float2 added = floats_of(add2(sum[0], sum[1]));
+        l += added.x + added.y;
         if (j > 0 && (raise || fold)) {
           // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
           const uint32_t next = r * 2 + (j + 1) % 2;
@@ -560,7 +566,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
       // (O and l are both lifted; partial results are not)
-      const float scale = alone ? s_sv / l : s_sv * 0.0078125f;
+      const float scale = alone ? 1.0f / l : 0.0078125f, sv = s_sv;  // (sv apart: a power of two that may be tiny)
       const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
       if (!alone && row < rows && half == 0) f.stats[at] = make_float2(l * 0.0078125f, m);
       // The warp's rows go out through shared memory (the queries' place: their products are done), so that a store writes
@@ -580,7 +586,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             for (uint32_t e = 0; e < 16; e += PIECE) {
               alignas(16) E x[PIECE];
 #pragma unroll
-              for (uint32_t i = 0; i < PIECE; ++i) x[i] = from_float<E>(l == 0.0f ? 0.0f : o[e + i] * scale);
+              for (uint32_t i = 0; i < PIECE; ++i) x[i] = from_float<E>(l == 0.0f ? 0.0f : o[e + i] * scale * sv);
               *reinterpret_cast<uint4 *>(stage + lane * (PIECES * 16) + (((h + e) / PIECE) ^ key) * 16) = *reinterpret_cast<const uint4 *>(x);
             }
           }
@@ -608,7 +614,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           const uint32_t d0 = half * (DP / 2) + c;
           if (row >= rows || d0 >= a.dim) continue;
 #pragma unroll
-          for (uint32_t e = 0; e < 16; ++e) out[d0 + e] = from_float<T>(l == 0.0f ? 0.0f : o[e] * scale);
+          for (uint32_t e = 0; e < 16; ++e) out[d0 + e] = from_float<T>(l == 0.0f ? 0.0f : o[e] * scale * sv);
         }
       }
     }
@@ -648,7 +654,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       skip[st] = slot < slots_end && !in;
       const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
       ks[st] = in && keys ? a.k_scale[sc] : 0.0f;
-      vs[st] = in ? a.v_scale[sc] : 0.0f;
+      vs[st] = in && keys ? a.v_scale[sc] : 0.0f;
       const int8_t *src = cache + (in ? page * a.cache_strides[0] + static_cast<int64_t>(row) * a.cache_strides[2] : 0);
       const uint32_t dst = base + raw_at + st * (2 * M::RAW) + lane * 16;
 #pragma unroll
@@ -669,27 +675,22 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     start_block();
-    float sv = 1e-30f;
-    if (!keys || FINE) {
-      // the largest value scale of the pages seen
+    // the largest value scale of the pages in the range: by the values' warps, which are not the first to be waited for
+    if (!keys) {
+      int32_t most = kNoScale;
       for (uint32_t p = start / a.page_tokens + threadIdx.x % 128; p < slots_end; p += 128) {
         const int32_t id = table[p];
-        if (id >= 0 && static_cast<uint32_t>(id) < a.pages) {
-          const float v = fabsf(a.v_scale[static_cast<size_t>(id) * a.heads + kh]);
-          if (v < -neg_inf()) sv = fmaxf(sv, v);
-        } else {
+        if (id >= 0 && static_cast<uint32_t>(id) < a.pages)
+          most = max(most, scale_exponent(a.v_scale[static_cast<size_t>(id) * a.heads + kh]));
+        else
           atomicMax(a.err_flag, 1u);
-        }
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sv = fmaxf(sv, __shfl_xor_sync(0xffffffffu, sv, o));
-      if (lane == 0) s_top[warp - SOFT_WARPS] = sv;
-      asm volatile("bar.sync %0, 128;" ::"r"(keys ? 1 : 2) : "memory");
-#pragma unroll
-      for (uint32_t i = 0; i < 4; ++i) sv = fmaxf(sv, s_top[(keys ? 0 : 4) + i]);
-      if (!keys && w == 0 && lane == 0) s_sv = sv;
+      most = __reduce_max_sync(0xffffffffu, most);
+      if (lane == 0) s_top[w] = most;
+      asm volatile("bar.arrive 1, 256;" ::: "memory");
     }
-    const float per_sv = 1.0f / sv;
+    int32_t unit = 0;  // of sv
+    float per_sv = 1.0f;
     uint32_t buf = 0;
     if (keys) {
       for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
@@ -708,12 +709,6 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             give_up();
             goto done;
           }
-          if (lane == 0) {
-            // (a value scale that is a NaN or an infinity: no number)
-            s_ks[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
-            s_skip[j % 8][w] = skip[st];
-            if constexpr (FINE) s_vr[j % 8][w] = fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f;
-          }
           // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
           const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
           unsigned char *kt = smem + M::K_AT + buf * M::K_TILE + w * 2 * (DP * 16) + kc * 256 + kr * 16;
@@ -730,6 +725,20 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             unsigned char *dst = kt + i / (DP / 64) * (DP * 16) + i % (DP / 64) * 1024;
             *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          if (j == 0) {  // (the values' warps have seen the scales)
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
+            per_sv = scalbnf(1.0f, -unit);
+            if (w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
+          }
+          if (lane == 0) {
+            // (a value scale that is a NaN or an infinity: no number)
+            const bool number = fabsf(vs[st]) < -neg_inf();
+            s_ks[j % 8][w] = number ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
+            s_skip[j % 8][w] = skip[st];
+            s_vr[j % 8][w] = number ? vs[st] * per_sv : 0.0f;
+            s_above[j % 8][w] = number ? scale_above(vs[st], unit) : 0.0f;
           }
           fence_async();
           __syncwarp();
@@ -765,7 +774,6 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             give_up();
             goto done;
           }
-          const __half2 ratio = __float2half2_rn(fabsf(vs[st]) < -neg_inf() ? vs[st] * per_sv : 0.0f);
           unsigned char *vt = smem + M::V_AT + buf * M::V_TILE + (quad >> 1) * V_GROUP + (w * 2 + vsub) * 128 + (quad & 1u) * 64;
 #pragma unroll
           for (uint32_t g = 0; g < VG; ++g) {
@@ -776,7 +784,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
               for (uint32_t e = 0; e < 4; ++e) {
                 const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
-                o[e][p] = half2_bits(FINE ? v : __hmul2(v, ratio));
+                o[e][p] = half2_bits(v);
               }
             }
 #pragma unroll

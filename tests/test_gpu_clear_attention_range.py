@@ -121,3 +121,71 @@ def at_the_ends(lib, dtype, exponent, new):
 @pytest.mark.parametrize("exponent", [-112, -60, 60, 118])
 def test_decoding_scales_at_the_ends_of_single_precision(lib, dtype, exponent):
     at_the_ends(lib, dtype, exponent, 1)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("new,heads,group,dim,page", PROMPTS)
+def test_prompts_beside_a_page_without_weight(lib, dtype, exponent, new, heads, group, dim, page):
+    if exponent < 90:
+        without_weight(lib, dtype, exponent, new, heads, group, dim, page, [150, 32 + new])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", [14, 27, 60])
+def test_prompts_over_ranges_of_a_long_context(lib, dtype, exponent):
+    without_weight(lib, dtype, exponent, 20, 1, 4, 128, 16, [3000, 1500])
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("exponent", EXPONENTS)
+@pytest.mark.parametrize("new,heads,group,dim,page", PROMPTS)
+def test_prompts_before_later_pages(lib, dtype, exponent, new, heads, group, dim, page):
+    """The last page's scale: tokens before it do not see it."""
+    lens = [150, new]
+    c, s, table = make_cache(5, lens, page, heads, dim)
+    rows = []
+    for b, n in enumerate(lens):
+        last = (n - 1) // page
+        s[1][table[b, last].long()] *= 2.0 ** exponent
+        rows.append(slice(0, max(0, last * page - (n - new))))
+    q = U.rand(6, 2, new, heads * group, dim).to(dtype)
+    check(lib, dtype, q, c, s, table, lens, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent", [14, 20, 27, 60])
+def test_prompts_over_values_that_shrink_from_page_to_page(lib, dtype, exponent):
+    lens, new, page, heads, dim = [200, 90], 60, 16, 2, 64
+    for sign in (-1, 1):
+        c, s, table = make_cache(7, lens, page, heads, dim)
+        q = (1 + 0.3 * U.rand(8, 2, new, heads * 2, dim)).to(dtype)
+        for b, n in enumerate(lens):
+            last = (n - 1) // page
+            for j in range(last + 1):
+                p = table[b, j].long()
+                s[1][p] *= 2.0 ** (sign * exponent * j / last)
+                c[0][p], s[0][p] = 127, 20 * (1 + sign * -j / last) / (127 * dim ** 0.5)
+        check(lib, dtype, q, c, s, table, lens)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_value_scales_of_either_sign_and_none(lib, dtype, new):
+    """Negative scales, pages of zeros first and last, and pages that hold nothing but zeros."""
+    lens, page, heads, dim = [180, 70], 16, 2, 64
+    c, s, table = make_cache(9, lens, page, heads, dim)
+    s[1] *= torch.where(torch.arange(s[1].numel()) % 3 == 0, -1.0, 1.0).reshape(s[1].shape)
+    for b, n in enumerate(lens):
+        s[1][table[b, 0].long()] = 0
+        s[1][table[b, (n - 1) // page].long()] = 0
+    q = U.rand(6, 2, new, heads * 2, dim).to(dtype)
+    check(lib, dtype, q, c, s, table, lens)
+    s[1].zero_()
+    check(lib, dtype, q, c, s, table, lens)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("exponent", [-112, -60, 60, 118])
+def test_prompts_scales_at_the_ends_of_single_precision(lib, dtype, exponent):
+    at_the_ends(lib, dtype, exponent, 60)
