@@ -475,7 +475,9 @@ int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const 
  * For the product with V the weights are rounded to 11 bits (BFLOAT16) or 22 (FLOAT16 and
  * FLOAT32, whose queries take part with 22 bits too), those far below a query's largest
  * weight times value scale to 2^-30 of it at least, whatever other pages' scales are: as long as
- * the value scales of a head lie within 2^80 of each other.
+ * the value scales of a head lie within 2^80 of each other.  Of 16-bit types an output is short
+ * of up to 2^-12 of sum p |v| besides, where values of one sign add up over 32768 positions
+ * (the tensor cores cut the terms of a sum off); longer contexts add such runs up in single precision.
  * group: 1 .. 128.  Errors: INVALID_ARG, CUDA, OOM. */
 int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch,
                             uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, const int8_t *k_cache,

@@ -13,11 +13,12 @@ struct AttendArgs {
   float2 *stats;            // the same: l, m
   uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
   uint32_t least;           // positions of a range at least
+  bool runs;                // a range may be longer than one accumulator takes: it adds up in the place of its partial result
 };
 
 // The tensor cores cut the terms of their sums off instead of rounding them: an output comes out up to 7e-9 of itself short for
 // every position that one accumulator has taken (values of one sign; 1e-9 otherwise).  So no accumulator takes more
-// positions than this (2^-12, half a unit of float16's rounding; bfloat16's prompts four times as many), and single
+// positions than this (2^-12, half a unit of float16's rounding), and single
 // precision adds its accumulators up much sooner (its running sums of longer ranges round off more than 2^-18).
 constexpr uint32_t kMostPositions = 1u << 15;
 
@@ -63,7 +64,7 @@ cudaError_t launch_attend_join(const AttendArgs &f, int type, uint32_t group_row
 // them are aligned).
 inline size_t attend_part_bytes(const AttendArgs &f) {
   const ClearAttentionArgs &a = f.a;
-  return f.splits == 1 ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
+  return f.splits == 1 && !f.runs ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
 }
 inline void attend_place(AttendArgs *f, void *work) {
   const ClearAttentionArgs &a = f->a;

@@ -637,7 +637,7 @@ bool attend_few_takes(const ClearAttentionArgs &a) {
 namespace {
 
 AttendArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
-  AttendArgs f{a, nullptr, nullptr, 1, 1, 1};
+  AttendArgs f{a, nullptr, nullptr, 1, 1, 1, false};
   const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a);
   f.groups = (rows + gr - 1) / gr;
   split(&f, sms);

@@ -49,6 +49,10 @@ constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-
 // Single precision adds its accumulators to a sum of their own every FOLD tiles: 256 positions lose up to 2e-6 (8 x 256 queries
 // at 4096 positions 305 us; 285 with 8 tiles, 265 without, where 4096 positions lose up to 3e-5).
 constexpr uint32_t FOLD = 4;
+// No accumulator takes more than this many tiles: a longer range's outputs so far, and its sum of weights, are then added up
+// aside (the outputs in the place of the row's partial result).
+constexpr uint32_t RUN = kMostPositions / POS;
+static_assert(RUN % FOLD == 0, "runs are whole folds");
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
@@ -177,13 +181,15 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
 }
 
-template <typename T, int DP>
+// RUNS: a block's range may be longer than one accumulator takes.  (A kernel of its own: its registers cost shorter ranges 3 %.)
+template <typename T, int DP, bool RUNS>
 __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
   constexpr bool SPLIT = kSplit<T>, FINE = kFine<T>;
   constexpr uint32_t SOFT_WARPS = kSoftWarps<T>, WARPS = kWarps<T>;
   constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
+  const auto tile_of = [](uint32_t j) { return RUNS ? j % RUN : j; };  // of a run
   extern __shared__ __align__(1024) unsigned char smem[];
   // USED: the values of tile j and the keys of tile j + 2; SFULL, PFULL: of each row tile, its two score tiles;
   // LAST, BEFORE: the products of the last tile's weights and of the one before it; FIRST: the scores of the first two
@@ -432,6 +438,20 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     };
     constexpr uint32_t COLS = POS / 2;
     float m = neg_inf(), l = 0.0f;
+    const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
+    // the runs before this one, as of the maximum then
+    float run_m = neg_inf(), run_l = 0.0f;
+    const auto run_fade = [&]() { return run_m == neg_inf() ? 0.0f : ex2(run_m - m); };
+    const auto add_runs = [&](uint32_t c, float fade, float (&o)[16]) {
+      const uint32_t d0 = half * (DP / 2) + c;
+      if (row >= rows || d0 >= a.dim) return;  // (dim is a multiple of 16)
+      const float4 *from = reinterpret_cast<const float4 *>(f.part + at * a.dim + d0);
+#pragma unroll
+      for (uint32_t e = 0; e < 16; e += 4) {
+        const float4 x = from[e / 4];
+        o[e] += fade * x.x, o[e + 1] += fade * x.y, o[e + 2] += fade * x.z, o[e + 3] += fade * x.w;
+      }
+    };
     if (r < row_tiles) {
       for (uint32_t j = 0; j < n; ++j) {
         const uint32_t buf = j % 8, two = r * 2 + j % 2, s_tile = tmem + lanes + two * POS;
@@ -475,7 +495,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
         const bool raise = meet(top > m + kRaise);
         if (other_left()) goto done;
-        const bool fold = SPLIT && j > 0 && j % FOLD == 0;
+        const bool fold = SPLIT && j > 0 && j % FOLD == 0, run = RUNS && j > 0 && j % RUN == 0;
         float keep = 1.0f;
         if (raise) {
           s_max[half][r * ROWS + row_in] = top;
@@ -512,7 +532,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         if constexpr (FINE) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
         const float2 added = floats_of(add2(sum[0], sum[1]));
         l += added.x + added.y;
-        if (j > 0 && (raise || fold)) {
+        if (j > 0 && (raise || fold || run)) {
           // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
           const uint32_t next = r * 2 + (j + 1) % 2;
           if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
@@ -520,11 +540,25 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             goto done;
           }
           fence_after();
+          const float fade = run ? run_fade() : 0.0f;
 #pragma unroll 1
           for (uint32_t c = 0; c < DP / 2; c += 16) {
             float o[16];
+            if (run) {  // (the next products begin anew)
+              read_all(c, true, o);
+#pragma unroll
+              for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
+              if (j > RUN) add_runs(c, fade, o);
+              const uint32_t d0 = half * (DP / 2) + c;
+              if (row < rows && d0 < a.dim) {
+                float4 *to = reinterpret_cast<float4 *>(f.part + at * a.dim + d0);
+#pragma unroll
+                for (uint32_t e = 0; e < 16; e += 4) to[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              }
+              continue;
+            }
             if (fold) {
-              read_all(c, j > FOLD, o);
+              read_all(c, tile_of(j) > FOLD, o);
             } else {
               tmem_ld16f(o_col + c, o);
               tmem_wait_ld();
@@ -538,7 +572,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
               for (uint32_t e = 0; e < 16; ++e) o[e] *= keep;
               tmem_st16f(o_col + DP + c, o);
-              if (j > FOLD) {
+              if (tile_of(j) > FOLD) {
                 tmem_ld16f(sum_col + c, o);
                 tmem_wait_ld();
 #pragma unroll
@@ -552,12 +586,21 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(PFULL + two));
+        if (run) {
+          // (l holds this tile's weights already: a tile more or less in a run's sum)
+          run_l = run_l * run_fade() + l;
+          run_m = m;
+          l = 0.0f;
+        }
       }
       if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
         leave();
         goto done;
       }
       fence_after();
+      const bool runs = RUNS && n > RUN;
+      const float fade = runs ? run_fade() : 0.0f;
+      if (runs) l += run_l * fade;
       s_max[half][r * ROWS + row_in] = l;
       meet(false);
       if (other_left()) goto done;
@@ -567,7 +610,6 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
       // (O and l are both lifted; partial results are not)
       const float scale = alone ? 1.0f / l : 0.0078125f, sv = s_sv;  // (sv apart: a power of two that may be tiny)
-      const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
       if (!alone && row < rows && half == 0) f.stats[at] = make_float2(l * 0.0078125f, m);
       // The warp's rows go out through shared memory (the queries' place: their products are done), so that a store writes
       // whole lines (16 bytes of 32 rows at a time: 5 % longer at 4 x 1024 queries, single precision 6 %).
@@ -581,7 +623,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll
           for (uint32_t h = 0; h < PASS; h += 16) {
             float o[16];
-            read_all(c + h, n > FOLD, o);
+            read_all(c + h, tile_of(n - 1) >= FOLD, o);
+            if (runs) add_runs(c + h, fade, o);
 #pragma unroll
             for (uint32_t e = 0; e < 16; e += PIECE) {
               alignas(16) E x[PIECE];
@@ -610,7 +653,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 #pragma unroll 1
         for (uint32_t c = 0; c < DP / 2; c += 16) {
           float o[16];
-          read_all(c, n > FOLD, o);
+          read_all(c, tile_of(n - 1) >= FOLD, o);
+          if (runs) add_runs(c, fade, o);
           const uint32_t d0 = half * (DP / 2) + c;
           if (row >= rows || d0 >= a.dim) continue;
 #pragma unroll
@@ -855,7 +899,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_after();
 #pragma unroll
         for (uint32_t k = 0; k < POS / 16; ++k)
-          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : j) | k) != 0, elect);
+          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : tile_of(j)) | k) != 0, elect);
         if constexpr (FINE) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
@@ -902,25 +946,33 @@ done:
 
 uint32_t block_rows_of(int type) { return type == kOutF32 ? ROWS : 2 * ROWS; }
 
-// Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least; and of contexts too long for one
-// accumulator.
+// Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least.  float16 and single precision under lists
+// too long for one accumulator are also split where that fills the last round of blocks better (2 x 2048 queries at 65536
+// positions, float16 4.8 ms with two against 5.5), but no further: splits that turn out empty cost a third of a short context
+// (1 x 1024 at 1024 positions under lists for 131072, bfloat16 46 us with four against 29; 8 x 2048 at 2048, float16 0.97 ms against
+// 0.45).
 AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t sms) {
-  AttendArgs f{a, nullptr, nullptr, 1, 1, 512};
+  AttendArgs f{a, nullptr, nullptr, 1, 1, 512, false};
   const uint32_t block = block_rows_of(type);
   f.groups = (a.tokens * a.group + block - 1) / block;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
   const uint64_t want = sms / blocks, longest = (most + 511) / 512;
-  const uint64_t each = type == kOutBf16 ? 4 * kMostPositions : kMostPositions, least = (most + each - 1) / each;
   f.splits = static_cast<uint32_t>(want < longest ? want : longest);
-  if (f.splits < least) f.splits = static_cast<uint32_t>(least);
   if (f.splits < 1) f.splits = 1;
+  if (type != kOutBf16) {
+    const auto rounds = [&](uint64_t splits) { return (blocks * splits + sms - 1) / sms; };
+    const uint64_t long_lists = (most + kMostPositions - 1) / kMostPositions, room = 8ull * sms / blocks;
+    for (uint32_t n = f.splits + 1; n <= long_lists && n <= room; ++n)
+      if (rounds(n) * f.splits * 10 < rounds(f.splits) * n * 9) f.splits = n;
+  }
+  f.runs = most > static_cast<uint64_t>(f.splits) * kMostPositions;
   attend_place(&f, work);
   return f;
 }
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = attend_many_kernel<T, DP>;
+  auto kern = f.runs ? attend_many_kernel<T, DP, true> : attend_many_kernel<T, DP, false>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
   kern<<<f.a.batch * f.a.heads * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);

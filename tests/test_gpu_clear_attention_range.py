@@ -189,3 +189,52 @@ def test_value_scales_of_either_sign_and_none(lib, dtype, new):
 @pytest.mark.parametrize("exponent", [-112, -60, 60, 118])
 def test_prompts_scales_at_the_ends_of_single_precision(lib, dtype, exponent):
     at_the_ends(lib, dtype, exponent, 60)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("context", [1 << 15, 1 << 17, 1 << 18])
+def test_sums_of_long_contexts_lose_no_more_than_said(lib, dtype, context):
+    """Values of one sign, one range for a whole context: what the tensor cores cut off is one-sided, so the mean of the errors
+    shows it below the outputs' own rounding (2^-9 of a bfloat16 at most: the mean of 100 outputs that have nothing in common
+    is within 1e-4, and there are 25600).  An accumulator loses 2^-12 at most."""
+    pages, page, dim, group, batch, own = 32, 64, 128, 50, 160, 4
+    kc, vc = U.int8(5, pages, 1, page, dim), U.int8(6, pages, 1, page, dim, lo=1)
+    g = torch.Generator().manual_seed(7)
+    ks, vs = torch.rand((pages, 1), generator=g) / 60, (1 + torch.rand((pages, 1), generator=g)) / 60
+    q = U.rand(9, own, 1, group, dim).to(dtype)
+    table = (torch.arange(context // page) * 7 % pages).to(torch.int32)
+    out = torch.empty((batch, 1, group, dim), dtype=dtype, device="cuda")
+    lib.attention(q.cuda().repeat(batch // own, 1, 1, 1), kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda(), table.cuda().expand(batch, -1).contiguous(),
+                  torch.full((batch,), context, dtype=torch.int32, device="cuda"), out)
+    lib.sync_status()
+    one = torch.arange(pages, dtype=torch.int32)[None].expand(own, -1).contiguous()
+    want, size = U.attention(q, kc, vc, ks, vs, one, [pages * page] * own, dim ** -0.5)
+    err = (out[:own].cpu().double() - want) / size
+    assert abs(float(err.mean())) <= 2.0 ** -12 + 1e-4, float(err.mean())
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("dim,rising", [(128, 30.0), (64, -30.0), (128, 0.0)])
+def test_ranges_of_more_than_one_run(lib, dtype, dim, rising):
+    """Contexts around multiples of 32768, under lists for more, whose scores rise or fall by `rising` on the way."""
+    lens, page, group, capacity = [70000, 32768, 32769, 33000, 65536, 65601, 500, 0], 64, 48, 1 << 17
+    pages = -(-max(lens) // page)
+    c = [U.int8(i, pages, 1, page, dim) for i in (1, 2)]
+    s = [(1 + U.rand(i, pages, 1).abs()) / 60 for i in (3, 4)]
+    if rising:
+        c[0][:] = torch.where(U.int8(5, *c[0].shape) > 0, 127, 120).to(torch.int8)
+        s[0][:, 0] = rising * torch.arange(pages) / pages / (124 * dim ** 0.5) + 1e-4
+    q = (1 + 0.3 * U.rand(6, len(lens), 1, group, dim)).to(dtype)
+    table = torch.zeros(len(lens), capacity // page, dtype=torch.int32)
+    table[:, :pages] = torch.arange(pages)
+    many = 20                       # (as many blocks as fill the GPU: no splits)
+    out = torch.empty((len(lens) * many, 1, group, dim), dtype=dtype, device="cuda")
+    lib.attention(q.cuda().repeat(many, 1, 1, 1), *[t.cuda() for t in (*c, *s)], table.cuda().repeat(many, 1),
+                  torch.tensor(lens * many, dtype=torch.int32, device="cuda"), out)
+    lib.sync_status()
+    got = out.cpu().reshape(many, len(lens), 1, group, dim)
+    assert bool((got == got[0]).all())
+    want, size = U.attention(q, *c, *s, table, lens, dim ** -0.5)
+    # the weights; for 16-bit types what accumulators lose besides
+    weights = {torch.float32: 2.0 ** -16, torch.float16: 2.0 ** -12 + 2.0 ** -16, torch.bfloat16: 2.0 ** -10 + 2.0 ** -12}[dtype]
+    assert torch.all((got[0].double() - want).abs() <= 1.01 * U.UNIT[dtype] * want.abs() + weights * size + 2.0 ** -25)
