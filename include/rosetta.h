@@ -478,6 +478,8 @@ int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const 
  * the value scales of a head lie within 2^80 of each other.  Of 16-bit types an output is short
  * of up to 2^-12 of sum p |v| besides, where values of one sign add up over 32768 positions
  * (the tensor cores cut the terms of a sum off); longer contexts add such runs up in single precision.
+ * The workspace holds at most 256 MiB of partial results, or those of one cached head of one
+ * sequence.
  * group: 1 .. 128.  Errors: INVALID_ARG, CUDA, OOM. */
 int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch,
                             uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, const int8_t *k_cache,

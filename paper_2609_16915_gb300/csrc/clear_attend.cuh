@@ -9,8 +9,9 @@ namespace rosetta {
 
 struct AttendArgs {
   ClearAttentionArgs a;
-  float *part;              // [batch][head][split][rows of all groups]: O [dim]
+  float *part;              // [batch, head of this launch][split][rows of all groups]: O [dim]
   float2 *stats;            // the same: l, m
+  uint32_t first, count;    // cached heads, of all sequences, that this launch takes
   uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
   uint32_t least;           // positions of a range at least
   bool runs;                // a range may be longer than one accumulator takes: it adds up in the place of its partial result
@@ -60,16 +61,38 @@ __device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64
 // Join the splits of every row; group_rows: rows that one block's ranges were laid out for.
 cudaError_t launch_attend_join(const AttendArgs &f, int type, uint32_t group_rows, cudaStream_t s);
 
-// Floats of the partial results, and their place in the workspace (rows of 16 floats at least: the statistics behind
+// Partial results take kMostPart bytes at most, or what one cached head of one sequence needs: beyond that the heads go
+// in several launches (each many times what fills the GPU).
+constexpr size_t kMostPart = size_t{256} << 20;
+
+inline size_t attend_part_rows(const AttendArgs &f) { return static_cast<size_t>(f.splits) * f.a.tokens * f.a.group; }  // of a head
+inline uint32_t attend_heads_at_once(const AttendArgs &f) {
+  const size_t heads = static_cast<size_t>(f.a.batch) * f.a.heads, each = attend_part_rows(f) * (f.a.dim + 2) * sizeof(float);
+  if ((f.splits == 1 && !f.runs) || heads * each <= kMostPart) return static_cast<uint32_t>(heads);
+  const size_t most = each < kMostPart ? kMostPart / each : 1, launches = (heads + most - 1) / most;
+  return static_cast<uint32_t>((heads + launches - 1) / launches);  // (about as many each time)
+}
+// Bytes of the partial results, and their place in the workspace (rows of 16 floats at least: the statistics behind
 // them are aligned).
 inline size_t attend_part_bytes(const AttendArgs &f) {
-  const ClearAttentionArgs &a = f.a;
-  return f.splits == 1 && !f.runs ? 0 : static_cast<size_t>(a.batch) * a.heads * f.splits * (a.tokens * a.group) * (a.dim + 2) * sizeof(float);
+  return f.splits == 1 && !f.runs ? 0 : attend_heads_at_once(f) * attend_part_rows(f) * (f.a.dim + 2) * sizeof(float);
 }
 inline void attend_place(AttendArgs *f, void *work) {
-  const ClearAttentionArgs &a = f->a;
+  f->first = 0;
+  f->count = attend_heads_at_once(*f);
   f->part = static_cast<float *>(work);
-  f->stats = reinterpret_cast<float2 *>(f->part + static_cast<size_t>(a.batch) * a.heads * f->splits * (a.tokens * a.group) * a.dim);
+  f->stats = reinterpret_cast<float2 *>(f->part + f->count * attend_part_rows(*f) * f->a.dim);
+}
+// launch(f) for all heads, the last time with fewer.
+template <typename F>
+cudaError_t attend_each(AttendArgs f, F launch) {
+  const uint32_t heads = f.a.batch * f.a.heads;
+  for (; f.first < heads; f.first += f.count) {
+    if (f.count > heads - f.first) f.count = heads - f.first;
+    const cudaError_t e = launch(f);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace rosetta

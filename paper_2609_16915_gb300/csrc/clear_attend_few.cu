@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   __shared__ int32_t s_top[kWarps];
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t split = blockIdx.x % f.splits, group = blockIdx.x / f.splits % f.groups;
-  const uint32_t bh = blockIdx.x / f.splits / f.groups, kh = bh % a.heads, b = bh / a.heads;
+  const uint32_t own_head = blockIdx.x / f.splits / f.groups, bh = f.first + own_head, kh = bh % a.heads, b = bh / a.heads;
   const uint32_t rows = a.tokens * a.group, row0 = group * (8 * NB);
   const int64_t len = length_of(a, b);
   const uint32_t end = group_end(a, len, min(row0 + 8 * NB, rows) - 1);
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         sum += mw == neg_inf() ? stats[(w * 8 + r) * 2 + 1] : stats[(w * 8 + r) * 2 + 1] * keep[w];
       }
       const float scale = alone ? (sum == 0.0f ? 0.0f : 1.0f / sum) : 1.0f;
-      const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
+      const size_t at = (static_cast<size_t>(own_head) * f.splits + split) * rows + row;
       float *part = f.part + at * a.dim;
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] +
                static_cast<int64_t>(row / a.group) * a.out_strides[1] +
@@ -510,14 +510,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const Atte
   const ClearAttentionArgs &a = f.a;
   const uint32_t warp = threadIdx.x / 32 % WARPS, lane = threadIdx.x % 32, rows = a.tokens * a.group;
   const uint32_t id = blockIdx.x * (kJoinWarps / WARPS) + threadIdx.x / (32 * WARPS);
-  const bool real = id < a.batch * a.heads * rows;
-  const uint32_t bh = real ? id / rows : 0, row = id % rows, kh = bh % a.heads, b = bh / a.heads;
+  const bool real = id < f.count * rows;
+  const uint32_t own_head = real ? id / rows : 0, bh = f.first + own_head, row = id % rows, kh = bh % a.heads, b = bh / a.heads;
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens, given = a.lengths[b], len = given > most ? most : given;
   const uint32_t end = group_end(a, len, min(row / group_rows * group_rows + group_rows, rows) - 1);
   const uint32_t share = split_share(f, end), count = (end + share - 1) / share;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!real || end <= share) return;  // (whole rows; written already)
-  const size_t at = static_cast<size_t>(bh) * f.splits * rows + row;
+  const size_t at = static_cast<size_t>(own_head) * f.splits * rows + row;
   float top = neg_inf(), sum = 0.0f;
   float4 o[2] = {};
   for (uint32_t s0 = warp; s0 < count; s0 += 32 * WARPS) {  // lane i: split s0 + WARPS i
@@ -610,7 +610,7 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   constexpr uint32_t smem = Few<DP>::RING > join ? Few<DP>::RING : join;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, 32 * kWarps, smem, s>>>(f);
+  kern<<<f.count * f.groups * f.splits, 32 * kWarps, smem, s>>>(f);
   return cudaGetLastError();
 }
 
@@ -637,7 +637,7 @@ bool attend_few_takes(const ClearAttentionArgs &a) {
 namespace {
 
 AttendArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
-  AttendArgs f{a, nullptr, nullptr, 1, 1, 1, false};
+  AttendArgs f{a, nullptr, nullptr, 0, 0, 1, 1, 1, false};
   const uint32_t rows = a.tokens * a.group, gr = group_rows_of(a);
   f.groups = (rows + gr - 1) / gr;
   split(&f, sms);
@@ -647,7 +647,7 @@ AttendArgs few_args(const ClearAttentionArgs &a, void *work, uint32_t sms) {
 
 template <typename T>
 cudaError_t launch_join(const AttendArgs &f, uint32_t group_rows, cudaStream_t s) {
-  const uint64_t rows = static_cast<uint64_t>(f.a.batch) * f.a.heads * f.a.tokens * f.a.group;
+  const uint64_t rows = static_cast<uint64_t>(f.count) * f.a.tokens * f.a.group;
   const bool many = f.splits > 8;  // a warp reads eight partial rows as fast as eight warps would start
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<uint32_t>(many ? rows : (rows + kJoinWarps - 1) / kJoinWarps));
@@ -673,9 +673,10 @@ cudaError_t launch_attend_join(const AttendArgs &f, int type, uint32_t group_row
 size_t attend_few_bytes(const ClearAttentionArgs &a, uint32_t sms) { return attend_part_bytes(few_args(a, nullptr, sms)); }
 
 cudaError_t launch_clear_attention_few(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s) {
-  const AttendArgs f = few_args(a, work, sms);
-  const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
-  return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, group_rows_of(a), s);
+  return attend_each(few_args(a, work, sms), [&](const AttendArgs &f) {
+    const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
+    return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, group_rows_of(a), s);
+  });
 }
 
 }  // namespace rosetta

@@ -225,8 +225,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   const auto bar = [&](uint32_t i) { return bar0 + 8u * i; };
 
   // (the blocks with the most positions first)
-  const uint32_t split = blockIdx.x % f.splits, bh = blockIdx.x / f.splits % (a.batch * a.heads), kh = bh % a.heads, b = bh / a.heads;
-  const uint32_t block = f.groups - 1 - blockIdx.x / f.splits / (a.batch * a.heads);
+  const uint32_t split = blockIdx.x % f.splits, own_head = blockIdx.x / f.splits % f.count, bh = f.first + own_head;
+  const uint32_t kh = bh % a.heads, b = bh / a.heads, block = f.groups - 1 - blockIdx.x / f.splits / f.count;
   const uint32_t rows = a.tokens * a.group, row0 = block * BLOCK_ROWS;
   int64_t len = a.lengths[b];
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     };
     constexpr uint32_t COLS = POS / 2;
     float m = neg_inf(), l = 0.0f;
-    const size_t at = (static_cast<size_t>(bh) * f.splits + split) * rows + row;
+    const size_t at = (static_cast<size_t>(own_head) * f.splits + split) * rows + row;
     // the runs before this one, as of the maximum then
     float run_m = neg_inf(), run_l = 0.0f;
     const auto run_fade = [&]() { return run_m == neg_inf() ? 0.0f : ex2(run_m - m); };
@@ -952,7 +952,7 @@ uint32_t block_rows_of(int type) { return type == kOutF32 ? ROWS : 2 * ROWS; }
 // (1 x 1024 at 1024 positions under lists for 131072, bfloat16 46 us with four against 29; 8 x 2048 at 2048, float16 0.97 ms against
 // 0.45).
 AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t sms) {
-  AttendArgs f{a, nullptr, nullptr, 1, 1, 512, false};
+  AttendArgs f{a, nullptr, nullptr, 0, 0, 1, 1, 512, false};
   const uint32_t block = block_rows_of(type);
   f.groups = (a.tokens * a.group + block - 1) / block;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
@@ -975,7 +975,7 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   auto kern = f.runs ? attend_many_kernel<T, DP, true> : attend_many_kernel<T, DP, false>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
-  kern<<<f.a.batch * f.a.heads * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
+  kern<<<f.count * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
   return cudaGetLastError();
 }
 
@@ -995,9 +995,10 @@ bool attend_many_takes(const ClearAttentionArgs &a) {
 size_t attend_many_bytes(const ClearAttentionArgs &a, int type, uint32_t sms) { return attend_part_bytes(many_args(a, type, nullptr, sms)); }
 
 cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s) {
-  const AttendArgs f = many_args(a, type, work, sms);
-  const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
-  return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, block_rows_of(type), s);
+  return attend_each(many_args(a, type, work, sms), [&](const AttendArgs &f) {
+    const cudaError_t e = type == kOutF32 ? launch<float>(f, s) : type == kOutF16 ? launch<__half>(f, s) : launch<__nv_bfloat16>(f, s);
+    return e != cudaSuccess || f.splits == 1 ? e : launch_attend_join(f, type, block_rows_of(type), s);
+  });
 }
 
 }  // namespace rosetta

@@ -238,3 +238,55 @@ def test_ranges_of_more_than_one_run(lib, dtype, dim, rising):
     # the weights; for 16-bit types what accumulators lose besides
     weights = {torch.float32: 2.0 ** -16, torch.float16: 2.0 ** -12 + 2.0 ** -16, torch.bfloat16: 2.0 ** -10 + 2.0 ** -12}[dtype]
     assert torch.all((got[0].double() - want).abs() <= 1.01 * U.UNIT[dtype] * want.abs() + weights * size + 2.0 ** -25)
+
+
+# ------------------------------------------------------------------ what a call asks memory for
+
+
+def used_by(call):
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    call()
+    return before - torch.cuda.mem_get_info()[0]
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("new,heads,group,dim,capacity", [(2048, 8, 4, 128, 1 << 17), (2048, 8, 4, 128, 1 << 20), (1024, 8, 2, 256, 1 << 20),
+                                                         (1, 8, 4, 128, 1 << 20)])
+def test_workspace_does_not_follow_the_page_lists(dtype, new, heads, group, dim, capacity):
+    """Short sequences under page lists for long ones: no more than 256 MiB, or what one cached head of one sequence takes."""
+    from paper_2609_16915_gb300 import clear
+    batch, page = 8, 64
+    kc = torch.zeros((64, heads, page, dim), dtype=torch.int8, device="cuda")
+    ks = torch.ones((64, heads), device="cuda")
+    table = (torch.arange(batch * (capacity // page), device="cuda") % 64).to(torch.int32).reshape(batch, -1)
+    q = torch.zeros((batch, new, heads * group, dim), dtype=dtype, device="cuda")
+    out = torch.empty_like(q)
+    lengths = torch.full((batch,), min(new + 100, 500), dtype=torch.int32, device="cuda")
+    lib = clear.Clear()
+    used = used_by(lambda: (lib.attention(q, kc, kc, ks, ks, table, lengths, out), lib.sync_status()))
+    lib.close()
+    assert used <= (256 << 20) + (64 << 20)
+
+
+@pytest.mark.parametrize("dtype,new,heads,group,dim,length", [(torch.float32, 512, 4, 2, 256, 3000), (torch.float32, 2048, 8, 4, 128, 2500),
+                                                             (torch.float32, 2048, 8, 4, 128, 33000)])
+def test_heads_in_several_launches(lib, dtype, new, heads, group, dim, length):
+    """More partial results than 256 MiB: the same as sequence by sequence under lists for no more than the length (each within
+    2^-16 of the sums of |v|, at most 127 x 1.5 / 60)."""
+    batch, page = 8, 64
+    each = -(-length // page)
+    c, s, _ = make_cache(3, [length], page, heads, dim, extra=0)
+    c, s = [t.cuda() for t in c], [t.cuda() for t in s]
+    table = (torch.arange(batch)[:, None] * 5 + torch.arange(each)) % each
+    lists = torch.zeros((batch, (1 << 20) // page), dtype=torch.int32)
+    lists[:, :each] = table
+    q = U.rand(4, batch, new, heads * group, dim).to(dtype).cuda()
+    lengths = torch.tensor([length - 3 * b for b in range(batch)], dtype=torch.int32, device="cuda")
+    out, one = torch.empty_like(q), torch.empty_like(q)
+    lib.attention(q, *c, *s, lists.cuda(), lengths, out)
+    short = table.to(torch.int32).cuda().contiguous()
+    for b in range(batch):
+        lib.attention(q[b:b + 1], *c, *s, short[b:b + 1], lengths[b:b + 1], one[b:b + 1])
+    lib.sync_status()
+    assert float((out - one).abs().max()) <= 2 * 2.0 ** -16 * 127 * 1.5 / 60
