@@ -104,10 +104,15 @@ int ensure_work(rosetta_clear *h, size_t bytes, cudaStream_t s) {
   } catch (...) {
     return ROSETTA_ERR_OOM;
   }
-  // (at least doubled, so that what stays behind is no more than the present one)
-  const size_t want = bytes > 2 * h->work_bytes ? bytes : 2 * h->work_bytes;
+  // (at least doubled where there is room for it, so that what stays behind is no more than the present one)
+  size_t want = bytes > 2 * h->work_bytes ? bytes : 2 * h->work_bytes;
   void *p = nullptr;
-  const cudaError_t e = cudaMalloc(&p, want);
+  cudaError_t e = cudaMalloc(&p, want);
+  if (e == cudaErrorMemoryAllocation && want > bytes) {
+    cudaGetLastError();
+    want = bytes;
+    e = cudaMalloc(&p, want);
+  }
   if (e != cudaSuccess) {
     cudaGetLastError();
     return cuda_fail(e);
