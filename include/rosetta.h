@@ -450,7 +450,7 @@ int rosetta_clear_linear_codes(rosetta_clear *h, const int8_t *q, int64_t q_pitc
  * For every page written and every head:
  *   scale' = max(scale of the rows before the new ones, if the page has any; max |new| / 127)
  *   old rows of the page: q' = rint(q * (scale / scale')), if the scale changed
- *   new rows: q = rint(new / scale')                          (0 where scale' = 0)
+ *   new rows: q = rint(new / scale') in [-127, 127]           (0 where scale' = 0)
  * Rows after the new ones are left as they are.  A NaN or an infinity among the new
  * values makes the scale NaN (and the page's values with it).  Page lists of different
  * sequences must not share a page that is written.  A position past the page list

@@ -25,6 +25,13 @@ struct alignas(sizeof(T) * VEC) Pack {
   T v[VEC];
 };
 
+// rint(x / div) in [-127, 127], in the low byte.  Past 127 where x is so small that div = max / 127 has been rounded to few bits
+// or none (below 2^-142; the quotient by multiplication is no number there).
+__device__ __forceinline__ uint32_t divided(float x, float div) {
+  const float v = x / div;
+  return rint_bits(v > 127.0f ? 127.0f : v < -127.0f ? -127.0f : v);  // (a NaN stays one)
+}
+
 // rint(x / div) of a pack, bytes in order.  The quotient by multiplication is off by less than 1e-4 (|x / div| <= 127 and
 // 2^-22 of it): only where it lies that close to a half, or is no number, the division decides.
 template <int VEC>
@@ -32,7 +39,7 @@ __device__ __forceinline__ Pack<int8_t, VEC> quotients(const float (&x)[VEC], fl
   Pack<int8_t, VEC> out;
   uint32_t bits[VEC];
   if constexpr (VEC == 1) {
-    bits[0] = rint_bits(x[0] / div);
+    bits[0] = divided(x[0], div);
     out.v[0] = static_cast<int8_t>(bits[0]);
   } else {
     const uint64_t inv2 = pair_of(inv, inv), minus2 = pair_of(-inv, -inv), magic2 = pair_of(kMagic, kMagic), back2 = pair_of(-kMagic, -kMagic);
@@ -47,7 +54,7 @@ __device__ __forceinline__ Pack<int8_t, VEC> quotients(const float (&x)[VEC], fl
     }
     if (!(far < 0.4999f)) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) bits[e] = rint_bits(x[e] / div);
+      for (int e = 0; e < VEC; ++e) bits[e] = divided(x[e], div);
     }
     uint32_t *words = reinterpret_cast<uint32_t *>(&out);
 #pragma unroll
