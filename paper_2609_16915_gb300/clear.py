@@ -31,10 +31,17 @@ def _strides(stride):
 
 
 class PackedWeights:
-    """int8 weights [channels][inner] laid out for Clear.linear."""
+    """int8 weights [channels][inner] laid out for Clear.linear.  `data` comes from torch's allocator on the stream that
+    packed them; the streams that have used it since are recorded with it, so that its memory is not given away under them."""
 
-    def __init__(self, data, channels: int, inner: int):
+    def __init__(self, data, channels: int, inner: int, stream: int | None = None):
         self.data, self.channels, self.inner = data, channels, inner
+        self.streams = {stream}
+
+    def used_on(self, stream: int):
+        if stream not in self.streams:
+            self.data.record_stream(torch.cuda.ExternalStream(stream, self.data.device))
+            self.streams.add(stream)
 
 
 def _need(ok, what: str):
@@ -120,39 +127,45 @@ class Clear:
         wp, ws = self._rows("weight", weight, torch.int8, n, k)
         size = self._L.rosetta_clear_packed_bytes(n, k)
         _need(size, f"weights of {n} x {k} are out of range")
-        data = torch.empty(size, dtype=torch.int8, device=weight.device)
-        _check("rosetta_clear_pack_weights", self._L.rosetta_clear_pack_weights(
-            self._h, wp, ws, n, k, data.data_ptr(), self._stream(stream)))
-        return PackedWeights(data, n, k)
+        stream = self._stream(stream)
+        # (from the pool of the stream that writes it: a block of another stream's may still be in use there)
+        other = stream != _current_stream(self.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, weight.device) if other else None):
+            data = torch.empty(size, dtype=torch.int8, device=weight.device)
+        _check("rosetta_clear_pack_weights", self._L.rosetta_clear_pack_weights(self._h, wp, ws, n, k, data.data_ptr(), stream))
+        return PackedWeights(data, n, k, stream)
 
-    def _linear(self, q, scale, weights, w_scale, bias):
+    def _linear(self, q, scale, weights, w_scale, bias, stream):
         _need(isinstance(weights, PackedWeights), "weights must come from pack_weights")
         _need(q.dim() == 2, "q must be a matrix")
         t, n, k = q.shape[0], weights.channels, weights.inner
         qp, qs = self._rows("q", q, torch.int8, t, k)
         data = self._at("weights", weights.data, torch.int8, tuple(weights.data.shape), True)
-        return t, n, (self._h, qp, qs, self._at("scale", scale, torch.float32, (t,)), t, data,
-                      self._at("w_scale", w_scale, torch.float32, (n,)),
-                      None if bias is None else self._at("bias", bias, torch.float32, (n,)), n, k)
+        args = (self._h, qp, qs, self._at("scale", scale, torch.float32, (t,)), t, data,
+                self._at("w_scale", w_scale, torch.float32, (n,)),
+                None if bias is None else self._at("bias", bias, torch.float32, (n,)), n, k)
+        stream = self._stream(stream)
+        weights.used_on(stream)
+        return t, n, args, stream
 
     def rosetta_clear_linear(self, q, scale, weights, w_scale, out, bias=None, stream=None):
         """out [tokens][channels] = (q weights^T) scale w_scale + bias."""
-        t, n, args = self._linear(q, scale, weights, w_scale, bias)
+        t, n, args, stream = self._linear(q, scale, weights, w_scale, bias, stream)
         kind = _float_type("out", out, 2)
         op, os = self._rows("out", out, out.dtype, t, n)
-        _check("rosetta_clear_linear", self._L.rosetta_clear_linear(*args, kind, op, os, self._stream(stream)))
+        _check("rosetta_clear_linear", self._L.rosetta_clear_linear(*args, kind, op, os, stream))
         return out
 
     def rosetta_clear_linear_codes(self, q, scale, weights, w_scale, code, bits, lo, hi, bias=None, table=None,
                                    values=None, stream=None):
         """The product's message codes (uint8) of a 2^bits-entry table on [lo, hi], and that table's int8 values."""
-        t, n, args = self._linear(q, scale, weights, w_scale, bias)
+        t, n, args, stream = self._linear(q, scale, weights, w_scale, bias, stream)
         _need((table is None) == (values is None), "table and values go together")
         cp, cs = self._rows("code", code, torch.uint8, t, n)
         tp = self._at("table", table, torch.int8, (1 << bits,)) if table is not None else None
         vp, vs = self._rows("values", values, torch.int8, t, n) if values is not None else (None, 0)
         _check("rosetta_clear_linear_codes", self._L.rosetta_clear_linear_codes(
-            *args, bits, lo, hi, cp, cs, tp, vp, vs, self._stream(stream)))
+            *args, bits, lo, hi, cp, cs, tp, vp, vs, stream))
         return code, values
 
     def _strided(self, name, t, dtype, shape):
