@@ -30,6 +30,11 @@ def _strides(stride):
     return _Strides(*stride[:3])
 
 
+def packed_size(channels: int, inner: int) -> int:
+    """Bytes of packed weights: tiles of 128 channels x 64 inputs."""
+    return -(-channels // 128) * -(-inner // 64) * 8192
+
+
 class PackedWeights:
     """int8 weights [channels][inner] laid out for Clear.linear.  `data` comes from torch's allocator on the stream that
     packed them; the streams that have used it since are recorded with it, so that its memory is not given away under them."""
@@ -141,6 +146,7 @@ class Clear:
         t, n, k = q.shape[0], weights.channels, weights.inner
         qp, qs = self._rows("q", q, torch.int8, t, k)
         data = self._at("weights", weights.data, torch.int8, tuple(weights.data.shape), True)
+        _need(weights.data.numel() >= packed_size(n, k), f"weights must hold {packed_size(n, k)} bytes for {n} x {k}")
         args = (self._h, qp, qs, self._at("scale", scale, torch.float32, (t,)), t, data,
                 self._at("w_scale", w_scale, torch.float32, (n,)),
                 None if bias is None else self._at("bias", bias, torch.float32, (n,)), n, k)
