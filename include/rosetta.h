@@ -362,7 +362,9 @@ const char *rosetta_status_string(int status);
  * element and hold `type` values; sums, norms and softmax statistics are 32-bit floats or
  * exact integers, and results are rounded to `type` once.  Calls are
  * asynchronous on `stream`; argument errors are detected before anything is
- * enqueued.  Sizes of zero (tokens, batch) are no-ops returning OK.
+ * enqueued.  Sizes of zero (tokens, batch) are no-ops returning OK.  Rows that are written
+ * lie apart: each stride of an output passes what its smaller strides span (outputs of stride 0,
+ * as an expanded tensor has, are INVALID_ARG; inputs may have them).
  *
  * A handle may be used from one host thread at a time, and its calls share one
  * workspace: they are ordered on one stream, or by the caller (or one handle per

@@ -55,6 +55,24 @@ bool good_strides(const int64_t *s) {
   return true;
 }
 
+// Do N dimensions of rows of `row` elements keep the rows apart?  (Each stride passes what the smaller ones span, in any order:
+// what slices, permutations and gaps of a buffer give.)
+template <int N>
+bool separate_rows(const int64_t (&strides)[N], const uint64_t (&sizes)[N], uint64_t row) {
+  bool taken[N] = {};
+  uint64_t span = row;
+  for (int n = 0; n < N; ++n) {
+    int next = -1;
+    for (int i = 0; i < N; ++i)
+      if (!taken[i] && (next < 0 || strides[i] < strides[next])) next = i;
+    taken[next] = true;
+    if (sizes[next] <= 1) continue;
+    if (static_cast<uint64_t>(strides[next]) < span) return false;
+    span += static_cast<uint64_t>(strides[next]) * (sizes[next] - 1);
+  }
+  return true;
+}
+
 bool good_channels(uint32_t channels, uint32_t inner) {
   return channels >= 1 && channels <= (1u << 24) && inner >= 1 && inner <= 131071u;
 }
@@ -299,6 +317,11 @@ int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const 
   if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) ||
       !k || !v || !first || !aligned(k, size) || !aligned(v, size) || !aligned(first, 4) || 2 * heads > 65535)
     return ROSETTA_ERR_INVALID_ARG;
+  // what is written: no byte of the caches twice, keys' and values' among them
+  const int64_t apart = v_cache > k_cache ? v_cache - k_cache : k_cache - v_cache;
+  if (!separate_rows<4>({cache_strides[0], cache_strides[1], cache_strides[2], apart}, {pages, heads, page_tokens, 2}, dim) ||
+      overlaps(k_scale, 4ull * pages * heads, v_scale, 4ull * pages * heads))
+    return ROSETTA_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
   ClearAppendArgs a{};
   a.src[0] = k;
@@ -346,7 +369,9 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
     return (static_cast<size_t>(batch - 1) * s[0] + static_cast<size_t>(tokens - 1) * s[1] +
             static_cast<size_t>(heads * group - 1) * s[2] + dim) * size;
   };
-  if (overlaps(out, reach(out_strides), q, reach(q_strides))) return ROSETTA_ERR_INVALID_ARG;
+  if (overlaps(out, reach(out_strides), q, reach(q_strides)) ||
+      !separate_rows<3>({out_strides[0], out_strides[1], out_strides[2]}, {batch, tokens, heads * group}, dim))
+    return ROSETTA_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
   ClearAttentionArgs a{};
   a.q = q;
