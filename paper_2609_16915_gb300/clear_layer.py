@@ -52,6 +52,17 @@ class Cache:
         self.k_scale, self.v_scale = (torch.zeros(shape[:2], device=device) for _ in range(2))
         self.pages = torch.arange(batch * each, dtype=torch.int32, device=device).reshape(batch, each)
         self.lengths = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.room = self.most = each * page     # positions; how many every sequence has left at least
+
+    def take(self, tokens):
+        """Room for `tokens` more positions of every sequence, or ValueError.  `lengths` is on the device and may be lowered there:
+        it is read only where the tokens taken so far would not leave room.  (What the device alone knows to be too long, a
+        length that was raised there or a graph replayed too often, Clear.sync_status reports.)"""
+        if tokens > self.room:
+            self.room = self.most - int(self.lengths.max())
+        if tokens > self.room:
+            raise ValueError(f"the cache holds {self.most} positions of a sequence: no room for {tokens} more")
+        self.room -= tokens
 
     def tensors(self):
         return self.k, self.v, self.k_scale, self.v_scale, self.pages
@@ -88,9 +99,11 @@ class Layer:
         return self.lib.linear(q, scale, self.packed[name], self.scales[name], y, bias=bias)
 
     def before_table(self, x, residual, cache: Cache):
-        """The 8-bit input of the up projection for new tokens x [batch][tokens][width]; residual and cache move on."""
+        """The 8-bit input of the up projection for new tokens x [batch][tokens][width]; residual and cache move on.
+        ValueError, and neither moves, where the cache is full."""
         b, t, w = x.shape
         hq, hk, d = self.heads, self.kv_heads, self.dim
+        cache.take(t)
         flat = residual.view(b * t, w)
         q, s = self._norm(x.reshape(b * t, w), "norm1", flat)
         qkv = self._linear(q, s, "qkv").view(b, t, hq + 2 * hk, d)
