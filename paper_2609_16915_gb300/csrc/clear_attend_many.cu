@@ -845,7 +845,6 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
       }
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512) : "memory");
@@ -929,6 +928,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   }
 done:
   __syncwarp();
+  // (also of warps that gave up: copies into shared memory and stores to tensor memory end before either is released)
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  tmem_wait_st();
   fence_before();
   __syncthreads();
   if (s_fail != 0u) {

@@ -372,12 +372,13 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
           }
         }
       }
-      if (!ok) {
-        give_up();
-        // let the copies already issued land before the shared memory is released
-        for (uint32_t i = issued > S::W_STAGES ? issued - S::W_STAGES : 0; i < issued; ++i)
-          if (!mbar_wait(wfull(i % S::W_STAGES), (i / S::W_STAGES) & 1u)) atomicExch(&s_unsafe, 1u);
-      }
+      if (!ok) give_up();
+      // the copies issued land before the shared memory is released, whichever warp gave up
+      for (uint32_t i = issued > S::W_STAGES ? issued - S::W_STAGES : 0; i < issued; ++i)
+        if (!mbar_wait(wfull(i % S::W_STAGES), (i / S::W_STAGES) & 1u)) {
+          atomicExch(&s_unsafe, 1u);
+          give_up();
+        }
     } else if (role == 1 && lane == 0) {
       // ---- token copies, after the kernel that makes the tiles ----
       asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -398,11 +399,12 @@ __global__ void __launch_bounds__(Shape<NT>::WARPS * 32, 1)
           }
         }
       }
-      if (!ok) {
-        give_up();
-        for (uint32_t i = issued > S::STAGES ? issued - S::STAGES : 0; i < issued; ++i)
-          if (!mbar_wait(bfull(i % S::STAGES), (i / S::STAGES) & 1u)) atomicExch(&s_unsafe, 1u);
-      }
+      if (!ok) give_up();
+      for (uint32_t i = issued > S::STAGES ? issued - S::STAGES : 0; i < issued; ++i)
+        if (!mbar_wait(bfull(i % S::STAGES), (i / S::STAGES) & 1u)) {
+          atomicExch(&s_unsafe, 1u);
+          give_up();
+        }
     } else if (role == 2) {
       // ---- MMAs ----
       const uint32_t elect = elected();
