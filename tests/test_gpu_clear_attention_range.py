@@ -290,3 +290,13 @@ def test_heads_in_several_launches(lib, dtype, new, heads, group, dim, length):
         lib.attention(q[b:b + 1], *c, *s, short[b:b + 1], lengths[b:b + 1], one[b:b + 1])
     lib.sync_status()
     assert float((out - one).abs().max()) <= 2 * 2.0 ** -16 * 127 * 1.5 / 60
+
+
+@pytest.mark.parametrize("lens,new,page,heads,group,dim", [
+    ([1], 1, 16, 1, 1, 64), ([5], 1, 16, 4, 4, 128), ([77, 30], 1, 16, 6, 2, 64), ([16, 3], 2, 16, 2, 8, 96), ([40], 20, 16, 2, 1, 256),
+    ([60, 50], 48, 16, 2, 1, 128), ([33], 33, 32, 2, 4, 64), ([300], 90, 16, 1, 4, 96)])
+def test_float16_weights_of_22_bits(lib, lens, new, page, heads, group, dim):
+    """Values whose terms cancel, so that the weights' rounding shows beside the output's: with 11 bits every one of these shapes
+    is past the bound."""
+    c, s, table = make_cache(11, lens, page, heads, dim)
+    check(lib, torch.float16, U.rand(12, len(lens), new, heads * group, dim).half(), c, s, table, lens)
