@@ -411,7 +411,8 @@ int rosetta_clear_pack_weights(rosetta_clear *h, const int8_t *weight, int64_t p
 /* Product of 8-bit integers with scales for each token and channel:
  *   acc[t][n] = sum_k q[t][k] weight[n][k]                (exact, 32-bit)
  *   out[t][n] = (float(acc) * scale[t]) * w_scale[n] + bias[n]
- * every step rounded to a 32-bit float, the result to `type`; bias may be NULL.
+ * every step rounded to a 32-bit float, the result to `type`; bias may be NULL.  Many tokens take
+ * about tokens * inner * 2 bytes of workspace (their f16 form).
  *   q [tokens][inner], scale [tokens], packed (rosetta_clear_pack_weights),
  *   w_scale, bias [channels], out [tokens][channels].
  * Errors: INVALID_ARG, CUDA, OOM. */
@@ -480,6 +481,8 @@ int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const 
  * the value scales of a head lie within 2^80 of each other.  Of 16-bit types an output is short
  * of up to 2^-12 of sum p |v| besides, where values of one sign add up over 32768 positions
  * (the tensor cores cut the terms of a sum off); longer contexts add such runs up in single precision.
+ * Fast for dim and page_tokens that are multiples of 16 with caches aligned as above, and for
+ * many query tokens for dim up to 128; other shapes are computed row by row, many times slower.
  * The workspace holds at most 256 MiB of partial results, or those of one cached head of one
  * sequence.
  * group: 1 .. 128.  Errors: INVALID_ARG, CUDA, OOM. */

@@ -9,6 +9,11 @@ the messages that are encrypted.  One step of the layer:
   h = h + norm(a) W_o
   code = message codes of norm(h) W_up + b_up on [lo, hi];  y = table[code] W_down
 
+It is a layer of a decoder's shape from those operators, not one of a named model: a root-mean-square
+norm stands before every product (the attention's output among them), there are no position
+embeddings, no gate beside the table and no biases but the table's, so a range calibrated on it is
+its own, and a model's layer is put together from the same calls where they fit it.
+
 Norms, products, cache and table values are 8-bit (clear.Clear); the residual stream is
 bfloat16.  The encrypted path replaces the table alone: encrypt(code) -> pbs_batch ->
 decrypt gives lut[code], and value_table() turns those output codes into the same 8-bit

@@ -7,7 +7,9 @@
 //
 // This kernel takes every head size: a warp per query row, 32 positions at a time, a
 // lane computing one position's score, then each lane summing its share of the
-// head's dimensions over the 32 positions.
+// head's dimensions over the 32 positions.  Every row reads all its keys and values again, and multiplies outside the
+// tensor cores: 64 sequences of 2048 positions, 32 heads over 8 of 128, pages of 8, 1.8 ms (62 us with pages of 16, which the
+// kernel for few rows takes); 4 x 256 queries at 1024 positions 5.1 ms (29 us).
 #include <stdint.h>
 
 #include "clear.h"

@@ -1,7 +1,7 @@
 // Causal attention over the paged 8-bit cache for few query rows a cached head: decoding.
 //
 // Bound by reading keys and values once (two 8-bit rows a position and cached head, 79.8 us of copies at the
-// measured rate for 64 sequences of up to 8192 positions, 8 heads of 128: 108 us, 5.0 TB/s; all of 8192: 188 us, 5.7 TB/s),
+// measured rate for 64 sequences of up to 8192 positions, 8 heads of 128: 108 us, 5.0 TB/s; all of 8192: 185 us, 5.8 TB/s),
 // and as closely by converting each value for at most 8 rows.  Query rows of one cached head (its
 // group's heads, and the tokens of a short run) share what is read: they are the columns of
 //   S^T = K Q^T (16 positions x 8 rows x 16 dimensions a product)  and  O^T = V^T P^T (16 dimensions x 8 rows x
@@ -12,12 +12,12 @@
 // and 2^-14 (the least normal f16) is far below the largest of the row's own terms, whatever the scales of pages without
 // weight in it or out of its sight.  (A reference of the scores alone, and terms over the largest scale, lost those bits.)
 // Single-precision queries are split into two f16 each, and the weights too but for bfloat16, whose own rounding hides that of
-// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 112 us against 108).  The tensor cores cut sums off
+// 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 64 sequences of up to 8192 110 us against 108).  The tensor cores cut sums off
 // instead of rounding them, so single precision adds each tile's products to the outputs (rounded) and the halves' scores at the end.
 //
 // A block of four warps takes one cached head, one group of 8 NB rows and one range of the positions; a warp
-// takes every fourth tile of 16 positions, copied ahead into a ring by cp.async (a lane copies what it will
-// read itself: no barriers).  Blocks of one sequence join through partial results (m, l, O) in the
+// takes every fourth tile of 16 positions, copied ahead into a ring of its own by cp.async (lanes read what others
+// of the warp copied: __syncwarp after each wait, no block-wide barrier but one each 256 tiles).  Blocks of one sequence join through partial results (m, l, O) in the
 // workspace and attend_join_kernel; a sequence that fits one range is written at once.
 #include <stdint.h>
 

