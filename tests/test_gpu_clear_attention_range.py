@@ -300,3 +300,23 @@ def test_float16_weights_of_22_bits(lib, lens, new, page, heads, group, dim):
     is past the bound."""
     c, s, table = make_cache(11, lens, page, heads, dim)
     check(lib, torch.float16, U.rand(12, len(lens), new, heads * group, dim).half(), c, s, table, lens)
+
+
+@pytest.mark.parametrize("rest", [-112, -50, 0, 60])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decoding_zeros_far_into_a_long_context(lib, dtype, rest):
+    """The first 4096 positions of every range are zeros, and the scales behind them are far from 1."""
+    batch, page, dim, group, context = 160, 64, 64, 4, 1 << 16
+    c = [U.int8(i, 64, 1, page, dim) for i in (1, 2)]
+    s = [(1 + U.rand(i, 64, 1).abs()) / 60 for i in (3, 4)]
+    s[1][:32], s[1][32:] = 0, s[1][32:] * 2.0 ** rest
+    q = U.rand(5, 1, 1, group, dim).to(dtype)
+    at = torch.arange(context // page)
+    table = torch.where(at % 70 < 66, at * 7 % 32, 32 + at * 5 % 32).to(torch.int32)[None]
+    out = torch.empty((batch, 1, group, dim), dtype=dtype, device="cuda")
+    lib.attention(q.cuda().expand(batch, -1, -1, -1).contiguous(), *[t.cuda() for t in (*c, *s)],
+                  table.cuda().expand(batch, -1).contiguous(), torch.full((batch,), context, dtype=torch.int32, device="cuda"), out)
+    lib.sync_status()
+    want, size = U.attention(q, *c, *s, table, [context], dim ** -0.5)
+    weights = 2.0 ** -10 if dtype == torch.bfloat16 else 2.0 ** -16
+    assert torch.all((out.cpu().double() - want).abs() <= 1.01 * U.UNIT[dtype] * want.abs() + weights * size + 1e-42)
