@@ -493,6 +493,94 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
                             uint32_t table_pitch, const int32_t *lengths, float softmax_scale, void *out,
                             const int64_t *out_strides, void *stream);
 
+/* Drafted tokens: a tree of up to 1024 nodes for each sequence goes through the layer in one
+ * step, the target's probabilities say which of them stand, and the cache keeps those.  Node 0 is
+ * the root (the last token that stands); parents[b][i] is the node before node i, less than i, or
+ * -1: a root of its own, or no node at all (padding). */
+
+/* The tree's mask: bit j % 32 of word j / 32 of mask[b][i] is set where node j is i or an
+ * ancestor of i.
+ *   parents int32 [batch][tokens], row pitch parents_pitch (0: one tree for all sequences)
+ *   mask uint32 [batch][tokens][(tokens + 31) / 32], element at b * s[0] + i * s[1] + word with
+ *     s = mask_strides (HOST array)
+ * A parent out of range counts as -1 and is reported by rosetta_clear_sync_status as INVALID_ARG.
+ * Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_tree_mask(rosetta_clear *h, const int32_t *parents, int64_t parents_pitch, uint32_t batch,
+                            uint32_t tokens, uint32_t *mask, const int64_t *mask_strides, void *stream);
+
+/* rosetta_clear_attention under a mask: the tokens are appended to the cache as the last `tokens`
+ * positions of each sequence, and query t of sequence b sees all positions before them, and
+ * position lengths[b] - tokens + j of its own where bit j of mask[b][t] is set (any bits, a tree's
+ * or others; a query that sees nothing gets zeros).  mask, mask_strides as above (strides of 0: one
+ * mask for all); bits from `tokens` on are ignored.  tokens: up to 1024.  All else as there.
+ * Errors: INVALID_ARG, CUDA, OOM. */
+int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch,
+                                 uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, const int8_t *k_cache,
+                                 const int8_t *v_cache, const int64_t *cache_strides, const float *k_scale,
+                                 const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                                 uint32_t table_pitch, const int32_t *lengths, const uint32_t *mask,
+                                 const int64_t *mask_strides, float softmax_scale, void *out, const int64_t *out_strides,
+                                 void *stream);
+
+/* Which drafted tokens stand, and the token after them, so that what comes out is distributed as
+ * by the target alone.  From node n = 0, with p = target[b][n], its children c are tried in order,
+ * each with token x = tokens[b][c] and number u = uniform[b][c]:
+ *   drawn from q = draft[b][n], each anew:  s = 0, Z = 1 at first;
+ *     accepted where u q(x) Z < max(p(x) - s q(x), 0), else s = s + Z, Z = sum_y max(p(y) - s q(y), 0)
+ *   given (draft NULL):  R = 1 at first;
+ *     accepted where u R < p(x), else R = R - p(x), and x has no weight here any more
+ * An accepted child is the next n.  Where none is, the next token is the first whose running sum of
+ * the weights that are left, max(p - s q, 0) or p without the rejected, passes uniform[b][0] times
+ * all of them (of p itself where nothing is left).
+ *   target, draft [batch][nodes][vocab] of `type`, element at b * s[0] + node * s[1] + token with
+ *     s = target_strides, draft_strides (HOST arrays): probabilities, in [0, 2], taken as whole
+ *     multiples of 2^-56; rows add up to 1 but for rounding.  All sums are exact from there on, so
+ *     that equal inputs give equal outputs whatever the sizes around them.
+ *   tokens, parents int32, uniform float [batch][nodes], in [0, 1), row pitches from 0 on
+ *   path int32 [batch][nodes] of pitch path_pitch: the accepted nodes, 0 first, then -1;
+ *     count [batch]: how many; next [batch]: the next token
+ * nodes: up to 1024, vocab: 1 .. 2^24.  Nodes of a parent or a token out of range take no part,
+ * probabilities out of range count as 0, a row of none but zeros or that adds up to 64 gives the
+ * token -1; each is reported by rosetta_clear_sync_status as INVALID_ARG (of what the walk reads).
+ * Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_verify(rosetta_clear *h, int type, const void *target, const int64_t *target_strides,
+                         const void *draft, const int64_t *draft_strides, const int32_t *tokens, int64_t tokens_pitch,
+                         const int32_t *parents, int64_t parents_pitch, const float *uniform, int64_t uniform_pitch,
+                         uint32_t batch, uint32_t nodes, uint32_t vocab, int32_t *path, int64_t path_pitch,
+                         int32_t *count, int32_t *next, void *stream);
+
+/* Bring accepted rows of the cache together: position first[b] + path[b][i] of sequence b becomes
+ * position first[b] + i, for i < count[b] (first[b] < 0: nothing moves), keys and values.
+ *   path int32 [batch][tokens] of pitch path_pitch: increasing, in [0, tokens); count [batch]
+ * For every page that holds kept rows (i < count[b]) and every head:
+ *   scale' = max of the scales of the pages that its rows come from, those before the kept ones
+ *     among them;  q' = rint(q * (scale / scale')) for each of these rows whose scale differs
+ *     (a NaN: bytes as they are)
+ * Rows after the kept ones, and pages without any, are left as they are.  A path or a count that is
+ * none moves nothing of its sequence, a position past the page list or a page outside [0, pages)
+ * is skipped; both are reported by rosetta_clear_sync_status as INVALID_ARG.  Page lists of
+ * different sequences must not share these pages.  tokens: up to 1024.  Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_cache_keep(rosetta_clear *h, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim,
+                             int8_t *k_cache, int8_t *v_cache, const int64_t *cache_strides, float *k_scale,
+                             float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                             uint32_t table_pitch, const int32_t *first, const int32_t *path, int64_t path_pitch,
+                             const int32_t *count, void *stream);
+
+/* Read rows of the cache back: row i of sequence b of k and v receives position first[b] + i as
+ * q * scale, a 32-bit float rounded to `type`, where that lies in [0, lengths[b]); other rows are left
+ * as they are.
+ *   k, v [batch][tokens][heads][dim] of `type`, element at b * s[0] + i * s[1] + head * s[2] + d with
+ *     s = k_strides, v_strides (HOST arrays); they may be slices of one buffer
+ *   first, lengths int32 [batch]; a length past the page list counts as the list's end, rows of a page
+ *     outside [0, pages) are skipped, and both are reported by rosetta_clear_sync_status as INVALID_ARG
+ * tokens: up to 2^24.  Errors: INVALID_ARG, CUDA. */
+int rosetta_clear_cache_read(rosetta_clear *h, int type, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim,
+                             const int8_t *k_cache, const int8_t *v_cache, const int64_t *cache_strides,
+                             const float *k_scale, const float *v_scale, uint32_t pages, uint32_t page_tokens,
+                             const int32_t *page_table, uint32_t table_pitch, const int32_t *first,
+                             const int32_t *lengths, void *k, const int64_t *k_strides, void *v,
+                             const int64_t *v_strides, void *stream);
+
 /* Wait for all work on `stream` and report deferred errors of the handle's calls
  * (CUDA; TIMEOUT; INVALID_ARG for a page or a length out of range), once. */
 int rosetta_clear_sync_status(rosetta_clear *h, void *stream);

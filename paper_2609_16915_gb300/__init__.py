@@ -32,7 +32,8 @@ EXPORTS = ("rosetta_params_init", "rosetta_upload_bsk", "rosetta_upload_ksk", "r
            "rosetta_sync_status", "rosetta_destroy", "rosetta_status_string",
            "rosetta_clear_init", "rosetta_clear_norm", "rosetta_clear_packed_bytes", "rosetta_clear_pack_weights",
            "rosetta_clear_linear", "rosetta_clear_linear_codes", "rosetta_clear_cache_append",
-           "rosetta_clear_attention", "rosetta_clear_sync_status", "rosetta_clear_destroy")
+           "rosetta_clear_attention", "rosetta_clear_tree_mask", "rosetta_clear_tree_attention", "rosetta_clear_verify",
+           "rosetta_clear_cache_keep", "rosetta_clear_cache_read", "rosetta_clear_sync_status", "rosetta_clear_destroy")
 
 
 class RosettaError(RuntimeError):
@@ -95,6 +96,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     cache = [vp, vp, strides, vp, vp, u32, u32, vp, u32]
     L.rosetta_clear_cache_append.argtypes = [vp, i32, vp, strides, vp, strides, u32, u32, u32, u32, *cache, vp, vp]
     L.rosetta_clear_attention.argtypes = [vp, i32, vp, strides, u32, u32, u32, u32, u32, *cache, vp, f32, vp, strides, vp]
+    L.rosetta_clear_tree_mask.argtypes = [vp, vp, i64, u32, u32, vp, strides, vp]
+    L.rosetta_clear_tree_attention.argtypes = [vp, i32, vp, strides, u32, u32, u32, u32, u32, *cache, vp, vp, strides, f32, vp,
+                                               strides, vp]
+    L.rosetta_clear_verify.argtypes = [vp, i32, vp, strides, vp, strides, vp, i64, vp, i64, vp, i64, u32, u32, u32, vp, i64, vp,
+                                       vp, vp]
+    L.rosetta_clear_cache_keep.argtypes = [vp, u32, u32, u32, u32, *cache, vp, vp, i64, vp, vp]
+    L.rosetta_clear_cache_read.argtypes = [vp, i32, u32, u32, u32, u32, *cache, vp, vp, vp, strides, vp, strides, vp]
     L.rosetta_clear_sync_status.argtypes = [vp, vp]
     L.rosetta_clear_destroy.argtypes = [vp]
     L.rosetta_clear_destroy.restype = None

@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["tables.cu", "bsk_transform.cu", "blind_rotate.cu", "blind_rotate3.cu", "blind_rotate_solo.cu", "blind_rotate_small.cu",
            "keyswitch.cu", "keyswitch_tc.cu", "keyswitch_fp8.cu",
            "rosetta_api.cu", "pbs_noalloc.cu", "trace.cu", "trace_solo.cu", "plain_mul.cu",
-           "clear_api.cu", "clear_norm.cu", "clear_linear.cu", "clear_linear_tc.cu", "clear_cache.cu", "clear_attend.cu", "clear_attend_few.cu", "clear_attend_many.cu"]
+           "clear_api.cu", "clear_norm.cu", "clear_linear.cu", "clear_linear_tc.cu", "clear_cache.cu", "clear_attend.cu", "clear_attend_few.cu", "clear_attend_many.cu",
+           "clear_draft.cu", "clear_rows.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

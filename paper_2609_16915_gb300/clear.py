@@ -203,9 +203,8 @@ class Clear:
             self._h, kind, kp, ks, vp, vs, b, t, h, d, *cache, self._at("first", first, torch.int32, (b,)),
             self._stream(stream)))
 
-    def rosetta_clear_attention(self, q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out,
-                                softmax_scale=None, stream=None):
-        """Causal attention of q [batch][tokens][query heads][dim] over the cache; softmax_scale: dim^-1/2 unless given."""
+    def _attention(self, q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out, softmax_scale):
+        """The attentions' arguments, up to the lengths and from the scale on."""
         kind = _float_type("q", q, 4)
         shape = b, t, hq, d = tuple(q.shape)
         heads = k_cache.shape[1]
@@ -213,11 +212,74 @@ class Clear:
         qp, qs = self._strided("q", q, q.dtype, shape)
         op, os = self._strided("out", out, q.dtype, shape)
         cache = self._cache(k_cache, v_cache, k_scale, v_scale, page_table, b, heads, d)
-        _check("rosetta_clear_attention", self._L.rosetta_clear_attention(
-            self._h, kind, qp, qs, b, t, heads, hq // heads, d, *cache,
-            self._at("lengths", lengths, torch.int32, (b,)), d ** -0.5 if softmax_scale is None else softmax_scale, op, os,
-            self._stream(stream)))
+        return ((self._h, kind, qp, qs, b, t, heads, hq // heads, d, *cache, self._at("lengths", lengths, torch.int32, (b,))),
+                (d ** -0.5 if softmax_scale is None else softmax_scale, op, os))
+
+    def rosetta_clear_attention(self, q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out,
+                                softmax_scale=None, stream=None):
+        """Causal attention of q [batch][tokens][query heads][dim] over the cache; softmax_scale: dim^-1/2 unless given."""
+        start, end = self._attention(q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out, softmax_scale)
+        _check("rosetta_clear_attention", self._L.rosetta_clear_attention(*start, *end, self._stream(stream)))
         return out
+
+    def _nodes(self, name, t, dtype, batch, nodes):
+        """(address, pitch) of a word for each node; the sequences may share a row."""
+        return self._at(name, t, dtype, (batch, nodes)), t.stride(0) if batch > 1 else nodes
+
+    def rosetta_clear_tree_mask(self, parents, mask, stream=None):
+        """mask int32 [batch][tokens][words of 32] of the trees parents int32 [batch][tokens] (-1: a root)."""
+        _need(parents.dim() == 2, "parents must be [batch][tokens]")
+        b, t = parents.shape
+        pp, ps = self._nodes("parents", parents, torch.int32, b, t)
+        mp, ms = self._strided("mask", mask, torch.int32, (b, t, -(-t // 32)))
+        _check("rosetta_clear_tree_mask", self._L.rosetta_clear_tree_mask(self._h, pp, ps, b, t, mp, ms, self._stream(stream)))
+        return mask
+
+    def rosetta_clear_tree_attention(self, q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, mask, out,
+                                     softmax_scale=None, stream=None):
+        """attention() of the last q.shape[1] positions under a mask [batch][tokens][words]: each sees the positions
+        before them and those of its bits."""
+        start, end = self._attention(q, k_cache, v_cache, k_scale, v_scale, page_table, lengths, out, softmax_scale)
+        b, t = q.shape[:2]
+        mp, ms = self._strided("mask", mask, torch.int32, (b, t, -(-t // 32)))
+        _check("rosetta_clear_tree_attention", self._L.rosetta_clear_tree_attention(*start, mp, ms, *end, self._stream(stream)))
+        return out
+
+    def rosetta_clear_verify(self, target, tokens, parents, uniform, path, count, next_token, draft=None, stream=None):
+        """The accepted nodes (path int32 [batch][nodes], then -1; count [batch]) of trees of drafted tokens, and the
+        token after them, from probabilities [batch][nodes][vocab] and given numbers uniform [batch][nodes]."""
+        kind = _float_type("target", target, 3)
+        b, n, v = shape = tuple(target.shape)
+        tp, ts = self._strided("target", target, target.dtype, shape)
+        dp, ds = self._strided("draft", draft, target.dtype, shape) if draft is not None else (None, None)
+        pp, ps = self._rows("path", path, torch.int32, b, n)
+        _check("rosetta_clear_verify", self._L.rosetta_clear_verify(
+            self._h, kind, tp, ts, dp, ds, *self._nodes("tokens", tokens, torch.int32, b, n),
+            *self._nodes("parents", parents, torch.int32, b, n), *self._nodes("uniform", uniform, torch.float32, b, n), b, n, v, pp, ps,
+            self._at("count", count, torch.int32, (b,)), self._at("next_token", next_token, torch.int32, (b,)), self._stream(stream)))
+        return path, count, next_token
+
+    def rosetta_clear_cache_keep(self, k_cache, v_cache, k_scale, v_scale, page_table, first, path, count, stream=None):
+        """Positions first[b] + path[b][i] become first[b] + i for i < count[b]."""
+        _need(k_cache.dim() == 4 and path.dim() == 2, "k_cache must be [pages][heads][page tokens][dim], path [batch][tokens]")
+        b, t = path.shape
+        heads, dim = k_cache.shape[1], k_cache.shape[3]
+        cache = self._cache(k_cache, v_cache, k_scale, v_scale, page_table, b, heads, dim)
+        _check("rosetta_clear_cache_keep", self._L.rosetta_clear_cache_keep(
+            self._h, b, t, heads, dim, *cache, self._at("first", first, torch.int32, (b,)),
+            *self._nodes("path", path, torch.int32, b, t), self._at("count", count, torch.int32, (b,)), self._stream(stream)))
+
+    def rosetta_clear_cache_read(self, k_cache, v_cache, k_scale, v_scale, page_table, first, lengths, k, v, stream=None):
+        """Positions first[b] .. of the cache, as far as lengths[b], into k, v [batch][tokens][heads][dim]."""
+        kind = _float_type("k", k, 4)
+        shape = b, t, h, d = tuple(k.shape)
+        kp, ks = self._strided("k", k, k.dtype, shape)
+        vp, vs = self._strided("v", v, k.dtype, shape)
+        cache = self._cache(k_cache, v_cache, k_scale, v_scale, page_table, b, h, d)
+        _check("rosetta_clear_cache_read", self._L.rosetta_clear_cache_read(
+            self._h, kind, b, t, h, d, *cache, self._at("first", first, torch.int32, (b,)),
+            self._at("lengths", lengths, torch.int32, (b,)), kp, ks, vp, vs, self._stream(stream)))
+        return k, v
 
     def rosetta_clear_sync_status(self, stream=None):
         _check("rosetta_clear_sync_status", self._L.rosetta_clear_sync_status(self._h, self._stream(stream)))
@@ -230,4 +292,9 @@ class Clear:
     linear_codes = rosetta_clear_linear_codes
     cache_append = rosetta_clear_cache_append
     attention = rosetta_clear_attention
+    tree_mask = rosetta_clear_tree_mask
+    tree_attention = rosetta_clear_tree_attention
+    verify = rosetta_clear_verify
+    cache_keep = rosetta_clear_cache_keep
+    cache_read = rosetta_clear_cache_read
     sync_status = rosetta_clear_sync_status

@@ -62,6 +62,49 @@ struct ClearAttentionArgs {
   const int32_t *page_table, *lengths;
   uint32_t batch, tokens, heads, group, dim, pages, page_tokens, table_pitch;
   float softmax_scale;
+  const uint32_t *mask;         // of a tree of drafted tokens; null: causal
+  int64_t mask_strides[2];      // batch, token (words)
+  uint32_t *err_flag;
+};
+
+struct ClearTreeArgs {
+  const int32_t *parents;
+  int64_t parents_pitch;
+  uint32_t *mask;
+  int64_t mask_strides[2];
+  uint32_t batch, tokens;
+  uint32_t *err_flag;
+};
+
+struct ClearVerifyArgs {
+  const void *target, *draft;   // draft null: the drafted tokens were given, not drawn
+  int64_t target_strides[2], draft_strides[2];  // batch, node
+  const int32_t *tokens, *parents;
+  const float *uniform;
+  int64_t tokens_pitch, parents_pitch, uniform_pitch, path_pitch;
+  int32_t *path, *count, *next;
+  uint32_t batch, nodes, vocab;
+  uint32_t *err_flag;
+};
+
+struct ClearKeepArgs {
+  int8_t *cache[2];
+  int64_t cache_strides[3];
+  float *scale[2];
+  const int32_t *page_table, *first, *path, *count;
+  int64_t path_pitch;
+  uint32_t batch, tokens, heads, dim, pages, page_tokens, table_pitch;
+  uint32_t *err_flag;
+};
+
+struct ClearReadArgs {
+  const int8_t *cache[2];
+  int64_t cache_strides[3];
+  const float *scale[2];
+  const int32_t *page_table, *first, *lengths;
+  void *out[2];
+  int64_t out_strides[2][3];    // batch, token, head
+  uint32_t batch, tokens, heads, dim, pages, page_tokens, table_pitch;
   uint32_t *err_flag;
 };
 
@@ -148,5 +191,10 @@ size_t attend_many_bytes(const ClearAttentionArgs &a, int type, uint32_t sms);
 cudaError_t launch_clear_attention_many(const ClearAttentionArgs &a, int type, void *work, uint32_t sms, cudaStream_t s);
 // and for every shape
 cudaError_t launch_clear_attention(const ClearAttentionArgs &a, int type, cudaStream_t s);
+// drafted tokens
+cudaError_t launch_clear_tree_mask(const ClearTreeArgs &a, cudaStream_t s);
+cudaError_t launch_clear_verify(const ClearVerifyArgs &a, int type, uint32_t sms, cudaStream_t s);
+cudaError_t launch_clear_keep(const ClearKeepArgs &a, cudaStream_t s);
+cudaError_t launch_clear_read(const ClearReadArgs &a, int type, cudaStream_t s);
 
 }  // namespace rosetta

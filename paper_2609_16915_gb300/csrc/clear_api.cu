@@ -168,6 +168,92 @@ bool good_cache(const int8_t *k_cache, const int8_t *v_cache, const int64_t *str
          aligned(k_scale, 4) && aligned(v_scale, 4) && aligned(page_table, 4);
 }
 
+// For calls that write to the caches: no byte of them twice, keys' and values' among them.
+bool separate_caches(const int8_t *k_cache, const int8_t *v_cache, const int64_t *strides, const float *k_scale, const float *v_scale,
+                     uint32_t heads, uint32_t dim, uint32_t pages, uint32_t page_tokens) {
+  const int64_t apart = v_cache > k_cache ? v_cache - k_cache : k_cache - v_cache;
+  return separate_rows<4>({strides[0], strides[1], strides[2], apart}, {pages, heads, page_tokens, 2}, dim) &&
+         !overlaps(k_scale, 4ull * pages * heads, v_scale, 4ull * pages * heads);
+}
+
+constexpr uint32_t kMostNodes = 1024;  // of a tree of drafted tokens
+
+// Bytes from a tensor's start to the end of its last row (three strides and `dim` elements; all sizes at least 1).
+size_t reach(const int64_t *s, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim, size_t size) {
+  return (static_cast<size_t>(batch - 1) * s[0] + static_cast<size_t>(tokens - 1) * s[1] + static_cast<size_t>(heads - 1) * s[2] + dim) * size;
+}
+
+// The attention's checks and dispatch, causal or under a tree's mask.
+int run_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch, uint32_t tokens, uint32_t heads,
+                  uint32_t group, uint32_t dim, const int8_t *k_cache, const int8_t *v_cache, const int64_t *cache_strides,
+                  const float *k_scale, const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                  uint32_t table_pitch, const int32_t *lengths, const uint32_t *mask, const int64_t *mask_strides, float softmax_scale,
+                  void *out, const int64_t *out_strides, void *stream) {
+  if (!h || !known_type(type) || !q_strides || !out_strides || !good_strides(q_strides) || !good_strides(out_strides) ||
+      group < 1 || group > 128 || tokens > (1u << 24) || batch > 65535 || !isfinite(softmax_scale))
+    return ROSETTA_ERR_INVALID_ARG;
+  if (batch == 0 || tokens == 0) return ROSETTA_OK;
+  const size_t size = type_size(type);
+  if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) ||
+      !q || !out || !lengths || !aligned(q, size) || !aligned(out, size) || !aligned(lengths, 4))
+    return ROSETTA_ERR_INVALID_ARG;
+  // (rows of q and out, over all batches: what the launches' grids count)
+  if (static_cast<double>(batch) * tokens * heads * group > 2147483000.0) return ROSETTA_ERR_INVALID_ARG;
+  const auto bytes = [&](const int64_t *s) { return reach(s, batch, tokens, heads * group, dim, size); };
+  if (overlaps(out, bytes(out_strides), q, bytes(q_strides)) ||
+      !separate_rows<3>({out_strides[0], out_strides[1], out_strides[2]}, {batch, tokens, heads * group}, dim))
+    return ROSETTA_ERR_INVALID_ARG;
+  if (mask && overlaps(out, bytes(out_strides), mask,
+                       4 * (static_cast<size_t>(batch - 1) * mask_strides[0] + static_cast<size_t>(tokens - 1) * mask_strides[1] + (tokens + 31) / 32)))
+    return ROSETTA_ERR_INVALID_ARG;
+  if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
+  ClearAttentionArgs a{};
+  a.q = q;
+  a.out = out;
+  for (int i = 0; i < 3; ++i) {
+    a.q_strides[i] = q_strides[i];
+    a.out_strides[i] = out_strides[i];
+    a.cache_strides[i] = cache_strides[i];
+  }
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.page_table = page_table;
+  a.lengths = lengths;
+  a.batch = batch;
+  a.tokens = tokens;
+  a.heads = heads;
+  a.group = group;
+  a.dim = dim;
+  a.pages = pages;
+  a.page_tokens = page_tokens;
+  a.table_pitch = table_pitch;
+  a.softmax_scale = softmax_scale;
+  if (mask) {
+    a.mask = mask;
+    a.mask_strides[0] = mask_strides[0];
+    a.mask_strides[1] = mask_strides[1];
+  }
+  a.err_flag = h->d_err;
+  const cudaStream_t s = as_stream(stream);
+  cudaError_t e;
+  if (mask) {
+    e = launch_clear_attention(a, type, s);
+  } else if (attend_many_takes(a)) {
+    const int r = ensure_work(h, attend_many_bytes(a, type, h->sms), s);
+    if (r != ROSETTA_OK) return r;
+    e = launch_clear_attention_many(a, type, h->work, h->sms, s);
+  } else if (attend_few_takes(a)) {
+    const int r = ensure_work(h, attend_few_bytes(a, h->sms), s);
+    if (r != ROSETTA_OK) return r;
+    e = launch_clear_attention_few(a, type, h->work, h->sms, s);
+  } else {
+    e = launch_clear_attention(a, type, s);
+  }
+  return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -317,11 +403,7 @@ int rosetta_clear_cache_append(rosetta_clear *h, int type, const void *k, const 
   if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) ||
       !k || !v || !first || !aligned(k, size) || !aligned(v, size) || !aligned(first, 4) || 2 * heads > 65535)
     return ROSETTA_ERR_INVALID_ARG;
-  // what is written: no byte of the caches twice, keys' and values' among them
-  const int64_t apart = v_cache > k_cache ? v_cache - k_cache : k_cache - v_cache;
-  if (!separate_rows<4>({cache_strides[0], cache_strides[1], cache_strides[2], apart}, {pages, heads, page_tokens, 2}, dim) ||
-      overlaps(k_scale, 4ull * pages * heads, v_scale, 4ull * pages * heads))
-    return ROSETTA_ERR_INVALID_ARG;
+  if (!separate_caches(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens)) return ROSETTA_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
   ClearAppendArgs a{};
   a.src[0] = k;
@@ -355,61 +437,217 @@ int rosetta_clear_attention(rosetta_clear *h, int type, const void *q, const int
                             const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
                             uint32_t table_pitch, const int32_t *lengths, float softmax_scale, void *out,
                             const int64_t *out_strides, void *stream) {
-  if (!h || !known_type(type) || !q_strides || !out_strides || !good_strides(q_strides) || !good_strides(out_strides) ||
-      group < 1 || group > 128 || tokens > (1u << 24) || batch > 65535 || !isfinite(softmax_scale))
+  return run_attention(h, type, q, q_strides, batch, tokens, heads, group, dim, k_cache, v_cache, cache_strides, k_scale, v_scale, pages,
+                       page_tokens, page_table, table_pitch, lengths, nullptr, nullptr, softmax_scale, out, out_strides, stream);
+}
+
+int rosetta_clear_tree_mask(rosetta_clear *h, const int32_t *parents, int64_t parents_pitch, uint32_t batch, uint32_t tokens,
+                            uint32_t *mask, const int64_t *mask_strides, void *stream) {
+  if (!h || !mask_strides || tokens > kMostNodes || batch > 65535 || parents_pitch < 0 || parents_pitch > kMostPitch)
     return ROSETTA_ERR_INVALID_ARG;
   if (batch == 0 || tokens == 0) return ROSETTA_OK;
-  const size_t size = type_size(type);
-  if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) ||
-      !q || !out || !lengths || !aligned(q, size) || !aligned(out, size) || !aligned(lengths, 4))
+  const uint32_t words = (tokens + 31) / 32;
+  for (int i = 0; i < 2; ++i)
+    if (mask_strides[i] < 0 || mask_strides[i] > kMostPitch) return ROSETTA_ERR_INVALID_ARG;
+  if (!parents || !mask || !aligned(parents, 4) || !aligned(mask, 4) ||
+      !separate_rows<2>({mask_strides[0], mask_strides[1]}, {batch, tokens}, words))
     return ROSETTA_ERR_INVALID_ARG;
-  // (rows of q and out, over all batches: what the launches' grids count)
-  if (static_cast<double>(batch) * tokens * heads * group > 2147483000.0) return ROSETTA_ERR_INVALID_ARG;
-  const auto reach = [&](const int64_t *s) {
-    return (static_cast<size_t>(batch - 1) * s[0] + static_cast<size_t>(tokens - 1) * s[1] +
-            static_cast<size_t>(heads * group - 1) * s[2] + dim) * size;
-  };
-  if (overlaps(out, reach(out_strides), q, reach(q_strides)) ||
-      !separate_rows<3>({out_strides[0], out_strides[1], out_strides[2]}, {batch, tokens, heads * group}, dim))
+  if (overlaps(mask, 4 * (static_cast<size_t>(batch - 1) * mask_strides[0] + static_cast<size_t>(tokens - 1) * mask_strides[1] + words), parents,
+               span(parents_pitch, batch, tokens, 4)))
     return ROSETTA_ERR_INVALID_ARG;
   if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
-  ClearAttentionArgs a{};
-  a.q = q;
-  a.out = out;
-  for (int i = 0; i < 3; ++i) {
-    a.q_strides[i] = q_strides[i];
-    a.out_strides[i] = out_strides[i];
-    a.cache_strides[i] = cache_strides[i];
+  ClearTreeArgs a{};
+  a.parents = parents;
+  a.parents_pitch = parents_pitch;
+  a.mask = mask;
+  a.mask_strides[0] = mask_strides[0];
+  a.mask_strides[1] = mask_strides[1];
+  a.batch = batch;
+  a.tokens = tokens;
+  a.err_flag = h->d_err;
+  const cudaError_t e = launch_clear_tree_mask(a, as_stream(stream));
+  return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
+}
+
+int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_strides, uint32_t batch,
+                                 uint32_t tokens, uint32_t heads, uint32_t group, uint32_t dim, const int8_t *k_cache,
+                                 const int8_t *v_cache, const int64_t *cache_strides, const float *k_scale,
+                                 const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                                 uint32_t table_pitch, const int32_t *lengths, const uint32_t *mask,
+                                 const int64_t *mask_strides, float softmax_scale, void *out, const int64_t *out_strides,
+                                 void *stream) {
+  if (!mask_strides || tokens > kMostNodes || !aligned(mask, 4)) return ROSETTA_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i)
+    if (mask_strides[i] < 0 || mask_strides[i] > kMostPitch) return ROSETTA_ERR_INVALID_ARG;
+  if (batch && tokens && !mask) return ROSETTA_ERR_INVALID_ARG;
+  return run_attention(h, type, q, q_strides, batch, tokens, heads, group, dim, k_cache, v_cache, cache_strides, k_scale, v_scale, pages,
+                       page_tokens, page_table, table_pitch, lengths, mask, mask_strides, softmax_scale, out, out_strides, stream);
+}
+
+int rosetta_clear_verify(rosetta_clear *h, int type, const void *target, const int64_t *target_strides, const void *draft,
+                         const int64_t *draft_strides, const int32_t *tokens, int64_t tokens_pitch, const int32_t *parents,
+                         int64_t parents_pitch, const float *uniform, int64_t uniform_pitch, uint32_t batch, uint32_t nodes,
+                         uint32_t vocab, int32_t *path, int64_t path_pitch, int32_t *count, int32_t *next, void *stream) {
+  if (!h || !known_type(type) || !target_strides || (draft && !draft_strides) || nodes > kMostNodes || batch > 65535 || vocab < 1 ||
+      vocab > (1u << 24))
+    return ROSETTA_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i)
+    if (target_strides[i] < 0 || target_strides[i] > kMostPitch || (draft && (draft_strides[i] < 0 || draft_strides[i] > kMostPitch)))
+      return ROSETTA_ERR_INVALID_ARG;
+  for (int64_t pitch : {tokens_pitch, parents_pitch, uniform_pitch})
+    if (pitch < 0 || pitch > kMostPitch) return ROSETTA_ERR_INVALID_ARG;
+  if (!good_pitch(path_pitch, nodes)) return ROSETTA_ERR_INVALID_ARG;
+  if (batch == 0 || nodes == 0) return ROSETTA_OK;
+  const size_t size = type_size(type);
+  if (!target || !tokens || !parents || !uniform || !path || !count || !next || !aligned(target, size) || !aligned(draft, size) ||
+      !aligned(tokens, 4) || !aligned(parents, 4) || !aligned(uniform, 4) || !aligned(path, 4) || !aligned(count, 4) || !aligned(next, 4))
+    return ROSETTA_ERR_INVALID_ARG;
+  const auto rows = [&](const int64_t *s) {
+    return (static_cast<size_t>(batch - 1) * s[0] + static_cast<size_t>(nodes - 1) * s[1] + vocab) * size;
+  };
+  const struct {
+    const void *p;
+    size_t n;
+  } in[] = {{target, rows(target_strides)}, {draft, draft ? rows(draft_strides) : 0}, {tokens, span(tokens_pitch, batch, nodes, 4)},
+            {parents, span(parents_pitch, batch, nodes, 4)}, {uniform, span(uniform_pitch, batch, nodes, 4)}},
+    out[] = {{path, span(path_pitch, batch, nodes, 4)}, {count, 4ull * batch}, {next, 4ull * batch}};
+  for (int o = 0; o < 3; ++o) {
+    for (const auto &i : in)
+      if (overlaps(out[o].p, out[o].n, i.p, i.n)) return ROSETTA_ERR_INVALID_ARG;
+    for (int i = 0; i < o; ++i)
+      if (overlaps(out[o].p, out[o].n, out[i].p, out[i].n)) return ROSETTA_ERR_INVALID_ARG;
   }
-  a.k_cache = k_cache;
-  a.v_cache = v_cache;
-  a.k_scale = k_scale;
-  a.v_scale = v_scale;
+  if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
+  ClearVerifyArgs a{};
+  a.target = target;
+  a.draft = draft;
+  for (int i = 0; i < 2; ++i) {
+    a.target_strides[i] = target_strides[i];
+    a.draft_strides[i] = draft ? draft_strides[i] : 0;
+  }
+  a.tokens = tokens;
+  a.parents = parents;
+  a.uniform = uniform;
+  a.tokens_pitch = tokens_pitch;
+  a.parents_pitch = parents_pitch;
+  a.uniform_pitch = uniform_pitch;
+  a.path = path;
+  a.path_pitch = path_pitch;
+  a.count = count;
+  a.next = next;
+  a.batch = batch;
+  a.nodes = nodes;
+  a.vocab = vocab;
+  a.err_flag = h->d_err;
+  const cudaError_t e = launch_clear_verify(a, type, h->sms, as_stream(stream));
+  return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
+}
+
+int rosetta_clear_cache_keep(rosetta_clear *h, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim, int8_t *k_cache,
+                             int8_t *v_cache, const int64_t *cache_strides, float *k_scale, float *v_scale, uint32_t pages,
+                             uint32_t page_tokens, const int32_t *page_table, uint32_t table_pitch, const int32_t *first,
+                             const int32_t *path, int64_t path_pitch, const int32_t *count, void *stream) {
+  if (!h || tokens > kMostNodes || batch > 65535 || path_pitch < 0 || path_pitch > kMostPitch) return ROSETTA_ERR_INVALID_ARG;
+  if (batch == 0 || tokens == 0) return ROSETTA_OK;
+  if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) || !first ||
+      !path || !count || !aligned(first, 4) || !aligned(path, 4) || !aligned(count, 4) ||
+      !separate_caches(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens))
+    return ROSETTA_ERR_INVALID_ARG;
+  if (pages) {  // what says which rows move is not among what is written
+    const size_t nc = reach(cache_strides, pages, heads, page_tokens, dim, 1), ns = 4ull * pages * heads;
+    const struct {
+      const void *p;
+      size_t n;
+    } in[] = {{first, 4ull * batch}, {path, span(path_pitch, batch, tokens, 4)}, {count, 4ull * batch}, {page_table, 4ull * batch * table_pitch}};
+    for (const auto &i : in)
+      if (overlaps(k_cache, nc, i.p, i.n) || overlaps(v_cache, nc, i.p, i.n) || overlaps(k_scale, ns, i.p, i.n) || overlaps(v_scale, ns, i.p, i.n))
+        return ROSETTA_ERR_INVALID_ARG;
+  }
+  if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
+  ClearKeepArgs a{};
+  a.cache[0] = k_cache;
+  a.cache[1] = v_cache;
+  a.scale[0] = k_scale;
+  a.scale[1] = v_scale;
+  for (int i = 0; i < 3; ++i) a.cache_strides[i] = cache_strides[i];
   a.page_table = page_table;
-  a.lengths = lengths;
+  a.first = first;
+  a.path = path;
+  a.path_pitch = path_pitch;
+  a.count = count;
   a.batch = batch;
   a.tokens = tokens;
   a.heads = heads;
-  a.group = group;
   a.dim = dim;
   a.pages = pages;
   a.page_tokens = page_tokens;
   a.table_pitch = table_pitch;
-  a.softmax_scale = softmax_scale;
   a.err_flag = h->d_err;
-  const cudaStream_t s = as_stream(stream);
-  cudaError_t e;
-  if (attend_many_takes(a)) {
-    const int r = ensure_work(h, attend_many_bytes(a, type, h->sms), s);
-    if (r != ROSETTA_OK) return r;
-    e = launch_clear_attention_many(a, type, h->work, h->sms, s);
-  } else if (attend_few_takes(a)) {
-    const int r = ensure_work(h, attend_few_bytes(a, h->sms), s);
-    if (r != ROSETTA_OK) return r;
-    e = launch_clear_attention_few(a, type, h->work, h->sms, s);
-  } else {
-    e = launch_clear_attention(a, type, s);
+  const cudaError_t e = launch_clear_keep(a, as_stream(stream));
+  return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
+}
+
+int rosetta_clear_cache_read(rosetta_clear *h, int type, uint32_t batch, uint32_t tokens, uint32_t heads, uint32_t dim,
+                             const int8_t *k_cache, const int8_t *v_cache, const int64_t *cache_strides, const float *k_scale,
+                             const float *v_scale, uint32_t pages, uint32_t page_tokens, const int32_t *page_table,
+                             uint32_t table_pitch, const int32_t *first, const int32_t *lengths, void *k, const int64_t *k_strides,
+                             void *v, const int64_t *v_strides, void *stream) {
+  if (!h || !known_type(type) || !k_strides || !v_strides || !good_strides(k_strides) || !good_strides(v_strides) || tokens > (1u << 24) ||
+      batch > 65535)
+    return ROSETTA_ERR_INVALID_ARG;
+  if (batch == 0 || tokens == 0) return ROSETTA_OK;
+  const size_t size = type_size(type);
+  if (!good_cache(k_cache, v_cache, cache_strides, k_scale, v_scale, heads, dim, pages, page_tokens, page_table, table_pitch) || !k || !v ||
+      !first || !lengths || !aligned(k, size) || !aligned(v, size) || !aligned(first, 4) || !aligned(lengths, 4))
+    return ROSETTA_ERR_INVALID_ARG;
+  // what is written: no element twice, keys' and values' (slices of one buffer) among them, and nothing that is read
+  const size_t nk = reach(k_strides, batch, tokens, heads, dim, size), nv = reach(v_strides, batch, tokens, heads, dim, size);
+  if (!separate_rows<3>({k_strides[0], k_strides[1], k_strides[2]}, {batch, tokens, heads}, dim) ||
+      !separate_rows<3>({v_strides[0], v_strides[1], v_strides[2]}, {batch, tokens, heads}, dim))
+    return ROSETTA_ERR_INVALID_ARG;
+  if (overlaps(k, nk, v, nv)) {
+    const int64_t apart = k < v ? static_cast<char *>(v) - static_cast<char *>(k) : static_cast<char *>(k) - static_cast<char *>(v);
+    for (int i = 0; i < 3; ++i)
+      if (k_strides[i] != v_strides[i]) return ROSETTA_ERR_INVALID_ARG;
+    if (apart % size ||
+        !separate_rows<4>({k_strides[0], k_strides[1], k_strides[2], static_cast<int64_t>(apart / size)}, {batch, tokens, heads, 2}, dim))
+      return ROSETTA_ERR_INVALID_ARG;
   }
+  if (pages) {
+    const size_t nc = reach(cache_strides, pages, heads, page_tokens, dim, 1), ns = 4ull * pages * heads;
+    const struct {
+      const void *p;
+      size_t n;
+    } in[] = {{k_cache, nc}, {v_cache, nc}, {k_scale, ns}, {v_scale, ns}, {page_table, 4ull * batch * table_pitch}, {first, 4ull * batch},
+              {lengths, 4ull * batch}};
+    for (const auto &i : in)
+      if (overlaps(k, nk, i.p, i.n) || overlaps(v, nv, i.p, i.n)) return ROSETTA_ERR_INVALID_ARG;
+  }
+  if (cudaSetDevice(h->device) != cudaSuccess) return ROSETTA_ERR_CUDA;
+  ClearReadArgs a{};
+  a.cache[0] = k_cache;
+  a.cache[1] = v_cache;
+  a.scale[0] = k_scale;
+  a.scale[1] = v_scale;
+  a.out[0] = k;
+  a.out[1] = v;
+  for (int i = 0; i < 3; ++i) {
+    a.cache_strides[i] = cache_strides[i];
+    a.out_strides[0][i] = k_strides[i];
+    a.out_strides[1][i] = v_strides[i];
+  }
+  a.page_table = page_table;
+  a.first = first;
+  a.lengths = lengths;
+  a.batch = batch;
+  a.tokens = tokens;
+  a.heads = heads;
+  a.dim = dim;
+  a.pages = pages;
+  a.page_tokens = page_tokens;
+  a.table_pitch = table_pitch;
+  a.err_flag = h->d_err;
+  const cudaError_t e = launch_clear_read(a, type, as_stream(stream));
   return e == cudaSuccess ? ROSETTA_OK : cuda_fail(e);
 }
 

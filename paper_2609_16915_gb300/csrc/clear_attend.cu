@@ -36,7 +36,9 @@ __global__ void __launch_bounds__(32 * kRowWarps) attend_row_kernel(const ClearA
     if (lane == 0) atomicMax(a.err_flag, 1u);
     len = most;
   }
-  const int64_t last = len - a.tokens + t;  // the last position this row sees
+  const int64_t context = len - a.tokens;               // under a mask every row sees the positions before, and bit j's after
+  const int64_t last = a.mask ? len - 1 : context + t;  // the last position this row sees
+  const uint32_t *mask = a.mask ? a.mask + static_cast<int64_t>(b) * a.mask_strides[0] + static_cast<int64_t>(t) * a.mask_strides[1] : nullptr;
   const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] + static_cast<int64_t>(t) * a.q_strides[1] +
                static_cast<int64_t>(head) * a.q_strides[2];
   for (uint32_t d = lane; d < a.dim; d += 32) qs[warp][d] = to_float(q[d]) * (a.softmax_scale * kLog2e);
@@ -47,7 +49,9 @@ __global__ void __launch_bounds__(32 * kRowWarps) attend_row_kernel(const ClearA
     const int64_t p = p0 + lane;
     float s = -__int_as_float(0x7f800000), vs = 0.0f;
     int64_t at = -1;
-    if (p <= last) {
+    bool seen = p <= last;
+    if (mask && seen && p >= context) seen = (mask[(p - context) / 32] >> ((p - context) % 32) & 1u) != 0u;
+    if (seen) {
       const int32_t page = table[p / a.page_tokens];
       if (page < 0 || static_cast<uint32_t>(page) >= a.pages) {
         atomicMax(a.err_flag, 1u);
