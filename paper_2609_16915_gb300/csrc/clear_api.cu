@@ -238,9 +238,7 @@ int run_attention(rosetta_clear *h, int type, const void *q, const int64_t *q_st
   a.err_flag = h->d_err;
   const cudaStream_t s = as_stream(stream);
   cudaError_t e;
-  if (mask) {
-    e = launch_clear_attention(a, type, s);
-  } else if (attend_many_takes(a)) {
+  if (attend_many_takes(a)) {
     const int r = ensure_work(h, attend_many_bytes(a, type, h->sms), s);
     if (r != ROSETTA_OK) return r;
     e = launch_clear_attention_many(a, type, h->work, h->sms, s);

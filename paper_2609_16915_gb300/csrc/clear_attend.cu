@@ -5,6 +5,8 @@
 //   m' = max(m, s),  l' = l 2^(m - m') + 2^(s - m'),  o' = o 2^(m - m') + 2^(s - m') V
 // (scores s in units of log 2).
 //
+// Under the mask of a tree of drafted tokens a row sees the positions before them, and of them the mask's bits.
+//
 // This kernel takes every head size: a warp per query row, 32 positions at a time, a
 // lane computing one position's score, then each lane summing its share of the
 // head's dimensions over the 32 positions.  Every row reads all its keys and values again, and multiplies outside the

@@ -52,10 +52,18 @@ __device__ __forceinline__ uint32_t split_share(const AttendArgs &f, uint32_t en
   return ((share < f.least ? f.least : share) + 63) / 64 * 64;
 }
 
-// Positions that the rows of a group see at most: up to the last token of the group.
+// Positions that the rows of a group see at most: up to the last token of the group; under a mask all of them.
 __device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64_t len, uint32_t last_row) {
-  const int64_t end = len - a.tokens + 1 + last_row / a.group;
+  const int64_t end = a.mask ? len : len - a.tokens + 1 + last_row / a.group;
   return end > 0 ? static_cast<uint32_t>(end) : 0u;
+}
+
+// Word `i` of a mask row, its bits from a position of the drafted ones on: before them (i < 0) all are seen, behind them none.
+__device__ __forceinline__ uint32_t mask_word(const uint32_t *row, uint32_t tokens, int32_t i) {
+  if (i < 0) return ~0u;
+  const uint32_t from = static_cast<uint32_t>(i) * 32;
+  if (from >= tokens) return 0u;
+  return tokens - from < 32 ? row[i] & ((1u << (tokens - from)) - 1u) : row[i];
 }
 
 // Join the splits of every row; group_rows: rows that one block's ranges were laid out for.

@@ -85,7 +85,8 @@ __device__ __forceinline__ int64_t length_of(const ClearAttentionArgs &a, uint32
   return len > most ? most : len;
 }
 
-template <typename T, int DP, int NB>
+// TREE: under a mask.  A row sees every position before the drafted ones, and of those the bits of its own row of the mask.
+template <typename T, int DP, int NB, bool TREE>
 __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) attend_few_kernel(const AttendArgs f) {
   using F = Few<DP>;
   constexpr bool SPLIT = sizeof(T) == 4;     // queries and weights in two halves
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   __shared__ int64_t s_at[kSegment];  // where the tiles lie in the caches
   __shared__ float s_ks[kSegment], s_vs[kSegment];
   __shared__ int32_t s_top[kWarps];
+  __shared__ uint32_t s_mask[TREE ? 8 * NB : 1][33];  // the rows' words (up to 32)
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const uint32_t split = blockIdx.x % f.splits, group = blockIdx.x / f.splits % f.groups;
   const uint32_t own_head = blockIdx.x / f.splits / f.groups, bh = f.first + own_head, kh = bh % a.heads, b = bh / a.heads;
@@ -139,6 +141,15 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   // of a lane's copies of a tile: place in the first, way on to the next (zero where it reads nothing)
   const uint32_t lane_at = inside ? lane / CH * row_step + lane % CH * 16 : 0, lane_on = inside ? 512 / DP * row_step : 0;
   int32_t whole = 0x7fffffff;  // the last position that every row sees
+  if constexpr (TREE) {
+    if (static_cast<int64_t>(hi) > len - a.tokens) {  // (the block meets before it uses them)
+      const uint32_t words = (a.tokens + 31) / 32;
+      for (uint32_t i = threadIdx.x; i < 8 * NB * words; i += blockDim.x) {
+        const uint32_t r = row0 + i / words;
+        s_mask[i / words][i % words] = r < rows ? a.mask[static_cast<int64_t>(b) * a.mask_strides[0] + static_cast<int64_t>(r / a.group) * a.mask_strides[1] + i % words] : 0u;
+      }
+    }
+  }
   for (uint32_t seg = lo / 16; seg < tiles_hi; seg += kSegment) {
     const uint32_t count = min(kSegment, tiles_hi - seg);
     __syncthreads();
@@ -278,7 +289,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         for (int i = 0; i < 2; ++i) {
           factor[n][i] = __shfl_sync(0xffffffffu, up, (2 * t + i) * 4) * (a.softmax_scale * kLog2e);
           const uint32_t r = row0 + n * 8 + 2 * t + i;
-          last[n][i] = r < rows ? static_cast<int32_t>(len - a.tokens + r / a.group) : -1;
+          last[n][i] = r < rows ? static_cast<int32_t>(TREE ? len - a.tokens - 1 : len - a.tokens + r / a.group) : -1;
         }
       }
 #pragma unroll
@@ -329,7 +340,11 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
         for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
+            bool seen = in && p0 + e / 2 * 8 <= last[n][e % 2];
+            if constexpr (TREE) {
+              const int32_t j = p0 + e / 2 * 8 - static_cast<int32_t>(len - a.tokens);  // (of rows past the last no more than zeros)
+              if (in && j >= 0 && j < static_cast<int32_t>(a.tokens)) seen = (s_mask[n * 8 + 2 * t + e % 2][j / 32] >> (j % 32) & 1u) != 0u;
+            }
             s[n][e] = seen ? s[n][e] * (ks * factor[n][e % 2]) : neg_inf();
             raise |= s[n][e] > m[n][e % 2] + limit;
           }
@@ -603,9 +618,9 @@ void split(AttendArgs *f, uint32_t sms) {
 
 uint32_t group_rows_of(const ClearAttentionArgs &a) { return a.tokens * a.group <= 8 ? 8 : 16; }
 
-template <typename T, int DP, int NB>
+template <typename T, int DP, int NB, bool TREE>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = attend_few_kernel<T, DP, NB>;
+  auto kern = attend_few_kernel<T, DP, NB, TREE>;
   constexpr uint32_t join = (kWarps * 8 * (DP + 4) + kWarps * 8 * 2) * 4;
   constexpr uint32_t smem = Few<DP>::RING > join ? Few<DP>::RING : join;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
@@ -616,7 +631,8 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  return group_rows_of(f.a) == 8 ? launch<T, DP, 1>(f, s) : launch<T, DP, 2>(f, s);
+  if (f.a.mask) return group_rows_of(f.a) == 8 ? launch<T, DP, 1, true>(f, s) : launch<T, DP, 2, true>(f, s);
+  return group_rows_of(f.a) == 8 ? launch<T, DP, 1, false>(f, s) : launch<T, DP, 2, false>(f, s);
 }
 
 template <typename T>

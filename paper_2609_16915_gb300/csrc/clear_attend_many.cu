@@ -182,7 +182,8 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
 }
 
 // RUNS: a block's range may be longer than one accumulator takes.  (A kernel of its own: its registers cost shorter ranges 3 %.)
-template <typename T, int DP, bool RUNS>
+// TREE: under a mask.  A row sees every position before the drafted ones, and of those the bits of its own row of the mask.
+template <typename T, int DP, bool RUNS, bool TREE>
 __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
@@ -418,7 +419,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     if (lane == 0) mbar_arrive(bar(QFULL));
     asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
-    const int32_t last = row < rows ? static_cast<int32_t>(len - a.tokens + row / a.group) : -1;
+    // (TREE: of the context; rows past the last see nothing)
+    const int32_t last = row >= rows ? (TREE ? -(1 << 30) - 1 : -1) : static_cast<int32_t>(TREE ? len - a.tokens - 1 : len - a.tokens + row / a.group);
+    const uint32_t *mask = TREE ? a.mask + static_cast<int64_t>(b) * a.mask_strides[0] + static_cast<int64_t>(min(row, rows - 1) / a.group) * a.mask_strides[1] : nullptr;
     const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
     // (SPLIT: behind O the products of the weights' second halves, in the other row tile's place of the scores the sum of the
     // tiles up to the last fold)
@@ -455,6 +458,13 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     if (r < row_tiles) {
       for (uint32_t j = 0; j < n; ++j) {
         const uint32_t buf = j % 8, two = r * 2 + j % 2, s_tile = tmem + lanes + two * POS;
+        // (the same for the warp)
+        const uint32_t first = start + j * POS + half * COLS;  // this half's first position
+        uint32_t bits = 0;                                     // TREE: of its 32 positions, those that the row sees
+        if constexpr (TREE) {
+          const int32_t from = static_cast<int32_t>(first) - last - 1;  // among the drafted ones
+          bits = __funnelshift_r(mask_word(mask, a.tokens, from >> 5), mask_word(mask, a.tokens, (from >> 5) + 1), from & 31);
+        }
         if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (j / 2) & 1u))) {
           leave();
           goto done;
@@ -462,8 +472,6 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_after();
         float v[COLS];
         tmem_ld32(s_tile + half * COLS, v);
-        // (the same for the warp)
-        const uint32_t first = start + j * POS + half * COLS;  // this half's first position
         const bool part = __any_sync(0xffffffffu, (s_skip[buf][half * 2] | s_skip[buf][half * 2 + 1]) != 0 ||
                                                       static_cast<int32_t>(first + COLS - 1) > last);
         float kf[2] = {s_ks[buf][half * 2] * factor, s_ks[buf][half * 2 + 1] * factor};
@@ -477,7 +485,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             float t = neg_inf();
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
-              const bool in = static_cast<int32_t>(first + i * 16 + e) <= last && !out;
+              const bool in = (TREE ? (bits >> (i * 16 + e) & 1u) != 0u : static_cast<int32_t>(first + i * 16 + e) <= last) && !out;
               v[i * 16 + e] = in ? v[i * 16 + e] * kf[i] : neg_inf();
               t = fmaxf(t, v[i * 16 + e]);
             }
@@ -974,7 +982,8 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = f.runs ? attend_many_kernel<T, DP, true> : attend_many_kernel<T, DP, false>;
+  auto kern = f.runs ? attend_many_kernel<T, DP, true, false> : attend_many_kernel<T, DP, false, false>;
+  if (f.a.mask) kern = f.runs ? attend_many_kernel<T, DP, true, true> : attend_many_kernel<T, DP, false, true>;
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
   kern<<<f.count * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
