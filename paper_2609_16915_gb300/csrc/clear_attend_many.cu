@@ -183,11 +183,15 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool v
 
 // RUNS: a block's range may be longer than one accumulator takes.  (A kernel of its own: its registers cost shorter ranges 3 %.)
 // TREE: under a mask.  A row sees every position before the drafted ones, and of those the bits of its own row of the mask.
-template <typename T, int DP, bool RUNS, bool TREE>
+// PAIR: the rows fill one row tile, and the two groups of softmax warps take turns at the positions, each with scores and outputs of its
+// own (chain r: tiles r, r + 2 ..), which are joined at the end.
+template <typename T, int DP, bool RUNS, bool TREE, bool PAIR>
 __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
   constexpr bool SPLIT = kSplit<T>, FINE = kFine<T>;
+  static_assert(!PAIR || (TREE && !RUNS && !SPLIT), "pairs: of 16-bit types, one accumulator a range");
+  constexpr uint32_t AHEAD = PAIR ? 4 : 2;  // tiles scored ahead of the weights that meet their values
   constexpr uint32_t SOFT_WARPS = kSoftWarps<T>, WARPS = kWarps<T>;
   constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
   const auto tile_of = [](uint32_t j) { return RUNS ? j % RUN : j; };  // of a run
@@ -241,7 +245,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   const bool alone = all <= share;
   if (split > 0 && start >= all) return;
   const uint32_t n = (end - start + POS - 1) / POS;
-  const uint32_t row_tiles = !SPLIT && rows - row0 > ROWS ? 2 : 1;
+  const uint32_t row_tiles = PAIR || (!SPLIT && rows - row0 > ROWS) ? 2 : 1;
+  const auto tiles_of = [&](uint32_t r) { return PAIR ? (n + 1 - r) / 2 : n; };  // of a row tile, or chain
   const int32_t *table = a.page_table + static_cast<size_t>(b) * a.table_pitch;
 
   if (n == 0) {  // no row of the block has a position: zeros
@@ -290,7 +295,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 
   if (warp < SOFT_WARPS) {
     // row tile, half of the columns, row: two threads a row, in warps that share a quarter of tensor memory
-    const uint32_t r = warp / 8, half = warp / 4 % 2, row_in = (warp % 4) * 32 + lane, row = row0 + r * ROWS + row_in;
+    const uint32_t r = warp / 8, half = warp / 4 % 2, row_in = (warp % 4) * 32 + lane, row = row0 + (PAIR ? 0 : r * ROWS) + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
     // The two warps of a row meet at barrier 3 + pair.  A warp whose wait gave up meets the other once more and says
     // at which meeting, so that neither waits for one that has left.
@@ -307,7 +312,12 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       return any != 0u;
     };
     const auto other_left = [&]() { return *const_cast<volatile uint32_t *>(&s_quit[pair]) == meetings; };
+    // (PAIR: at barrier 13 all softmax warps meet once, those that leave among them, without waiting)
+    const auto pass = [&]() {
+      if constexpr (PAIR) asm volatile("bar.arrive 13, 512;" ::: "memory");
+    };
     const auto leave = [&]() {
+      pass();
       give_up();
       s_quit[pair] = meetings + 1;
       meet(false);
@@ -365,7 +375,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       uint4 raw[2][DP / 32];
 #pragma unroll
       for (uint32_t g = 0; g < 2; ++g) {
-        const uint32_t rw = row0 + r * ROWS + (warp % 8) * 16 + g * 8 + qr;
+        const uint32_t rw = row0 + (PAIR ? r * rows : r * ROWS) + (warp % 8) * 16 + g * 8 + qr;  // (PAIR: chain 0 loads them)
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
 #pragma unroll
@@ -403,7 +413,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
         const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -126), 126);
         const float down = copysignf(__int_as_float((127 - ex) << 23), a.softmax_scale);
+        if (PAIR && r == 1) continue;
         if (qc == 0) s_up[r * ROWS + in_tile] = __int_as_float((127 + ex) << 23);
+        if (PAIR && qc == 0) s_up[ROWS + in_tile] = __int_as_float((127 + ex) << 23);
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
           uint32_t w[4];
@@ -417,10 +429,13 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     fence_async();
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(QFULL));
-    asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
+    if constexpr (PAIR)
+      asm volatile("bar.sync 11, 512;" ::: "memory");  // s_up of the rows
+    else
+      asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
-    // (TREE: of the context; rows past the last see nothing)
-    const int32_t last = row >= rows ? (TREE ? -(1 << 30) - 1 : -1) : static_cast<int32_t>(TREE ? len - a.tokens - 1 : len - a.tokens + row / a.group);
+    // (TREE: of the context; rows past the last, of queries of zeros, see everything: a warp with some of them takes the short way)
+    const int32_t last = row >= rows ? (TREE ? 1 << 30 : -1) : static_cast<int32_t>(TREE ? len - a.tokens - 1 : len - a.tokens + row / a.group);
     const uint32_t *mask = TREE ? a.mask + static_cast<int64_t>(b) * a.mask_strides[0] + static_cast<int64_t>(min(row, rows - 1) / a.group) * a.mask_strides[1] : nullptr;
     const uint32_t o_col = tmem + lanes + M::O_COL + r * DP + half * (DP / 2);
     // (SPLIT: behind O the products of the weights' second halves, in the other row tile's place of the scores the sum of the
@@ -455,9 +470,22 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         o[e] += fade * x.x, o[e + 1] += fade * x.y, o[e + 2] += fade * x.z, o[e + 3] += fade * x.w;
       }
     };
-    if (r < row_tiles) {
-      for (uint32_t j = 0; j < n; ++j) {
-        const uint32_t buf = j % 8, two = r * 2 + j % 2, s_tile = tmem + lanes + two * POS;
+    const uint32_t own_tiles = tiles_of(r);
+    if (TREE && r < row_tiles && row - lane >= rows) {  // no row of the warp is any: its scores are zeros, and so its weights
+      for (uint32_t i = 0; i < own_tiles; ++i) {
+        const uint32_t two = r * 2 + i % 2;
+        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (i / 2) & 1u))) {
+          pass();
+          give_up();
+          goto done;
+        }
+        if (lane == 0) mbar_arrive(bar(PFULL + two));
+      }
+      pass();
+    } else if (r < row_tiles) {
+      for (uint32_t i = 0; i < own_tiles; ++i) {
+        const uint32_t j = PAIR ? 2 * i + r : i;
+        const uint32_t buf = j % 8, two = r * 2 + i % 2, s_tile = tmem + lanes + two * POS;
         // (the same for the warp)
         const uint32_t first = start + j * POS + half * COLS;  // this half's first position
         uint32_t bits = 0;                                     // TREE: of its 32 positions, those that the row sees
@@ -465,7 +493,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           const int32_t from = static_cast<int32_t>(first) - last - 1;  // among the drafted ones
           bits = __funnelshift_r(mask_word(mask, a.tokens, from >> 5), mask_word(mask, a.tokens, (from >> 5) + 1), from & 31);
         }
-        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (j / 2) & 1u))) {
+        if (!__all_sync(0xffffffffu, wait_quick(bar(SFULL + two), (i / 2) & 1u))) {
           leave();
           goto done;
         }
@@ -502,13 +530,19 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
         const bool raise = meet(top > m + kRaise);
-        if (other_left()) goto done;
+        if (other_left()) {
+          pass();
+          goto done;
+        }
         const bool fold = SPLIT && j > 0 && j % FOLD == 0, run = RUNS && j > 0 && j % RUN == 0;
         float keep = 1.0f;
         if (raise) {
           s_max[half][r * ROWS + row_in] = top;
           meet(false);
-          if (other_left()) goto done;
+          if (other_left()) {
+          pass();
+          goto done;
+        }
           const float raised = fmaxf(fmaxf(m, top), s_max[half ^ 1u][r * ROWS + row_in]);
           keep = m == neg_inf() ? 0.0f : ex2(m - raised);
           m = raised;
@@ -540,10 +574,10 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         if constexpr (FINE) tmem_st16(s_tile + POS / 2 + half * (COLS / 2), rest);
         const float2 added = floats_of(add2(sum[0], sum[1]));
         l += added.x + added.y;
-        if (j > 0 && (raise || fold || run)) {
-          // O with the weights of tile j - 1: done before the scores of tile j + 1, where there is one
-          const uint32_t next = r * 2 + (j + 1) % 2;
-          if (!__all_sync(0xffffffffu, j + 1 < n ? wait_quick(bar(SFULL + next), ((j + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
+        if (i > 0 && (raise || fold || run)) {
+          // O with the weights of tile i - 1: done before the scores of tile i + 1, where there is one
+          const uint32_t next = r * 2 + (i + 1) % 2;
+          if (!__all_sync(0xffffffffu, i + 1 < own_tiles ? wait_quick(bar(SFULL + next), ((i + 1) / 2) & 1u) : wait_quick(bar(BEFORE + r), 0))) {
             leave();
             goto done;
           }
@@ -601,7 +635,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           l = 0.0f;
         }
       }
-      if (!__all_sync(0xffffffffu, wait_quick(bar(LAST + r), 0))) {
+      // (PAIR: chain 1 writes to where keys and values were)
+      if (!__all_sync(0xffffffffu, (own_tiles == 0 || wait_quick(bar(LAST + r), 0)) && (!PAIR || r == 0 || wait_quick(bar(LAST), 0)))) {
         leave();
         goto done;
       }
@@ -611,8 +646,48 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       if (runs) l += run_l * fade;
       s_max[half][r * ROWS + row_in] = l;
       meet(false);
-      if (other_left()) goto done;
+      if (other_left()) {
+          pass();
+          goto done;
+        }
       l += s_max[half ^ 1u][r * ROWS + row_in];
+      constexpr uint32_t PITCH = DP + 4;
+      float *joined = reinterpret_cast<float *>(smem + M::K_AT) + row_in * PITCH + half * (DP / 2);
+      float2 *s_other = reinterpret_cast<float2 *>(smem + M::K_AT + ROWS * PITCH * 4);  // chain 1's sum and maximum
+      static_assert(ROWS * (PITCH * 4 + 8) <= RING * (M::K_TILE + M::V_TILE), "outputs of a row tile fit where keys and values were");
+      float own_part = 1.0f, other_part = 0.0f;
+      if constexpr (PAIR) {
+        if (r == 1) {
+          if (half == 0) s_other[row_in] = make_float2(l, m);
+#pragma unroll 1
+          for (uint32_t c = 0; c < DP / 2 && own_tiles != 0; c += 16) {
+            float o[16];
+            read_all(c, false, o);
+#pragma unroll
+            for (uint32_t e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(joined + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+          pass();
+          goto done;
+        }
+        asm volatile("bar.sync 13, 512;" ::: "memory");
+        const float2 other = s_other[row_in];
+        const float top = fmaxf(m, other.y);
+        own_part = m == neg_inf() ? 0.0f : ex2(m - top);
+        other_part = other.y == neg_inf() ? 0.0f : ex2(other.y - top);
+        // (a NaN sum under m = -inf stays)
+        l = (m == neg_inf() ? l : l * own_part) + (other.y == neg_inf() ? other.x : other.x * other_part);
+        m = top;
+      }
+      const auto add_other = [&](uint32_t c, float (&o)[16]) {
+        if constexpr (PAIR) {
+#pragma unroll
+          for (uint32_t e = 0; e < 16; e += 4) {
+            const float4 x = n > 1 ? *reinterpret_cast<const float4 *>(joined + c + e) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            o[e] = o[e] * own_part + x.x * other_part, o[e + 1] = o[e + 1] * own_part + x.y * other_part;
+            o[e + 2] = o[e + 2] * own_part + x.z * other_part, o[e + 3] = o[e + 3] * own_part + x.w * other_part;
+          }
+        }
+      };
       T *out = static_cast<T *>(a.out) + static_cast<int64_t>(b) * a.out_strides[0] + static_cast<int64_t>(row / a.group) * a.out_strides[1] +
                static_cast<int64_t>(kh * a.group + row % a.group) * a.out_strides[2];
       const bool wide = (reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>((a.out_strides[0] | a.out_strides[1] | a.out_strides[2]) * sizeof(T))) % 16 == 0;
@@ -633,6 +708,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             float o[16];
             read_all(c + h, tile_of(n - 1) >= FOLD, o);
             if (runs) add_runs(c + h, fade, o);
+            add_other(c + h, o);
 #pragma unroll
             for (uint32_t e = 0; e < 16; e += PIECE) {
               alignas(16) E x[PIECE];
@@ -663,6 +739,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           float o[16];
           read_all(c, tile_of(n - 1) >= FOLD, o);
           if (runs) add_runs(c, fade, o);
+          add_other(c, o);
           const uint32_t d0 = half * (DP / 2) + c;
           if (row >= rows || d0 >= a.dim) continue;
 #pragma unroll
@@ -755,9 +832,11 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           uint4 k[DP / 32];
 #pragma unroll
           for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
-          // the keys that lay here were tile j - 3's, used with tile j - 5's values, or among the first two
-          if (j >= RING && !__all_sync(0xffffffffu, j >= 5 ? wait_quick(bar(USED + (j - 5) % RING), ((j - 5) / RING) & 1u)
-                                                           : wait_quick(bar(FIRST), 0))) {
+          // the keys that lay here were tile j - 3's, used with tile j - 5's values (PAIR: j - 7's; the fourth tile's before the first values'),
+          // or among the first two (three)
+          const uint32_t with = PAIR && j == 6 ? 0 : j - RING - AHEAD;
+          if (j >= RING && !__all_sync(0xffffffffu, j >= RING + AHEAD || (PAIR && j == 6) ? wait_quick(bar(USED + with % RING), (with / RING) & 1u)
+                                                                                        : wait_quick(bar(FIRST), 0))) {
             give_up();
             goto done;
           }
@@ -861,9 +940,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     // ---- products ----
     const uint32_t elect = elected();
     const auto ready = [&](uint32_t i, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar(i), parity)); };
-    const auto scores = [&](uint32_t r, uint32_t j, uint32_t kbuf) {
-      const uint32_t two = r * 2 + j % 2;
-      const uint64_t qd = desc_of(base + r * M::Q_TILE, DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
+    const auto scores = [&](uint32_t r, uint32_t i, uint32_t kbuf) {  // of the row tile's, or the chain's, tile i
+      const uint32_t two = r * 2 + i % 2;
+      const uint64_t qd = desc_of(base + (PAIR ? 0 : r * M::Q_TILE), DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
       if constexpr (SPLIT) {  // (the small products first: less is cut off)
         const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
 #pragma unroll
@@ -879,44 +958,49 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       give_up();
       goto done;
     }
-    for (uint32_t j = 0; j < 2 && j < n; ++j) {
-      if (!ready(KFULL + j, 0)) {
+    constexpr uint32_t AT_FIRST = PAIR ? 3 : 2;  // tiles scored before the first commit (PAIR: the fourth's keys lie where the first's did)
+    for (uint32_t j = 0; j < AHEAD && j < n; ++j) {
+      if (j == AT_FIRST) commit(bar(FIRST), elect);
+      if (!ready(KFULL + j % RING, (j / RING) & 1u)) {
         give_up();
         goto done;
       }
       fence_after();
-      for (uint32_t r = 0; r < row_tiles; ++r) scores(r, j, j);
+      if constexpr (PAIR)
+        scores(j % 2, j / 2, j % RING);
+      else
+        for (uint32_t r = 0; r < row_tiles; ++r) scores(r, j, j);
     }
-    commit(bar(FIRST), elect);
-    uint32_t vbuf = 0, kbuf = 2, vpar = 0, kpar = 0;
+    if (AT_FIRST == AHEAD || n <= AT_FIRST) commit(bar(FIRST), elect);
+    uint32_t vbuf = 0, kbuf = AHEAD % RING, vpar = 0, kpar = (AHEAD / RING) & 1u;
     for (uint32_t j = 0; j < n; ++j) {
-      if (!ready(VFULL + vbuf, vpar) || (j + 2 < n && !ready(KFULL + kbuf, kpar))) {
+      if (!ready(VFULL + vbuf, vpar) || (j + AHEAD < n && !ready(KFULL + kbuf, kpar))) {
         give_up();
         goto done;
       }
       const uint64_t vd = desc_of(base + M::V_AT + vbuf * M::V_TILE, V_GROUP);
 #pragma unroll
-      for (uint32_t r = 0; r < 2; ++r) {
-        if (r >= row_tiles) break;
-        const uint32_t two = r * 2 + j % 2;
-        if (!ready(PFULL + two, (j / 2) & 1u)) {
+      for (uint32_t each = 0; each < (PAIR ? 1 : 2); ++each) {
+        if (each >= row_tiles) break;
+        const uint32_t r = PAIR ? j % 2 : each, i = PAIR ? j / 2 : j, two = r * 2 + i % 2;
+        if (!ready(PFULL + two, (i / 2) & 1u)) {
           give_up();
           goto done;
         }
         fence_after();
 #pragma unroll
         for (uint32_t k = 0; k < POS / 16; ++k)
-          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : tile_of(j)) | k) != 0, elect);
+          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : tile_of(i)) | k) != 0, elect);
         if constexpr (FINE) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
             mma_ts(tmem + M::O_COL + (SPLIT ? DP : r * DP), tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), !SPLIT || (j % FOLD | k) != 0,
                      elect);
         }
-        if (j + 2 < n)
-          scores(r, j + 2, kbuf);
+        if (j + AHEAD < n)
+          scores(r, i + 2, kbuf);
         else
-          commit(bar((j + 1 == n ? LAST : BEFORE) + r), elect);
+          commit(bar((i + 1 == tiles_of(r) ? LAST : BEFORE) + r), elect);
       }
       commit(bar(USED + vbuf), elect);
       if (++vbuf == RING) {
@@ -931,7 +1015,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     // no commit arrives after the block's end: each barrier's last one (the softmax waits for SFULL)
     bool ok = ready(FIRST, 0);
     for (uint32_t j = n > RING ? n - RING : 0; j < n; ++j) ok = ready(USED + j % RING, (j / RING) & 1u) && ok;
-    for (uint32_t r = 0; r < row_tiles; ++r) ok = ready(LAST + r, 0) && (n == 1 || ready(BEFORE + r, 0)) && ok;
+    for (uint32_t r = 0; r < row_tiles; ++r) ok = (tiles_of(r) < 1 || ready(LAST + r, 0)) && (tiles_of(r) < 2 || ready(BEFORE + r, 0)) && ok;
     if (!ok) give_up();
   }
 done:
@@ -982,8 +1066,13 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = f.runs ? attend_many_kernel<T, DP, true, false> : attend_many_kernel<T, DP, false, false>;
-  if (f.a.mask) kern = f.runs ? attend_many_kernel<T, DP, true, true> : attend_many_kernel<T, DP, false, true>;
+  auto kern = f.runs ? attend_many_kernel<T, DP, true, false, false> : attend_many_kernel<T, DP, false, false, false>;
+  if (f.a.mask) {
+    kern = f.runs ? attend_many_kernel<T, DP, true, true, false> : attend_many_kernel<T, DP, false, true, false>;
+    if constexpr (!kSplit<T>) {
+      if (!f.runs && f.a.tokens * f.a.group <= ROWS) kern = attend_many_kernel<T, DP, false, true, true>;
+    }
+  }
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
   kern<<<f.count * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
