@@ -18,13 +18,14 @@
 
 #include "clear.h"
 #include "dsmem.cuh"
+#include "pairs.cuh"
 
 namespace rosetta {
 
 namespace {
 
 constexpr uint64_t kOne = 1ull << 56, kMost = 1ull << 62;  // sums stay at kMost: no probabilities
-constexpr uint32_t kThreads = 512, kWarps = kThreads / 32;
+constexpr uint32_t kMostThreads = 512, kMostWarps = kMostThreads / 32;
 
 __global__ void __launch_bounds__(256) tree_mask_kernel(const ClearTreeArgs a) {
   extern __shared__ int32_t up[];
@@ -58,11 +59,32 @@ __device__ __forceinline__ uint64_t times(uint64_t a, uint64_t b) { return __umu
 
 __device__ __forceinline__ uint64_t less(uint64_t a, uint64_t b) { return a > b ? a - b : 0; }
 
-// a probability in units of 2^-56; what is none counts as zero
-__device__ __forceinline__ uint64_t fixed(float p, bool &bad) {
+// A probability p in [0, 2] as whole multiples of 2^-56, from additions that round to a grid each: p + 4 in the last bits of its word has
+// p to 2^-21, what is left over (exact) plus 1.5 x 2^-21 has it to 2^-44, and what is left of that plus 1.5 x 2^-33 to 2^-56.  (Converting
+// to 64-bit integers instead: 33 MB of rows 35 us.)
+constexpr float kGrid1 = 4.0f, kGrid2 = 1.5f / 2097152.0f, kGrid3 = 1.5f / 8589934592.0f;
+__device__ __forceinline__ uint64_t joined(uint32_t s1, uint32_t s2, uint32_t s3) {  // of sums of the words' differences to the grids'
+  return (static_cast<uint64_t>(s1) << 35) + static_cast<uint64_t>(static_cast<int64_t>(static_cast<int32_t>(s2)) << 12) +
+         static_cast<uint64_t>(static_cast<int64_t>(static_cast<int32_t>(s3)));
+}
+__device__ __forceinline__ uint64_t fixed(float p, bool &bad) {  // what is no probability counts as zero
   const bool in = p >= 0.0f && p <= 2.0f;  // (rounded sums may pass 1)
   bad |= !in;
-  return in ? __float2ull_rn(p * 72057594037927936.0f) : 0;
+  if (!in) p = 0.0f;
+  const float t1 = __fadd_rn(p, kGrid1), r = __fsub_rn(p, __fsub_rn(t1, kGrid1)), t2 = __fadd_rn(r, kGrid2);
+  const float t3 = __fadd_rn(__fsub_rn(r, __fsub_rn(t2, kGrid2)), kGrid3);
+  return joined(__float_as_uint(t1) - __float_as_uint(kGrid1), __float_as_uint(t2) - __float_as_uint(kGrid2),
+                __float_as_uint(t3) - __float_as_uint(kGrid3));
+}
+
+// the words of two probabilities on the three grids
+struct Words {
+  float2 t1, t2, t3;
+};
+__device__ __forceinline__ Words words_of(float x, float y) {
+  const uint64_t p = pair_of(x, y), minus = pair_of(-1.0f, -1.0f), g1 = pair_of(kGrid1, kGrid1), g2 = pair_of(kGrid2, kGrid2), g3 = pair_of(kGrid3, kGrid3);
+  const uint64_t t1 = add2(p, g1), r = add2(p, fma2(t1, minus, g1)), t2 = add2(r, g2), t3 = add2(add2(r, fma2(t2, minus, g2)), g3);
+  return {floats_of(t1), floats_of(t2), floats_of(t3)};
 }
 
 // a number in [0, 1) in units of 2^-64
@@ -76,13 +98,15 @@ struct alignas(sizeof(T) * VEC) Pack {
   T v[VEC];
 };
 
-// A cluster of CTAs for each sequence; a warp takes a run of the vocabulary, a lane VEC of every 32 VEC.
-template <typename T, bool DRAFT, int VEC>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const ClearVerifyArgs a, uint32_t ranks, uint32_t run) {
+// A cluster of CTAs for each sequence; a warp takes a run of the vocabulary.
+template <typename T, bool DRAFT>
+__global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVerifyArgs a, uint32_t ranks, uint32_t run) {
+  constexpr int VEC = 4;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ uint64_t s_warp[2][kWarps], s_total[2];
+  __shared__ uint64_t s_warp[2][kMostWarps], s_total[2];
   __shared__ uint32_t s_bad;
   const uint32_t nodes = a.nodes, tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t threads = blockDim.x, warps = threads / 32;
   const uint32_t rank = blockIdx.x % ranks, b = blockIdx.x / ranks;
   // of each node: p and q of its token under its parent, its number, parent, token; the tokens rejected at the present
   // node and their p (DRAFT has none)
@@ -94,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const ClearVerifyArgs 
   const float *uniform = a.uniform + static_cast<int64_t>(b) * a.uniform_pitch;
   bool bad = false;
   // Each CTA gathers every ranks-th node and all take it over, so that they decide alike whatever becomes of the buffers meanwhile.
-  for (uint32_t c = rank + tid * ranks; c < nodes; c += kThreads * ranks) {
+  for (uint32_t c = rank + tid * ranks; c < nodes; c += threads * ranks) {
     int32_t up = c ? a.parents[static_cast<int64_t>(b) * a.parents_pitch + c] : -1;
     const int32_t x = c ? a.tokens[static_cast<int64_t>(b) * a.tokens_pitch + c] : 0;
     if (up < -1 || up >= static_cast<int32_t>(c) || (up >= 0 && (x < 0 || static_cast<uint32_t>(x) >= a.vocab))) {
@@ -109,68 +133,124 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const ClearVerifyArgs 
   }
   if (ranks > 1) {
     cluster_sync_shared();
-    for (uint32_t c = tid; c < nodes; c += kThreads) {
+    for (uint32_t c = tid; c < nodes; c += threads) {
       const uint32_t from = c % ranks;
       if (from == rank) continue;
-      s_up[c] = static_cast<int32_t>(dsmem_ld_u32(dsmem_map(smem_addr(s_up + c), from)));
-      s_token[c] = static_cast<int32_t>(dsmem_ld_u32(dsmem_map(smem_addr(s_token + c), from)));
-      s_u[c] = dsmem_ld_u64(dsmem_map(smem_addr(s_u + c), from));
-      s_p[c] = dsmem_ld_u64(dsmem_map(smem_addr(s_p + c), from));
-      if constexpr (DRAFT) s_q[c] = dsmem_ld_u64(dsmem_map(smem_addr(s_q + c), from));
+      const uint32_t up = dsmem_ld_u32(dsmem_map(smem_addr(s_up + c), from)), x = dsmem_ld_u32(dsmem_map(smem_addr(s_token + c), from));
+      const uint64_t u = dsmem_ld_u64(dsmem_map(smem_addr(s_u + c), from)), p = dsmem_ld_u64(dsmem_map(smem_addr(s_p + c), from));
+      const uint64_t q = DRAFT ? dsmem_ld_u64(dsmem_map(smem_addr(s_q + c), from)) : 0;
+      s_up[c] = static_cast<int32_t>(up);
+      s_token[c] = static_cast<int32_t>(x);
+      s_u[c] = u;
+      s_p[c] = p;
+      if constexpr (DRAFT) s_q[c] = q;
     }
   }
   __syncthreads();
 
-  const uint32_t lo = (rank * kWarps + warp) * run, hi = min(a.vocab, lo + run);  // this warp's run
+  const uint32_t lo = (rank * warps + warp) * run, hi = min(a.vocab, lo + run);  // this warp's run
   const auto row_of = [&](const T *rows, const int64_t (&strides)[2], uint32_t n) { return rows + static_cast<int64_t>(n) * strides[1]; };
-  // what is left of VEC tokens from x on
-  const auto load = [&](const T *p, const T *q, uint32_t x, uint64_t s, uint64_t (&w)[VEC]) {
-    if (VEC > 1 && x + VEC > hi) {
+  // what is left of a token
+  const auto one = [&](const T *p, const T *q, uint32_t x, uint64_t s) {
+    const uint64_t w = fixed(to_float(p[x]), bad);
+    return DRAFT && s != 0 ? less(w, times(fixed(to_float(q[x]), bad), s)) : w;
+  };
+  // what is left of this thread's share of the warp's run.  Rows that lie alike to 16 bytes are read in such pieces, but for their ends.
+  const auto own_sum = [&](const T *p, const T *q, uint64_t s) {
+    uint64_t sum = 0;
+    const auto away = [](const T *row, uint32_t x) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row + x) / sizeof(T) % VEC); };
+    const bool both = DRAFT && s != 0;
+    uint32_t x = min(lo, hi), end = x;
+    if (!both || away(p, 0) == away(q, 0)) {
+      x = min(hi, x + (VEC - away(p, x)) % VEC);  // the first piece
+      end = x + (hi - x) / VEC * VEC;
+      const uint32_t edge = lo < hi ? x - lo + (hi - end) : 0;  // tokens outside the pieces: fewer than 2 VEC
+      if (lane < edge) sum = one(p, q, lane < x - lo ? lo + lane : end + lane - (x - lo), s);
+      const uint64_t begun = sum;
+      uint32_t largest = 0;  // of the numbers' bits: past 2.0's where one is none
+      // Two pieces of each row are asked for at once; what lies behind the end counts as zeros.  Of the row itself, or after one
+      // rejection (s = 1, max(p - q, 0)), the words' sums: 64 tokens at a time fit them, 2^63 of them together.  (Longer pieces and
+      // more of them, unrolled, are slower: the code of a kernel that runs through once comes from far away.)
+      for (uint32_t at = x + lane * VEC; at < end;) {
+        uint32_t s1 = 0, s2 = 0, s3 = 0;
+        uint64_t part = 0;
+#pragma unroll 1
+        for (uint32_t turn = 0; turn < 64 / VEC / 2 && at < end; ++turn, at += 2 * 32 * VEC) {
+          Pack<T, VEC> pv[2], qv[2];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        w[e] = x + e < hi ? fixed(to_float(p[x + e]), bad) : 0;
-        if (DRAFT && x + e < hi) w[e] = less(w[e], times(fixed(to_float(q[x + e]), bad), s));
+          for (uint32_t i = 0; i < 2; ++i) {
+            const uint32_t own = at + i * 32 * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) pv[i].v[e] = qv[i].v[e] = from_float<T>(0.0f);
+            if (own < end) {
+              pv[i] = *reinterpret_cast<const Pack<T, VEC> *>(p + own);
+              if (both) qv[i] = *reinterpret_cast<const Pack<T, VEC> *>(q + own);
+            }
+          }
+          if (both && s != kOne) {
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) part += less(fixed(to_float(pv[i].v[e]), bad), times(fixed(to_float(qv[i].v[e]), bad), s));
+            continue;
+          }
+#pragma unroll
+          for (uint32_t i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+              // (of the row itself q is zeros: its words are the grids' own)
+              const float px = to_float(pv[i].v[e]), py = to_float(pv[i].v[e + 1]), qx = to_float(qv[i].v[e]), qy = to_float(qv[i].v[e + 1]);
+              const Words w = words_of(px, py), v = words_of(qx, qy);
+              largest = max(max(largest, max(__float_as_uint(px), __float_as_uint(py))), max(__float_as_uint(qx), __float_as_uint(qy)));
+              if (px > qx) {
+                s1 += __float_as_uint(w.t1.x) - __float_as_uint(v.t1.x);
+                s2 += __float_as_uint(w.t2.x) - __float_as_uint(v.t2.x);
+                s3 += __float_as_uint(w.t3.x) - __float_as_uint(v.t3.x);
+              }
+              if (py > qy) {
+                s1 += __float_as_uint(w.t1.y) - __float_as_uint(v.t1.y);
+                s2 += __float_as_uint(w.t2.y) - __float_as_uint(v.t2.y);
+                s3 += __float_as_uint(w.t3.y) - __float_as_uint(v.t3.y);
+              }
+            }
+        }
+        part += joined(s1, s2, s3);
+        sum = add_most(sum, part < kMost ? part : kMost);
       }
-      return;
+      if (largest > 0x40000000u) {  // one by one
+        sum = begun;
+#pragma unroll 1
+        for (uint32_t at = x + lane * VEC; at < end; at += 32 * VEC)
+#pragma unroll 1
+          for (int e = 0; e < VEC; ++e) sum = add_most(sum, one(p, q, at + e, s));
+      }
+      return sum;
     }
-    const Pack<T, VEC> pv = *reinterpret_cast<const Pack<T, VEC> *>(p + x);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) w[e] = fixed(to_float(pv.v[e]), bad);
     if constexpr (DRAFT) {
-      if (s != 0) {
-        const Pack<T, VEC> qv = *reinterpret_cast<const Pack<T, VEC> *>(q + x);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] = less(w[e], times(fixed(to_float(qv.v[e]), bad), s));
-      }
+#pragma unroll 2
+      for (x += lane; x < hi; x += 32) sum = add_most(sum, one(p, q, x, s));
     }
+    return sum;
   };
   uint32_t turn = 0;
   uint64_t before = 0;  // the sum of the CTAs before this one
   // the sum of what is left of node n's row, over the cluster; the warps' sums stay in s_warp[turn ^ 1]
   const auto row_sum = [&](uint32_t n, uint64_t s, uint32_t gone) {
     const T *p = row_of(target, a.target_strides, n), *q = DRAFT ? row_of(draft, a.draft_strides, n) : nullptr;
-    uint64_t sum = 0;
-    for (uint32_t x = lo + lane * VEC; x < hi; x += 32 * VEC) {
-      uint64_t w[VEC];
-      load(p, q, x, s, w);
-#pragma unroll
-      for (int e = 1; e < VEC; ++e) w[0] += w[e];  // (2^60)
-      sum = add_most(sum, w[0]);
-    }
+    uint64_t sum = own_sum(p, q, s);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum = add_most(sum, __shfl_xor_sync(0xffffffffu, sum, o));
     if (lane == 0) s_warp[turn][warp] = sum;
     __syncthreads();
     if (!DRAFT && gone) {
-      for (uint32_t i = tid; i < gone; i += kThreads) {
+      for (uint32_t i = tid; i < gone; i += threads) {
         const uint32_t w = static_cast<uint32_t>(s_gone[i]) / run;
-        if (w / kWarps == rank) atomicAdd(reinterpret_cast<unsigned long long *>(&s_warp[turn][w % kWarps]), 0ull - s_gone_p[i]);
+        if (w / warps == rank) atomicAdd(reinterpret_cast<unsigned long long *>(&s_warp[turn][w % warps]), 0ull - s_gone_p[i]);
       }
       __syncthreads();
     }
     uint64_t total = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kWarps; ++w) total = add_most(total, s_warp[turn][w]);
+    for (uint32_t w = 0; w < warps; ++w) total = add_most(total, s_warp[turn][w]);
     before = 0;
     if (ranks > 1) {
       if (tid == 0) s_total[turn] = total;
@@ -187,72 +267,76 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const ClearVerifyArgs 
     return total;
   };
 
-  // ---- the walk: every warp for itself, all alike ----
-  uint32_t n = 0, length = 1, gone = 0;
-  uint64_t s = 0, z = kOne, left = kOne;
-  bool stale = false;  // z is that of the s before
+  // ---- the walk: every warp for itself, all alike; it stops where a sum is wanted, and at its end ----
+  uint32_t n = 0, length = 1, gone = 0, c0 = 1;
+  uint64_t s = 0, z = kOne, left = kOne, total;
+  bool stale = false, ended = false;  // (stale: z is that of the s before)
   if (tid == 0) s_path[0] = 0;
-  for (uint32_t c0 = 1; c0 < nodes;) {
-    const uint32_t hit = __ballot_sync(0xffffffffu, c0 + lane < nodes && s_up[min(c0 + lane, nodes - 1)] == static_cast<int32_t>(n));
-    if (hit == 0) {
-      c0 += 32;
-      continue;
-    }
-    const uint32_t c = c0 + __ffs(hit) - 1;
-    c0 = c + 1;
-    const uint64_t u = s_u[c];
-    bool yes;
-    if constexpr (DRAFT) {
-      if (stale) z = row_sum(n, s, 0);
-      stale = false;
-      yes = __umul64hi(u, times(s_q[c], z)) < less(s_p[c], times(s_q[c], s));
-      if (!yes) {
-        s = add_most(s, z);
-        stale = true;
+  while (true) {
+    while (!ended) {
+      uint32_t hit = 0;
+      for (; c0 < nodes; c0 += 32) {
+        hit = __ballot_sync(0xffffffffu, c0 + lane < nodes && s_up[min(c0 + lane, nodes - 1)] == static_cast<int32_t>(n));
+        if (hit) break;
       }
-    } else {
-      uint64_t p = s_p[c];
-      bool again = false;  // a token that has been rejected here
-      for (uint32_t i = lane; i < gone; i += 32) again |= s_gone[i] == s_token[c];
-      if (__any_sync(0xffffffffu, again)) p = 0;
-      yes = __umul64hi(u, left) < p;
-      if (!yes && p) {
-        left = less(left, p);
-        __syncthreads();  // (all have looked at the list)
-        if (tid == 0) {
-          s_gone[gone] = s_token[c];
-          s_gone_p[gone] = p;
+      ended = hit == 0;
+      if (ended || stale) break;
+      const uint32_t c = c0 + __ffs(hit) - 1;
+      c0 = c + 1;
+      const uint64_t u = s_u[c];
+      bool yes;
+      if constexpr (DRAFT) {
+        yes = __umul64hi(u, times(s_q[c], z)) < less(s_p[c], times(s_q[c], s));
+        if (!yes) {
+          s = add_most(s, z);
+          stale = true;
         }
-        ++gone;
-        __syncthreads();
+      } else {
+        uint64_t p = s_p[c];
+        bool again = false;  // a token that has been rejected here
+        for (uint32_t i = lane; i < gone; i += 32) again |= s_gone[i] == s_token[c];
+        if (__any_sync(0xffffffffu, again)) p = 0;
+        yes = __umul64hi(u, left) < p;
+        if (!yes && p) {
+          left = less(left, p);
+          __syncthreads();  // (all have looked at the list)
+          if (tid == 0) {
+            s_gone[gone] = s_token[c];
+            s_gone_p[gone] = p;
+          }
+          ++gone;
+          __syncthreads();
+        }
+      }
+      if (yes) {
+        if (tid == 0) s_path[length] = static_cast<int32_t>(c);
+        ++length;
+        n = c;
+        s = 0;
+        z = left = kOne;
+        gone = 0;
       }
     }
-    if (yes) {
-      if (tid == 0) s_path[length] = static_cast<int32_t>(c);
-      ++length;
-      n = c;
-      s = 0;
-      z = left = kOne;
+    total = row_sum(n, s, gone);
+    if (!ended) {
+      z = total;
       stale = false;
+    } else if (total == 0 && (s != 0 || gone != 0)) {  // nothing is left: the target's row itself
+      s = 0;
       gone = 0;
-      __syncthreads();
+    } else {
+      break;
     }
   }
 
   // ---- the next token ----
-  uint64_t total = row_sum(n, s, gone);
-  if (total == 0 && (s != 0 || gone != 0)) {  // nothing is left: the target's row itself
-    s = 0;
-    gone = 0;
-    total = row_sum(n, s, gone);
-  }
   if (tid == 0) s_bad = 0;
   __syncthreads();
   if (bad) s_bad = 1;
   __syncthreads();
   if (tid == 0 && (s_bad || total == 0 || total >= kMost)) atomicMax(a.err_flag, 1u);
   if (rank == 0) {
-    for (uint32_t i = tid; i < nodes; i += kThreads) a.path[static_cast<int64_t>(b) * a.path_pitch + i] = i < length ? s_path[i] : -1;
+    for (uint32_t i = tid; i < nodes; i += threads) a.path[static_cast<int64_t>(b) * a.path_pitch + i] = i < length ? s_path[i] : -1;
     if (tid == 0) {
       a.count[b] = static_cast<int32_t>(length);
       if (total == 0 || total >= kMost) a.next[b] = -1;
@@ -260,63 +344,73 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const ClearVerifyArgs 
   }
   const uint64_t goal = __umul64hi(s_u[0], total);  // the first running sum above it
   const uint32_t last = turn ^ 1;
-  for (uint32_t w = 0; w < warp; ++w) before = add_most(before, s_warp[last][w]);
-  if (total < kMost && before <= goal && goal < before + s_warp[last][warp]) {
+  uint32_t owner = 0;  // the warp in whose run it passes
+  for (; owner < warps && total < kMost; ++owner) {
+    if (before <= goal && goal < before + s_warp[last][owner]) break;
+    before = add_most(before, s_warp[last][owner]);
+  }
+  if (owner < warps && total < kMost) {  // (the same for the CTA)
     const T *p = row_of(target, a.target_strides, n), *q = DRAFT ? row_of(draft, a.draft_strides, n) : nullptr;
-    for (uint32_t x0 = lo; x0 < hi; x0 += 32 * VEC) {
-      const uint32_t x = x0 + lane * VEC;
-      uint64_t w[VEC] = {};
-      if (x < hi) load(p, q, x, s, w);
-      if constexpr (!DRAFT) {
-        for (uint32_t i = 0; i < gone; ++i) {
-          const uint32_t e = static_cast<uint32_t>(s_gone[i]) - x;
+    // a thread takes consecutive tokens of the run
+    const uint32_t first = (rank * warps + owner) * run, size = min(a.vocab, first + run) - first, each = (size + threads - 1) / threads;
+    const uint32_t from = first + min(size, tid * each), to = min(first + size, from + each);
+    uint64_t own = 0;
+#pragma unroll 4
+    for (uint32_t x = from; x < to; ++x) own += one(p, q, x, s);
+    if constexpr (!DRAFT) {
+      for (uint32_t i = 0; i < gone; ++i)
+        if (static_cast<uint32_t>(s_gone[i]) >= from && static_cast<uint32_t>(s_gone[i]) < to) own -= s_gone_p[i];
+    }
+    uint64_t sum = own;
 #pragma unroll
-          for (int j = 0; j < VEC; ++j)
-            if (e == static_cast<uint32_t>(j)) w[j] = 0;
-        }
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= static_cast<uint32_t>(o)) sum += v;
+    }
+    if (lane == 31) s_warp[turn][warp] = sum;
+    __syncthreads();
+    uint64_t at = before + sum - own;
+    for (uint32_t w = 0; w < warp; ++w) at += s_warp[turn][w];
+    if (at <= goal && goal < at + own) {
+      uint32_t x = from;
+      for (; x + 1 < to; ++x) {
+        bool here = true;
+        if constexpr (!DRAFT)
+          for (uint32_t i = 0; i < gone; ++i) here = here && s_gone[i] != static_cast<int32_t>(x);
+        if (here) at += one(p, q, x, s);
+        if (at > goal) break;
       }
-      uint64_t own = 0, sum;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) own += w[e];
-      sum = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint64_t v = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= static_cast<uint32_t>(o)) sum += v;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, before + sum > goal);
-      if (past) {
-        if (lane == static_cast<uint32_t>(__ffs(past) - 1)) {
-          uint64_t at = before + sum - own;
-          int e = 0;
-          while (e + 1 < VEC && at + w[e] <= goal) at += w[e++];
-          a.next[b] = static_cast<int32_t>(x + e);
-        }
-        break;
-      }
-      before += __shfl_sync(0xffffffffu, sum, 31);
+      a.next[b] = static_cast<int32_t>(x);
     }
   }
   if (ranks > 1) cluster_sync_shared();  // (the others' sums are read until here)
 }
 
-template <typename T, bool DRAFT, int VEC>
+template <typename T, bool DRAFT>
 cudaError_t launch(const ClearVerifyArgs &a, uint32_t sms, cudaStream_t s) {
-  const uint32_t ranks = 1;
-  const uint32_t parts = ranks * kWarps, each = 32 * VEC;
-  const uint32_t run = ((a.vocab + parts - 1) / parts + each - 1) / each * each;
-  const size_t smem = static_cast<size_t>(a.nodes) * (8 * 3 + 4 * 4);
-  verify_kernel<T, DRAFT, VEC><<<a.batch * ranks, kThreads, smem, s>>>(a, ranks, run);
-  return cudaGetLastError();
+  // As many CTAs for each sequence as are resident at once for all of them, of 2048 tokens at least, and eight at most (the portable
+  // cluster); 512 threads each, or 256 where those leave room for more of them.
+  uint32_t ranks = 8;
+  while (ranks > 1 && (static_cast<uint64_t>(a.batch) * ranks > 4ull * sms || a.vocab < 2048 * ranks)) ranks /= 2;
+  const uint32_t threads = static_cast<uint64_t>(a.batch) * ranks > 2ull * sms && ranks > 1 ? 256 : 512, parts = ranks * (threads / 32);
+  const uint32_t run = ((a.vocab + parts - 1) / parts + 31) / 32 * 32;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.batch * ranks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(a.nodes) * (8 * 3 + 4 * 4);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = ranks;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, DRAFT>, a, ranks, run);
 }
 
 template <typename T>
 cudaError_t launch(const ClearVerifyArgs &a, uint32_t sms, cudaStream_t s) {
-  constexpr int WIDE = 16 / sizeof(T);
-  uintptr_t at = reinterpret_cast<uintptr_t>(a.target) | static_cast<uintptr_t>((a.target_strides[0] | a.target_strides[1]) * sizeof(T));
-  if (!a.draft) return at % 16 == 0 ? launch<T, false, WIDE>(a, sms, s) : launch<T, false, 1>(a, sms, s);
-  at |= reinterpret_cast<uintptr_t>(a.draft) | static_cast<uintptr_t>((a.draft_strides[0] | a.draft_strides[1]) * sizeof(T));
-  return at % 16 == 0 ? launch<T, true, WIDE>(a, sms, s) : launch<T, true, 1>(a, sms, s);
+  return a.draft ? launch<T, true>(a, sms, s) : launch<T, false>(a, sms, s);
 }
 
 }  // namespace
