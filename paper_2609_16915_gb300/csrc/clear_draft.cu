@@ -150,10 +150,24 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
 
   const uint32_t lo = (rank * warps + warp) * run, hi = min(a.vocab, lo + run);  // this warp's run
   const auto row_of = [&](const T *rows, const int64_t (&strides)[2], uint32_t n) { return rows + static_cast<int64_t>(n) * strides[1]; };
+  // s q in two floats, the second to 2^-48 of it, for s other than 0 and 1; what is left of p (whole multiples of 2^-56 again, none of them
+  // below zero) counts from kLeast on
+  float high = 0.0f, low = 0.0f;
+  const auto take = [&](uint64_t s) {
+    high = __ull2float_rn(s) * 0x1p-56f;
+    low = __ll2float_rn(static_cast<int64_t>(s - __float2ull_rn(high * 0x1p56f))) * 0x1p-56f;
+  };
+  constexpr float kLeast = 0x1p-55f;
   // what is left of a token
   const auto one = [&](const T *p, const T *q, uint32_t x, uint64_t s) {
     const uint64_t w = fixed(to_float(p[x]), bad);
-    return DRAFT && s != 0 ? less(w, times(fixed(to_float(q[x]), bad), s)) : w;
+    if (!DRAFT || s == 0) return w;
+    const uint64_t v = fixed(to_float(q[x]), bad);
+    if (s == kOne) return less(w, v);
+    const float px = to_float(p[x]), given = to_float(q[x]), qx = given >= 0.0f && given <= 2.0f ? given : 0.0f, h = __fmul_rn(qx, high), l = __fmaf_rn(qx, low, __fmaf_rn(qx, high, -h));
+    if (w == 0 || !(__fsub_rn(px, h) > __fadd_rn(l, kLeast))) return uint64_t{0};
+    const float t2 = __fadd_rn(l, kGrid2), t3 = __fadd_rn(__fsub_rn(l, __fsub_rn(t2, kGrid2)), kGrid3);
+    return w - fixed(h, bad) - joined(0, __float_as_uint(t2) - __float_as_uint(kGrid2), __float_as_uint(t3) - __float_as_uint(kGrid3));
   };
   // what is left of this thread's share of the warp's run.  Rows that lie alike to 16 bytes are read in such pieces, but for their ends.
   const auto own_sum = [&](const T *p, const T *q, uint64_t s) {
@@ -167,6 +181,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
       const uint32_t edge = lo < hi ? x - lo + (hi - end) : 0;  // tokens outside the pieces: fewer than 2 VEC
       if (lane < edge) sum = one(p, q, lane < x - lo ? lo + lane : end + lane - (x - lo), s);
       const uint64_t begun = sum;
+      const uint64_t s_high = pair_of(high, high), s_low = pair_of(low, low);
       uint32_t largest = 0;  // of the numbers' bits: past 2.0's where one is none
       // Two pieces of each row are asked for at once; what lies behind the end counts as zeros.  Of the row itself, or after one
       // rejection (s = 1, max(p - q, 0)), the words' sums: 64 tokens at a time fit them, 2^63 of them together.  (Longer pieces and
@@ -191,7 +206,26 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i)
 #pragma unroll
-              for (int e = 0; e < VEC; ++e) part += less(fixed(to_float(pv[i].v[e]), bad), times(fixed(to_float(qv[i].v[e]), bad), s));
+              for (int e = 0; e < VEC; e += 2) {
+                const float px = to_float(pv[i].v[e]), py = to_float(pv[i].v[e + 1]), qx = to_float(qv[i].v[e]), qy = to_float(qv[i].v[e + 1]);
+                largest = max(max(largest, max(__float_as_uint(px), __float_as_uint(py))), max(__float_as_uint(qx), __float_as_uint(qy)));
+                const uint64_t q2 = pair_of(qx, qy), h2 = mul2(q2, s_high), minus = pair_of(-1.0f, -1.0f);
+                const uint64_t l2 = fma2(q2, s_low, fma2(q2, s_high, mul2(h2, minus)));
+                const float2 h = floats_of(h2), limit = floats_of(add2(l2, pair_of(kLeast, kLeast))), off = floats_of(add2(pair_of(px, py), mul2(h2, minus)));
+                const Words w = words_of(px, py), v = words_of(h.x, h.y);
+                const uint64_t g2 = pair_of(kGrid2, kGrid2), g3 = pair_of(kGrid3, kGrid3), u2 = add2(l2, g2);
+                const float2 t2 = floats_of(u2), t3 = floats_of(add2(add2(l2, fma2(u2, minus, g2)), g3));
+                if (off.x > limit.x) {
+                  s1 += __float_as_uint(w.t1.x) - __float_as_uint(v.t1.x);
+                  s2 += __float_as_uint(w.t2.x) - __float_as_uint(v.t2.x) - (__float_as_uint(t2.x) - __float_as_uint(kGrid2));
+                  s3 += __float_as_uint(w.t3.x) - __float_as_uint(v.t3.x) - (__float_as_uint(t3.x) - __float_as_uint(kGrid3));
+                }
+                if (off.y > limit.y) {
+                  s1 += __float_as_uint(w.t1.y) - __float_as_uint(v.t1.y);
+                  s2 += __float_as_uint(w.t2.y) - __float_as_uint(v.t2.y) - (__float_as_uint(t2.y) - __float_as_uint(kGrid2));
+                  s3 += __float_as_uint(w.t3.y) - __float_as_uint(v.t3.y) - (__float_as_uint(t3.y) - __float_as_uint(kGrid3));
+                }
+              }
             continue;
           }
 #pragma unroll
@@ -237,6 +271,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
   // the sum of what is left of node n's row, over the cluster; the warps' sums stay in s_warp[turn ^ 1]
   const auto row_sum = [&](uint32_t n, uint64_t s, uint32_t gone) {
     const T *p = row_of(target, a.target_strides, n), *q = DRAFT ? row_of(draft, a.draft_strides, n) : nullptr;
+    if constexpr (DRAFT) take(s);
     uint64_t sum = own_sum(p, q, s);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum = add_most(sum, __shfl_xor_sync(0xffffffffu, sum, o));
@@ -280,13 +315,14 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
         if (hit) break;
       }
       ended = hit == 0;
-      if (ended || stale) break;
+      if (ended) break;
       const uint32_t c = c0 + __ffs(hit) - 1;
-      c0 = c + 1;
       const uint64_t u = s_u[c];
       bool yes;
       if constexpr (DRAFT) {
-        yes = __umul64hi(u, times(s_q[c], z)) < less(s_p[c], times(s_q[c], s));
+        // (Z only falls, but for rows that add up to a little more than 1: what the one before would accept needs no sum)
+        yes = __umul64hi(u, times(s_q[c], stale ? z + (z >> 6) : z)) < less(s_p[c], times(s_q[c], s));
+        if (!yes && stale) break;
         if (!yes) {
           s = add_most(s, z);
           stale = true;
@@ -308,6 +344,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
           __syncthreads();
         }
       }
+      c0 = c + 1;
       if (yes) {
         if (tid == 0) s_path[length] = static_cast<int32_t>(c);
         ++length;
@@ -315,6 +352,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
         s = 0;
         z = left = kOne;
         gone = 0;
+        stale = false;
       }
     }
     total = row_sum(n, s, gone);
