@@ -14,6 +14,10 @@ norm stands before every product (the attention's output among them), there are 
 embeddings, no gate beside the table and no biases but the table's, so a range calibrated on it is
 its own, and a model's layer is put together from the same calls where they fit it.
 
+Drafted tokens: one bootstrapped table takes milliseconds for one ciphertext and little more for hundreds, so a decoder
+around such tables checks a tree of drafted tokens in one step.  step() takes the tree's mask, Head gives the target's
+probabilities, and drafted_step() runs the whole of it: layer, verification, and the cache keeps what stands.
+
 Norms, products, cache and table values are 8-bit (clear.Clear); the residual stream is
 bfloat16.  The encrypted path replaces the table alone: encrypt(code) -> pbs_batch ->
 decrypt gives lut[code], and value_table() turns those output codes into the same 8-bit
@@ -72,6 +76,13 @@ class Cache:
     def tensors(self):
         return self.k, self.v, self.k_scale, self.v_scale, self.pages
 
+    def keep(self, lib: Clear, path, count):
+        """Of the last path.shape[1] positions of each sequence, those that `path` names, count[b] of them: the others are
+        dropped.  (`room` stays as it is: how many were dropped the device alone knows.)"""
+        nodes = path.shape[1]
+        lib.cache_keep(*self.tensors(), self.lengths - nodes, path, count)
+        self.lengths += count - nodes
+
 
 class Layer:
     """weights: floats qkv [(heads + 2 kv_heads) dim][width], o [width][heads dim], up [inner][width], down [width][inner]."""
@@ -103,9 +114,10 @@ class Layer:
         y = torch.empty((q.shape[0], self.packed[name].channels), dtype=torch.bfloat16, device=q.device)
         return self.lib.linear(q, scale, self.packed[name], self.scales[name], y, bias=bias)
 
-    def before_table(self, x, residual, cache: Cache):
+    def before_table(self, x, residual, cache: Cache, mask=None):
         """The 8-bit input of the up projection for new tokens x [batch][tokens][width]; residual and cache move on.
-        ValueError, and neither moves, where the cache is full."""
+        Each token sees those before it, or under a mask (Clear.tree_mask) those of a tree.  ValueError, and neither moves,
+        where the cache is full."""
         b, t, w = x.shape
         hq, hk, d = self.heads, self.kv_heads, self.dim
         cache.take(t)
@@ -115,7 +127,10 @@ class Layer:
         self.lib.cache_append(qkv[:, :, hq:hq + hk], qkv[:, :, hq + hk:], *cache.tensors(), cache.lengths)
         cache.lengths += t
         a = torch.empty((b, t, hq, d), dtype=torch.bfloat16, device=x.device)
-        self.lib.attention(qkv[:, :, :hq], *cache.tensors(), cache.lengths, a)
+        if mask is None:
+            self.lib.attention(qkv[:, :, :hq], *cache.tensors(), cache.lengths, a)
+        else:
+            self.lib.tree_attention(qkv[:, :, :hq], *cache.tensors(), cache.lengths, mask, a)
         q, s = self._norm(a.view(b * t, hq * d), "norm_a")
         return self._norm(self._linear(q, s, "o"), "norm2", flat)
 
@@ -127,16 +142,69 @@ class Layer:
         self.lo, self.hi = float(y[k]), float(y[-1 - k])
         return self.lo, self.hi
 
-    def step(self, x, residual, cache: Cache):
+    def step(self, x, residual, cache: Cache, mask=None):
         """(y [batch][tokens][width], message codes [batch * tokens][inner]) of new tokens."""
         b, t, w = x.shape
-        q, s = self.before_table(x, residual, cache)
+        q, s = self.before_table(x, residual, cache, mask)
         code = torch.empty((b * t, self.inner), dtype=torch.uint8, device=x.device)
         value = torch.empty((b * t, self.inner), dtype=torch.int8, device=x.device)
         self.lib.linear_codes(q, s, self.packed["up"], self.scales["up"], code, self.bits, self.lo, self.hi, bias=self.bias,
                               table=self.table, values=value)
         scale = torch.full((b * t,), self.table_scale, device=x.device)
         return self._linear(value, scale, "down").view(b, t, w), code
+
+
+class Head:
+    """The tokens' probabilities after the last layer: softmax(norm(y + residual) weight^T), weight [vocab][width]."""
+
+    def __init__(self, weight, lib: Clear):
+        q, self.scale = quantise_channels(weight)
+        self.lib, self.packed, self.gamma = lib, lib.pack_weights(q), torch.ones(weight.shape[1], device=weight.device)
+
+    def __call__(self, y, residual=None):
+        """float32 [batch][tokens][vocab] of y (+ residual) [batch][tokens][width]."""
+        b, t, w = y.shape
+        q = torch.empty((b * t, w), dtype=torch.int8, device=y.device)
+        s = torch.empty(b * t, device=y.device)
+        self.lib.norm(y.reshape(b * t, w), self.gamma, q, s, residual=None if residual is None else residual.reshape(b * t, w), eps=EPS)
+        logits = torch.empty((b * t, self.packed.channels), device=y.device)
+        self.lib.linear(q, s, self.packed, self.scale, logits)
+        return torch.softmax(logits, 1).view(b, t, -1)
+
+
+def drafted_step(layer: Layer, head: Head, embedding, cache: Cache, tokens, parents, uniform, draft=None):
+    """One step over trees of drafted tokens: tokens, parents int32 and uniform [batch][nodes], node 0 the last token that stands
+    (see rosetta.h).  (path, count, next token, message codes of all nodes); the cache keeps the path.
+
+    The next call's node 0 is the next token, whose position comes behind the path."""
+    b, nodes = tokens.shape
+    lib, device = layer.lib, tokens.device
+    mask = torch.empty((b, nodes, -(-nodes // 32)), dtype=torch.int32, device=device)
+    lib.tree_mask(parents, mask)
+    x = embedding[tokens.long()]
+    residual = torch.zeros_like(x)
+    y, code = layer.step(x, residual, cache, mask)
+    path = torch.empty((b, nodes), dtype=torch.int32, device=device)
+    count, following = (torch.empty(b, dtype=torch.int32, device=device) for _ in range(2))
+    lib.verify(head(y, residual), tokens, parents, uniform, path, count, following, draft=draft)
+    cache.keep(lib, path, count)
+    return path, count, following, code
+
+
+def draw_tree(head: Head, embedding, roots, parents, generator=None):
+    """(tokens, draft): trees of one shape (parents [nodes]), each child drawn from the head's probabilities of its parent's
+    embedding alone, a draft that knows the last token only."""
+    b, nodes = roots.shape[0], parents.shape[0]
+    tokens = torch.zeros((b, nodes), dtype=torch.int32, device=roots.device)
+    tokens[:, 0] = roots
+    draft = torch.zeros((b, nodes, head.packed.channels), device=roots.device)
+    up = parents.tolist()
+    for n in range(nodes):
+        children = [c for c in range(n + 1, nodes) if up[c] == n]
+        if children:
+            draft[:, n] = head(embedding[tokens[:, n:n + 1].long()])[:, 0]
+            tokens[:, children] = torch.multinomial(draft[:, n], len(children), replacement=True, generator=generator).to(torch.int32)
+    return tokens, draft
 
 
 def random_weights(width, inner, heads, kv_heads, dim, seed=0, device="cuda"):
@@ -183,6 +251,25 @@ def main():
         print(f"{name}: {batch} x {n} tokens, {events[0].elapsed_time(events[1]) / times * 1e3:.0f} us a step;"
               f" codes 0 and {2 ** bits - 1} (clipped): {float(((code == 0) | (code == 2 ** bits - 1)).float().mean()):.2%};"
               f" messages to encrypt a token: {inner}")
+    # trees of two, then two, then one child each
+    vocab, up = 2000, torch.tensor([-1, 0, 0, 1, 1, 2, 2, 3, 5], dtype=torch.int32, device="cuda")
+    nodes, steps = len(up), 8
+    embedding = torch.randn((vocab, width), device="cuda", generator=g).to(torch.bfloat16)
+    head = Head(0.01 * embedding.float(), layer.lib)
+    cache = Cache(batch, (steps + 1) * nodes, heads, dim)
+    last = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    stood, us = 0, 0.0
+    for i in range(steps + 1):      # (the first is warm-up)
+        trees, draft = draw_tree(head, embedding, last, up, g)
+        uniform = torch.rand((batch, nodes), device="cuda", generator=g)
+        events[0].record()
+        path, count, last, code = drafted_step(layer, head, embedding, cache, trees, up.expand(batch, nodes), uniform, draft)
+        events[1].record()
+        layer.lib.sync_status()
+        if i:
+            stood, us = stood + int(count.sum()), us + events[0].elapsed_time(events[1]) * 1e3
+    print(f"drafted: {batch} trees of {nodes} nodes, {us / steps:.0f} us a step; tokens a sequence and step: {stood / batch / steps:.2f};"
+          f" messages to encrypt a step: {code.numel()}")
 
 
 if __name__ == "__main__":
