@@ -176,23 +176,25 @@ __device__ __forceinline__ bool wait_quick(uint32_t bar, uint32_t parity) {
   return done || mbar_wait(bar, parity);
 }
 
-__device__ __forceinline__ void copy_async(uint32_t dst, const void *src, bool valid) {
-  const uint32_t size = valid ? 16 : 0;  // (nothing is read for 0: zeros)
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // RUNS: a block's range may be longer than one accumulator takes.  (A kernel of its own: its registers cost shorter ranges 3 %.)
 // TREE: under a mask.  A row sees every position before the drafted ones, and of those the bits of its own row of the mask.
-// PAIR: the rows fill one row tile, and the two groups of softmax warps take turns at the positions, each with scores and outputs of its
-// own (chain r: tiles r, r + 2 ..), which are joined at the end.
-template <typename T, int DP, bool RUNS, bool TREE, bool PAIR>
+// TURNS: the rows fill one row tile, and the two groups of softmax warps take turns at the positions, each with scores and outputs of its
+// own (chain r: tiles r, r + 2 ..), which are joined at the end.  HALF: the rows fill half of it, and the softmax warps of the other
+// half convert every second tile.
+enum Rows : int { ALL = 0, TURNS = 1, HALF = 2 };
+template <typename T, int DP, bool RUNS, bool TREE, int KIND>
 __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const AttendArgs f) {
   const ClearAttentionArgs &a = f.a;
   using M = Many<DP>;
-  constexpr bool SPLIT = kSplit<T>, FINE = kFine<T>;
+  constexpr bool SPLIT = kSplit<T>, FINE = kFine<T>, PAIR = KIND != ALL, WIDE = KIND == HALF;
   static_assert(!PAIR || (TREE && !RUNS && !SPLIT), "pairs: of 16-bit types, one accumulator a range");
   constexpr uint32_t AHEAD = PAIR ? 4 : 2;  // tiles scored ahead of the weights that meet their values
   constexpr uint32_t SOFT_WARPS = kSoftWarps<T>, WARPS = kWarps<T>;
+  constexpr uint32_t ACTIVE = WIDE ? 2 : 1;  // one of so many softmax warps is one
   constexpr uint32_t BLOCK_ROWS = SPLIT ? ROWS : 2 * ROWS;
   const auto tile_of = [](uint32_t j) { return RUNS ? j % RUN : j; };  // of a run
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   if (threadIdx.x == (WARPS - 1) * 32) {  // (of the MMA warp)
     s_fail = 0u;
     for (uint32_t i = 0; i < TILE_WARPS; ++i) s_quit[i] = 0u;
-    mbar_init(bar(QFULL), SOFT_WARPS);
+    mbar_init(bar(QFULL), SOFT_WARPS / ACTIVE);
     for (uint32_t i = 0; i < RING; ++i) {
       mbar_init(bar(KFULL + i), 4);
       mbar_init(bar(VFULL + i), 4);
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     }
     for (uint32_t i = 0; i < 4; ++i) {
       mbar_init(bar(SFULL + i), 2);
-      mbar_init(bar(PFULL + i), TILE_WARPS);
+      mbar_init(bar(PFULL + i), TILE_WARPS / ACTIVE);
     }
     mbar_init(bar(FIRST), 1);
     mbar_init(bar(FREE), 1);
@@ -293,7 +295,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     atomicExch(&s_fail, 1u);
   };
 
-  if (warp < SOFT_WARPS) {
+  const bool helps = WIDE && warp < SOFT_WARPS && warp % 4 >= 2;  // a softmax warp that converts
+  if (warp < SOFT_WARPS && !helps) {
     // row tile, half of the columns, row: two threads a row, in warps that share a quarter of tensor memory
     const uint32_t r = warp / 8, half = warp / 4 % 2, row_in = (warp % 4) * 32 + lane, row = row0 + (PAIR ? 0 : r * ROWS) + row_in;
     const uint32_t lanes = ((warp % 4) * 32u) << 16;
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const auto other_left = [&]() { return *const_cast<volatile uint32_t *>(&s_quit[pair]) == meetings; };
     // (PAIR: at barrier 13 all softmax warps meet once, those that leave among them, without waiting)
     const auto pass = [&]() {
-      if constexpr (PAIR) asm volatile("bar.arrive 13, 512;" ::: "memory");
+      if constexpr (PAIR) asm volatile("bar.arrive 13, %0;" ::"n"(512 / ACTIVE) : "memory");
     };
     const auto leave = [&]() {
       pass();
@@ -324,7 +327,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     };
     // ---- the warp's 16 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
     // eight dimensions at a time ----
-    const uint32_t qr = lane % 8, qc = lane / 8;
+    const uint32_t qr = lane % 8, qc = lane / 8, loader = WIDE ? warp % 4 + 2 * half : warp % 8;
     const bool wide_q = (reinterpret_cast<uintptr_t>(a.q) | static_cast<uintptr_t>((a.q_strides[0] | a.q_strides[1] | a.q_strides[2]) * sizeof(T))) % 16 == 0;
     if constexpr (SPLIT) {
       start_block();
@@ -375,7 +378,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       uint4 raw[2][DP / 32];
 #pragma unroll
       for (uint32_t g = 0; g < 2; ++g) {
-        const uint32_t rw = row0 + (PAIR ? r * rows : r * ROWS) + (warp % 8) * 16 + g * 8 + qr;  // (PAIR: chain 0 loads them)
+        const uint32_t rw = row0 + (PAIR ? r * rows : r * ROWS) + loader * 16 + g * 8 + qr;  // (PAIR: chain 0 loads them)
         const T *q = static_cast<const T *>(a.q) + static_cast<int64_t>(b) * a.q_strides[0] +
                      static_cast<int64_t>(rw / a.group) * a.q_strides[1] + static_cast<int64_t>(kh * a.group + rw % a.group) * a.q_strides[2];
 #pragma unroll
@@ -398,7 +401,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       start_block();
 #pragma unroll
       for (uint32_t g = 0; g < 2; ++g) {
-        const uint32_t in_tile = (warp % 8) * 16 + g * 8 + qr;
+        const uint32_t in_tile = loader * 16 + g * 8 + qr;
         float x[DP / 32][8], top = 0.0f;
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(QFULL));
     if constexpr (PAIR)
-      asm volatile("bar.sync 11, 512;" ::: "memory");  // s_up of the rows
+      asm volatile("bar.sync 11, %0;" ::"n"(512 / ACTIVE) : "memory");  // s_up of the rows
     else
       asm volatile("bar.sync %0, 256;" ::"r"(11 + r) : "memory");  // s_up of the row tile
     const float factor = s_up[r * ROWS + row_in] * (fabsf(a.softmax_scale) * kLog2e);
@@ -669,7 +672,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           pass();
           goto done;
         }
-        asm volatile("bar.sync 13, 512;" ::: "memory");
+        asm volatile("bar.sync 13, %0;" ::"n"(512 / ACTIVE) : "memory");
         const float2 other = s_other[row_in];
         const float top = fmaxf(m, other.y);
         own_part = m == neg_inf() ? 0.0f : ex2(m - top);
@@ -748,12 +751,17 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       }
     }
   } else if (warp < SOFT_WARPS + CONVERT_WARPS) {
-    // ---- keys (four warps) and values (four) to f16: a warp 16 positions of each tile, in one page ----
-    const uint32_t w = warp % 4;
-    const bool keys = warp < SOFT_WARPS + 4;
+    // ---- keys (four warps) and values (four) to f16: a warp 16 positions of each tile, in one page.  WIDE: of each second tile,
+    // `set` the first of them, with three stages for each set (two of the six where other rows' queries would be) ----
+    constexpr uint32_t STEP = WIDE ? 2 : 1, STAGES = WIDE ? 3 : STAGED;
+    const uint32_t set = helps ? 1 : 0;
+    const uint32_t w = helps ? warp / 4 % 2 * 2 + warp % 4 - 2 : warp % 4;
+    const bool keys = helps ? warp < TILE_WARPS : warp < SOFT_WARPS + 4;
+    const uint32_t turns = set < n ? (n - set + STEP - 1) / STEP : 0;  // tiles of the set
     // the tiles to copy next: their pages, loaded a ring ahead; of the first, the page's slot in the list and the first row in it
-    const uint32_t slots = POS / a.page_tokens, more = POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
-    uint32_t slot = (start + w * 16) / a.page_tokens, row = (start + w * 16) % a.page_tokens;
+    const uint32_t slots = STEP * POS / a.page_tokens, more = STEP * POS % a.page_tokens, slots_end = (end + a.page_tokens - 1) / a.page_tokens;
+    const uint32_t begin = start + set * POS + w * 16;
+    uint32_t slot = begin / a.page_tokens, row = begin % a.page_tokens;
     uint32_t ahead_slot = slot, ahead_row = row;
     const auto next = [&](uint32_t &at_slot, uint32_t &at_row) {
       at_slot += slots;
@@ -763,49 +771,62 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         ++at_slot;
       }
     };
-    int32_t pages[STAGED];
+    int32_t pages[STAGES];
 #pragma unroll
-    for (uint32_t i = 0; i < STAGED; ++i) {
+    for (uint32_t i = 0; i < STAGES; ++i) {
       pages[i] = ahead_slot < slots_end ? table[ahead_slot] : -1;
       next(ahead_slot, ahead_row);
     }
-    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1];
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
     // of the tiles copied: scales, and whether the page is out of range
-    float ks[STAGED] = {}, vs[STAGED] = {};
-    bool skip[STAGED] = {};
+    float ks[STAGES] = {}, vs[STAGES] = {};
+    bool skip[STAGES] = {};
     // a warp's share of a staged tile: keys [row of 8][chunk of 16 bytes] by the lane that reads them, values row by row
-    const uint32_t raw_at = M::RAW_AT + (keys ? 0 : M::RAW) + w * (16 * DP);
+    const auto raw_at = [&](uint32_t st) {
+      const uint32_t of = STEP * st + set, share = (keys ? 0 : M::RAW) + w * (16 * DP);
+      return (WIDE && of >= STAGED ? M::Q_TILE + (of - STAGED) * (2 * M::RAW) : M::RAW_AT + of * (2 * M::RAW)) + share;
+    };
+    static_assert(2 * 2 * M::RAW <= M::Q_TILE, "two stages fit where the second row tile's queries are");
     const uint32_t kr = lane % 8, kc = lane / 8;  // a key row of 8, a chunk of four
-    const auto copy = [&](uint32_t st) {          // (st: a constant)
+    // A lane's pieces of a tile: every DP / 64th of its keys 8 rows on (the others 64 bytes on), of its values 512 / DP rows on.  What lies
+    // behind the head's end meets zeros, or goes where nobody looks: it is not copied, nor are pages out of range.
+    const int64_t line = a.cache_strides[2];
+    const uint32_t piece_row = keys ? kr : lane / (DP / 16), piece_d = keys ? kc * 16 : lane % (DP / 16) * 16;
+    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + piece_row * line + piece_d;
+    const int64_t piece_on = keys ? 8 * line : 512 / DP * line;
+    const bool near = piece_d < a.dim, far = keys ? piece_d + 64 < a.dim : near;  // (dim is a multiple of 16)
+    const auto copy = [&](uint32_t st) {  // (st: a constant)
       const int32_t page = pages[st];
       const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
       skip[st] = slot < slots_end && !in;
-      const size_t sc = in ? static_cast<size_t>(page) * a.heads + kh : 0;
-      ks[st] = in && keys ? a.k_scale[sc] : 0.0f;
-      vs[st] = in && keys ? a.v_scale[sc] : 0.0f;
-      const int8_t *src = cache + (in ? page * a.cache_strides[0] + static_cast<int64_t>(row) * a.cache_strides[2] : 0);
-      const uint32_t dst = base + raw_at + st * (2 * M::RAW) + lane * 16;
+      ks[st] = vs[st] = 0.0f;
+      if (in) {
+        if (keys) {
+          const size_t sc = static_cast<size_t>(page) * a.heads + kh;
+          ks[st] = a.k_scale[sc];
+          vs[st] = a.v_scale[sc];
+        }
+        const int8_t *src = cache + (page * a.cache_strides[0] + row * line);
+        const uint32_t dst = base + raw_at(st) + lane * 16;
 #pragma unroll
-      for (uint32_t i = 0; i < DP / 32; ++i) {
-        const uint32_t piece = i * 32 + lane;
-        const uint32_t r = keys ? i / (DP / 64) * 8 + kr : piece / (DP / 16);
-        const uint32_t d = keys ? (kc + 4 * (i % (DP / 64))) * 16 : piece % (DP / 16) * 16;
-        const bool ok = in && d < a.dim;
-        copy_async(dst + i * 512, ok ? src + r * a.cache_strides[2] + d : cache, ok);
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          if (keys && DP == 128 ? (i % 2 ? far : near) : near)
+            copy_async(dst + i * 512, keys && DP == 128 ? src + i % 2 * 64 : src);
+          if (!keys || DP == 64 || i % 2) src += piece_on;
+        }
       }
       next(slot, row);
       pages[st] = ahead_slot < slots_end ? table[ahead_slot] : -1;
       next(ahead_slot, ahead_row);
     };
 #pragma unroll
-    for (uint32_t i = 0; i + 1 < STAGED; ++i) {
-      if (i < n) copy(i);
+    for (uint32_t i = 0; i + 1 < STAGES; ++i) {
+      if (i < turns) copy(i);
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     start_block();
     // the largest value scale of the pages in the range: by the values' warps, which are not the first to be waited for
-    if (!keys) {
+    if (!keys && set == 0) {
       int32_t most = kNoScale;
       for (uint32_t p = start / a.page_tokens + threadIdx.x % 128; p < slots_end; p += 128) {
         const int32_t id = table[p];
@@ -816,19 +837,21 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       }
       most = __reduce_max_sync(0xffffffffu, most);
       if (lane == 0) s_top[w] = most;
-      asm volatile("bar.arrive 1, 256;" ::: "memory");
+      asm volatile("bar.arrive 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
     }
     int32_t unit = 0;  // of sv
     float per_sv = 1.0f;
-    uint32_t buf = 0;
+    uint32_t buf = set;
+    const auto on = [&]() { buf = buf + STEP >= RING ? buf + STEP - RING : buf + STEP; };
     if (keys) {
-      for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
+      if (turns == 0) asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");  // (as the others, below)
+      for (uint32_t t0 = 0; t0 < turns; t0 += STAGES) {
 #pragma unroll
-        for (uint32_t st = 0; st < STAGED; ++st) {
-          const uint32_t j = j0 + st;
-          if (j >= n) break;
-          asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
-          const unsigned char *src = smem + raw_at + st * (2 * M::RAW) + lane * 16;
+        for (uint32_t st = 0; st < STAGES; ++st) {
+          const uint32_t t = t0 + st, j = STEP * t + set;
+          if (t >= turns) break;
+          asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+          const unsigned char *src = smem + raw_at(st) + lane * 16;
           uint4 k[DP / 32];
 #pragma unroll
           for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
@@ -857,11 +880,11 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
             *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
           }
-          if (j == 0) {  // (the values' warps have seen the scales)
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+          if (t == 0) {  // (the values' warps have seen the scales)
+            asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
             unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
             per_sv = scalbnf(1.0f, -unit);
-            if (w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
+            if (set == 0 && w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
           }
           if (lane == 0) {
             // (a value scale that is a NaN or an infinity: no number)
@@ -874,9 +897,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           fence_async();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(KFULL + buf));
-          if (++buf == RING) buf = 0;
+          on();
           // into the place read in the round before this one
-          if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
+          if (t + STAGES - 1 < turns) copy((st + STAGES - 1) % STAGES);
           asm volatile("cp.async.commit_group;" ::: "memory");
         }
       }
@@ -888,14 +911,14 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       const uint32_t turn = lane / 2 % 4;
       const uint32_t sel_a = turn == 0 ? 0x5140u : turn == 1 ? 0x6251u : turn == 2 ? 0x7362u : 0x4073u;
       const uint32_t sel_b = turn == 0 ? 0x7362u : turn == 1 ? 0x4073u : turn == 2 ? 0x5140u : 0x6251u;
-      for (uint32_t j0 = 0; j0 < n; j0 += STAGED) {
+      for (uint32_t t0 = 0; t0 < turns; t0 += STAGES) {
 #pragma unroll
-        for (uint32_t st = 0; st < STAGED; ++st) {
-          const uint32_t j = j0 + st;
-          if (j >= n) break;
-          asm volatile("cp.async.wait_group %0;" ::"n"(STAGED - 2) : "memory");
+        for (uint32_t st = 0; st < STAGES; ++st) {
+          const uint32_t t = t0 + st, j = STEP * t + set;
+          if (t >= turns) break;
+          asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
           __syncwarp();
-          const unsigned char *src = smem + raw_at + st * (2 * M::RAW) + quad * 4;
+          const unsigned char *src = smem + raw_at(st) + quad * 4;
           uint32_t x[VG][8];
 #pragma unroll
           for (uint32_t g = 0; g < VG; ++g)
@@ -925,9 +948,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           fence_async();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(VFULL + buf));
-          if (++buf == RING) buf = 0;
+          on();
           // into the place read in the round before this one (all lanes have passed a barrier since)
-          if (j + STAGED - 1 < n) copy((st + STAGED - 1) % STAGED);
+          if (t + STAGES - 1 < turns) copy((st + STAGES - 1) % STAGES);
           asm volatile("cp.async.commit_group;" ::: "memory");
         }
       }
@@ -1066,11 +1089,12 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = f.runs ? attend_many_kernel<T, DP, true, false, false> : attend_many_kernel<T, DP, false, false, false>;
+  auto kern = f.runs ? attend_many_kernel<T, DP, true, false, ALL> : attend_many_kernel<T, DP, false, false, ALL>;
   if (f.a.mask) {
-    kern = f.runs ? attend_many_kernel<T, DP, true, true, false> : attend_many_kernel<T, DP, false, true, false>;
+    kern = f.runs ? attend_many_kernel<T, DP, true, true, ALL> : attend_many_kernel<T, DP, false, true, ALL>;
     if constexpr (!kSplit<T>) {
-      if (!f.runs && f.a.tokens * f.a.group <= ROWS) kern = attend_many_kernel<T, DP, false, true, true>;
+      const uint32_t rows = f.a.tokens * f.a.group;
+      if (!f.runs && rows <= ROWS) kern = rows <= ROWS / 2 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
     }
   }
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
