@@ -771,16 +771,17 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         ++at_slot;
       }
     };
-    int32_t pages[STAGES];
+    int32_t pages[STAGES];  // of the next tiles to copy
 #pragma unroll
     for (uint32_t i = 0; i < STAGES; ++i) {
       pages[i] = ahead_slot < slots_end ? table[ahead_slot] : -1;
       next(ahead_slot, ahead_row);
     }
     const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));  // 1152
-    // of the tiles copied: scales, and whether the page is out of range
-    float ks[STAGES] = {}, vs[STAGES] = {};
-    bool skip[STAGES] = {};
+    // of the tiles copied and not converted yet: scales, and whether the page is out of range.  (These lists move on by one each turn:
+    // the code is a quarter of what constant places, in turns unrolled, would make it, and three roles share the instruction caches.)
+    float ks[STAGES - 1] = {}, vs[STAGES - 1] = {};
+    bool skip[STAGES - 1] = {};
     // a warp's share of a staged tile: keys [row of 8][chunk of 16 bytes] by the lane that reads them, values row by row
     const auto raw_at = [&](uint32_t st) {
       const uint32_t of = STEP * st + set, share = (keys ? 0 : M::RAW) + w * (16 * DP);
@@ -795,19 +796,20 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + piece_row * line + piece_d;
     const int64_t piece_on = keys ? 8 * line : 512 / DP * line;
     const bool near = piece_d < a.dim, far = keys ? piece_d + 64 < a.dim : near;  // (dim is a multiple of 16)
-    const auto copy = [&](uint32_t st) {  // (st: a constant)
-      const int32_t page = pages[st];
+    uint32_t to_stage = 0;  // of the next tile to copy
+    const auto copy = [&](uint32_t at) {  // (at: its place in the lists, a constant)
+      const int32_t page = pages[0];
       const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
-      skip[st] = slot < slots_end && !in;
-      ks[st] = vs[st] = 0.0f;
+      skip[at] = slot < slots_end && !in;
+      ks[at] = vs[at] = 0.0f;
       if (in) {
         if (keys) {
           const size_t sc = static_cast<size_t>(page) * a.heads + kh;
-          ks[st] = a.k_scale[sc];
-          vs[st] = a.v_scale[sc];
+          ks[at] = a.k_scale[sc];
+          vs[at] = a.v_scale[sc];
         }
         const int8_t *src = cache + (page * a.cache_strides[0] + row * line);
-        const uint32_t dst = base + raw_at(st) + lane * 16;
+        const uint32_t dst = base + raw_at(to_stage) + lane * 16;
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
           if (keys && DP == 128 ? (i % 2 ? far : near) : near)
@@ -816,8 +818,15 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
       }
       next(slot, row);
-      pages[st] = ahead_slot < slots_end ? table[ahead_slot] : -1;
+      to_stage = to_stage + 1 == STAGES ? 0 : to_stage + 1;
+#pragma unroll
+      for (uint32_t i = 0; i + 1 < STAGES; ++i) pages[i] = pages[i + 1];
+      pages[STAGES - 1] = ahead_slot < slots_end ? table[ahead_slot] : -1;
       next(ahead_slot, ahead_row);
+    };
+    const auto forget = [&]() {  // the first of the lists: its tile is converted
+#pragma unroll
+      for (uint32_t i = 0; i + 2 < STAGES; ++i) ks[i] = ks[i + 1], vs[i] = vs[i + 1], skip[i] = skip[i + 1];
     };
 #pragma unroll
     for (uint32_t i = 0; i + 1 < STAGES; ++i) {
@@ -845,63 +854,63 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const auto on = [&]() { buf = buf + STEP >= RING ? buf + STEP - RING : buf + STEP; };
     if (keys) {
       if (turns == 0) asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");  // (as the others, below)
-      for (uint32_t t0 = 0; t0 < turns; t0 += STAGES) {
+      uint32_t st = 0;
+#pragma unroll 1
+      for (uint32_t t = 0; t < turns; ++t) {
+        const uint32_t j = STEP * t + set;
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        const unsigned char *src = smem + raw_at(st) + lane * 16;
+        uint4 k[DP / 32];
 #pragma unroll
-        for (uint32_t st = 0; st < STAGES; ++st) {
-          const uint32_t t = t0 + st, j = STEP * t + set;
-          if (t >= turns) break;
-          asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-          const unsigned char *src = smem + raw_at(st) + lane * 16;
-          uint4 k[DP / 32];
-#pragma unroll
-          for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
-          // the keys that lay here were tile j - 3's, used with tile j - 5's values (PAIR: j - 7's; the fourth tile's before the first values'),
-          // or among the first two (three)
-          const uint32_t with = PAIR && j == 6 ? 0 : j - RING - AHEAD;
-          if (j >= RING && !__all_sync(0xffffffffu, j >= RING + AHEAD || (PAIR && j == 6) ? wait_quick(bar(USED + with % RING), (with / RING) & 1u)
-                                                                                        : wait_quick(bar(FIRST), 0))) {
-            give_up();
-            goto done;
-          }
-          // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
-          const __half2 sg = bits_half2(ks[st] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
-          unsigned char *kt = smem + M::K_AT + buf * M::K_TILE + w * 2 * (DP * 16) + kc * 256 + kr * 16;
-#pragma unroll
-          for (uint32_t i = 0; i < DP / 32; ++i) {
-            const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
-            uint32_t o[8];
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-              const uint32_t u = x[e] ^ 0x80808080u;
-              o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
-              o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
-            }
-            unsigned char *dst = kt + i / (DP / 64) * (DP * 16) + i % (DP / 64) * 1024;
-            *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
-          }
-          if (t == 0) {  // (the values' warps have seen the scales)
-            asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
-            unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
-            per_sv = scalbnf(1.0f, -unit);
-            if (set == 0 && w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
-          }
-          if (lane == 0) {
-            // (a value scale that is a NaN or an infinity: no number)
-            const bool number = fabsf(vs[st]) < -neg_inf();
-            s_ks[j % 8][w] = number ? fabsf(ks[st]) : __int_as_float(0x7fc00000);
-            s_skip[j % 8][w] = skip[st];
-            s_vr[j % 8][w] = number ? vs[st] * per_sv : 0.0f;
-            s_above[j % 8][w] = number ? scale_above(vs[st], unit) : 0.0f;
-          }
-          fence_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(KFULL + buf));
-          on();
-          // into the place read in the round before this one
-          if (t + STAGES - 1 < turns) copy((st + STAGES - 1) % STAGES);
-          asm volatile("cp.async.commit_group;" ::: "memory");
+        for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
+        // the keys that lay here were tile j - 3's, used with tile j - 5's values (PAIR: j - 7's; the fourth tile's before the first values'),
+        // or among the first two (three)
+        const uint32_t with = PAIR && j == 6 ? 0 : j - RING - AHEAD;
+        if (j >= RING && !__all_sync(0xffffffffu, j >= RING + AHEAD || (PAIR && j == 6) ? wait_quick(bar(USED + with % RING), (with / RING) & 1u)
+                                                                                      : wait_quick(bar(FIRST), 0))) {
+          give_up();
+          goto done;
         }
+        // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
+        const __half2 sg = bits_half2(ks[0] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
+        unsigned char *kt = smem + M::K_AT + buf * M::K_TILE + w * 2 * (DP * 16) + kc * 256 + kr * 16;
+#pragma unroll
+        for (uint32_t i = 0; i < DP / 32; ++i) {
+          const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+          uint32_t o[8];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            const uint32_t u = x[e] ^ 0x80808080u;
+            o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
+            o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
+          }
+          unsigned char *dst = kt + i / (DP / 64) * (DP * 16) + i % (DP / 64) * 1024;
+          *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+        if (t == 0) {  // (the values' warps have seen the scales)
+          asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
+          unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
+          per_sv = scalbnf(1.0f, -unit);
+          if (set == 0 && w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
+        }
+        if (lane == 0) {
+          // (a value scale that is a NaN or an infinity: no number)
+          const bool number = fabsf(vs[0]) < -neg_inf();
+          s_ks[j % 8][w] = number ? fabsf(ks[0]) : __int_as_float(0x7fc00000);
+          s_skip[j % 8][w] = skip[0];
+          s_vr[j % 8][w] = number ? vs[0] * per_sv : 0.0f;
+          s_above[j % 8][w] = number ? scale_above(vs[0], unit) : 0.0f;
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(KFULL + buf));
+        on();
+        // into the place read in the round before this one
+        forget();
+        if (t + STAGES - 1 < turns) copy(STAGES - 2);
+        st = st + 1 == STAGES ? 0 : st + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
     } else {
       constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
@@ -911,48 +920,48 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       const uint32_t turn = lane / 2 % 4;
       const uint32_t sel_a = turn == 0 ? 0x5140u : turn == 1 ? 0x6251u : turn == 2 ? 0x7362u : 0x4073u;
       const uint32_t sel_b = turn == 0 ? 0x7362u : turn == 1 ? 0x4073u : turn == 2 ? 0x5140u : 0x6251u;
-      for (uint32_t t0 = 0; t0 < turns; t0 += STAGES) {
+      uint32_t st = 0;
+#pragma unroll 1
+      for (uint32_t t = 0; t < turns; ++t) {
+        const uint32_t j = STEP * t + set;
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        __syncwarp();
+        const unsigned char *src = smem + raw_at(st) + quad * 4;
+        uint32_t x[VG][8];
 #pragma unroll
-        for (uint32_t st = 0; st < STAGES; ++st) {
-          const uint32_t t = t0 + st, j = STEP * t + set;
-          if (t >= turns) break;
-          asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-          __syncwarp();
-          const unsigned char *src = smem + raw_at(st) + quad * 4;
-          uint32_t x[VG][8];
+        for (uint32_t g = 0; g < VG; ++g)
 #pragma unroll
-          for (uint32_t g = 0; g < VG; ++g)
-#pragma unroll
-            for (uint32_t p = 0; p < 8; ++p) x[g][p] = *reinterpret_cast<const uint32_t *>(src + ((g + vsub) * 8 + p) * DP) ^ 0x80808080u;
-          if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
-            give_up();
-            goto done;
-          }
-          unsigned char *vt = smem + M::V_AT + buf * M::V_TILE + (quad >> 1) * V_GROUP + (w * 2 + vsub) * 128 + (quad & 1u) * 64;
-#pragma unroll
-          for (uint32_t g = 0; g < VG; ++g) {
-            uint32_t o[4][4];  // [round][pair of positions]
-#pragma unroll
-            for (uint32_t p = 0; p < 4; ++p) {
-              const uint32_t t0 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_a), t1 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_b);
-#pragma unroll
-              for (uint32_t e = 0; e < 4; ++e) {
-                const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
-                o[e][p] = half2_bits(v);
-              }
-            }
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-              *reinterpret_cast<uint4 *>(vt + g * 128 + (e + turn) % 4 * 16) = make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
-          }
-          fence_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(VFULL + buf));
-          on();
-          // into the place read in the round before this one (all lanes have passed a barrier since)
-          if (t + STAGES - 1 < turns) copy((st + STAGES - 1) % STAGES);
-          asm volatile("cp.async.commit_group;" ::: "memory");
+          for (uint32_t p = 0; p < 8; ++p) x[g][p] = *reinterpret_cast<const uint32_t *>(src + ((g + vsub) * 8 + p) * DP) ^ 0x80808080u;
+        if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
+          give_up();
+          goto done;
         }
+        unsigned char *vt = smem + M::V_AT + buf * M::V_TILE + (quad >> 1) * V_GROUP + (w * 2 + vsub) * 128 + (quad & 1u) * 64;
+#pragma unroll
+        for (uint32_t g = 0; g < VG; ++g) {
+          uint32_t o[4][4];  // [round][pair of positions]
+#pragma unroll
+          for (uint32_t p = 0; p < 4; ++p) {
+            const uint32_t t0 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_a), t1 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_b);
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+              const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
+              o[e][p] = half2_bits(v);
+            }
+          }
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e)
+            *reinterpret_cast<uint4 *>(vt + g * 128 + (e + turn) % 4 * 16) = make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(VFULL + buf));
+        on();
+        // into the place read in the round before this one (all lanes have passed a barrier since)
+        forget();
+        if (t + STAGES - 1 < turns) copy(STAGES - 2);
+        st = st + 1 == STAGES ? 0 : st + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
     }
   } else {
@@ -1063,6 +1072,11 @@ done:
 
 uint32_t block_rows_of(int type) { return type == kOutF32 ? ROWS : 2 * ROWS; }
 
+// Do two chains of softmax warps take turns at the positions?  Then a block's range may be twice as long.
+bool takes_turns(const ClearAttentionArgs &a, int type) {
+  return a.mask && type != kOutF32 && static_cast<uint64_t>(a.tokens) * a.group <= ROWS;
+}
+
 // Splits where the blocks do not fill the SMs: as many as do, of 512 positions at least.  float16 and single precision under lists
 // too long for one accumulator are also split where that fills the last round of blocks better (2 x 2048 queries at 65536
 // positions, float16 4.8 ms with two against 5.5), but no further: splits that turn out empty cost a third of a short context
@@ -1082,7 +1096,13 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
     for (uint32_t n = f.splits + 1; n <= long_lists && n <= room; ++n)
       if (rounds(n) * f.splits * 10 < rounds(f.splits) * n * 9) f.splits = n;
   }
-  f.runs = most > static_cast<uint64_t>(f.splits) * kMostPositions;
+  const uint64_t range = takes_turns(a, type) ? 2 * kMostPositions : kMostPositions;
+  if (takes_turns(a, type) && most > f.splits * range && most <= 256 * range) {
+    // (no runs for them; of a list that is mostly unused the ranges behind the first are empty)
+    if (f.splits == 1) f.least = static_cast<uint32_t>(range);
+    f.splits = static_cast<uint32_t>((most + range - 1) / range);
+  }
+  f.runs = most > f.splits * range;
   attend_place(&f, work);
   return f;
 }
@@ -1093,8 +1113,8 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   if (f.a.mask) {
     kern = f.runs ? attend_many_kernel<T, DP, true, true, ALL> : attend_many_kernel<T, DP, false, true, ALL>;
     if constexpr (!kSplit<T>) {
-      const uint32_t rows = f.a.tokens * f.a.group;
-      if (!f.runs && rows <= ROWS) kern = rows <= ROWS / 2 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
+      if (!f.runs && f.a.tokens * f.a.group <= ROWS)
+        kern = f.a.tokens * f.a.group <= ROWS / 2 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
     }
   }
   const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
@@ -1111,9 +1131,10 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
 }  // namespace
 
 // From 48 rows a cached head on: the other kernel takes 16 at a time (0.65 us an SM for 64 positions), this one 256 in 1.4 us
-// (128 of single precision).
+// (128 of single precision).  Under a mask from 17 on, where the other takes them in two (16 sequences of 4096 positions, 24 rows of
+// 128: 56 us against 92, single precision 89 against 103; 16 rows 57 against 54).
 bool attend_many_takes(const ClearAttentionArgs &a) {
-  return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= 48 && attend_few_takes(a);
+  return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= (a.mask ? 17 : 48) && attend_few_takes(a);
 }
 
 size_t attend_many_bytes(const ClearAttentionArgs &a, int type, uint32_t sms) { return attend_part_bytes(many_args(a, type, nullptr, sms)); }

@@ -129,6 +129,53 @@ def test_tree_attention_scales(lib, dtype, new, group):
         check_tree(lib, dtype, [200, 90], new, 16, 2, group, 128, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("new,group", [(1, 2), (9, 2), (16, 4), (32, 4), (40, 4)])
+@pytest.mark.parametrize("pages_each", [40, 5000, 70000])
+def test_tree_attention_under_long_lists(lib, dtype, new, group, pages_each):
+    """Lists with room for many more positions than there are: what a cache of a long context gives."""
+    lens, page, heads, dim = [new + 200, new + 3, new + 1], 16, 2, 64
+    c, s, table = make_cache(3, lens, page, heads, dim)
+    wide = torch.full((3, pages_each), 1 << 30, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    q, seen = U.rand(4, 3, new, heads * group, dim).to(dtype), D.ancestors(D.random_tree(1, 3, new))
+    out = torch.empty_like(q, device="cuda")
+    lib.tree_attention(q.cuda(), *[t.cuda() for t in (*c, *s)], wide.cuda(), ints(lens).cuda(), D.words(seen).cuda(), out)
+    lib.sync_status()
+    want, size = D.tree_attention(q, *c, *s, table, lens, seen, dim ** -0.5)
+    weights = 2.0 ** -16 if dtype == torch.float32 else 2.0 ** -10
+    assert torch.all((out.cpu().double() - want).abs() <= 1.01 * U.UNIT[dtype] * want.abs() + weights * size + 1e-9)
+
+
+@pytest.mark.parametrize("dtype,context", [(torch.float32, 1 << 16), (torch.float32, 1 << 18), (torch.float16, 1 << 18), (torch.bfloat16, 1 << 18)])
+@pytest.mark.parametrize("new,group", [(2, 4), (8, 4), (24, 4), (48, 4)])
+def test_tree_attention_of_long_contexts(lib, dtype, context, new, group):
+    """Page lists that repeat 2048 positions, values of one sign: what sums lose as they grow would show.  Behind them a chain of
+    drafted positions; bounds as for causal attention of such contexts."""
+    batch, pages, page, dim = 40, 33, 64, 128
+    kc, vc = U.int8(5, pages, 1, page, dim), U.int8(6, pages, 1, page, dim, lo=1)
+    ks, vs = torch.rand(pages, 1, generator=torch.Generator().manual_seed(7)) / 60, torch.rand(pages, 1, generator=torch.Generator().manual_seed(8)) / 60
+    q = U.rand(9, 1, new, group, dim).to(dtype)
+    each = context // page
+    table = torch.cat([(torch.arange(each) * 7 % 32), torch.tensor([32])]).to(torch.int32)     # the drafted ones in page 32
+    mask = D.words(torch.ones(1, new, new).tril().bool()).cuda().expand(batch, -1, -1)
+    out = torch.empty((batch, new, group, dim), dtype=dtype, device="cuda")
+    lib.tree_attention(q.cuda().expand(batch, -1, -1, -1).contiguous(), kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda(),
+                       table.cuda().expand(batch, -1).contiguous(), torch.full((batch,), context + new, dtype=torch.int32, device="cuda"), mask, out)
+    lib.sync_status()
+    # the context's positions `context / 2048` times each: once, with that added to their scores' exponent
+    k = (kc[:32, 0].double() * ks[:32, :, None].double()).flatten(0, 1)
+    v = (vc[:32, 0].double() * vs[:32, :, None].double()).flatten(0, 1)
+    kd, vd = kc[32, 0, :new].double() * ks[32].double(), vc[32, 0, :new].double() * vs[32].double()
+    for t in range(new):
+        for h in range(group):
+            z = torch.cat([k @ q[0, t, h].double() * dim ** -0.5 + math.log(context / 2048), kd[:t + 1] @ q[0, t, h].double() * dim ** -0.5])
+            p = torch.softmax(z, 0)
+            want = p @ torch.cat([v, vd[:t + 1]])       # (all values positive: the sum of p |v| too)
+            bound = 2.0 ** -18 * want if dtype == torch.float32 else (U.UNIT[dtype] + 2.0 ** -10) * want
+            assert torch.all((out[:, t, h].cpu().double() - want).abs() <= bound)
+
+
 @pytest.mark.parametrize("new,group", [(6, 2), (40, 2)])
 @pytest.mark.parametrize("dim", [64, 128, 20])
 def test_tree_attention_never_reads_what_is_masked(lib, new, group, dim):
