@@ -534,8 +534,9 @@ int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, cons
  * all of them (of p itself where nothing is left).
  *   target, draft [batch][nodes][vocab] of `type`, element at b * s[0] + node * s[1] + token with
  *     s = target_strides, draft_strides (HOST arrays): probabilities, in [0, 2], taken as whole
- *     multiples of 2^-56; rows add up to 1 but for rounding.  All sums are exact from there on, so
- *     that equal inputs give equal outputs whatever the sizes around them.
+ *     multiples of 2^-56; rows add up to 1 but for rounding.  Sums are exact from there on, so that equal
+ *     inputs give equal outputs whatever the sizes around them (s q is held to 2^-48 of itself where s is
+ *     neither 0 nor 1, and what is left below 2^-55 then counts as nothing).
  *   tokens, parents int32, uniform float [batch][nodes], in [0, 1), row pitches from 0 on
  *   path int32 [batch][nodes] of pitch path_pitch: the accepted nodes, 0 first, then -1;
  *     count [batch]: how many; next [batch]: the next token

@@ -11,9 +11,13 @@
 // draft rows a child is given, not drawn: accepted where u R < p(x), else its p(x) leaves R, which begins at 1.  The first
 // token whose running sum of what is left passes u_0 of all of it is next.
 //
-// All sums are of whole multiples of 2^-56, so no order changes them, and they are compared as integers.
-// What is read: p(x) and q(x) of every node at once, and whole rows only of nodes whose children have been rejected,
-// twice where they are the last (the second time by one warp).  Latency bound for a few sequences; for many by reading one or two rows of each.
+// All sums are of whole multiples of 2^-56, so no order changes them, and they are compared as integers.  (64 bits all the way: the next
+// token is where a running sum over the vocabulary passes a number, and sums in single precision would now and then pass it at
+// another token.)
+// What is read: p(x) and q(x) of every node at once, and whole rows only where a sum is wanted: of nodes whose children were rejected
+// and of the last one, of that a warp's run again.  Bound by the chain of these steps (nodes, their probabilities, a row at a time, each with a
+// meeting of the cluster) and by 13 instructions a pair of probabilities: a sequence of 5 nodes over 50257 tokens 8 us; 64 of 64
+// nodes over 128256 with draft rows 54 us, of which one target row of each takes 17.
 #include <stdint.h>
 
 #include "clear.h"

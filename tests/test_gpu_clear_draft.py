@@ -489,6 +489,35 @@ def test_verify_rows_of_wider_buffers(lib, dtype, drawn):
     assert torch.equal(paths[:, 2:8].cpu(), want[0]) and bool((paths[:, :2] == 55).all()) and bool((paths[:, 8:] == 55).all())
 
 
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("vocab", [333, 9001])
+def test_verify_target_and_draft_rows_that_lie_differently(lib, dtype, vocab):
+    """Target rows on 16 bytes, draft rows not, and the other way round."""
+    args = drafted(14, 4, 8, vocab, dtype, True, sharp=1.0)
+    want = check_verify(lib, *args)
+    assert int(want.max()) > 1
+    pitch = (vocab + 31) // 16 * 16
+    for off_p, off_q in ((0, 1), (3, 0), (2, 5)):
+        wide = [torch.full((4, 8, pitch), math.nan, dtype=dtype, device="cuda") for _ in range(2)]
+        for w, x, off in zip(wide, args[:2], (off_p, off_q)):
+            w[:, :, off:off + vocab] = x.cuda()
+        check_verify(lib, wide[0][:, :, off_p:off_p + vocab], wide[1][:, :, off_q:off_q + vocab], *args[2:])
+
+
+@pytest.mark.parametrize("batch", [1, 30, 60, 90, 170, 700])
+def test_verify_clusters_of_every_size(lib, batch):
+    """The CTAs of a sequence go by the batch: the same results whatever their number."""
+    args = drafted(15, 10, 6, 16500, torch.float32, True, sharp=1.5)
+    one = run_verify(lib, *[x[:1] for x in args])
+    many = run_verify(lib, *[torch.cat([x] * (-(-batch // 10)))[:batch] for x in args])
+    lib.sync_status()
+    for b in range(10):
+        want = D.verify(*[x[b] for x in args])
+        for i in range(b, batch, 10):
+            assert (many[0][i, :want[1]].tolist(), int(many[1][i]), int(many[2][i])) == want
+    assert all(torch.equal(x, y[:1]) for x, y in zip(one, many))
+
+
 def test_verify_beyond_32_bits(lib):
     """Rows whose places pass 2^32 elements."""
     nodes, vocab = 40, 120_000_000 // 1024
@@ -753,11 +782,11 @@ def test_beyond_32_bits(lib):
 # ------------------------------------------------------------------ together: streams, graphs, two handles
 
 
-def step_state(nodes, seed=1):
+def step_state(nodes, seed=1, vocab=700):
     """What one step over drafted tokens takes: the tree in the cache, its queries, the probabilities behind it."""
     lens = [90 + nodes, 41 + nodes]
     c, s, table = make_cache(seed, lens, 16, 2, 64)
-    target, draft, tokens, parents, uniform = (x.cuda() for x in drafted(seed, 2, nodes, 700, torch.float32, True))
+    target, draft, tokens, parents, uniform = (x.cuda() for x in drafted(seed, 2, nodes, vocab, torch.float32, True))
     n = ints(lens).cuda()
     return dict(c=[t.cuda() for t in (*c, *s)], table=table.cuda(), lengths=n, first=n - nodes, q=U.rand(seed, 2, nodes, 8, 64).half().cuda(),
                 target=target, draft=draft, tokens=tokens, parents=parents, uniform=uniform,
@@ -777,14 +806,14 @@ def step(lib, t, stream=None):
 RESULTS = ("mask", "out", "path", "count", "following", "k", "v")
 
 
-@pytest.mark.parametrize("nodes", [5, 40])
-def test_a_step_on_other_streams_handles_and_in_graphs(lib, nodes):
+@pytest.mark.parametrize("nodes,vocab", [(5, 700), (40, 700), (12, 20000)])
+def test_a_step_on_other_streams_handles_and_in_graphs(lib, nodes, vocab):
     from paper_2609_16915_gb300 import clear
-    a = step_state(nodes)
+    a = step_state(nodes, vocab=vocab)
     step(lib, a)
     lib.sync_status()
     want = {n: a[n].clone() for n in RESULTS}
-    pages, table = [t.cpu() for t in step_state(nodes)["c"]], a["table"].cpu()
+    pages, table = [t.cpu() for t in step_state(nodes, vocab=vocab)["c"]], a["table"].cpu()
     ref, size = D.tree_attention(a["q"].cpu(), *pages, table, a["lengths"].tolist(), D.ancestors(a["parents"].cpu()), 0.125)
     assert torch.all((a["out"].cpu().double() - ref).abs() <= U.UNIT[torch.float16] * ref.abs() + 2.0 ** -10 * size + 1e-9)
     for b in range(2):
@@ -796,7 +825,7 @@ def test_a_step_on_other_streams_handles_and_in_graphs(lib, nodes):
         assert torch.equal(a[name].cpu(), D.read(held, scale, table, a["first"].tolist(), a["lengths"].tolist(), torch.zeros(2, 140, 2, 64)))
 
     # two handles at once, on streams of their own
-    others = [(clear.Clear(), step_state(nodes), torch.cuda.Stream()) for _ in range(2)]
+    others = [(clear.Clear(), step_state(nodes, vocab=vocab), torch.cuda.Stream()) for _ in range(2)]
     torch.cuda.synchronize()
     for handle, t, s in others:
         step(handle, t, stream=s)
@@ -804,7 +833,7 @@ def test_a_step_on_other_streams_handles_and_in_graphs(lib, nodes):
         handle.sync_status(s)
         assert all(torch.equal(t[n], want[n]) for n in RESULTS)
 
-    b = step_state(nodes)
+    b = step_state(nodes, vocab=vocab)
     start = [x.clone() for x in b["c"]]
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
