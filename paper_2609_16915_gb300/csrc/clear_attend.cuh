@@ -14,6 +14,7 @@ struct AttendArgs {
   uint32_t first, count;    // cached heads, of all sequences, that this launch takes
   uint32_t splits, groups;  // ranges of a sequence's positions at most, row groups of a cached head
   uint32_t least;           // positions of a range at least
+  bool by_length;           // blocks of the longest sequences first
   bool runs;                // a range may be longer than one accumulator takes: it adds up in the place of its partial result
 };
 

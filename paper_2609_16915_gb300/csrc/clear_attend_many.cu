@@ -180,6 +180,23 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
+// The sequence that is the `wanted`-th by length, longest first: every block sorts for itself.  (No memory is set aside for it:
+// `lengths` and `found` are free until the block begins its work; whoever writes to `found` next does so behind another barrier.)
+constexpr uint32_t kMostSorted = 128;
+__device__ __forceinline__ uint32_t place_by_length(const ClearAttentionArgs &a, uint32_t wanted, int32_t *lengths, int32_t *found) {
+  const uint32_t t = threadIdx.x;
+  if (t < a.batch) lengths[t] = a.lengths[t];
+  __syncthreads();
+  if (t < a.batch) {
+    const int32_t own = lengths[t];
+    uint32_t longer = 0;
+    for (uint32_t i = 0; i < a.batch; ++i) longer += lengths[i] > own || (lengths[i] == own && i < t);
+    if (longer == wanted) *found = static_cast<int32_t>(t);
+  }
+  __syncthreads();
+  return static_cast<uint32_t>(*found);
+}
+
 // RUNS: a block's range may be longer than one accumulator takes.  (A kernel of its own: its registers cost shorter ranges 3 %.)
 // TREE: under a mask.  A row sees every position before the drafted ones, and of those the bits of its own row of the mask.
 // TURNS: the rows fill one row tile, and the two groups of softmax warps take turns at the positions, each with scores and outputs of its
@@ -233,7 +250,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
 
   // (the blocks with the most positions first)
   const uint32_t split = blockIdx.x % f.splits, own_head = blockIdx.x / f.splits % f.count, bh = f.first + own_head;
-  const uint32_t kh = bh % a.heads, b = bh / a.heads, block = f.groups - 1 - blockIdx.x / f.splits / f.count;
+  const uint32_t kh = bh % a.heads, b = TREE && f.by_length ? place_by_length(a, bh / a.heads, reinterpret_cast<int32_t *>(smem), s_top) : bh / a.heads, block = f.groups - 1 - blockIdx.x / f.splits / f.count;
   const uint32_t rows = a.tokens * a.group, row0 = block * BLOCK_ROWS;
   int64_t len = a.lengths[b];
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens;
@@ -491,8 +508,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         const uint32_t buf = j % 8, two = r * 2 + i % 2, s_tile = tmem + lanes + two * POS;
         // (the same for the warp)
         const uint32_t first = start + j * POS + half * COLS;  // this half's first position
-        uint32_t bits = 0;                                     // TREE: of its 32 positions, those that the row sees
-        if constexpr (TREE) {
+        uint32_t bits = ~0u;                                   // TREE: of its 32 positions, those that the row sees
+        if (TREE && static_cast<int32_t>(first + COLS - 1) > last) {
           const int32_t from = static_cast<int32_t>(first) - last - 1;  // among the drafted ones
           bits = __funnelshift_r(mask_word(mask, a.tokens, from >> 5), mask_word(mask, a.tokens, (from >> 5) + 1), from & 31);
         }
@@ -1083,7 +1100,7 @@ bool takes_turns(const ClearAttentionArgs &a, int type) {
 // (1 x 1024 at 1024 positions under lists for 131072, bfloat16 46 us with four against 29; 8 x 2048 at 2048, float16 0.97 ms against
 // 0.45).
 AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t sms) {
-  AttendArgs f{a, nullptr, nullptr, 0, 0, 1, 1, 512, false};
+  AttendArgs f{a, nullptr, nullptr, 0, 0, 1, 1, 512, false, false};
   const uint32_t block = block_rows_of(type);
   f.groups = (a.tokens * a.group + block - 1) / block;
   const uint64_t blocks = static_cast<uint64_t>(a.batch) * a.heads * f.groups, most = static_cast<uint64_t>(a.table_pitch) * a.page_tokens;
@@ -1103,6 +1120,8 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
     f.splits = static_cast<uint32_t>((most + range - 1) / range);
   }
   f.runs = most > f.splits * range;
+  // uneven sequences over more than one round of blocks (32 of 64 drafted tokens, up to 8192 positions: 161 us, in the batch's order 194)
+  f.by_length = a.mask && f.splits == 1 && blocks > sms && a.batch > 1 && a.batch <= kMostSorted;
   attend_place(&f, work);
   return f;
 }

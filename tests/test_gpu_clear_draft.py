@@ -107,6 +107,14 @@ def test_tree_attention(lib, dtype, lens, new, page, heads, group, dim):
 
 
 @pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("batch,new,group", [(100, 20, 1), (100, 33, 2), (100, 70, 4), (128, 9, 8), (129, 9, 8), (300, 18, 1)])
+def test_tree_attention_of_many_uneven_sequences(lib, dtype, batch, new, group):
+    """More blocks than run at once, equal lengths, sequences shorter than their trees and empty ones among them."""
+    lens = [new + (i * 37) % 90 if i % 7 else i % 5 for i in range(batch)]
+    check_tree(lib, dtype, lens, new, 16, 2, group, 64)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
 @pytest.mark.parametrize("lens,new,page,heads,group,dim", [
     ([40, 3, 0, 70], 40, 16, 2, 4, 128),        # rows before the first position among them
     ([13, 12], 13, 16, 1, 1, 64), ([65, 31], 64, 32, 2, 2, 96), ([50, 20], 33, 24, 1, 3, 20), ([300, 260], 257, 64, 1, 1, 64)])
