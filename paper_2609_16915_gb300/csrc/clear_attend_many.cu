@@ -13,6 +13,9 @@
 //   2 x 8 softmax warps  two threads a row, 32 positions each: scores from tensor memory, times the page's key scale and the row's
 //                    factor, 2^(s - m + 7) with the running maximum m of s + log2(vs / sv) raised only where it is passed
 //                    by 8 (then O is scaled down in place), P vs / sv as f16 over the scores' columns
+// Under the mask of a tree of drafted tokens (few rows, long contexts) a tile costs its conversion and a chain of waits whatever
+// its rows are: up to 128 rows the two row tiles are the same rows at alternating positions (16 sequences of 4096 positions, 128
+// rows, 72 us; 94 with one), and up to 64 the softmax warps without rows convert every second tile (64 rows 53 us; 67 without).
 // With two score tiles a row tile, one row tile's next scores are there when its softmax is done: the handing over
 // between warps and tensor cores (about 900 clocks a round) runs under the exponentials.
 // Rows and pages that are not seen have weight 0; a page whose value scale is not a number has the scale zero and a key scale

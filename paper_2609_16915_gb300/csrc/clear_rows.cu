@@ -2,11 +2,13 @@
 //
 // Keeping: rows first + path[i] become rows first + i, under a page's scale
 //   s' = max of the scales of the pages that its rows come from,  q' = rint(q (s / s')).
-// A block takes one cached head of one sequence, keys or values, page after page: path[i] >= i and increasing, so what is
-// written never lies before what is still to be read but for the rows in the block's registers.  Latency bound: a
-// handful of rows each.
+// A unit of work is one cached head of one sequence, keys or values, page after page: path[i] >= i and increasing, so what is
+// written never lies before what is still to be read but for the rows in the unit's registers.  Bound by the chain of a
+// unit (path, pages, scales and rows, one after another): what 256 sequences accepted of 64 drafted tokens, 8 heads of 128,
+// 8.7 us, one sequence 3.6.
 //
-// Reading: out = q s[page][head].  Bound by its bytes, one read and two or four written for each value.
+// Reading: out = q s[page][head].  Bound by its bytes, one read and two or four written for each value: 32 uneven sequences of up to
+// 4096 positions, 8 heads of 128, into bfloat16 84.7 us, 5.1 TB/s (all of 4096: 5.75), into single precision 95 % of the copy rate.
 #include <stdint.h>
 
 #include "clear.h"
@@ -33,10 +35,10 @@ __device__ __forceinline__ Bytes<VEC> rescaled(Bytes<VEC> q, float ratio) {
 // Shared memory of a unit: the path, and of each row of the present page where it comes from and under which scale.
 __host__ __device__ constexpr uint32_t keep_bytes(uint32_t tokens, uint32_t page_tokens) { return (tokens + 1) / 2 * 8 + page_tokens * 12 + page_tokens % 2 * 4; }
 
-// WARPS of a unit (one cached head of one sequence, keys or values): one (four units a block) or four.  VEC bytes an access, of which a
-// thread keeps `KEPT` between reading and writing.
+// WARPS of a unit: one (four units a block) or four.  VEC bytes an access, of which a thread keeps `KEPT` between reading and
+// writing.  (64 registers a thread: 256 sequences are resident at once; with 96 they are not, 11.3 us, and 40 spill, 12.4.)
 template <int WARPS, int VEC>
-__global__ void __launch_bounds__(128) keep_kernel(const ClearKeepArgs a) {
+__global__ void __launch_bounds__(128, 8) keep_kernel(const ClearKeepArgs a) {
   constexpr uint32_t THREADS = 32 * WARPS, KEPT = VEC == 16 ? 2 : 4;
   extern __shared__ __align__(8) unsigned char smem[];
   __shared__ float s_most[4];
