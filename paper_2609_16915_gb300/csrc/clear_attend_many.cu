@@ -1131,15 +1131,22 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  auto kern = f.runs ? attend_many_kernel<T, DP, true, false, ALL> : attend_many_kernel<T, DP, false, false, ALL>;
-  if (f.a.mask) {
+  static std::atomic<uint64_t> told[6] = {};  // of each kernel
+  auto kern = attend_many_kernel<T, DP, false, false, ALL>;
+  uint32_t which = f.runs;
+  if (!f.a.mask) {
+    if (f.runs) kern = attend_many_kernel<T, DP, true, false, ALL>;
+  } else {
+    which += 2;
     kern = f.runs ? attend_many_kernel<T, DP, true, true, ALL> : attend_many_kernel<T, DP, false, true, ALL>;
     if constexpr (!kSplit<T>) {
-      if (!f.runs && f.a.tokens * f.a.group <= ROWS)
-        kern = f.a.tokens * f.a.group <= ROWS / 2 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
+      if (!f.runs && f.a.tokens * f.a.group <= ROWS) {
+        which = f.a.tokens * f.a.group <= ROWS / 2 ? 5 : 4;
+        kern = which == 5 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
+      }
     }
   }
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
+  const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kern), Many<DP>::SMEM, &told[which]);
   if (e != cudaSuccess) return e;
   kern<<<f.count * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
   return cudaGetLastError();

@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
     s_p[c] = up >= 0 ? fixed(to_float(target[static_cast<int64_t>(up) * a.target_strides[1] + x]), bad) : 0;
     if constexpr (DRAFT) s_q[c] = up >= 0 ? fixed(to_float(draft[static_cast<int64_t>(up) * a.draft_strides[1] + x]), bad) : 0;
   }
+  __syncwarp();  // (here and below: the cluster's barrier wants whole warps)
   if (ranks > 1) {
     cluster_sync_shared();
     for (uint32_t c = tid; c < nodes; c += threads) {
@@ -293,6 +294,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
     before = 0;
     if (ranks > 1) {
       if (tid == 0) s_total[turn] = total;
+      __syncwarp();
       cluster_sync_shared();
       const uint32_t at = smem_addr(&s_total[turn]);
       const uint64_t of = lane < ranks ? dsmem_ld_u64(dsmem_map(at, lane)) : 0;
@@ -425,6 +427,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
       a.next[b] = static_cast<int32_t>(x);
     }
   }
+  __syncwarp();
   if (ranks > 1) cluster_sync_shared();  // (the others' sums are read until here)
 }
 
