@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(128, 8) keep_kernel(const ClearKeepArgs a) {
 
 template <int VEC>
 cudaError_t launch_keep(const ClearKeepArgs &a, cudaStream_t s) {
-  // a warp a unit where its share of a path is short; smem: at most 16 KB a unit, 64 KB never
+  // a warp a unit where the path is short (256 sequences of 64 tokens 9 us against 19, 64 of 200 5.6 against 5.2); shared memory: 32 KB
+  // at most
   const uint32_t bytes = keep_bytes(a.tokens, a.page_tokens);
   if (a.tokens <= 128 && bytes <= 8192)
     keep_kernel<1, VEC><<<dim3((2 * a.heads + 3) / 4, a.batch), 128, 4 * bytes, s>>>(a);
