@@ -58,12 +58,11 @@ constexpr uint32_t RUN = kMostPositions / POS;
 static_assert(RUN % FOLD == 0, "runs are whole folds");
 constexpr float kRaise = 8.0f, kLift = 7.0f;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr uint32_t V_GROUP = POS * 16;  // bytes of eight dimensions of a value tile
 
 template <int DP>
 struct Many {
-  static constexpr uint32_t Q_TILE = ROWS * DP * 2, K_TILE = POS * DP * 2, V_TILE = DP / 8 * V_GROUP, RAW = POS * DP;
-  static constexpr uint32_t K_AT = 2 * Q_TILE, V_AT = K_AT + RING * K_TILE, RAW_AT = V_AT + RING * V_TILE;
+  static constexpr uint32_t Q_TILE = ROWS * DP * 2, TILE = POS * DP * 2, RAW = POS * DP;
+  static constexpr uint32_t K_AT = 2 * Q_TILE, V_AT = K_AT + RING * TILE, RAW_AT = V_AT + RING * TILE;
   static constexpr uint32_t SMEM = RAW_AT + STAGED * 2 * RAW;
   static constexpr uint32_t O_COL = 4 * POS;  // score tiles of the two row tiles: two of 64 columns each
 };
@@ -86,8 +85,17 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, uint32_t group) {
          (static_cast<uint64_t>(group >> 4) << 32) | (1ull << 46);
 }
 
-// kind::f16: D f32, A and B f16, both K-major, M = 128
-__host__ __device__ constexpr uint32_t idesc(uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
+// The same memory as a B operand whose N is what lies together (values: 8 positions x 16 bytes of dimensions a core matrix): N-adjacent
+// core matrices 128 bytes apart, K-adjacent ones (8 positions) `group` bytes apart.
+__device__ __forceinline__ uint64_t desc_across(uint32_t saddr, uint32_t group) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(group >> 4) << 16) |
+         (static_cast<uint64_t>(128u >> 4) << 32) | (1ull << 46);
+}
+
+// kind::f16: D f32, A and B f16, A K-major, B K-major or `across`, M = 128
+__host__ __device__ constexpr uint32_t idesc(uint32_t n, bool across = false) {
+  return (1u << 4) | (across ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
 
 // One lane of the warp, the same each time.  The MMA warp runs converged and its instructions are predicated on this
 // lane, so that descriptors stay in uniform registers: with one lane branching off, issuing a product cost about 60 clocks.
@@ -677,7 +685,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       constexpr uint32_t PITCH = DP + 4;
       float *joined = reinterpret_cast<float *>(smem + M::K_AT) + row_in * PITCH + half * (DP / 2);
       float2 *s_other = reinterpret_cast<float2 *>(smem + M::K_AT + ROWS * PITCH * 4);  // chain 1's sum and maximum
-      static_assert(ROWS * (PITCH * 4 + 8) <= RING * (M::K_TILE + M::V_TILE), "outputs of a row tile fit where keys and values were");
+      static_assert(ROWS * (PITCH * 4 + 8) <= 2 * RING * M::TILE, "outputs of a row tile fit where keys and values were");
       float own_part = 1.0f, other_part = 0.0f;
       if constexpr (PAIR) {
         if (r == 1) {
@@ -802,20 +810,21 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     // the code is a quarter of what constant places, in turns unrolled, would make it, and three roles share the instruction caches.)
     float ks[STAGES - 1] = {}, vs[STAGES - 1] = {};
     bool skip[STAGES - 1] = {};
-    // a warp's share of a staged tile: keys [row of 8][chunk of 16 bytes] by the lane that reads them, values row by row
+    // a warp's share of a staged tile: row by row, as a warp copies it (halves of eight rows at a time take longer)
     const auto raw_at = [&](uint32_t st) {
       const uint32_t of = STEP * st + set, share = (keys ? 0 : M::RAW) + w * (16 * DP);
       return (WIDE && of >= STAGED ? M::Q_TILE + (of - STAGED) * (2 * M::RAW) : M::RAW_AT + of * (2 * M::RAW)) + share;
     };
     static_assert(2 * 2 * M::RAW <= M::Q_TILE, "two stages fit where the second row tile's queries are");
-    const uint32_t kr = lane % 8, kc = lane / 8;  // a key row of 8, a chunk of four
-    // A lane's pieces of a tile: every DP / 64th of its keys 8 rows on (the others 64 bytes on), of its values 512 / DP rows on.  What lies
-    // behind the head's end meets zeros, or goes where nobody looks: it is not copied, nor are pages out of range.
+    // A lane reads row kr of 8 and every fourth chunk of 16 bytes from kc on, moved by the row so that eight lanes meet every bank once.
+    const uint32_t kr = lane % 8, kc = lane / 8;
+    const auto chunk = [&](uint32_t i) { return (kc + 4 * (i % (DP / 64)) + (DP == 128 ? kr : kr / 2)) % (DP / 16); };
+    // A lane's pieces of a tile, 512 / DP rows from each other.  What lies behind the head's end meets zeros, or goes where nobody
+    // looks: it is not copied, nor are pages out of range.
     const int64_t line = a.cache_strides[2];
-    const uint32_t piece_row = keys ? kr : lane / (DP / 16), piece_d = keys ? kc * 16 : lane % (DP / 16) * 16;
-    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + piece_row * line + piece_d;
-    const int64_t piece_on = keys ? 8 * line : 512 / DP * line;
-    const bool near = piece_d < a.dim, far = keys ? piece_d + 64 < a.dim : near;  // (dim is a multiple of 16)
+    const uint32_t piece_d = lane % (DP / 16) * 16;
+    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + lane / (DP / 16) * line + piece_d;
+    const bool inside = piece_d < a.dim;  // (dim is a multiple of 16)
     uint32_t to_stage = 0;  // of the next tile to copy
     const auto copy = [&](uint32_t at) {  // (at: its place in the lists, a constant)
       const int32_t page = pages[0];
@@ -832,9 +841,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         const uint32_t dst = base + raw_at(to_stage) + lane * 16;
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
-          if (keys && DP == 128 ? (i % 2 ? far : near) : near)
-            copy_async(dst + i * 512, keys && DP == 128 ? src + i % 2 * 64 : src);
-          if (!keys || DP == 64 || i % 2) src += piece_on;
+          if (inside) copy_async(dst + i * 512, src);
+          src += 512 / DP * line;
         }
       }
       next(slot, row);
@@ -871,118 +879,65 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     int32_t unit = 0;  // of sv
     float per_sv = 1.0f;
     uint32_t buf = set;
-    const auto on = [&]() { buf = buf + STEP >= RING ? buf + STEP - RING : buf + STEP; };
-    if (keys) {
-      if (turns == 0) asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");  // (as the others, below)
-      uint32_t st = 0;
+    if (keys && turns == 0) asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");  // (as the others, below)
+    uint32_t st = 0;
 #pragma unroll 1
-      for (uint32_t t = 0; t < turns; ++t) {
-        const uint32_t j = STEP * t + set;
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-        const unsigned char *src = smem + raw_at(st) + lane * 16;
-        uint4 k[DP / 32];
+    for (uint32_t t = 0; t < turns; ++t) {
+      const uint32_t j = STEP * t + set;
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncwarp();
+      const unsigned char *src = smem + raw_at(st) + kr * DP;
+      uint4 x[DP / 32];
 #pragma unroll
-        for (uint32_t i = 0; i < DP / 32; ++i) k[i] = *reinterpret_cast<const uint4 *>(src + i * 512);
-        // the keys that lay here were tile j - 3's, used with tile j - 5's values (PAIR: j - 7's; the fourth tile's before the first values'),
-        // or among the first two (three)
-        const uint32_t with = PAIR && j == 6 ? 0 : j - RING - AHEAD;
-        if (j >= RING && !__all_sync(0xffffffffu, j >= RING + AHEAD || (PAIR && j == 6) ? wait_quick(bar(USED + with % RING), (with / RING) & 1u)
-                                                                                      : wait_quick(bar(FIRST), 0))) {
-          give_up();
-          goto done;
-        }
-        // 1024 + (k + 128) by byte permute, times the scale's sign, minus 1152 times it
-        const __half2 sg = bits_half2(ks[0] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
-        unsigned char *kt = smem + M::K_AT + buf * M::K_TILE + w * 2 * (DP * 16) + kc * 256 + kr * 16;
-#pragma unroll
-        for (uint32_t i = 0; i < DP / 32; ++i) {
-          const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
-          uint32_t o[8];
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e) {
-            const uint32_t u = x[e] ^ 0x80808080u;
-            o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
-            o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
-          }
-          unsigned char *dst = kt + i / (DP / 64) * (DP * 16) + i % (DP / 64) * 1024;
-          *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-          *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
-        }
-        if (t == 0) {  // (the values' warps have seen the scales)
-          asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
-          unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
-          per_sv = scalbnf(1.0f, -unit);
-          if (set == 0 && w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
-        }
-        if (lane == 0) {
-          // (a value scale that is a NaN or an infinity: no number)
-          const bool number = fabsf(vs[0]) < -neg_inf();
-          s_ks[j % 8][w] = number ? fabsf(ks[0]) : __int_as_float(0x7fc00000);
-          s_skip[j % 8][w] = skip[0];
-          s_vr[j % 8][w] = number ? vs[0] * per_sv : 0.0f;
-          s_above[j % 8][w] = number ? scale_above(vs[0], unit) : 0.0f;
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(KFULL + buf));
-        on();
-        // into the place read in the round before this one
-        forget();
-        if (t + STAGES - 1 < turns) copy(STAGES - 2);
-        st = st + 1 == STAGES ? 0 : st + 1;
-        asm volatile("cp.async.commit_group;" ::: "memory");
+      for (uint32_t i = 0; i < DP / 32; ++i) x[i] = *reinterpret_cast<const uint4 *>(src + i / (DP / 64) * (8 * DP) + chunk(i) * 16);
+      // What lay here was tile j - 3's.  Values: used in its turn; keys: with tile j - 5's values (PAIR: j - 7's; the fourth tile's before
+      // the first values'), or among the first two (three).
+      const uint32_t behind = keys ? RING + AHEAD : RING, with = PAIR && keys && j == 6 ? 0 : j - behind;
+      if (j >= RING && !__all_sync(0xffffffffu, j >= behind || (PAIR && j == 6) ? wait_quick(bar(USED + with % RING), (with / RING) & 1u)
+                                                                               : wait_quick(bar(FIRST), 0))) {
+        give_up();
+        goto done;
       }
-    } else {
-      constexpr uint32_t VG = DP == 128 ? 2 : 1;  // groups of 8 positions that a lane takes in turn
-      const uint32_t quad = lane % (DP / 4), vsub = DP == 128 ? 0 : lane / 16;
-      // A lane transposes four dimensions of eight positions, rotated by its place so that the eight lanes of a store
-      // phase write the eight rows of a core matrix: dimension (e + turn) % 4 of its four in round e.
-      const uint32_t turn = lane / 2 % 4;
-      const uint32_t sel_a = turn == 0 ? 0x5140u : turn == 1 ? 0x6251u : turn == 2 ? 0x7362u : 0x4073u;
-      const uint32_t sel_b = turn == 0 ? 0x7362u : turn == 1 ? 0x4073u : turn == 2 ? 0x5140u : 0x6251u;
-      uint32_t st = 0;
-#pragma unroll 1
-      for (uint32_t t = 0; t < turns; ++t) {
-        const uint32_t j = STEP * t + set;
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-        __syncwarp();
-        const unsigned char *src = smem + raw_at(st) + quad * 4;
-        uint32_t x[VG][8];
+      // 1024 + (x + 128) by byte permute, times the sign of the keys' scale, minus 1152 times it
+      const __half2 sg = bits_half2(keys && ks[0] < 0.0f ? 0xbc00bc00u : 0x3c003c00u), so = __hneg2(__hmul2(sg, off));
+      unsigned char *tile = smem + (keys ? M::K_AT : M::V_AT) + buf * M::TILE + w * 2 * (DP * 16) + kr * 16;
 #pragma unroll
-        for (uint32_t g = 0; g < VG; ++g)
+      for (uint32_t i = 0; i < DP / 32; ++i) {
+        const uint32_t word[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t o[8];
 #pragma unroll
-          for (uint32_t p = 0; p < 8; ++p) x[g][p] = *reinterpret_cast<const uint32_t *>(src + ((g + vsub) * 8 + p) * DP) ^ 0x80808080u;
-        if (j >= RING && !__all_sync(0xffffffffu, wait_quick(bar(USED + buf), ((j - RING) / RING) & 1u))) {
-          give_up();
-          goto done;
+        for (uint32_t e = 0; e < 4; ++e) {
+          const uint32_t u = word[e] ^ 0x80808080u;
+          o[2 * e] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4140)), sg, so));
+          o[2 * e + 1] = half2_bits(__hfma2(bits_half2(__byte_perm(u, 0x64646464u, 0x4342)), sg, so));
         }
-        unsigned char *vt = smem + M::V_AT + buf * M::V_TILE + (quad >> 1) * V_GROUP + (w * 2 + vsub) * 128 + (quad & 1u) * 64;
-#pragma unroll
-        for (uint32_t g = 0; g < VG; ++g) {
-          uint32_t o[4][4];  // [round][pair of positions]
-#pragma unroll
-          for (uint32_t p = 0; p < 4; ++p) {
-            const uint32_t t0 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_a), t1 = __byte_perm(x[g][2 * p], x[g][2 * p + 1], sel_b);
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-              const __half2 v = __hsub2(bits_half2(__byte_perm(e < 2 ? t0 : t1, 0x64646464u, e % 2 ? 0x4342 : 0x4140)), off);
-              o[e][p] = half2_bits(v);
-            }
-          }
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e)
-            *reinterpret_cast<uint4 *>(vt + g * 128 + (e + turn) % 4 * 16) = make_uint4(o[e][0], o[e][1], o[e][2], o[e][3]);
-        }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(VFULL + buf));
-        on();
-        // into the place read in the round before this one (all lanes have passed a barrier since)
-        forget();
-        if (t + STAGES - 1 < turns) copy(STAGES - 2);
-        st = st + 1 == STAGES ? 0 : st + 1;
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        unsigned char *dst = tile + i / (DP / 64) * (DP * 16) + chunk(i) * 256;
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4 *>(dst + 128) = make_uint4(o[4], o[5], o[6], o[7]);
       }
+      if (keys && t == 0) {  // (the values' warps have seen the scales)
+        asm volatile("bar.sync 1, %0;" ::"n"(WIDE ? 384 : 256) : "memory");
+        unit = scale_unit(max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3])));
+        per_sv = scalbnf(1.0f, -unit);
+        if (set == 0 && w == 0 && lane == 0) s_sv = scalbnf(1.0f, unit);
+      }
+      if (keys && lane == 0) {
+        // (a value scale that is a NaN or an infinity: no number)
+        const bool number = fabsf(vs[0]) < -neg_inf();
+        s_ks[j % 8][w] = number ? fabsf(ks[0]) : __int_as_float(0x7fc00000);
+        s_skip[j % 8][w] = skip[0];
+        s_vr[j % 8][w] = number ? vs[0] * per_sv : 0.0f;
+        s_above[j % 8][w] = number ? scale_above(vs[0], unit) : 0.0f;
+      }
+      fence_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar((keys ? KFULL : VFULL) + buf));
+      buf = buf + STEP >= RING ? buf + STEP - RING : buf + STEP;
+      // into the place read in the round before this one (all lanes have passed a barrier since)
+      forget();
+      if (t + STAGES - 1 < turns) copy(STAGES - 2);
+      st = st + 1 == STAGES ? 0 : st + 1;
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
   } else {
     __syncwarp();
@@ -994,7 +949,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const auto ready = [&](uint32_t i, uint32_t parity) { return __all_sync(0xffffffffu, wait_quick(bar(i), parity)); };
     const auto scores = [&](uint32_t r, uint32_t i, uint32_t kbuf) {  // of the row tile's, or the chain's, tile i
       const uint32_t two = r * 2 + i % 2;
-      const uint64_t qd = desc_of(base + (PAIR ? 0 : r * M::Q_TILE), DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::K_TILE, DP * 16);
+      const uint64_t qd = desc_of(base + (PAIR ? 0 : r * M::Q_TILE), DP * 16), kd = desc_of(base + M::K_AT + kbuf * M::TILE, DP * 16);
       if constexpr (SPLIT) {  // (the small products first: less is cut off)
         const uint64_t rest = desc_of(base + M::Q_TILE, DP * 16);
 #pragma unroll
@@ -1030,7 +985,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         give_up();
         goto done;
       }
-      const uint64_t vd = desc_of(base + M::V_AT + vbuf * M::V_TILE, V_GROUP);
+      const uint64_t vd = desc_across(base + M::V_AT + vbuf * M::TILE, DP * 16);
 #pragma unroll
       for (uint32_t each = 0; each < (PAIR ? 1 : 2); ++each) {
         if (each >= row_tiles) break;
@@ -1042,11 +997,11 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_after();
 #pragma unroll
         for (uint32_t k = 0; k < POS / 16; ++k)
-          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * 16u, idesc(DP), ((SPLIT ? j % FOLD : tile_of(i)) | k) != 0, elect);
+          mma_ts(tmem + M::O_COL + r * DP, tmem + two * POS + k * 8u, vd + k * (2u * DP), idesc(DP, true), ((SPLIT ? j % FOLD : tile_of(i)) | k) != 0, elect);
         if constexpr (FINE) {
 #pragma unroll
           for (uint32_t k = 0; k < POS / 16; ++k)
-            mma_ts(tmem + M::O_COL + (SPLIT ? DP : r * DP), tmem + two * POS + POS / 2 + k * 8u, vd + k * 16u, idesc(DP), !SPLIT || (j % FOLD | k) != 0,
+            mma_ts(tmem + M::O_COL + (SPLIT ? DP : r * DP), tmem + two * POS + POS / 2 + k * 8u, vd + k * (2u * DP), idesc(DP, true), !SPLIT || (j % FOLD | k) != 0,
                      elect);
         }
         if (j + AHEAD < n)
