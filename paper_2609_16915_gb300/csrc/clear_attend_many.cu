@@ -821,23 +821,23 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     const auto chunk = [&](uint32_t i) { return (kc + 4 * (i % (DP / 64)) + (DP == 128 ? kr : kr / 2)) % (DP / 16); };
     // A lane's pieces of a tile, 512 / DP rows from each other.  What lies behind the head's end meets zeros, or goes where nobody
     // looks: it is not copied, nor are pages out of range.
-    const int64_t line = a.cache_strides[2];
+    const uint32_t line = static_cast<uint32_t>(a.cache_strides[2]);  // (below 2^26: attend_few_takes)
     const uint32_t piece_d = lane % (DP / 16) * 16;
-    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + lane / (DP / 16) * line + piece_d;
+    const int8_t *cache = (keys ? a.k_cache : a.v_cache) + static_cast<int64_t>(kh) * a.cache_strides[1] + lane / (DP / 16) * static_cast<uint64_t>(line) + piece_d;
     const bool inside = piece_d < a.dim;  // (dim is a multiple of 16)
     uint32_t to_stage = 0;  // of the next tile to copy
     const auto copy = [&](uint32_t at) {  // (at: its place in the lists, a constant)
-      const int32_t page = pages[0];
-      const bool in = page >= 0 && static_cast<uint32_t>(page) < a.pages;
+      const uint32_t page = static_cast<uint32_t>(pages[0]);  // (a negative one is too large)
+      const bool in = page < a.pages;
       skip[at] = slot < slots_end && !in;
       ks[at] = vs[at] = 0.0f;
       if (in) {
         if (keys) {
-          const size_t sc = static_cast<size_t>(page) * a.heads + kh;
+          const uint64_t sc = static_cast<uint64_t>(page) * a.heads + kh;
           ks[at] = a.k_scale[sc];
           vs[at] = a.v_scale[sc];
         }
-        const int8_t *src = cache + (page * a.cache_strides[0] + row * line);
+        const int8_t *src = cache + (page * static_cast<uint64_t>(a.cache_strides[0]) + static_cast<uint64_t>(row) * line);
         const uint32_t dst = base + raw_at(to_stage) + lane * 16;
 #pragma unroll
         for (uint32_t i = 0; i < DP / 32; ++i) {
