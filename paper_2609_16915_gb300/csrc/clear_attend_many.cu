@@ -245,11 +245,10 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
   __shared__ __align__(8) uint64_t bars[BARS];
   __shared__ uint32_t tmem_slot, s_fail;
   __shared__ uint32_t s_quit[TILE_WARPS];  // the meeting at which one of two softmax warps gave up
-  // of the last eight tiles (the conversion is at most four ahead of a softmax), by groups of 16 positions: key
-  // scales, pages out of range
-  __shared__ float s_ks[8][POS / 16];
-  __shared__ uint32_t s_skip[8][POS / 16];
-  __shared__ float s_vr[8][POS / 16], s_above[8][POS / 16];  // value scales over sv, and what they add to scores in the running maximum
+  // of the last eight tiles (the conversion is at most four ahead of a softmax), by groups of 16 positions: key scales (below zero: a
+  // page out of range) and what the value scales add to scores in the running maximum; value scales over sv
+  __shared__ __align__(16) float2 s_ka[8][POS / 16];
+  __shared__ __align__(8) float s_vr[8][POS / 16];
   __shared__ int32_t s_top[4];
   __shared__ float s_sv;
   // what the two threads of a row exchange; before the first tile, the power of two of each row's queries
@@ -351,7 +350,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       pass();
       give_up();
       s_quit[pair] = meetings + 1;
-      meet(false);
+      meet(true);  // (the other looks where a row is raised)
     };
     // ---- the warp's 16 queries, each brought to [1, 2) by a power of two, as f16: eight rows x four chunks of
     // eight dimensions at a time ----
@@ -531,16 +530,16 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         fence_after();
         float v[COLS];
         tmem_ld32(s_tile + half * COLS, v);
-        const bool part = __any_sync(0xffffffffu, (s_skip[buf][half * 2] | s_skip[buf][half * 2 + 1]) != 0 ||
-                                                      static_cast<int32_t>(first + COLS - 1) > last);
-        float kf[2] = {s_ks[buf][half * 2] * factor, s_ks[buf][half * 2 + 1] * factor};
-        const float above[2] = {s_above[buf][half * 2], s_above[buf][half * 2 + 1]};
+        const float4 ka = *reinterpret_cast<const float4 *>(&s_ka[buf][half * 2]);
+        const bool part = __any_sync(0xffffffffu, fminf(ka.x, ka.z) < 0.0f || static_cast<int32_t>(first + COLS - 1) > last);
+        float kf[2] = {ka.x * factor, ka.z * factor};
+        const float above[2] = {ka.y, ka.w};
         tmem_wait_ld();
         float top = neg_inf();
         if (part) {
 #pragma unroll
           for (uint32_t i = 0; i < 2; ++i) {
-            const bool out = s_skip[buf][half * 2 + i] != 0;
+            const bool out = (i == 0 ? ka.x : ka.z) < 0.0f;
             float t = neg_inf();
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e) {
@@ -561,13 +560,13 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         }
         // the two warps agree to raise; both have read their scores by then, so that the weights may overwrite them
         const bool raise = meet(top > m + kRaise);
-        if (other_left()) {
-          pass();
-          goto done;
-        }
         const bool fold = SPLIT && j > 0 && j % FOLD == 0, run = RUNS && j > 0 && j % RUN == 0;
         float keep = 1.0f;
         if (raise) {
+          if (other_left()) {
+            pass();
+            goto done;
+          }
           s_max[half][r * ROWS + row_in] = top;
           meet(false);
           if (other_left()) {
@@ -583,12 +582,13 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
         const uint64_t off2 = pair_of(off, off), kf2[2] = {pair_of(kf[0], kf[0]), pair_of(kf[1], kf[1])};
         uint64_t sum[2] = {};
         uint32_t w[16], rest[16];
+        const float2 both_vr = *reinterpret_cast<const float2 *>(&s_vr[buf][half * 2]);
 #pragma unroll
         for (uint32_t e = 0; e < COLS; e += 2) {
           const float2 x = floats_of(fma2(pair_of(v[e], v[e + 1]), kf2[e / 16], off2));
           float p0 = ex2(x.x), p1 = ex2(x.y);
           sum[e / 2 % 2] = add2(sum[e / 2 % 2], pair_of(p0, p1));
-          const float vr = s_vr[buf][half * 2 + e / 16];
+          const float vr = e < 16 ? both_vr.x : both_vr.y;
           if constexpr (FINE) {  // (2 - 3 % faster than both in one instruction; 2 % slower for bfloat16)
             p0 *= vr;
             p1 *= vr;
@@ -924,10 +924,8 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       if (keys && lane == 0) {
         // (a value scale that is a NaN or an infinity: no number)
         const bool number = fabsf(vs[0]) < -neg_inf();
-        s_ks[j % 8][w] = number ? fabsf(ks[0]) : __int_as_float(0x7fc00000);
-        s_skip[j % 8][w] = skip[0];
+        s_ka[j % 8][w] = make_float2(skip[0] ? -1.0f : number ? fabsf(ks[0]) : __int_as_float(0x7fc00000), number ? scale_above(vs[0], unit) : 0.0f);
         s_vr[j % 8][w] = number ? vs[0] * per_sv : 0.0f;
-        s_above[j % 8][w] = number ? scale_above(vs[0], unit) : 0.0f;
       }
       fence_async();
       __syncwarp();
