@@ -1,21 +1,21 @@
 // Causal attention over the paged 8-bit cache for many query rows: prompts.
 //
-// Bound by the issue of the softmax's and the conversions' instructions (about 60 % of the issue slots; the tensor pipe is
-// active for 35 % of the time, DRAM for 5 %): 8 x 256 queries at 4096 positions, 32 heads over 8 of 128, 167 us, 797 TFLOP/s
+// Bound by the issue of the softmax's and the conversions' instructions (63 to 68 % of the issue slots; the tensor pipe is
+// active for 36 to 42 % of the time, DRAM for 5 %): 8 x 256 queries at 4096 positions, 32 heads over 8 of 128, 155 us, 860 TFLOP/s
 // of 4 D operations per row and visible position.  tcgen05, scores, weights and outputs in tensor memory.
 //
 // A block takes 256 query rows of one cached head (its group's heads, token by token), as two tiles of 128, and walks
 // over the positions 64 at a time:
 //   4 + 4 convert warps  the 8-bit keys and values, copied ahead from the pages by cp.async (four tiles in flight), to f16
-//                    in shared memory, both K-major and exact: keys [position][dimension], with the sign of their
-//                    scale, values transposed by byte permutes to [dimension][position]
-//   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory
+//                    in shared memory, both [position][dimension] and exact, keys with the sign of their scale
+//   MMA warp         S = Q K^T, 128 x 64 a tile, two of them ahead; O += P V with P from tensor memory, V across
+//                    its rows (no transposing: the same code converts keys and values)
 //   2 x 8 softmax warps  two threads a row, 32 positions each: scores from tensor memory, times the page's key scale and the row's
 //                    factor, 2^(s - m + 7) with the running maximum m of s + log2(vs / sv) raised only where it is passed
 //                    by 8 (then O is scaled down in place), P vs / sv as f16 over the scores' columns
 // Under the mask of a tree of drafted tokens (few rows, long contexts) a tile costs its conversion and a chain of waits whatever
 // its rows are: up to 128 rows the two row tiles are the same rows at alternating positions (16 sequences of 4096 positions, 128
-// rows, 72 us; 94 with one), and up to 64 the softmax warps without rows convert every second tile (64 rows 53 us; 67 without).
+// rows, 68 us; 90 with one), and up to 64 the softmax warps without rows convert every second tile (64 rows 51 us; 67 without).
 // With two score tiles a row tile, one row tile's next scores are there when its softmax is done: the handing over
 // between warps and tensor cores (about 900 clocks a round) runs under the exponentials.
 // Rows and pages that are not seen have weight 0; a page whose value scale is not a number has the scale zero and a key scale
@@ -41,7 +41,7 @@ constexpr uint32_t ROWS = 128, POS = 64, TILE_WARPS = 8, CONVERT_WARPS = 8;  // 
 template <typename T>
 constexpr bool kSplit = sizeof(T) == 4;
 // Weights in two halves: all but bfloat16, whose own rounding hides that of weights to 11 bits (float16 outputs 2.1e-4 off, their rounding alone, against 3.0e-4; 8 x 256 queries at
-// 4096 positions 186 us against 167).
+// 4096 positions 183 us against 155).
 template <typename T>
 constexpr bool kFine = !std::is_same<T, __nv_bfloat16>::value;
 template <typename T>
@@ -50,7 +50,7 @@ template <typename T>
 constexpr uint32_t kWarps = kSoftWarps<T> + CONVERT_WARPS + 1;  // (25 leave 72 registers a thread)
 constexpr uint32_t RING = 3, STAGED = 4;  // f16 tiles of keys and of values; 8-bit tiles of both
 // Single precision adds its accumulators to a sum of their own every FOLD tiles: 256 positions lose up to 2e-6 (8 x 256 queries
-// at 4096 positions 305 us; 285 with 8 tiles, 265 without, where 4096 positions lose up to 3e-5).
+// at 4096 positions 299 us; with 8 tiles 6 % less, without 13 %, where 4096 positions lose up to 3e-5).
 constexpr uint32_t FOLD = 4;
 // No accumulator takes more than this many tiles: a longer range's outputs so far, and its sum of weights, are then added up
 // aside (the outputs in the place of the row's partial result).
@@ -1076,7 +1076,7 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
     f.splits = static_cast<uint32_t>((most + range - 1) / range);
   }
   f.runs = most > f.splits * range;
-  // uneven sequences over more than one round of blocks (32 of 64 drafted tokens, up to 8192 positions: 161 us, in the batch's order 194)
+  // uneven sequences over more than one round of blocks (32 of 64 drafted tokens, up to 8192 positions: 152 us, in the batch's order 18 % more)
   f.by_length = a.mask && f.splits == 1 && blocks > sms && a.batch > 1 && a.batch <= kMostSorted;
   attend_place(&f, work);
   return f;
@@ -1112,9 +1112,9 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
 
 }  // namespace
 
-// From 48 rows a cached head on: the other kernel takes 16 at a time (0.65 us an SM for 64 positions), this one 256 in 1.4 us
+// From 48 rows a cached head on: the other kernel takes 16 at a time (0.65 us an SM for 64 positions), this one 256 in 1.2 us
 // (128 of single precision).  Under a mask from 17 on, where the other takes them in two (16 sequences of 4096 positions, 24 rows of
-// 128: 56 us against 92, single precision 89 against 103; 16 rows 57 against 54).
+// 128: 51 us against 87, single precision 84 against 98; 16 rows 52 against 49).
 bool attend_many_takes(const ClearAttentionArgs &a) {
   return a.dim <= 128 && static_cast<uint64_t>(a.tokens) * a.group >= (a.mask ? 17 : 48) && attend_few_takes(a);
 }
