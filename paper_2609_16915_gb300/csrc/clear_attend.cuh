@@ -3,8 +3,6 @@
 #pragma once
 #include <stdint.h>
 
-#include <atomic>
-
 #include "clear.h"
 
 namespace rosetta {
@@ -67,18 +65,6 @@ __device__ __forceinline__ uint32_t mask_word(const uint32_t *row, uint32_t toke
   const uint32_t from = static_cast<uint32_t>(i) * 32;
   if (from >= tokens) return 0u;
   return tokens - from < 32 ? row[i] & ((1u << (tokens - from)) - 1u) : row[i];
-}
-
-// Let a kernel use `bytes` of dynamic shared memory, once a device (about a microsecond of the host's time; `told`: the kernel's own).
-inline cudaError_t allow_shared(const void *kern, uint32_t bytes, std::atomic<uint64_t> *told) {
-  int device = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  if (e != cudaSuccess) return e;
-  const uint64_t bit = device < 64 ? 1ull << device : 0;
-  if (told->load(std::memory_order_relaxed) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-  if (e == cudaSuccess) told->fetch_or(bit, std::memory_order_relaxed);
-  return e;
 }
 
 // Join the splits of every row; group_rows: rows that one block's ranges were laid out for.

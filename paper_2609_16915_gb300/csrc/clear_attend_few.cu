@@ -623,8 +623,7 @@ cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
   auto kern = attend_few_kernel<T, DP, NB, TREE>;
   constexpr uint32_t join = (kWarps * 8 * (DP + 4) + kWarps * 8 * 2) * 4;
   constexpr uint32_t smem = Few<DP>::RING > join ? Few<DP>::RING : join;
-  static std::atomic<uint64_t> told{0};
-  const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kern), smem, &told);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   kern<<<f.count * f.groups * f.splits, 32 * kWarps, smem, s>>>(f);
   return cudaGetLastError();

@@ -570,9 +570,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
           s_max[half][r * ROWS + row_in] = top;
           meet(false);
           if (other_left()) {
-          pass();
-          goto done;
-        }
+            pass();
+            goto done;
+          }
           const float raised = fmaxf(fmaxf(m, top), s_max[half ^ 1u][r * ROWS + row_in]);
           keep = m == neg_inf() ? 0.0f : ex2(m - raised);
           m = raised;
@@ -678,9 +678,9 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
       s_max[half][r * ROWS + row_in] = l;
       meet(false);
       if (other_left()) {
-          pass();
-          goto done;
-        }
+        pass();
+        goto done;
+      }
       l += s_max[half ^ 1u][r * ROWS + row_in];
       constexpr uint32_t PITCH = DP + 4;
       float *joined = reinterpret_cast<float *>(smem + M::K_AT) + row_in * PITCH + half * (DP / 2);
@@ -1084,22 +1084,17 @@ AttendArgs many_args(const ClearAttentionArgs &a, int type, void *work, uint32_t
 
 template <typename T, int DP>
 cudaError_t launch(const AttendArgs &f, cudaStream_t s) {
-  static std::atomic<uint64_t> told[6] = {};  // of each kernel
   auto kern = attend_many_kernel<T, DP, false, false, ALL>;
-  uint32_t which = f.runs;
   if (!f.a.mask) {
     if (f.runs) kern = attend_many_kernel<T, DP, true, false, ALL>;
   } else {
-    which += 2;
     kern = f.runs ? attend_many_kernel<T, DP, true, true, ALL> : attend_many_kernel<T, DP, false, true, ALL>;
     if constexpr (!kSplit<T>) {
-      if (!f.runs && f.a.tokens * f.a.group <= ROWS) {
-        which = f.a.tokens * f.a.group <= ROWS / 2 ? 5 : 4;
-        kern = which == 5 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
-      }
+      const uint32_t rows = f.a.tokens * f.a.group;
+      if (!f.runs && rows <= ROWS) kern = rows <= ROWS / 2 ? attend_many_kernel<T, DP, false, true, HALF> : attend_many_kernel<T, DP, false, true, TURNS>;
     }
   }
-  const cudaError_t e = allow_shared(reinterpret_cast<const void *>(kern), Many<DP>::SMEM, &told[which]);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Many<DP>::SMEM));
   if (e != cudaSuccess) return e;
   kern<<<f.count * f.groups * f.splits, kWarps<T> * 32, Many<DP>::SMEM, s>>>(f);
   return cudaGetLastError();
