@@ -181,7 +181,7 @@ def drafted_step(layer: Layer, head: Head, embedding, cache: Cache, tokens, pare
     lib, device = layer.lib, tokens.device
     mask = torch.empty((b, nodes, -(-nodes // 32)), dtype=torch.int32, device=device)
     lib.tree_mask(parents, mask)
-    x = embedding[tokens.long()]
+    x = embedding[tokens.long().clamp(0, embedding.shape[0] - 1)]   # (what is no token has any embedding: verification skips it)
     residual = torch.zeros_like(x)
     y, code = layer.step(x, residual, cache, mask)
     path = torch.empty((b, nodes), dtype=torch.int32, device=device)

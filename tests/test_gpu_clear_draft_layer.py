@@ -109,6 +109,24 @@ def test_drafted_steps_and_single_tokens_agree():
     assert float((outs[0] - outs[1]).norm() / outs[1].norm()) < 0.06
 
 
+def test_nodes_without_a_token_take_no_part():
+    """Padding (no parent, any token) is left out silently; a child whose token is none is left out and reported."""
+    L, layer, embedding, head = drafted_state()
+    up = torch.tensor([[-1, 0, 0, -1]], dtype=torch.int32, device="cuda")
+    uniform = torch.full((1, 4), 0.5, device="cuda")
+    for lone, bad in ((300, False), (-7, False), (1 << 30, False), (5, True)):
+        cache = L.Cache(1, 16, KV, DIM, page=16)
+        trees = torch.tensor([[1, -1 if bad else 2, 300 if bad else 3, lone]], dtype=torch.int32, device="cuda")
+        path, count, following, _ = L.drafted_step(layer, head, embedding, cache, trees, up, uniform)
+        if bad:
+            with pytest.raises(RuntimeError, match="rosetta_clear_sync_status failed"):
+                layer.lib.sync_status()
+            assert int(count[0]) == 1
+        layer.lib.sync_status()
+        assert 3 not in path[0].tolist() and 0 <= int(following[0]) < 300
+        assert int(cache.lengths[0]) == int(count[0])
+
+
 def test_a_full_cache_stops_a_drafted_step():
     L, layer, embedding, head = drafted_state()
     cache = L.Cache(1, 16, KV, DIM, page=16)
