@@ -540,7 +540,8 @@ int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, cons
  *   tokens, parents int32, uniform float [batch][nodes], in [0, 1), row pitches from 0 on
  *   path int32 [batch][nodes] of pitch path_pitch: the accepted nodes, 0 first, then -1;
  *     count [batch]: how many; next [batch]: the next token
- * nodes: up to 1024, vocab: 1 .. 2^24.  Nodes of a parent or a token out of range take no part,
+ * nodes: up to 1024, vocab: 1 .. 2^24.  Nodes of a parent or a token out of range take no part (where
+ * it is node 0: path -1 throughout, count 0, the token -1),
  * probabilities out of range count as 0, a row of none but zeros or that adds up to 64 gives the
  * token -1; each is reported by rosetta_clear_sync_status as INVALID_ARG (of what the walk reads).
  * Errors: INVALID_ARG, CUDA. */

@@ -172,16 +172,24 @@ class Head:
         return torch.softmax(logits, 1).view(b, t, -1)
 
 
+def embed(embedding, head: Head, tokens):
+    """Rows of the embedding [head's tokens or more][width].  What is no token has any of them: verification leaves it out."""
+    if embedding.shape[0] < head.packed.channels:
+        raise ValueError(f"the embedding has {embedding.shape[0]} rows for the head's {head.packed.channels} tokens")
+    return embedding[tokens.long().clamp(0, embedding.shape[0] - 1)]
+
+
 def drafted_step(layer: Layer, head: Head, embedding, cache: Cache, tokens, parents, uniform, draft=None):
     """One step over trees of drafted tokens: tokens, parents int32 and uniform [batch][nodes], node 0 the last token that stands
     (see rosetta.h).  (path, count, next token, message codes of all nodes); the cache keeps the path.
 
-    The next call's node 0 is the next token, whose position comes behind the path."""
+    The next call's node 0 is the next token, whose position comes behind the path.  A sequence whose node 0 is no token keeps nothing
+    (count 0, next token -1, its length as before), and Clear.sync_status reports it."""
     b, nodes = tokens.shape
     lib, device = layer.lib, tokens.device
+    x = embed(embedding, head, tokens)
     mask = torch.empty((b, nodes, -(-nodes // 32)), dtype=torch.int32, device=device)
     lib.tree_mask(parents, mask)
-    x = embedding[tokens.long().clamp(0, embedding.shape[0] - 1)]   # (what is no token has any embedding: verification skips it)
     residual = torch.zeros_like(x)
     y, code = layer.step(x, residual, cache, mask)
     path = torch.empty((b, nodes), dtype=torch.int32, device=device)

@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
   // Each CTA gathers every ranks-th node and all take it over, so that they decide alike whatever becomes of the buffers meanwhile.
   for (uint32_t c = rank + tid * ranks; c < nodes; c += threads * ranks) {
     int32_t up = c ? a.parents[static_cast<int64_t>(b) * a.parents_pitch + c] : -1;
-    const int32_t x = c ? a.tokens[static_cast<int64_t>(b) * a.tokens_pitch + c] : 0;
+    const int32_t x = a.tokens[static_cast<int64_t>(b) * a.tokens_pitch + c];
     if (up < -1 || up >= static_cast<int32_t>(c) || (up >= 0 && (x < 0 || static_cast<uint32_t>(x) >= a.vocab))) {
       bad = true;
       up = -1;
@@ -152,6 +152,19 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
     }
   }
   __syncthreads();
+  if (static_cast<uint32_t>(s_token[0]) >= a.vocab) {  // the root is no token: nothing stands behind it (the same for the cluster)
+    if (rank == 0) {
+      for (uint32_t i = tid; i < nodes; i += threads) a.path[static_cast<int64_t>(b) * a.path_pitch + i] = -1;
+      if (tid == 0) {
+        a.count[b] = 0;
+        a.next[b] = -1;
+        atomicMax(a.err_flag, 1u);
+      }
+    }
+    __syncwarp();
+    if (ranks > 1) cluster_sync_shared();  // (the nodes are read until here)
+    return;
+  }
 
   const uint32_t lo = (rank * warps + warp) * run, hi = min(a.vocab, lo + run);  // this warp's run
   const auto row_of = [&](const T *rows, const int64_t (&strides)[2], uint32_t n) { return rows + static_cast<int64_t>(n) * strides[1]; };
