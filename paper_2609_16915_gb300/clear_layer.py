@@ -201,7 +201,7 @@ def drafted_step(layer: Layer, head: Head, embedding, cache: Cache, tokens, pare
 
 def draw_tree(head: Head, embedding, roots, parents, generator=None):
     """(tokens, draft): trees of one shape (parents [nodes]), each child drawn from the head's probabilities of its parent's
-    embedding alone, a draft that knows the last token only."""
+    embedding alone, a draft that knows the last token only.  (From a root that is no token trees are drawn as from any.)"""
     b, nodes = roots.shape[0], parents.shape[0]
     tokens = torch.zeros((b, nodes), dtype=torch.int32, device=roots.device)
     tokens[:, 0] = roots
@@ -210,7 +210,7 @@ def draw_tree(head: Head, embedding, roots, parents, generator=None):
     for n in range(nodes):
         children = [c for c in range(n + 1, nodes) if up[c] == n]
         if children:
-            draft[:, n] = head(embedding[tokens[:, n:n + 1].long()])[:, 0]
+            draft[:, n] = head(embed(embedding, head, tokens[:, n:n + 1]))[:, 0]
             tokens[:, children] = torch.multinomial(draft[:, n], len(children), replacement=True, generator=generator).to(torch.int32)
     return tokens, draft
 

@@ -1,0 +1,41 @@
+"""Drafted tokens through the layer: what is decided before anything reaches the GPU."""
+
+import pytest
+import torch
+
+from paper_2609_16915_gb300 import clear_layer as L
+
+VOCAB, WIDTH = 12, 8
+
+
+class OneToken:
+    """A head that always gives the token 3, on the CPU."""
+    class packed:
+        channels = VOCAB
+
+    def __call__(self, y, residual=None):
+        return torch.eye(VOCAB)[3].expand(*y.shape[:2], VOCAB)
+
+
+@pytest.mark.parametrize("rows", [VOCAB, VOCAB + 5])
+def test_trees_are_drawn_from_roots_without_a_token(rows):
+    """Such a root stays as it is (the step over the tree reports it), and no row outside the embedding is asked for."""
+    seen = []
+
+    class Embedding(torch.Tensor):
+        @classmethod
+        def __torch_function__(cls, func, types, args=(), kwargs=None):
+            if func is torch.Tensor.__getitem__:
+                seen.append(torch.as_tensor(args[1]))
+            return super().__torch_function__(func, types, args, kwargs or {})
+
+    roots = torch.tensor([2, -1, VOCAB, rows, 1 << 30, -(1 << 31)], dtype=torch.int32)
+    tokens, draft = L.draw_tree(OneToken(), torch.rand(rows, WIDTH).as_subclass(Embedding), roots, torch.tensor([-1, 0, 0, 1]))
+    assert torch.equal(tokens[:, 0], roots) and bool((tokens[:, 1:] == 3).all())
+    assert draft[:, :2, 3].tolist() == [[1.0, 1.0]] * 6 and not draft[:, 2:].any()
+    assert seen and all(0 <= int(s.min()) and int(s.max()) < rows for s in seen)
+
+
+def test_trees_are_not_drawn_from_an_embedding_without_the_heads_tokens():
+    with pytest.raises(ValueError, match="embedding"):
+        L.draw_tree(OneToken(), torch.rand(VOCAB - 1, WIDTH), torch.zeros(1, dtype=torch.int32), torch.tensor([-1, 0]))
