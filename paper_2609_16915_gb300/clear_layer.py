@@ -181,12 +181,21 @@ def embed(embedding, head: Head, tokens):
 
 def drafted_step(layer: Layer, head: Head, embedding, cache: Cache, tokens, parents, uniform, draft=None):
     """One step over trees of drafted tokens: tokens, parents int32 and uniform [batch][nodes], node 0 the last token that stands
-    (see rosetta.h).  (path, count, next token, message codes of all nodes); the cache keeps the path.
+    (see rosetta.h).  (path, count, next token, message codes of all nodes); the cache keeps the path.  Arguments that do not fit are
+    refused (ValueError) before anything moves.
 
     The next call's node 0 is the next token, whose position comes behind the path.  A sequence whose node 0 is no token keeps nothing
     (count 0, next token -1, its length as before), and Clear.sync_status reports it."""
+    if tokens.dim() != 2:
+        raise ValueError("tokens must be [batch][nodes]")
     b, nodes = tokens.shape
     lib, device = layer.lib, tokens.device
+    # (what verification would refuse is refused before the cache moves)
+    for name, t, dtype in (("tokens", tokens, torch.int32), ("parents", parents, torch.int32), ("uniform", uniform, torch.float32)):
+        lib._nodes(name, t, dtype, b, nodes)
+    if draft is not None:
+        lib._strided("draft", draft, torch.float32, (b, nodes, head.packed.channels))
+    lib._at("the cache's lengths", cache.lengths, torch.int32, (b,))
     x = embed(embedding, head, tokens)
     mask = torch.empty((b, nodes, -(-nodes // 32)), dtype=torch.int32, device=device)
     lib.tree_mask(parents, mask)

@@ -39,3 +39,32 @@ def test_trees_are_drawn_from_roots_without_a_token(rows):
 def test_trees_are_not_drawn_from_an_embedding_without_the_heads_tokens():
     with pytest.raises(ValueError, match="embedding"):
         L.draw_tree(OneToken(), torch.rand(VOCAB - 1, WIDTH), torch.zeros(1, dtype=torch.int32), torch.tensor([-1, 0]))
+
+
+class NoCalls:
+    def __getattr__(self, name):
+        def call(*args):
+            raise AssertionError(f"{name} was called")
+        return call
+
+
+@pytest.fixture
+def layer():
+    from paper_2609_16915_gb300 import clear
+    layer = L.Layer.__new__(L.Layer)
+    layer.lib = clear.Clear.__new__(clear.Clear)
+    layer.lib._h, layer.lib.device, layer.lib._L = None, -1, NoCalls()      # (tensors of the CPU are on device -1)
+    return layer
+
+
+def test_a_drafted_step_refuses_before_anything_moves(layer):
+    b, nodes = 2, 5
+    cache = L.Cache(b, 64, 2, 16, device="cpu")
+    n, u = torch.zeros((b, nodes), dtype=torch.int32), torch.zeros(b, nodes)
+    base = dict(cache=cache, tokens=n, parents=n, uniform=u, draft=torch.zeros(b, nodes, VOCAB))
+    for bad in [dict(tokens=n.long()), dict(tokens=n[0]), dict(parents=n.long()), dict(parents=n[:, :4]), dict(uniform=u.double()),
+                dict(uniform=u[:1]), dict(draft=torch.zeros(b, nodes, VOCAB).half()), dict(draft=torch.zeros(b, nodes, VOCAB - 1)),
+                dict(draft=torch.zeros(b, nodes - 1, VOCAB)), dict(cache=L.Cache(b + 1, 64, 2, 16, device="cpu"))]:
+        with pytest.raises(ValueError):
+            L.drafted_step(layer, OneToken(), torch.rand(VOCAB, WIDTH), **{**base, **bad})
+    assert cache.room == 64 and cache.lengths.tolist() == [0, 0]
