@@ -541,9 +541,9 @@ int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, cons
  *   path int32 [batch][nodes] of pitch path_pitch: the accepted nodes, 0 first, then -1;
  *     count [batch]: how many; next [batch]: the next token
  * nodes: up to 1024, vocab: 1 .. 2^24.  Nodes of a parent or a token out of range take no part (where
- * it is node 0: path -1 throughout, count 0, the token -1),
- * probabilities out of range count as 0, a row of none but zeros or that adds up to 64 gives the
- * token -1; each is reported by rosetta_clear_sync_status as INVALID_ARG (of what the walk reads).
+ * it is node 0: path -1 throughout, count 0, the token -1), probabilities out of range count as 0, a row
+ * of none but zeros or that adds up to 64 (after rejected tokens that were drawn: what is left of it)
+ * gives the token -1; each is reported by rosetta_clear_sync_status as INVALID_ARG (of what the walk reads).
  * Errors: INVALID_ARG, CUDA. */
 int rosetta_clear_verify(rosetta_clear *h, int type, const void *target, const int64_t *target_strides,
                          const void *draft, const int64_t *draft_strides, const int32_t *tokens, int64_t tokens_pitch,

@@ -298,7 +298,9 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
     if (!DRAFT && gone) {
       for (uint32_t i = tid; i < gone; i += threads) {
         const uint32_t w = static_cast<uint32_t>(s_gone[i]) / run;
-        if (w / warps == rank) atomicAdd(reinterpret_cast<unsigned long long *>(&s_warp[turn][w % warps]), 0ull - s_gone_p[i]);
+        // (a sum that stopped at kMost is none to take from; the others are below it from beginning to end)
+        if (w / warps == rank && *const_cast<volatile uint64_t *>(&s_warp[turn][w % warps]) < kMost)
+          atomicAdd(reinterpret_cast<unsigned long long *>(&s_warp[turn][w % warps]), 0ull - s_gone_p[i]);
       }
       __syncthreads();
     }
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
 
   // ---- the walk: every warp for itself, all alike; it stops where a sum is wanted, and at its end ----
   uint32_t n = 0, length = 1, gone = 0, c0 = 1;
-  uint64_t s = 0, z = kOne, left = kOne, total;
+  uint64_t s = 0, z = kOne, left = kOne, off = 0, total;  // (off: of the rejected tokens that were given, which left may not hold in full)
   bool stale = false, ended = false;  // (stale: z is that of the s before)
   if (tid == 0) s_path[0] = 0;
   while (true) {
@@ -354,6 +356,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
         yes = __umul64hi(u, left) < p;
         if (!yes && p) {
           left = less(left, p);
+          off = add_most(off, p);
           __syncthreads();  // (all have looked at the list)
           if (tid == 0) {
             s_gone[gone] = s_token[c];
@@ -370,16 +373,19 @@ __global__ void __launch_bounds__(kMostThreads, 2) verify_kernel(const ClearVeri
         n = c;
         s = 0;
         z = left = kOne;
+        off = 0;
         gone = 0;
         stale = false;
       }
     }
     total = row_sum(n, s, gone);
+    // given: it is the row that adds up to too much or does not, the rejected tokens in it (so that the runs' sizes do not matter)
+    if (!DRAFT && add_most(total, off) == kMost) total = kMost;
     if (!ended) {
       z = total;
       stale = false;
     } else if (total == 0 && (s != 0 || gone != 0)) {  // nothing is left: the target's row itself
-      s = 0;
+      s = off = 0;
       gone = 0;
     } else {
       break;

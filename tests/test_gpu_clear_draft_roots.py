@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests.test_gpu_clear import FLOATS, lib  # noqa: F401  (lib: the fixture)
-from tests.test_gpu_clear_draft import drafted, ints, reported, run_verify
+from tests.test_gpu_clear_draft import drafted, reported, run_verify
 from tests.test_gpu_clear_draft_layer import DIM, KV, drafted_state
 
 pytestmark = pytest.mark.gpu
