@@ -53,9 +53,10 @@ __device__ __forceinline__ uint32_t split_share(const AttendArgs &f, uint32_t en
   return ((share < f.least ? f.least : share) + 63) / 64 * 64;
 }
 
-// Positions that the rows of a group see at most: up to the last token of the group; under a mask all of them.
+// Positions that the rows of a group see at most: up to the last token of the group; under a mask (TREE) all of them.
+template <bool TREE>
 __device__ __forceinline__ uint32_t group_end(const ClearAttentionArgs &a, int64_t len, uint32_t last_row) {
-  const int64_t end = a.mask ? len : len - a.tokens + 1 + last_row / a.group;
+  const int64_t end = TREE ? len : len - a.tokens + 1 + last_row / a.group;
   return end > 0 ? static_cast<uint32_t>(end) : 0u;
 }
 

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(32 * kWarps, NB == 1 ? Few<DP>::BLOCKS : 2) at
   const uint32_t own_head = blockIdx.x / f.splits / f.groups, bh = f.first + own_head, kh = bh % a.heads, b = bh / a.heads;
   const uint32_t rows = a.tokens * a.group, row0 = group * (8 * NB);
   const int64_t len = length_of(a, b);
-  const uint32_t end = group_end(a, len, min(row0 + 8 * NB, rows) - 1);
+  const uint32_t end = group_end<TREE>(a, len, min(row0 + 8 * NB, rows) - 1);
   const uint32_t share = split_share(f, end), lo = split * share, hi = min(end, lo + share);
   if (split > 0 && lo >= end) return;
   const bool alone = end <= share;  // (the first block of an empty sequence writes its zeros)
@@ -528,7 +528,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attend_join_kernel(const Atte
   const bool real = id < f.count * rows;
   const uint32_t own_head = real ? id / rows : 0, bh = f.first + own_head, row = id % rows, kh = bh % a.heads, b = bh / a.heads;
   const int64_t most = static_cast<int64_t>(a.table_pitch) * a.page_tokens, given = a.lengths[b], len = given > most ? most : given;
-  const uint32_t end = group_end(a, len, min(row / group_rows * group_rows + group_rows, rows) - 1);
+  const uint32_t last_row = min(row / group_rows * group_rows + group_rows, rows) - 1;
+  const uint32_t end = a.mask ? group_end<true>(a, len, last_row) : group_end<false>(a, len, last_row);
   const uint32_t share = split_share(f, end), count = (end + share - 1) / share;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!real || end <= share) return;  // (whole rows; written already)

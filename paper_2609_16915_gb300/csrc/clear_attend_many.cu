@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kWarps<T> * 32, 1) attend_many_kernel(const At
     len = most;
   }
   // this block's range of the positions that its rows see
-  const uint32_t all = group_end(a, len, min(row0 + BLOCK_ROWS, rows) - 1), share = split_share(f, all);
+  const uint32_t all = group_end<TREE>(a, len, min(row0 + BLOCK_ROWS, rows) - 1), share = split_share(f, all);
   const uint32_t start = split * share, end = min(all, start + share);
   const bool alone = all <= share;
   if (split > 0 && start >= all) return;
