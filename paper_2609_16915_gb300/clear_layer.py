@@ -117,9 +117,13 @@ class Layer:
     def before_table(self, x, residual, cache: Cache, mask=None):
         """The 8-bit input of the up projection for new tokens x [batch][tokens][width]; residual and cache move on.
         Each token sees those before it, or under a mask (Clear.tree_mask) those of a tree.  ValueError, and neither moves,
-        where the cache is full."""
+        where the cache is full or the mask is another tree's."""
         b, t, w = x.shape
         hq, hk, d = self.heads, self.kv_heads, self.dim
+        if mask is not None:        # (what the attention would refuse is refused before the cache moves)
+            if t > 1024:
+                raise ValueError(f"{t} tokens under a mask: up to 1024")
+            self.lib._strided("mask", mask, torch.int32, (b, t, -(-t // 32)))
         cache.take(t)
         flat = residual.view(b * t, w)
         q, s = self._norm(x.reshape(b * t, w), "norm1", flat)

@@ -68,3 +68,15 @@ def test_a_drafted_step_refuses_before_anything_moves(layer):
         with pytest.raises(ValueError):
             L.drafted_step(layer, OneToken(), torch.rand(VOCAB, WIDTH), **{**base, **bad})
     assert cache.room == 64 and cache.lengths.tolist() == [0, 0]
+
+
+def test_a_step_under_a_mask_that_does_not_fit_moves_nothing(layer):
+    layer.heads, layer.kv_heads, layer.dim = 2, 1, 16
+    for tokens, bad in [(5, torch.zeros(2, 5, 1)), (5, torch.zeros(2, 4, 1, dtype=torch.int32)), (5, torch.zeros(2, 5, 2, dtype=torch.int32)),
+                        (33, torch.zeros(2, 33, 1, dtype=torch.int32)), (5, torch.zeros(1, 5, 1, dtype=torch.int32)), (5, torch.zeros(5, 1, dtype=torch.int32)),
+                        (1025, torch.zeros(2, 1025, 33, dtype=torch.int32))]:
+        cache = L.Cache(2, 2048, 1, 16, device="cpu")
+        x = torch.zeros(2, tokens, 32, dtype=torch.bfloat16)
+        with pytest.raises(ValueError):
+            layer.step(x, torch.zeros_like(x), cache, bad)
+        assert cache.room == 2048 and cache.lengths.tolist() == [0, 0]
