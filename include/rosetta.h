@@ -534,7 +534,8 @@ int rosetta_clear_tree_attention(rosetta_clear *h, int type, const void *q, cons
  * all of them (of p itself where nothing is left).
  *   target, draft [batch][nodes][vocab] of `type`, element at b * s[0] + node * s[1] + token with
  *     s = target_strides, draft_strides (HOST arrays): probabilities, in [0, 2], taken as whole
- *     multiples of 2^-56; rows add up to 1 but for rounding.  Sums are exact from there on, so that equal
+ *     multiples of 2^-56; rows add up to 1 but for rounding (target rows of drawn tokens to 1 + 2^-6 at most:
+ *     beyond it a child may be accepted that these formulas reject).  Sums are exact from there on, so that equal
  *     inputs give equal outputs whatever the sizes around them (s q is held to 2^-48 of itself where s is
  *     neither 0 nor 1, and what is left below 2^-55 then counts as nothing).
  *   tokens, parents int32, uniform float [batch][nodes], in [0, 1), row pitches from 0 on
@@ -558,6 +559,10 @@ int rosetta_clear_verify(rosetta_clear *h, int type, const void *target, const i
  *   scale' = max of the scales of the pages that its rows come from, those before the kept ones
  *     among them;  q' = rint(q * (scale / scale')) for each of these rows whose scale differs
  *     (a NaN: bytes as they are)
+ * Scales are 0, positive or a NaN, as rosetta_clear_cache_append writes them (a negative one gives bytes that stand
+ * for other values).  They are the pages' scales, not those of the kept rows: a page that held a rejected row of large
+ * values stays as coarse as the append made it for that row, rows before the drafts among them, until it is
+ * appended to from its first row on.
  * Rows after the kept ones, and pages without any, are left as they are.  A path or a count that is
  * none moves nothing of its sequence, a position past the page list or a page outside [0, pages)
  * is skipped; both are reported by rosetta_clear_sync_status as INVALID_ARG.  Page lists of
