@@ -14,9 +14,11 @@ norm stands before every product (the attention's output among them), there are 
 embeddings, no gate beside the table and no biases but the table's, so a range calibrated on it is
 its own, and a model's layer is put together from the same calls where they fit it.
 
-Drafted tokens: one bootstrapped table takes milliseconds for one ciphertext and little more for hundreds, so a decoder
-around such tables checks a tree of drafted tokens in one step.  step() takes the tree's mask, Head gives the target's
-probabilities, and drafted_step() runs the whole of it: layer, verification, and the cache keeps what stands.
+Drafted tokens: in the clear a tree of them costs up to twice one token, since weights and cache are read once for all
+nodes.  step() takes the tree's mask, Head gives the target's probabilities, and drafted_step() runs the whole of it: layer,
+verification, and the cache keeps what stands.  (Under encryption it is no gain: each node has `inner` messages of its own, and
+batches of a thousand ciphertexts already run at the full rate.)  Rejected drafts leave their mark: a page's scale is raised for all drafted
+tokens in it and stays, so that rows beside rejected values ten times as large keep a tenth of their precision.
 
 Norms, products, cache and table values are 8-bit (clear.Clear); the residual stream is
 bfloat16.  The encrypted path replaces the table alone: encrypt(code) -> pbs_batch ->
